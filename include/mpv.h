@@ -67,12 +67,13 @@
 extern "C" {
 #endif
 
-#define MPV_ABI_VERSION 9
+#define MPV_ABI_VERSION 10
 
 /* limits (larger requests return MPV_ERR_UNSUPPORTED) */
 #define MPV_MAX_NODES    64   /* nodes per tree, root included            */
 #define MPV_MAX_CHILDREN 16   /* children of one node                      */
 #define MPV_MAX_VOCAB    (1 << 21)
+#define MPV_MAX_HEAD_DIM 256  /* values of one attention head               */
 /* and B * (N + 2) <= 2^30 */
 
 #define MPV_METHOD_SPECINFER 0
@@ -87,12 +88,15 @@ extern "C" {
                                * within +-65504; magnitudes below 2^-14 are used to within 2^-25
                                * (an error of log2(e)/T * 2^-25 in the exponent of e^(z/T): nothing
                                * for T >= 0.01).  -inf marks a token of probability zero.        */
+#define MPV_DTYPE_F16  2      /* IEEE binary16: the calls around a verification only (mpv_tree_attention,
+                               * mpv_verify_chains, mpv_append_paths); logits are F32 or BF16.        */
 
 /* error codes: 0 = success, negative = failure (nothing was launched unless the
  * code is MPV_ERR_HIP, in which case some kernels may already be enqueued) */
 #define MPV_OK                   0
 #define MPV_ERR_NULL            -1   /* a required pointer is NULL                   */
-#define MPV_ERR_BAD_SHAPE       -2   /* B < 0, N < 1, V < 1, max_depth < tree depth   */
+#define MPV_ERR_BAD_SHAPE       -2   /* B < 0, N < 1, V < 1, max_depth < tree depth; a size or stride of
+                                        the calls around a verification that cannot be   */
 #define MPV_ERR_BAD_TREE        -3   /* parent[0] != -1 or parent[n] not in [0, n)    */
 #define MPV_ERR_BAD_TEMPERATURE -4   /* T is not a finite number > 0                  */
 #define MPV_ERR_BAD_METHOD      -5
@@ -101,7 +105,8 @@ extern "C" {
 #define MPV_ERR_UNSUPPORTED     -8   /* beyond MPV_MAX_*; stats / edge_probs with methods >= 2;
                                         acceptance rates of MPV_METHOD_TRAVERSAL        */
 #define MPV_ERR_HIP             -9   /* a HIP call failed; see mpv_last_hip_error()   */
-#define MPV_ERR_ALIGNMENT      -10   /* a logit base pointer is not 16-byte aligned   */
+#define MPV_ERR_ALIGNMENT      -10   /* a logit base pointer (or a pointer, stride or row length of the calls
+                                        around a verification) is not a multiple of 16 bytes */
 #define MPV_ERR_BAD_TOP_P      -11   /* top_p is not in (0, 1]                        */
 
 /* Problem description.  Host memory, read during the call only. */
@@ -319,6 +324,167 @@ int mpv_row_stats(const void* logits, int32_t logit_dtype, int64_t rows, int32_t
  * the top 24 bits of the SplitMix64 finaliser applied to
  * seed + (i+1) * 0x9E3779B97F4A7C15, times 2^-24. */
 int mpv_fill_uniforms(uint64_t seed, int64_t count, float* d_u, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * The calls around a verification in a serving loop.  One step of such a loop is
+ *   target pass over the trees: mpv_tree_attention once per layer; the logits of every node;
+ *   mpv_verify (or mpv_verify_merged; mpv_verify_chains where drafts are chains with probabilities);
+ *   mpv_extend_tables: room in the paged cache for the root and the accepted path (new_len =
+ *     accept_len, extra = 1);
+ *   mpv_append_paths: their keys and values, of all layers, enter the cache;
+ *   the bonus token is the root of the next step's trees.
+ * The cache holds accepted tokens only: what was drafted in vain never enters it.  All calls work on lengths
+ * that live on the device, allocate nothing, do not synchronise and can be captured in a graph.
+ * --------------------------------------------------------------------------------------------- */
+
+/* Attention of the nodes of B draft trees over a paged cache and over their own tree.
+ * Node n of tree b is at position context_len[b] + depth(n).  It sees position j < context_len[b] of the cache and
+ * the tree nodes that are its ancestors or itself, each of them only if, with `window` > 0, the position is larger
+ * than its own minus `window` or smaller than `sinks`.  With s the scaled products over what it sees,
+ * out = sum_j softmax(s)_j v_j; query head h reads cache head h / (heads / kv_heads).
+ * Position j of tree b lies in page block_table[b, j / page_size], slot j % page_size; a page outside
+ * [0, num_pages) is not seen, context_len is taken within [0, table_width * page_size].
+ * What a node does not see does not reach its output, whatever it holds (NaN included).
+ * Sums and softmax statistics are float32; weights are rounded to `dtype` before they meet the values (F32: not). */
+typedef struct mpv_attention {
+    int32_t B, N;            /* trees; nodes per tree (<= MPV_MAX_NODES); N = 1: single tokens               */
+    int32_t heads, kv_heads; /* heads is a multiple of kv_heads                                              */
+    int32_t head_dim;        /* <= MPV_MAX_HEAD_DIM, a multiple of 16 bytes                                  */
+    int32_t dtype;           /* MPV_DTYPE_*, of all tensors                                                  */
+    int32_t num_pages, page_size, table_width;  /* the cache's pages, their slots, pages in a row of block_table */
+    int32_t window, sinks;   /* window <= 0: everything is seen                                              */
+    float   scale;           /* finite; multiplies q.k                                                       */
+    int64_t q_stride, kv_stride, out_stride;    /* elements from a node's row [heads, head_dim] (tree_k, tree_v:
+                                [kv_heads, head_dim]) to the next node's; trees follow each other            */
+    int64_t page_stride, slot_stride;           /* elements from page to page, from slot to slot; a slot holds
+                                                   [kv_heads, head_dim]                                       */
+    const int32_t* parent;   /* HOST [N], as in mpv_problem; not read with tree_parent                       */
+} mpv_attention;
+
+typedef struct mpv_attention_buffers {    /* DEVICE, borrowed until the work has run */
+    const void* q;                /* [B,N,heads,head_dim]                                                    */
+    const void* tree_k;           /* [B,N,kv_heads,head_dim]: the nodes' own keys and values                 */
+    const void* tree_v;
+    const void* cache_k;          /* [num_pages,page_size,kv_heads,head_dim]                                 */
+    const void* cache_v;
+    const int32_t* block_table;   /* [B,table_width]                                                         */
+    const int32_t* context_len;   /* [B] cached tokens                                                       */
+    const int32_t* num_nodes;     /* [B] or NULL: only the first num_nodes[b] nodes of a tree exist; rows of
+                                     `out` behind them are left as they were                                 */
+    const int32_t* tree_parent;   /* [B,N] or NULL: a parent array per tree (as merged_parent); an entry outside
+                                     [0,n) makes node n a root                                               */
+    void* out;                    /* [B,N,heads,head_dim]; must not overlap the inputs                       */
+} mpv_attention_buffers;
+
+int mpv_tree_attention_workspace_bytes(const mpv_attention* attention, size_t* out);
+
+/* Errors: MPV_ERR_NULL, _BAD_SHAPE, _UNSUPPORTED (N or head_dim too large, B * heads or a stride beyond 2^31),
+ * _BAD_TREE, _BAD_DTYPE, _BAD_TEMPERATURE (scale not finite), _ALIGNMENT, _WORKSPACE, _HIP. */
+int mpv_tree_attention(const mpv_attention* attention, const mpv_attention_buffers* buffers,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Verification of B chains of drafted tokens against the target's probabilities, from given random numbers
+ * (Sec. 3.2 on a tree of one path, with probabilities in the place of logits).  Row n of a chain belongs to the context
+ * that ends with its n-th drafted token (row 0: the current context); tokens[b,n], n >= 1, was drafted from draft row
+ * n - 1.  Token n is accepted iff every token before it is and u_n q(x_n) < p(x_n) (doubles, exact); the first that is
+ * not sends the bonus token to (p - q)_+ of its row, otherwise the bonus token comes from the last row's p.  Without draft
+ * probabilities a draft is certain: q is 1 at x_n and 0 elsewhere.  Rows need not be normalised; values that are not
+ * positive (NaN included) count as 0.  Where (p - q)_+ has no mass the row's p is drawn from (counted); where p has none
+ * the token is 0.  The bonus token is the smallest t whose cumulative mass exceeds uniforms[b,0] times the total (the last
+ * token with mass if none does); sums are double.  A drafted token outside [0,V) is not accepted (counted), and
+ * takes nothing away from p if there are no draft probabilities. */
+typedef struct mpv_chains {
+    int32_t B, N, V;              /* chains; rows of a chain (N - 1 drafted tokens, <= MPV_MAX_NODES rows); vocabulary */
+    int32_t dtype;                /* MPV_DTYPE_* of the probabilities                                         */
+    int32_t max_depth;            /* row width of path_nodes / path_tokens, >= N - 1 and >= 1                 */
+    int64_t target_stride, draft_stride;   /* elements from a row to the next (>= V); chains follow each other */
+} mpv_chains;
+
+typedef struct mpv_chain_buffers {         /* DEVICE */
+    const void*    target_probs;  /* [B,N,V], at any element's address                                        */
+    const void*    draft_probs;   /* [B,N,V] or NULL; the row of a chain's last token is never read           */
+    const int32_t* tokens;        /* [B,N]; tokens[b,0] ignored                                               */
+    const float*   uniforms;      /* [B,N] in [0,1), as in mpv_buffers                                        */
+    const int32_t* num_nodes;     /* [B] or NULL: rows of this chain, taken within [1,N]                      */
+    int32_t*  accept_len;         /* outputs as in mpv_buffers; path_nodes[b,i] = i + 1                       */
+    int32_t*  path_nodes;
+    int32_t*  path_tokens;
+    int32_t*  bonus_token;
+    uint32_t* counters;           /* [MPV_COUNTER_COUNT]: ZERO_MASS and BAD_TOKEN; zeroed by the call         */
+} mpv_chain_buffers;
+
+int mpv_verify_chains_workspace_bytes(const mpv_chains* chains, size_t* out);
+
+/* Errors: MPV_ERR_NULL, _BAD_SHAPE, _UNSUPPORTED (N or V too large), _BAD_DTYPE, _ALIGNMENT (a pointer is no multiple of
+ * its element's size), _WORKSPACE, _HIP. */
+int mpv_verify_chains(const mpv_chains* chains, const mpv_chain_buffers* buffers,
+                      void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Block tables and slot maps from request lengths, on the GPU.  Request b, with context_len[b] tokens in the cache,
+ * gets room for n = new_len[b] + extra more: the pages it needs are taken from the end of the list of free pages (in
+ * request order, ascending position), entered into its row of the block table, and the slots of its new tokens
+ * (page * page_size + place in it) are written.  new_len[b] < 0: the request is finished; its pages go to the end of the
+ * list (before any are taken, in request order) and its context becomes empty.
+ * Requests are served in order.  One that cannot fit its row of the block table or (slot rows) whose n exceeds the row
+ * is refused; so is every request that needs a page from the first one on whose pages, with those asked for before it, exceed
+ * the free ones, and (packed slots) every request with n > 0 from the first one on whose tokens, with those asked for before it, exceed
+ * the slot map.  What a refused request asked for (unless it could never fit its row) counts for those behind it.  A refused request keeps its
+ * context and pages and gets granted = -1.  A table entry of an earlier page outside [0,num_pages) gives slots of -1. */
+typedef struct mpv_tables {
+    int32_t B, page_size, table_width, num_pages;
+    int32_t extra;                /* >= 0, added to every new_len that is not negative                       */
+    int32_t packed;               /* 0: slot_map[b * slot_width + i], -1 behind a request's tokens;
+                                     1: slot_map[offsets[b] + i], `slot_width` slots in all, what lies behind the last
+                                     token is left as it was                                                  */
+    int64_t slot_width;
+} mpv_tables;
+
+typedef struct mpv_table_buffers {         /* DEVICE */
+    const int32_t* new_len;       /* [B]                                                                      */
+    const int32_t* context_len;   /* [B] >= 0 (a negative one counts as 0)                                    */
+    int32_t* block_table;         /* [B,table_width], in and out; entries behind a request's pages are left alone */
+    int32_t* free_pages;          /* [num_pages], in and out                                                  */
+    const int32_t* free_count;    /* [1], taken within [0,num_pages]                                          */
+    int32_t* context_len_out;     /* [B]; may be context_len                                                  */
+    int32_t* free_count_out;      /* [1]; may be free_count                                                   */
+    int64_t* slot_map;
+    int32_t* granted;             /* [B] tokens placed, -1: refused, 0 for a finished request                 */
+    int32_t* offsets;             /* [B+1] or NULL (packed: required): exclusive sums of the tokens placed    */
+} mpv_table_buffers;
+
+int mpv_extend_tables_workspace_bytes(const mpv_tables* tables, size_t* out);
+
+/* Errors: MPV_ERR_NULL, _BAD_SHAPE, _UNSUPPORTED (slots beyond 2^31), _WORKSPACE, _HIP. */
+int mpv_extend_tables(const mpv_tables* tables, const mpv_table_buffers* buffers,
+                      void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The keys and values of the root and of the accepted path of every tree enter the cache, for all layers at once:
+ * row i <= accept_len[b] of tree b, node 0 for i = 0 and path_nodes[b, i - 1] otherwise (path_nodes NULL: node i), goes to slot
+ * slot_map[b, i].  Slots or nodes out of range are skipped (a refused request has slots of -1).  No slot may appear twice;
+ * tree and cache tensors must not overlap. */
+typedef struct mpv_append {
+    int32_t layers, B, N;
+    int32_t dtype;
+    int32_t row;                  /* kv_heads * head_dim, a multiple of 16 bytes                               */
+    int32_t max_depth;            /* row width of path_nodes (0 without)                                       */
+    int32_t slot_width;           /* row width of slot_map                                                     */
+    int32_t num_pages, page_size;
+    int64_t tree_layer_stride, tree_stride;              /* elements from layer to layer, from node to node    */
+    int64_t cache_layer_stride, page_stride, slot_stride;
+} mpv_append;
+
+typedef struct mpv_append_buffers {        /* DEVICE */
+    const void* tree_k;           /* [layers,B,N,row]                                                         */
+    const void* tree_v;
+    void* cache_k;                /* [layers,num_pages,page_size,row]                                         */
+    void* cache_v;
+    const int64_t* slot_map;      /* [B,slot_width]                                                           */
+    const int32_t* accept_len;    /* [B]                                                                      */
+    const int32_t* path_nodes;    /* [B,max_depth] or NULL                                                    */
+} mpv_append_buffers;
+
+/* Errors: MPV_ERR_NULL, _BAD_SHAPE, _UNSUPPORTED, _BAD_DTYPE, _ALIGNMENT, _HIP. */
+int mpv_append_paths(const mpv_append* append, const mpv_append_buffers* buffers, void* hip_stream);
 
 /* Per-launch timing for benchmarks (process-wide state, not thread-safe).
  * mpv_timing_enable(n > 0) creates n pairs of HIP events; from then on every

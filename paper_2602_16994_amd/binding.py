@@ -27,6 +27,7 @@ MPV_COUNTER_NODE_TASKS_CANCELLED = 6
 MPV_COUNTER_NODE_TASKS_RESUMED = 7
 MPV_DTYPE_F32 = 0
 MPV_DTYPE_BF16 = 1
+MPV_DTYPE_F16 = 2           # mpv_tree_attention, mpv_verify_chains and mpv_append_paths only
 
 _PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 
@@ -56,6 +57,48 @@ class _Buffers(ctypes.Structure):
         "target_logits", "draft_logits", "tokens", "uniforms",
         "accept_len", "path_nodes", "path_tokens", "bonus_token", "counters",
         "stats", "edge_probs", "accept_prob", "final_residual", "draw_uniforms")]
+
+
+class _Attention(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("B", "N", "heads", "kv_heads", "head_dim", "dtype", "num_pages", "page_size", "table_width",
+                                               "window", "sinks")]
+                + [("scale", ctypes.c_float)]
+                + [(n, ctypes.c_int64) for n in ("q_stride", "kv_stride", "out_stride", "page_stride", "slot_stride")]
+                + [("parent", ctypes.POINTER(ctypes.c_int32))])
+
+
+class _AttentionBuffers(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "tree_k", "tree_v", "cache_k", "cache_v", "block_table", "context_len", "num_nodes",
+                                               "tree_parent", "out")]
+
+
+class _Chains(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("B", "N", "V", "dtype", "max_depth")]
+                + [(n, ctypes.c_int64) for n in ("target_stride", "draft_stride")])
+
+
+class _ChainBuffers(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("target_probs", "draft_probs", "tokens", "uniforms", "num_nodes", "accept_len", "path_nodes",
+                                               "path_tokens", "bonus_token", "counters")]
+
+
+class _Tables(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("B", "page_size", "table_width", "num_pages", "extra", "packed")]
+                + [("slot_width", ctypes.c_int64)])
+
+
+class _TableBuffers(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("new_len", "context_len", "block_table", "free_pages", "free_count", "context_len_out",
+                                               "free_count_out", "slot_map", "granted", "offsets")]
+
+
+class _Append(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("layers", "B", "N", "dtype", "row", "max_depth", "slot_width", "num_pages", "page_size")]
+                + [(n, ctypes.c_int64) for n in ("tree_layer_stride", "tree_stride", "cache_layer_stride", "page_stride", "slot_stride")])
+
+
+class _AppendBuffers(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("tree_k", "tree_v", "cache_k", "cache_v", "slot_map", "accept_len", "path_nodes")]
 
 
 _lib = None
@@ -117,6 +160,14 @@ def load_library(path=None):
                                   ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p]
     lib.mpv_fill_uniforms.restype = ctypes.c_int
     lib.mpv_fill_uniforms.argtypes = [ctypes.c_uint64, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p]
+    for name, shape, bufs in (("mpv_tree_attention", _Attention, _AttentionBuffers), ("mpv_verify_chains", _Chains, _ChainBuffers),
+                              ("mpv_extend_tables", _Tables, _TableBuffers)):
+        call, size = getattr(lib, name), getattr(lib, name + "_workspace_bytes")
+        call.restype = size.restype = ctypes.c_int
+        call.argtypes = [ctypes.POINTER(shape), ctypes.POINTER(bufs), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+        size.argtypes = [ctypes.POINTER(shape), ctypes.POINTER(ctypes.c_size_t)]
+    lib.mpv_append_paths.restype = ctypes.c_int
+    lib.mpv_append_paths.argtypes = [ctypes.POINTER(_Append), ctypes.POINTER(_AppendBuffers), ctypes.c_void_p]
     lib.mpv_timing_enable.restype = ctypes.c_int
     lib.mpv_timing_enable.argtypes = [ctypes.c_int32]
     lib.mpv_timing_read.restype = ctypes.c_int
@@ -480,6 +531,263 @@ def mpv_fill_uniforms(seed, count, out=None, device="cuda", stream=None):
     if rc != 0:
         raise MpvError(rc, "mpv_fill_uniforms")
     return out
+
+
+# ------------------------------------------------------------------ the calls around a verification
+
+
+def _dtype_of(t):
+    import torch
+    ids = {torch.float32: MPV_DTYPE_F32, torch.bfloat16: MPV_DTYPE_BF16, torch.float16: MPV_DTYPE_F16}
+    if t.dtype not in ids:
+        raise TypeError(f"tensors must be float32, bfloat16 or float16, got {t.dtype}")
+    return ids[t.dtype]
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else 0
+
+
+def _on_device(dev, **tensors):
+    for name, t in tensors.items():
+        if t is not None and (not t.is_cuda or t.device != dev):
+            raise ValueError(f"{name} must be a CUDA tensor on {dev}")
+
+
+def _whole(dev, dtype, **tensors):
+    """Contiguous tensors of one type on one device: name=(tensor or None, shape)."""
+    for name, (t, shape) in tensors.items():
+        if t is None:
+            continue
+        _on_device(dev, **{name: t})
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if not t.is_contiguous() or tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} must be a contiguous tensor {list(shape)}, got {list(t.shape)} with strides {list(t.stride())}")
+
+
+def _row_stride(name, t, lead, inner):
+    """Elements between the rows of a tensor [*lead, *inner] whose rows (the inner dimensions) are contiguous and whose leading
+    dimensions follow each other."""
+    if tuple(t.shape) != (*lead, *inner):
+        raise ValueError(f"{name} must be {[*lead, *inner]}, got {list(t.shape)}")
+    n = len(lead)
+    want = 1
+    for d in range(len(inner) - 1, -1, -1):
+        if inner[d] != 1 and t.stride(n + d) != want:
+            raise ValueError(f"the rows of {name} must be contiguous, got strides {list(t.stride())}")
+        want *= inner[d]
+    stride, count = None, 1
+    for d in range(n - 1, -1, -1):
+        if lead[d] != 1:
+            if stride is None:
+                if t.stride(d) % count:
+                    raise ValueError(f"the rows of {name} must be evenly spaced, got strides {list(t.stride())}")
+                stride = t.stride(d) // count
+            elif t.stride(d) != stride * count:
+                raise ValueError(f"the rows of {name} must be evenly spaced, got strides {list(t.stride())}")
+        count *= lead[d]
+    return want if stride is None else stride
+
+
+def _cache_strides(k, v, shape):
+    """(page stride, slot stride) of the cache tensors [num_pages, page_size, kv_heads, head_dim]."""
+    strides = []
+    for name, t in (("cache_k", k), ("cache_v", v)):
+        if t.dim() != 4 or tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+        if (shape[3] != 1 and t.stride(3) != 1) or (shape[2] != 1 and t.stride(2) != shape[3]):
+            raise ValueError(f"the slots of {name} must be contiguous, got strides {list(t.stride())}")
+        slot = t.stride(1) if shape[1] != 1 else shape[2] * shape[3]
+        strides.append((t.stride(0) if shape[0] != 1 else slot * shape[1], slot))
+    if strides[0] != strides[1]:
+        raise ValueError("cache_k and cache_v must have the same strides")
+    return strides[0]
+
+
+def _call(name, shape, bufs, out, dev, stream):
+    """A call with a workspace, which is kept in out.workspace."""
+    import torch
+    lib = load_library()
+    need = ctypes.c_size_t(0)
+    rc = getattr(lib, name + "_workspace_bytes")(ctypes.byref(shape), ctypes.byref(need))
+    if rc != 0:
+        raise MpvError(rc, name + "_workspace_bytes")
+    if out.workspace is None or out.workspace.numel() < need.value or out.workspace.device != dev:
+        out.workspace = torch.empty(max(need.value, 256), dtype=torch.uint8, device=dev)
+    with torch.cuda.device(dev):
+        rc = getattr(lib, name)(ctypes.byref(shape), ctypes.byref(bufs), out.workspace.data_ptr(), out.workspace.numel(), _stream_ptr(stream))
+    if rc != 0:
+        raise MpvError(rc, name)
+    return out
+
+
+@dataclass
+class TreeAttentionResult:
+    out: "object"               # [B,N,heads,head_dim]
+    workspace: Optional["object"] = None
+
+
+def mpv_tree_attention(parent, q, tree_k, tree_v, cache_k, cache_v, block_table, context_len, scale=None, window=0, sinks=0,
+                       num_nodes=None, tree_parent=None, out=None, stream=None):
+    """Attention of the nodes of B draft trees over a paged cache and their own tree (see include/mpv.h), enqueued on the current
+    (or given) torch stream; returns a TreeAttentionResult.
+
+    parent: list of N ints (host).  q [B,N,heads,head_dim], tree_k / tree_v [B,N,kv_heads,head_dim], cache_k / cache_v
+    [num_pages,page_size,kv_heads,head_dim]: CUDA tensors of one type (float32, bfloat16 or float16).  The rows of a node and the
+    slots of a cache are contiguous; nodes may lie further apart (slices of a projection's output), and so may slots and pages.
+    block_table int32 [B,table_width], context_len int32 [B].  scale: head_dim ** -0.5 unless given.  num_nodes int32 [B]: only
+    so many nodes of a tree exist (rows of `out` behind them are left as they were).  tree_parent int32 [B,N], on the device: a
+    parent array per tree, in the place of `parent`.  `out` may be a previous TreeAttentionResult whose buffers are reused."""
+    import torch
+    if q.dim() != 4 or tree_k.dim() != 4 or cache_k.dim() != 4 or block_table.dim() != 2:
+        raise ValueError("q, tree_k, tree_v, cache_k and cache_v must have 4 dimensions, block_table 2")
+    B, N, heads, head_dim = q.shape
+    kv_heads, dev = tree_k.shape[2], q.device
+    _on_device(dev, q=q, tree_k=tree_k, tree_v=tree_v, cache_k=cache_k, cache_v=cache_v)
+    if any(t.dtype != q.dtype for t in (tree_k, tree_v, cache_k, cache_v)):
+        raise TypeError("q, tree_k, tree_v, cache_k and cache_v must have the same dtype")
+    dtype = _dtype_of(q)
+    kv_stride = _row_stride("tree_k", tree_k, (B, N), (kv_heads, head_dim))
+    if _row_stride("tree_v", tree_v, (B, N), (kv_heads, head_dim)) != kv_stride:
+        raise ValueError("tree_k and tree_v must have the same strides")
+    num_pages, page_size = cache_k.shape[0], cache_k.shape[1]
+    page_stride, slot_stride = _cache_strides(cache_k, cache_v, (num_pages, page_size, kv_heads, head_dim))
+    width = block_table.shape[1]
+    _whole(dev, torch.int32, block_table=(block_table, (B, width)), context_len=(context_len, (B,)), num_nodes=(num_nodes, (B,)),
+           tree_parent=(tree_parent, (B, N)))
+    if tree_parent is None and len(parent) != N:
+        raise ValueError("parent must have as many entries as a tree has nodes")
+    if out is None:
+        out = TreeAttentionResult(out=torch.empty(B, N, heads, head_dim, dtype=q.dtype, device=dev))
+    _on_device(dev, out=out.out)
+    if out.out.dtype != q.dtype:
+        raise TypeError("out must have the dtype of q")
+    arr = (ctypes.c_int32 * N)(*[int(x) for x in parent]) if tree_parent is None else None
+    shape = _Attention(B, N, heads, kv_heads, head_dim, dtype, num_pages, page_size, width, int(window), int(sinks),
+                       float(head_dim ** -0.5 if scale is None else scale), _row_stride("q", q, (B, N), (heads, head_dim)), kv_stride,
+                       _row_stride("out", out.out, (B, N), (heads, head_dim)), page_stride, slot_stride, arr)
+    bufs = _AttentionBuffers(_ptr(q), _ptr(tree_k), _ptr(tree_v), _ptr(cache_k), _ptr(cache_v), _ptr(block_table), _ptr(context_len),
+                             _ptr(num_nodes), _ptr(tree_parent), _ptr(out.out))
+    return _call("mpv_tree_attention", shape, bufs, out, dev, stream)
+
+
+def mpv_verify_chains(tokens, target_probs, draft_probs, uniforms, num_nodes=None, max_depth=None, out=None, stream=None):
+    """Verification of drafted chains against the target's probabilities (see include/mpv.h), enqueued on the current (or given)
+    torch stream; returns a VerifyResult, as mpv_verify does.
+
+    tokens int32 [B,N], uniforms float32 [B,N], target_probs and draft_probs [B,N,V] (float32, bfloat16 or float16; rows may lie
+    further apart than V): CUDA tensors.  draft_probs=None: the drafts are certain (looked up, or greedy).  num_nodes int32 [B]: rows
+    of each chain, one more than its drafted tokens.  `out` may be a previous VerifyResult whose buffers are reused."""
+    import torch
+    if target_probs.dim() != 3:
+        raise ValueError("target_probs must be [B,N,V]")
+    B, N, V = target_probs.shape
+    dev = target_probs.device
+    _on_device(dev, target_probs=target_probs, draft_probs=draft_probs)
+    if draft_probs is not None and draft_probs.dtype != target_probs.dtype:
+        raise TypeError("target and draft probabilities must have the same dtype")
+    dtype = _dtype_of(target_probs)
+    _whole(dev, torch.int32, tokens=(tokens, (B, N)), num_nodes=(num_nodes, (B,)))
+    _whole(dev, torch.float32, uniforms=(uniforms, (B, N)))
+    if max_depth is None:
+        max_depth = out.path_nodes.shape[1] if out is not None else max(1, N - 1)
+    i32 = dict(dtype=torch.int32, device=dev)
+    if out is None:
+        out = VerifyResult(accept_len=torch.empty(B, **i32), path_nodes=torch.empty(B, max_depth, **i32),
+                           path_tokens=torch.empty(B, max_depth, **i32), bonus_token=torch.empty(B, **i32), counters=torch.empty(8, **i32))
+    _whole(dev, torch.int32, accept_len=(out.accept_len, (B,)), path_nodes=(out.path_nodes, (B, max_depth)),
+           path_tokens=(out.path_tokens, (B, max_depth)), bonus_token=(out.bonus_token, (B,)), counters=(out.counters, (8,)))
+    shape = _Chains(B, N, V, dtype, max_depth, _row_stride("target_probs", target_probs, (B, N), (V,)),
+                    _row_stride("draft_probs", draft_probs, (B, N), (V,)) if draft_probs is not None else 0)
+    bufs = _ChainBuffers(_ptr(target_probs), _ptr(draft_probs), _ptr(tokens), _ptr(uniforms), _ptr(num_nodes), _ptr(out.accept_len),
+                         _ptr(out.path_nodes), _ptr(out.path_tokens), _ptr(out.bonus_token), _ptr(out.counters))
+    return _call("mpv_verify_chains", shape, bufs, out, dev, stream)
+
+
+@dataclass
+class TablesResult:
+    context_len: "object"       # int32 [B]    tokens in the cache after the call
+    free_count: "object"        # int32 [1]
+    granted: "object"           # int32 [B]    tokens placed; -1: refused
+    slot_map: "object"          # int64, the tensor that was passed
+    offsets: "object"           # int32 [B+1]  exclusive sums of the tokens placed
+    workspace: Optional["object"] = None
+
+
+def mpv_extend_tables(block_table, context_len, new_len, free_pages, free_count, page_size, slot_map, extra=0, inplace=False, out=None,
+                      stream=None):
+    """Room for new tokens in a paged cache: block tables and slot maps from request lengths (see include/mpv.h), enqueued on the
+    current (or given) torch stream; returns a TablesResult.
+
+    block_table int32 [B,table_width] and free_pages int32 [num_pages] are changed in place; context_len int32 [B] and
+    free_count int32 [1] are, too, with inplace=True, otherwise their new values are in the result alone.  new_len int32 [B]: tokens to
+    place beside `extra`, negative for a finished request.  slot_map int64: [B,n] for a row of slots per request, [n] for all of them
+    packed.  `out` may be a previous TablesResult whose buffers are reused."""
+    import torch
+    if block_table.dim() != 2 or free_pages.dim() != 1 or slot_map.dim() not in (1, 2):
+        raise ValueError("block_table must be [B,table_width], free_pages [num_pages], slot_map [B,n] or [n]")
+    B, width = block_table.shape
+    dev, pages = block_table.device, free_pages.shape[0]
+    packed = slot_map.dim() == 1
+    _whole(dev, torch.int32, block_table=(block_table, (B, width)), context_len=(context_len, (B,)), new_len=(new_len, (B,)),
+           free_pages=(free_pages, (pages,)), free_count=(free_count, (1,)))
+    _whole(dev, torch.int64, slot_map=(slot_map, tuple(slot_map.shape) if packed else (B, slot_map.shape[1])))
+    i32 = dict(dtype=torch.int32, device=dev)
+    if out is None:
+        out = TablesResult(context_len=context_len if inplace else torch.empty(B, **i32),
+                           free_count=free_count if inplace else torch.empty(1, **i32), granted=torch.empty(B, **i32), slot_map=slot_map,
+                           offsets=torch.empty(B + 1, **i32))
+    elif inplace:
+        out.context_len, out.free_count = context_len, free_count
+    out.slot_map = slot_map
+    _whole(dev, torch.int32, context_len=(out.context_len, (B,)), free_count=(out.free_count, (1,)), granted=(out.granted, (B,)),
+           offsets=(out.offsets, (B + 1,)))
+    shape = _Tables(B, int(page_size), width, pages, int(extra), int(packed), slot_map.shape[-1])
+    bufs = _TableBuffers(_ptr(new_len), _ptr(context_len), _ptr(block_table), _ptr(free_pages), _ptr(free_count), _ptr(out.context_len),
+                         _ptr(out.free_count), _ptr(slot_map), _ptr(out.granted), _ptr(out.offsets))
+    return _call("mpv_extend_tables", shape, bufs, out, dev, stream)
+
+
+def mpv_append_paths(tree_k, tree_v, cache_k, cache_v, slot_map, accept_len, path_nodes=None, stream=None):
+    """Moves the keys and values of the root and of the accepted path of every tree into the cache (see include/mpv.h), enqueued
+    on the current (or given) torch stream.
+
+    tree_k / tree_v [layers,B,N,kv_heads,head_dim] and cache_k / cache_v [layers,num_pages,page_size,kv_heads,head_dim], or all four
+    without the first dimension for one layer; slot_map int64 [B,n]; accept_len int32 [B] and path_nodes int32 [B,max_depth] as a
+    verification writes them (path_nodes=None: chains, nodes 1, 2, ...)."""
+    import torch
+    if tree_k.dim() == 4 and cache_k.dim() == 4:
+        tree_k, tree_v, cache_k, cache_v = (t.unsqueeze(0) for t in (tree_k, tree_v, cache_k, cache_v))
+    if tree_k.dim() != 5 or tree_v.dim() != 5 or cache_k.dim() != 5 or cache_v.dim() != 5 or slot_map.dim() != 2:
+        raise ValueError("tree_k, tree_v, cache_k and cache_v must all have a dimension of layers or all have none, slot_map is [B,n]")
+    layers, B, N, kv_heads, head_dim = tree_k.shape
+    num_pages, page_size = cache_k.shape[1], cache_k.shape[2]
+    dev = tree_k.device
+    _on_device(dev, tree_k=tree_k, tree_v=tree_v, cache_k=cache_k, cache_v=cache_v)
+    if any(t.dtype != tree_k.dtype for t in (tree_v, cache_k, cache_v)):
+        raise TypeError("tree_k, tree_v, cache_k and cache_v must have the same dtype")
+    dtype = _dtype_of(tree_k)
+    if tuple(tree_v.shape) != tuple(tree_k.shape) or tuple(cache_v.shape) != tuple(cache_k.shape) or cache_k.shape[0] != layers:
+        raise ValueError("keys and values must have the same shapes, tree and cache the same number of layers")
+    deep = path_nodes.shape[1] if path_nodes is not None and path_nodes.dim() == 2 else 0
+    _whole(dev, torch.int64, slot_map=(slot_map, (B, slot_map.shape[1])))
+    _whole(dev, torch.int32, accept_len=(accept_len, (B,)), path_nodes=(path_nodes, (B, deep)))
+    if layers == 0 or B == 0:
+        return
+    tree_stride = _row_stride("tree_k", tree_k[0], (B, N), (kv_heads, head_dim))
+    page_stride, slot_stride = _cache_strides(cache_k[0], cache_v[0], (num_pages, page_size, kv_heads, head_dim))
+    tree_layer, cache_layer = (t.stride(0) if layers > 1 else 0 for t in (tree_k, cache_k))
+    if (_row_stride("tree_v", tree_v[0], (B, N), (kv_heads, head_dim)) != tree_stride
+            or (layers > 1 and (tree_v.stride(0) != tree_layer or cache_v.stride(0) != cache_layer))):
+        raise ValueError("keys and values must have the same strides")
+    shape = _Append(layers, B, N, dtype, kv_heads * head_dim, deep, slot_map.shape[1], num_pages, page_size, tree_layer, tree_stride,
+                    cache_layer, page_stride, slot_stride)
+    bufs = _AppendBuffers(_ptr(tree_k), _ptr(tree_v), _ptr(cache_k), _ptr(cache_v), _ptr(slot_map), _ptr(accept_len), _ptr(path_nodes))
+    with torch.cuda.device(dev):
+        rc = load_library().mpv_append_paths(ctypes.byref(shape), ctypes.byref(bufs), _stream_ptr(stream))
+    if rc != 0:
+        raise MpvError(rc, "mpv_append_paths")
 
 
 MPV_KERNEL_NAMES = {0: "init", 1: "node_task", 2: "debug_stats"}

@@ -3570,15 +3570,15 @@ const char* mpv_strerror(int code) {
     switch (code) {
         case MPV_OK: return "success";
         case MPV_ERR_NULL: return "a required pointer is NULL";
-        case MPV_ERR_BAD_SHAPE: return "invalid B, N, V or max_depth smaller than the tree depth";
+        case MPV_ERR_BAD_SHAPE: return "invalid B, N, V or max_depth smaller than the tree depth, or another size or stride that cannot be";
         case MPV_ERR_BAD_TREE: return "invalid parent array (need parent[0] = -1 and 0 <= parent[n] < n)";
-        case MPV_ERR_BAD_TEMPERATURE: return "temperature must be a finite number > 0";
+        case MPV_ERR_BAD_TEMPERATURE: return "temperature must be a finite number > 0 (scale: finite)";
         case MPV_ERR_BAD_METHOD: return "unknown method id";
-        case MPV_ERR_BAD_DTYPE: return "unknown logit dtype";
+        case MPV_ERR_BAD_DTYPE: return "unknown dtype, or one that this call does not take";
         case MPV_ERR_WORKSPACE: return "workspace is NULL, not 256-byte aligned or too small";
         case MPV_ERR_UNSUPPORTED: return "problem exceeds MPV_MAX_NODES / MPV_MAX_CHILDREN / MPV_MAX_VOCAB, or a debug output this method does not provide was requested";
         case MPV_ERR_HIP: return "a HIP call failed (see mpv_last_hip_error)";
-        case MPV_ERR_ALIGNMENT: return "logit base pointers must be 16-byte aligned";
+        case MPV_ERR_ALIGNMENT: return "logit base pointers must be 16-byte aligned (other calls: a pointer, stride or row length is not aligned)";
         case MPV_ERR_BAD_TOP_P: return "top_p must lie in (0, 1]";
         default: return "unknown error code";
     }

@@ -1,0 +1,302 @@
+// Block tables and slot maps from request lengths, and the move of accepted rows into the paged cache: device and host code.
+
+#include "mpv_host.h"
+
+namespace mpv {
+
+// ------------------------------------------------------------------ tables
+
+constexpr int kPlanBlock = 1024;
+constexpr int kFillBlock = 256;
+constexpr int kFillSlots = 2048;           // slots of one workgroup of the fill kernel
+// Up to so many slots the plan's workgroup fills them itself, in one launch.
+constexpr int64_t kFillAtOnce = 4096;
+
+struct PlanEntry {                         // what the fill needs of a request
+    int32_t old, given;                    // cached tokens before the call, tokens placed (0 or more)
+    int32_t have;                          // pages before the call
+    int32_t top;                           // place in the list of free pages of its first new page; the next ones lie before it
+};
+
+struct TableArgs {
+    mpv_tables t;
+    mpv_table_buffers b;
+    PlanEntry* plan;                       // [B]
+};
+
+// Inclusive sum over the workgroup; *total gets the sum of all.  `part`: LDS of a value per wave.
+__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* part, int64_t* total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t o = __shfl_up(v, d);
+        if (lane >= d) v += o;
+    }
+    __syncthreads();
+    if (lane == 63) part[wave] = v;
+    __syncthreads();
+    int64_t before = 0, all = 0;
+    for (int w = 0; w < waves; ++w) {
+        if (w < wave) before += part[w];
+        all += part[w];
+    }
+    *total = all;
+    return v + before;
+}
+
+__device__ __forceinline__ void fill_slot(const TableArgs& a, int b, const PlanEntry& e, int i, int64_t* to) {
+    const int page_size = a.t.page_size;
+    int64_t slot = -1;
+    if (i < e.given) {
+        const int at = e.old + i, column = at / page_size, place = at - column * page_size;
+        int32_t* row = a.b.block_table + static_cast<int64_t>(b) * a.t.table_width;
+        int page;
+        if (column < e.have) {
+            page = row[column];
+        } else {
+            page = a.b.free_pages[e.top - (column - e.have)];
+            if (place == 0) row[column] = page;            // the page's first slot is always a new token's
+        }
+        if (page >= 0 && page < a.t.num_pages) slot = static_cast<int64_t>(page) * page_size + place;
+    }
+    *to = slot;
+}
+
+// One workgroup: who gets what (sums over the requests in their order), and the pages of finished requests.
+__global__ __launch_bounds__(kPlanBlock) void plan_tables_kernel(TableArgs a, int fill) {
+    __shared__ int64_t part[kPlanBlock / 64];
+    const int B = a.t.B, lane = threadIdx.x & 63;
+    const int64_t page_size = a.t.page_size, width = a.t.table_width;
+    const int count0 = min(max(a.b.free_count[0], 0), a.t.num_pages);
+    int64_t count = count0;
+    for (int base = 0; base < B; base += kPlanBlock) {
+        const int b = base + threadIdx.x;
+        int64_t back = 0;
+        if (b < B && a.b.new_len[b] < 0)
+            back = min((max(a.b.context_len[b], 0) + page_size - 1) / page_size, width);
+        int64_t total;
+        const int64_t begin = count + block_scan(back, part, &total) - back;
+        count += total;
+        for (uint64_t m = __ballot(back > 0); m; m &= m - 1) {
+            const int l = __ffsll(static_cast<unsigned long long>(m)) - 1;
+            const int64_t pages = __shfl(back, l), to = __shfl(begin, l);
+            const int32_t* row = a.b.block_table + (static_cast<int64_t>(b) - lane + l) * width;
+            for (int64_t i = lane; i < pages; i += 64)
+                if (to + i < a.t.num_pages) a.b.free_pages[to + i] = row[i];
+        }
+    }
+    count = min(count, static_cast<int64_t>(a.t.num_pages));
+    int64_t asked = 0, tokens = 0, placed = 0, taken = 0;          // sums over the requests before this round's
+    for (int base = 0; base < B; base += kPlanBlock) {
+        const int b = base + threadIdx.x;
+        int64_t old = 0, n = 0, have = 0, need = 0;
+        bool done = false, never = true;
+        if (b < B) {
+            const int64_t more = a.b.new_len[b];
+            old = max(a.b.context_len[b], 0);
+            done = more < 0;
+            n = done ? 0 : more + a.t.extra;
+            have = (old + page_size - 1) / page_size;
+            const int64_t want = (old + n + page_size - 1) / page_size;
+            never = done || want > width || (!a.t.packed && n > a.t.slot_width);
+            need = never ? 0 : want - have;
+        }
+        int64_t total;
+        const int64_t upto = asked + block_scan(need, part, &total);
+        asked += total;
+        const int64_t token = tokens + block_scan(never ? 0 : n, part, &total);
+        tokens += total;
+        const bool fits = !never && (need == 0 || upto <= count) && (!a.t.packed || n == 0 || token <= a.t.slot_width);
+        const int64_t given = fits ? n : 0;
+        const int64_t end = placed + block_scan(given, part, &total);
+        placed += total;
+        (void)block_scan(fits ? need : 0, part, &total);
+        taken += total;
+        if (b < B) {
+            a.b.granted[b] = static_cast<int32_t>(fits ? n : done ? 0 : -1);
+            a.b.context_len_out[b] = static_cast<int32_t>(done ? 0 : old + given);
+            if (a.b.offsets) a.b.offsets[b] = static_cast<int32_t>(end - given);
+            PlanEntry e;
+            e.old = static_cast<int32_t>(old);
+            e.given = static_cast<int32_t>(given);
+            e.have = static_cast<int32_t>(have);
+            e.top = static_cast<int32_t>(count - 1 - (upto - need));
+            a.plan[b] = e;
+        }
+    }
+    if (threadIdx.x == 0) {
+        a.b.free_count_out[0] = static_cast<int32_t>(count - taken);
+        if (a.b.offsets) a.b.offsets[B] = static_cast<int32_t>(placed);
+    }
+    if (!fill) return;
+    __syncthreads();
+    if (a.t.packed) {
+        for (int b = threadIdx.x >> 6; b < B; b += kPlanBlock / 64) {
+            const PlanEntry e = a.plan[b];
+            const int64_t begin = a.b.offsets[b];
+            for (int i = lane; i < e.given; i += 64) fill_slot(a, b, e, i, a.b.slot_map + begin + i);
+        }
+    } else {
+        const int slot_width = static_cast<int>(a.t.slot_width);
+        for (int x = threadIdx.x; x < B * slot_width; x += kPlanBlock) {
+            const int b = x / slot_width;
+            fill_slot(a, b, a.plan[b], x - b * slot_width, a.b.slot_map + x);
+        }
+    }
+}
+
+__global__ __launch_bounds__(kFillBlock) void fill_rows_kernel(TableArgs a) {
+    const int64_t slots = a.t.slot_width * a.t.B;
+    for (int64_t x = static_cast<int64_t>(blockIdx.x) * kFillSlots + threadIdx.x, j = 0; j < kFillSlots / kFillBlock; ++j, x += kFillBlock)
+        if (x < slots) {
+            const int b = static_cast<int>(x / a.t.slot_width);
+            fill_slot(a, b, a.plan[b], static_cast<int>(x - b * a.t.slot_width), a.b.slot_map + x);
+        }
+}
+
+// Requests of a workgroup's slots: the number of requests that end at or before the first of them, found by counting, then a
+// search between there and the last.
+__global__ __launch_bounds__(kFillBlock) void fill_packed_kernel(TableArgs a) {
+    __shared__ int lo_hi[2];
+    const int B = a.t.B;
+    const int64_t total = a.b.offsets[B];
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * kFillSlots;
+    if (first >= total) return;
+    const int64_t last = min(first + kFillSlots, total) - 1;
+    if (threadIdx.x < 2) lo_hi[threadIdx.x] = 0;
+    __syncthreads();
+    int lo = 0, hi = 0;
+    for (int b = threadIdx.x; b < B; b += kFillBlock) {
+        const int end = a.b.offsets[b + 1];
+        lo += end <= first;
+        hi += end <= last;
+    }
+    for (int d = 32; d; d >>= 1) { lo += __shfl_xor(lo, d); hi += __shfl_xor(hi, d); }
+    if ((threadIdx.x & 63) == 0) { atomicAdd(&lo_hi[0], lo); atomicAdd(&lo_hi[1], hi); }
+    __syncthreads();
+    for (int64_t x = first + threadIdx.x; x <= last; x += kFillBlock) {
+        int l = lo_hi[0], h = lo_hi[1];                     // the request lies in [l, h]
+        while (l < h) {
+            const int m = (l + h) >> 1;
+            if (a.b.offsets[m + 1] <= x) l = m + 1; else h = m;
+        }
+        fill_slot(a, l, a.plan[l], static_cast<int>(x - a.b.offsets[l]), a.b.slot_map + x);
+    }
+}
+
+// ------------------------------------------------------------------ append
+
+constexpr int kAppendBlock = 256;
+constexpr int kAppendLayers = 8;           // layers of one workgroup
+
+struct AppendArgs {
+    mpv_append p;
+    mpv_append_buffers b;
+    int rows;                              // rows a tree can have: what slot_map, path_nodes and N allow
+    int bytes;                             // of an element
+};
+
+// A workgroup moves one row of one tree, keys and values, for kAppendLayers layers; a wave takes a (layer, keys or values) at a time.
+__global__ __launch_bounds__(kAppendBlock) void append_kernel(AppendArgs a) {
+    const int b = blockIdx.x / a.rows, i = blockIdx.x - b * a.rows;
+    if (i > a.b.accept_len[b]) return;
+    int node = i;
+    if (i > 0 && a.b.path_nodes) node = a.b.path_nodes[static_cast<int64_t>(b) * a.p.max_depth + i - 1];
+    const int64_t slot = a.b.slot_map[static_cast<int64_t>(b) * a.p.slot_width + i];
+    const int64_t page = slot / a.p.page_size;
+    if (slot < 0 || page >= a.p.num_pages || node < 0 || node >= a.p.N) return;
+    const int64_t from = (static_cast<int64_t>(b) * a.p.N + node) * a.p.tree_stride;
+    const int64_t to = page * a.p.page_stride + (slot - page * a.p.page_size) * a.p.slot_stride;
+    const int vectors = a.p.row * a.bytes / 16, lane = threadIdx.x & 63;
+    const int layer0 = blockIdx.y * kAppendLayers;
+    const int layers = min(kAppendLayers, a.p.layers - layer0);
+    for (int j = threadIdx.x >> 6; j < 2 * layers; j += kAppendBlock / 64) {
+        const int64_t layer = layer0 + (j >> 1);
+        const char* src = static_cast<const char*>(j & 1 ? a.b.tree_v : a.b.tree_k) + (layer * a.p.tree_layer_stride + from) * a.bytes;
+        char* dst = static_cast<char*>(j & 1 ? a.b.cache_v : a.b.cache_k) + (layer * a.p.cache_layer_stride + to) * a.bytes;
+        for (int x = lane; x < vectors; x += 64) reinterpret_cast<uint4*>(dst)[x] = reinterpret_cast<const uint4*>(src)[x];
+    }
+}
+
+static int check_tables(const mpv_tables* t) {
+    if (!t) return MPV_ERR_NULL;
+    if (t->B < 0 || t->page_size < 1 || t->table_width < 0 || t->num_pages < 0 || t->extra < 0 || t->slot_width < 0 ||
+        (t->packed != 0 && t->packed != 1))
+        return MPV_ERR_BAD_SHAPE;
+    // positions, tokens and slots are counted in 32 bits on the device, sums of them in 64
+    if (span(0, t->table_width, t->page_size) > INT32_MAX || span(0, t->packed ? 1 : t->B, t->slot_width) > INT32_MAX ||
+        t->B > (1 << 30))
+        return MPV_ERR_UNSUPPORTED;
+    return MPV_OK;
+}
+
+}  // namespace mpv
+
+extern "C" {
+
+int mpv_extend_tables_workspace_bytes(const mpv_tables* tables, size_t* out) {
+    if (!out) return MPV_ERR_NULL;
+    const int rc = mpv::check_tables(tables);
+    if (rc != MPV_OK) return rc;
+    *out = (static_cast<size_t>(tables->B) * sizeof(mpv::PlanEntry) + 255) / 256 * 256;
+    return MPV_OK;
+}
+
+int mpv_extend_tables(const mpv_tables* tables, const mpv_table_buffers* buf, void* workspace, size_t workspace_bytes,
+                      void* hip_stream) {
+    size_t need;
+    const int rc = mpv_extend_tables_workspace_bytes(tables, &need);
+    if (rc != MPV_OK) return rc;
+    if (!buf) return MPV_ERR_NULL;
+    if (tables->B == 0) return MPV_OK;
+    if (!buf->new_len || !buf->context_len || !buf->free_count || !buf->context_len_out || !buf->free_count_out || !buf->granted ||
+        (!buf->block_table && tables->table_width > 0) || (!buf->free_pages && tables->num_pages > 0) ||
+        (!buf->slot_map && tables->slot_width > 0) || (!buf->offsets && tables->packed))
+        return MPV_ERR_NULL;
+    if (!workspace || !mpv::aligned(workspace, 256) || workspace_bytes < need) return MPV_ERR_WORKSPACE;
+    mpv::TableArgs a;
+    a.t = *tables; a.b = *buf; a.plan = static_cast<mpv::PlanEntry*>(workspace);
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    const int64_t slots = tables->slot_width * (tables->packed ? 1 : tables->B);
+    const int fill = slots <= mpv::kFillAtOnce;
+    (void)hipGetLastError();
+    hipLaunchKernelGGL(mpv::plan_tables_kernel, dim3(1), dim3(mpv::kPlanBlock), 0, s, a, fill);
+    if (!fill) {
+        const dim3 grid(static_cast<unsigned>((slots + mpv::kFillSlots - 1) / mpv::kFillSlots));
+        if (tables->packed) hipLaunchKernelGGL(mpv::fill_packed_kernel, grid, dim3(mpv::kFillBlock), 0, s, a);
+        else hipLaunchKernelGGL(mpv::fill_rows_kernel, grid, dim3(mpv::kFillBlock), 0, s, a);
+    }
+    return mpv::launched();
+}
+
+int mpv_append_paths(const mpv_append* p, const mpv_append_buffers* buf, void* hip_stream) {
+    if (!p || !buf) return MPV_ERR_NULL;
+    if (p->layers < 0 || p->B < 0 || p->N < 1 || p->row < 1 || p->max_depth < 0 || p->slot_width < 0 || p->num_pages < 0 || p->page_size < 1)
+        return MPV_ERR_BAD_SHAPE;
+    if (!mpv::known_dtype(p->dtype)) return MPV_ERR_BAD_DTYPE;
+    if (p->N > MPV_MAX_NODES || p->row > (1 << 24)) return MPV_ERR_UNSUPPORTED;
+    mpv::AppendArgs a;
+    a.p = *p; a.b = *buf; a.bytes = mpv::elem_bytes(p->dtype);
+    const int64_t most = buf->path_nodes ? static_cast<int64_t>(p->max_depth) + 1 : p->N;
+    a.rows = static_cast<int>(most < p->slot_width ? most : p->slot_width);
+    if (p->layers == 0 || p->B == 0 || a.rows == 0 || p->num_pages == 0) return MPV_OK;
+    // a row must not reach into the next one
+    if (p->tree_stride < p->row || p->slot_stride < p->row || (p->layers > 1 && (p->tree_layer_stride < 0 || p->cache_layer_stride < 0)) ||
+        p->page_stride < 0)
+        return MPV_ERR_BAD_SHAPE;
+    const int64_t layers = (p->layers + mpv::kAppendLayers - 1) / mpv::kAppendLayers;
+    if (layers > 65535 || static_cast<int64_t>(p->B) * a.rows > INT32_MAX || mpv::span(0, p->num_pages, p->page_size) == INT64_MAX ||
+        mpv::span(0, mpv::span(mpv::span(0, p->layers, p->tree_layer_stride), static_cast<int64_t>(p->B) * p->N, p->tree_stride), 4) == INT64_MAX ||
+        mpv::span(0, mpv::span(mpv::span(mpv::span(0, p->layers, p->cache_layer_stride), p->num_pages, p->page_stride), p->page_size, p->slot_stride), 4) == INT64_MAX)
+        return MPV_ERR_UNSUPPORTED;
+    if (!buf->tree_k || !buf->tree_v || !buf->cache_k || !buf->cache_v || !buf->slot_map || !buf->accept_len) return MPV_ERR_NULL;
+    const int64_t strides = p->row | p->tree_stride | p->slot_stride | p->page_stride | (p->layers > 1 ? p->tree_layer_stride | p->cache_layer_stride : 0);
+    if (!mpv::aligned(buf->tree_k, 16) || !mpv::aligned(buf->tree_v, 16) || !mpv::aligned(buf->cache_k, 16) || !mpv::aligned(buf->cache_v, 16) ||
+        (strides * a.bytes) % 16 != 0)
+        return MPV_ERR_ALIGNMENT;
+    (void)hipGetLastError();
+    hipLaunchKernelGGL(mpv::append_kernel, dim3(static_cast<unsigned>(p->B * a.rows), static_cast<unsigned>(layers)), dim3(mpv::kAppendBlock),
+                       0, static_cast<hipStream_t>(hip_stream), a);
+    return mpv::launched();
+}
+
+}  // extern "C"
