@@ -27,7 +27,8 @@ UNITS = {
     # the task loops are long and cold: loop-invariant constants hoisted out of them would be
     # held in registers across whole tasks and push the kept row pair into scratch memory
     "mpv.hip": ["-mllvm", "-disable-machine-licm"],
-    "mpv_attention.hip": [],
+    # (so are the paths of a tile that few tiles take)
+    "mpv_attention.hip": ["-mllvm", "-disable-machine-licm"],
     "mpv_chains.hip": [],
     "mpv_cache.hip": [],
 }

@@ -1,7 +1,20 @@
 // Attention of draft-tree nodes over a paged cache: device and host code.
+//
+// With s the scaled products of a query with the keys it sees, out = sum_j e^(s_j - m) v_j / sum_j e^(s_j - m), in one pass over the
+// keys with a running reference m (log2 units).  The work is cut into tiles of kTile keys; the rows (node, query head) that share a
+// cache head, kRows of them, are a unit, and a unit's tiles are its part of the sinks, of the window (or the whole context), and
+// of the tree.  All tiles of all units form one list, which is divided evenly among the workgroups, whatever the lengths
+// of the contexts: a workgroup carries on across units, and a unit that several workgroups share is put together by
+// combine_kernel from their partial sums.
+//
+// A tile of keys and values goes straight from memory to LDS (16 bytes a lane), a tile ahead of the one that is worked on.
+//   products    S^T = K Q^T: keys are the rows of the matrix instruction's first operand, read from LDS; queries stay in registers
+//   weights     lane l then holds 4 consecutive keys for query l % 16: the statistics of a query lie in 4 lanes, and the weights are
+//               where the second product wants them (the order of keys within an instruction does not matter if both operands have it)
+//   out^T = V^T W^T   16-bit values come out of LDS transposed (ds_read_b64_tr_b16), float32 ones are read a value a lane
+// Rows of a tile lie in LDS with their 16-byte chunks exchanged by row, so that 16 rows' equal chunks lie in different banks.
 
-#include <hip/hip_bf16.h>
-#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
 
 #include <cmath>
 #include <cstring>
@@ -14,94 +27,824 @@ struct AttentionArgs {
     mpv_attention a;
     mpv_attention_buffers b;
     int8_t parent[MPV_MAX_NODES];          // the shared shape (without tree_parent)
+    int workgroups;
+    int blocks;                            // row blocks of the largest tree
+    float factor;                          // |scale| log2(e): products to exponents (1 where the scale is 0)
+    int sign;                              // of the scale: -1, 0, 1
+    float* partial;                        // [workgroups][2][rows][columns]
+    float2* partial_stats;                 // [workgroups][2][rows]: reference, sum of weights
+    int4* split;                           // [workgroups]: tree, cache head, row block, last workgroup of a unit that begins there and
+                                           // is shared; x < 0: none
 };
 
-__device__ __forceinline__ float value(const float* p, int64_t i) { return p[i]; }
-__device__ __forceinline__ float value(const uint16_t* p, int64_t i) { return __uint_as_float(static_cast<uint32_t>(p[i]) << 16); }
-__device__ __forceinline__ float value(const __half* p, int64_t i) { return __half2float(p[i]); }
-__device__ __forceinline__ void store(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store(uint16_t* p, float v) {
-    const __hip_bfloat16 h = __float2bfloat16(v);
-    *reinterpret_cast<__hip_bfloat16*>(p) = h;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(4))) short i16x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
+template <int DTYPE> struct Elem;
+template <> struct Elem<MPV_DTYPE_F32> {
+    typedef float T;
+    static constexpr int kBytes = 4;
+    static constexpr float kBias = 0.0f;
+    static __device__ __forceinline__ void put4(char* to, const f32x4& v) { *reinterpret_cast<f32x4*>(to) = v; }
+};
+template <> struct Elem<MPV_DTYPE_BF16> {
+    typedef __bf16 T;
+    typedef bf16x8 Vec;
+    static constexpr int kBytes = 2;
+    static constexpr float kBias = 0.0f;
+    static constexpr uint32_t kInf = 0x7f80;
+    static __device__ __forceinline__ f32x4 mfma(const u32x4& a, const u32x4& b, const f32x4& c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ void put4(char* to, const f32x4& v) {
+        typedef __attribute__((ext_vector_type(4))) __bf16 x4;
+        x4 r;
+        for (int i = 0; i < 4; ++i) r[i] = static_cast<__bf16>(v[i]);
+        *reinterpret_cast<x4*>(to) = r;
+    }
+};
+template <> struct Elem<MPV_DTYPE_F16> {
+    typedef _Float16 T;
+    typedef f16x8 Vec;
+    static constexpr int kBytes = 2;
+    static constexpr float kBias = 6.0f;   // weights are kept 2^6 times as large, so that the small ones stay normal numbers
+    static constexpr uint32_t kInf = 0x7c00;
+    static __device__ __forceinline__ f32x4 mfma(const u32x4& a, const u32x4& b, const f32x4& c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ void put4(char* to, const f32x4& v) {
+        typedef __attribute__((ext_vector_type(4))) _Float16 x4;
+        x4 r;
+        for (int i = 0; i < 4; ++i) r[i] = static_cast<_Float16>(v[i]);
+        *reinterpret_cast<x4*>(to) = r;
+    }
+};
+
+// What an invalid key's row is read from.
+__device__ const uint4 kZeros = {0u, 0u, 0u, 0u};
+
+__device__ __forceinline__ void to_lds(const void* from, void* to) {      // 16 bytes a lane; `to`: the wave's first lane's
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
-__device__ __forceinline__ void store(__half* p, float v) { *p = __float2half(v); }
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ unsigned long long shfl64(unsigned long long v, int lane) {
+    const uint32_t lo = __shfl(static_cast<uint32_t>(v), lane), hi = __shfl(static_cast<uint32_t>(v >> 32), lane);
+    return static_cast<unsigned long long>(hi) << 32 | lo;
+}
 
-// A wave per (tree, node, head): 64 keys at a time, a lane each; then the lanes share the values' columns.
-template <class T>
-__global__ __launch_bounds__(64) void tree_attention_kernel(AttentionArgs g) {
+constexpr int kTableChunk = 1024;          // entries of a block table kept in LDS
+// The reference of a softmax moves only where a product exceeds it by more than this (log2 units): weights are at most 2^8.
+constexpr float kSlack = 8.0f;
+
+// A tree's part of the list of tiles.
+struct TreeWork {
+    int context, nodes;
+    int sink_tiles, low, context_tiles;    // tiles of the sinks, first position (a whole tile) of the rest, its tiles
+    int tiles;                             // of a unit, the tree's own among them
+    int blocks;                            // row blocks
+};
+
+template <int TILE, int ROWS>
+__device__ __forceinline__ TreeWork tree_work(const AttentionArgs& g, int b) {
+    TreeWork t;
     const mpv_attention& a = g.a;
-    const int lane = threadIdx.x;
-    const int h = blockIdx.x % a.heads, n = blockIdx.x / a.heads, b = blockIdx.y;
-    const int nodes = g.b.num_nodes ? min(max(g.b.num_nodes[b], 0), a.N) : a.N;
-    if (n >= nodes) return;
-    auto parent_of = [&](int m) {
-        const int p = g.b.tree_parent ? g.b.tree_parent[static_cast<int64_t>(b) * a.N + m] : g.parent[m];
-        return p >= 0 && p < m ? p : -1;
-    };
-    unsigned long long line = 0;                              // ancestors and the node itself
-    for (int m = n; m >= 0; m = parent_of(m)) line |= 1ull << m;
-    const int depth = __popcll(line) - 1;
-    const int64_t context = min(static_cast<int64_t>(max(g.b.context_len[b], 0)), static_cast<int64_t>(a.table_width) * a.page_size);
-    const int64_t at = context + depth;
-    const int64_t low = a.window > 0 ? at - a.window + 1 : 0;
-    const int64_t tree = static_cast<int64_t>(b) * a.N;
-    const int kv = h / (a.heads / a.kv_heads);
-    const T* q = static_cast<const T*>(g.b.q) + (tree + n) * a.q_stride + static_cast<int64_t>(h) * a.head_dim;
-    float top = -INFINITY, sum = 0.0f, out[MPV_MAX_HEAD_DIM / 64] = {};
+    t.context = min(max(g.b.context_len[b], 0), a.table_width * a.page_size);
+    t.nodes = g.b.num_nodes ? min(max(g.b.num_nodes[b], 0), a.N) : a.N;
+    t.low = t.sink_tiles = 0;
+    if (a.window > 0) {
+        t.low = max(0, t.context - a.window + 1) / TILE * TILE;
+        t.sink_tiles = (min(max(a.sinks, 0), t.low) + TILE - 1) / TILE;
+    }
+    t.context_tiles = (t.context - t.low + TILE - 1) / TILE;
+    t.tiles = t.sink_tiles + t.context_tiles + (t.nodes + TILE - 1) / TILE;
+    t.blocks = (t.nodes * (a.heads / a.kv_heads) + ROWS - 1) / ROWS;
+    return t;
+}
 
-    auto take = [&](bool seen, const T* k, const T* v) {      // 64 keys
-        float s = -INFINITY;
-        if (seen) {
-            s = 0.0f;
-            for (int d = 0; d < a.head_dim; ++d) s += value(q, d) * value(k, d);
-            s *= a.scale;
-        }
-        float m = s;
-        for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
-        const float now = fmaxf(top, m), base = now == -INFINITY ? 0.0f : now;
-        const float fade = expf(top - base);
-        const float w = seen ? expf(s - base) : 0.0f;
-        top = now;
-        sum *= fade;
-        for (int c = 0; c < MPV_MAX_HEAD_DIM / 64; ++c) out[c] *= fade;
-        float all = w;
-        for (int x = 32; x; x >>= 1) all += __shfl_xor(all, x);
-        sum += all;
-        for (unsigned long long m2 = __ballot(seen); m2; m2 &= m2 - 1) {
-            const int l = __ffsll(m2) - 1;
-            const float wl = __shfl(w, l);
-            const T* vl = reinterpret_cast<const T*>(__shfl(reinterpret_cast<unsigned long long>(v), l));
-            for (int c = 0; c < MPV_MAX_HEAD_DIM / 64; ++c)
-                if (lane + 64 * c < a.head_dim) out[c] += wl * value(vl, lane + 64 * c);
-        }
+// DTYPE; DP: columns of a row in LDS (head_dim, rounded up); QT: 16-row groups of a wave; WQ: waves side by side over the rows;
+// WK: waves side by side over a tile's keys; TILE: keys.
+template <int DTYPE, int DP, int QT, int WQ, int WK, int TILE>
+struct Attention {
+    typedef Elem<DTYPE> E;
+    static constexpr int kWaves = WQ * WK;
+    static constexpr int kThreads = 64 * kWaves;
+    static constexpr int kRows = 16 * QT * WQ;
+    static constexpr int kChunks = DP * E::kBytes / 16;            // 16-byte chunks of a row
+    static constexpr int kSteps = kChunks / 4;                     // of the first product: 4 chunks of every row
+    static constexpr int kKeys = TILE / WK;                        // of a wave
+    static constexpr int kGroups = kKeys / 16;
+    static constexpr int kColumns = DP / 16;                       // 16-column groups of the output
+    static constexpr int kTileBytes = TILE * DP * E::kBytes;
+    static constexpr int kRowsPerLoad = 64 / kChunks;              // rows that a wave's load brings
+    static constexpr int kLoads = TILE / kRowsPerLoad;             // of keys; as many of values
+    static constexpr int kMyLoads = (kLoads + kWaves - 1) / kWaves;
+    static constexpr int kTile = TILE;
+    static constexpr bool k16 = E::kBytes == 2;
+    static_assert(kChunks >= 8 && kChunks <= 64 && kMyLoads * kRowsPerLoad <= 64 && kKeys % (k16 ? 32 : 16) == 0 && kGroups * 4 <= 32, "tile");
+
+    struct Shared {
+        __align__(16) char keys[2][kTileBytes];
+        __align__(16) char values[2][kTileBytes];
+        int table[kTableChunk];
+        __align__(4) uint8_t seen[2][TILE];                        // whether anybody sees the key
+        int hidden[2][kWaves];                                     // whether a wave found one that nobody sees
+        int spoiled;                                               // whether a tile held values that are no numbers, see spoil
+        int64_t sum[kWaves];
     };
 
-    const int64_t sinks = a.window > 0 ? min(static_cast<int64_t>(max(a.sinks, 0)), context) : 0;
-    for (int64_t base = 0; base < context; base += 64) {
-        if (base >= sinks && base + 64 <= low) base = low / 64 * 64;     // nothing is seen between the sinks and the window
-        if (base >= context) break;
-        const int64_t j = base + lane;
-        bool seen = j < context && (j >= low || j < sinks);
-        const T *k = nullptr, *v = nullptr;
-        if (seen) {
-            const int64_t page = g.b.block_table[static_cast<int64_t>(b) * a.table_width + j / a.page_size];
-            seen = page >= 0 && page < a.num_pages;
-            const int64_t where = page * a.page_stride + j % a.page_size * a.slot_stride + static_cast<int64_t>(kv) * a.head_dim;
-            k = static_cast<const T*>(g.b.cache_k) + where;
-            v = static_cast<const T*>(g.b.cache_v) + where;
+    // A tile: positions of the cache from `base` on, or nodes.
+    struct Tile { int base; bool tree; };
+
+    const AttentionArgs& g;
+    Shared& sh;
+    const int lane, wave, l16, quad, wq, wk;
+    // the unit
+    int b, kv;
+    TreeWork t;
+    int table_first = -1;                                          // first column of sh.table; -1: none
+
+    __device__ Attention(const AttentionArgs& args, Shared& s)
+        : g(args), sh(s), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), l16(lane & 15), quad(lane >> 4),
+          wq(wave % WQ), wk(wave / WQ) {}
+
+    static __device__ __forceinline__ int swizzle(int row) { return kChunks >= 16 ? row & 15 : (row >> 1) & 7; }
+
+    __device__ __forceinline__ Tile tile_at(int i) const {
+        Tile x;
+        x.tree = i >= t.sink_tiles + t.context_tiles;
+        x.base = i < t.sink_tiles ? i * TILE : x.tree ? (i - t.sink_tiles - t.context_tiles) * TILE : t.low + (i - t.sink_tiles) * TILE;
+        return x;
+    }
+
+    // The block table's entries that a tile of the cache needs are in LDS afterwards.  Every wave calls it.
+    __device__ __forceinline__ void have_table(const Tile& x) {
+        if (x.tree) return;
+        const int first = x.base / g.a.page_size, last = (min(x.base + TILE, t.context) - 1) / g.a.page_size;
+        if (table_first >= 0 && first >= table_first && last < table_first + kTableChunk) return;
+        __syncthreads();                                           // nobody reads the old ones any more
+        const int32_t* row = g.b.block_table + static_cast<int64_t>(b) * g.a.table_width;
+        for (int i = threadIdx.x; i < kTableChunk; i += kThreads) sh.table[i] = first + i < g.a.table_width ? row[first + i] : -1;
+        table_first = first;
+        __syncthreads();
+    }
+
+    // Asks for a tile.  A key that nobody sees is read as zeros.
+    __device__ __forceinline__ void ask(const Tile& x, int stage) {
+        // lane i finds out where the i-th of this wave's rows lies
+        const int mine = (wave + kWaves * (lane / kRowsPerLoad)) * kRowsPerLoad + lane % kRowsPerLoad;
+        const int at = x.base + mine;
+        bool seen = mine < TILE && lane < kMyLoads * kRowsPerLoad;
+        int64_t offset = 0;
+        const char *keys, *values;
+        if (x.tree) {
+            seen = seen && at < t.nodes;
+            offset = (static_cast<int64_t>(b) * g.a.N + at) * g.a.kv_stride;
+            keys = static_cast<const char*>(g.b.tree_k);
+            values = static_cast<const char*>(g.b.tree_v);
+        } else {
+            seen = seen && at < t.context && (g.a.window <= 0 || at > t.context - g.a.window || at < g.a.sinks);
+            if (seen) {
+                const int column = at / g.a.page_size, page = sh.table[column - table_first];
+                seen = page >= 0 && page < g.a.num_pages;
+                offset = page * g.a.page_stride + (at - column * g.a.page_size) * g.a.slot_stride;
+            }
+            keys = static_cast<const char*>(g.b.cache_k);
+            values = static_cast<const char*>(g.b.cache_v);
         }
-        take(seen, k, v);
+        offset = seen ? (offset + static_cast<int64_t>(kv) * g.a.head_dim) * E::kBytes : -1;
+        const bool mine_real = mine < TILE && lane < kMyLoads * kRowsPerLoad;
+        if (mine_real) sh.seen[stage][mine] = seen;
+        const bool any_hidden = __ballot(mine_real && !seen) != 0;
+        if (lane == 0) sh.hidden[stage][wave] = any_hidden;
+#pragma unroll
+        for (int j = 0; j < kMyLoads; ++j) {
+            const int load = wave + kWaves * j;
+            if (kLoads % kWaves == 0 || load < kLoads) {
+                const int row = load * kRowsPerLoad + lane / kChunks;
+                const int chunk = (lane % kChunks) ^ swizzle(row);
+                const int64_t from = static_cast<int64_t>(shfl64(static_cast<unsigned long long>(offset), j * kRowsPerLoad + lane / kChunks));
+                const bool real = from >= 0 && chunk * 16 < g.a.head_dim * E::kBytes;
+                const int64_t place = from + chunk * 16;
+                to_lds(real ? keys + place : reinterpret_cast<const char*>(&kZeros), sh.keys[stage] + load * 1024);
+                to_lds(real ? values + place : reinterpret_cast<const char*>(&kZeros), sh.values[stage] + load * 1024);
+            }
+        }
     }
-    {
-        bool seen = lane < nodes && ((line >> lane) & 1);
-        const int64_t place = context + __popcll(line & ((1ull << lane) - 1));
-        seen = seen && (place >= low || place < max(a.sinks, 0));
-        const int64_t where = (tree + lane) * a.kv_stride + static_cast<int64_t>(kv) * a.head_dim;
-        take(seen, static_cast<const T*>(g.b.tree_k) + where, static_cast<const T*>(g.b.tree_v) + where);
+
+    // Waits until the tile before the last one that was asked for (ahead) or the last one is there, for all waves.
+    __device__ __forceinline__ void arrive(bool ahead) {
+        if (!ahead) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        else if (kLoads % kWaves == 0 || wave < kLoads % kWaves) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kMyLoads) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kMyLoads - 2) : "memory");
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
-    T* to = static_cast<T*>(g.b.out) + (tree + n) * a.out_stride + static_cast<int64_t>(h) * a.head_dim;
-    for (int c = 0; c < MPV_MAX_HEAD_DIM / 64; ++c)
-        if (lane + 64 * c < a.head_dim) store(to + lane + 64 * c, out[c] / sum);
+    // All waves are done with what they read.
+    __device__ __forceinline__ void leave() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+    // ---- the rows of this lane's queries
+    u32x4 query[QT][kSteps];
+    unsigned long long line[QT];                                   // the node and its ancestors
+    int low[QT];                                                   // first position seen (but for the sinks)
+    f32x4 out[QT][kColumns];
+    float top[QT], weight[QT];                                     // reference; sum of weights (this lane's keys)
+
+    __device__ __forceinline__ void begin(int block) {
+        const int group = g.a.heads / g.a.kv_heads;
+        // ancestors of node `lane`: in each round twice as many steps up
+        unsigned long long mask = 1ull << lane;
+        int up = -1;
+        if (lane < t.nodes) {
+            up = g.b.tree_parent ? g.b.tree_parent[static_cast<int64_t>(b) * g.a.N + lane] : g.parent[lane];
+            if (up >= lane) up = -1;
+        }
+        for (int round = 0; round < 6 && __ballot(up >= 0); ++round) {
+            const unsigned long long theirs = shfl64(mask, max(up, 0));
+            const int further = __shfl(up, max(up, 0));
+            if (up >= 0) { mask |= theirs; up = further; }
+        }
+#pragma unroll
+        for (int q = 0; q < QT; ++q) {
+            const int row = block * kRows + (wq * QT + q) * 16 + l16;
+            const int node = row / group;
+            const bool real = node < t.nodes;
+            line[q] = shfl64(mask, real ? node : 0);
+            low[q] = g.a.window > 0 ? t.context + __popcll(line[q]) - g.a.window : INT32_MIN;
+            const char* from = static_cast<const char*>(g.b.q) +
+                ((static_cast<int64_t>(b) * g.a.N + node) * g.a.q_stride + static_cast<int64_t>(kv * group + row - node * group) * g.a.head_dim) * E::kBytes;
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                const int chunk = s * 4 + quad;
+                u32x4 v = {0u, 0u, 0u, 0u};
+                if (real && chunk * 16 < g.a.head_dim * E::kBytes && g.sign != 0) v = *reinterpret_cast<const u32x4*>(from + chunk * 16);
+                if (g.sign < 0) v ^= k16 ? 0x80008000u : 0x80000000u;
+                query[q][s] = v;
+            }
+            top[q] = -INFINITY;
+            weight[q] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < kColumns; ++c) out[q][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+
+    // A tile in LDS: products, weights, and their sum over the values.
+    __device__ __forceinline__ void work(const Tile& x, int stage) {
+        const char* keys = sh.keys[stage] + wk * kKeys * kChunks * 16;
+        char* values = sh.values[stage] + wk * kKeys * kChunks * 16;
+        f32x4 s[QT][kGroups];
+        const int key_swizzle = swizzle(l16);
+#pragma unroll
+        for (int k = 0; k < kGroups; ++k) {
+#pragma unroll
+            for (int q = 0; q < QT; ++q) s[q][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int d = 0; d < kSteps; ++d) {
+                const u32x4 a = *reinterpret_cast<const u32x4*>(keys + ((k * 16 + l16) * kChunks + ((d * 4 + quad) ^ key_swizzle)) * 16);
+#pragma unroll
+                for (int q = 0; q < QT; ++q) {
+                    if constexpr (k16) {
+                        s[q][k] = E::mfma(a, query[q][d], s[q][k]);
+                    } else {
+                        const f32x4 fa = __builtin_bit_cast(f32x4, a), fq = __builtin_bit_cast(f32x4, query[q][d]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s[q][k] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[i], fq[i], s[q][k], 0, 0, 0);
+                    }
+                }
+            }
+        }
+        // ---- what is not seen
+        const bool differ = differs(x);
+        bool hidden = x.tree || differ;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) hidden = hidden || sh.hidden[stage][w];
+        if (hidden) {
+#pragma unroll
+            for (int k = 0; k < kGroups; ++k) {
+                const int key = wk * kKeys + k * 16 + quad * 4;
+                const uint32_t there = *reinterpret_cast<const uint32_t*>(&sh.seen[stage][key]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int q = 0; q < QT; ++q)
+                        if (!(there >> (8 * i) & 1) || !sees(x, key + i, q)) s[q][k][i] = -INFINITY;
+            }
+            // a value that is no number must not reach the nodes that do not see it
+            if (differ && !all_numbers(values)) {
+                only_numbers(values);
+                sh.spoiled = 1;
+            }
+        }
+        // ---- references
+#pragma unroll
+        for (int q = 0; q < QT; ++q) {
+            float most = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < kGroups; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) most = fmaxf(most, s[q][k][i]);
+            most *= g.factor;
+            if (__ballot(most > top[q] + kSlack)) {
+                most = fmaxf(most, __shfl_xor(most, 16));
+                most = fmaxf(most, __shfl_xor(most, 32));
+                const float now = fmaxf(top[q], most);
+                const float fade = now == -INFINITY ? 1.0f : exp2_of(top[q] - now);
+                top[q] = now;
+                weight[q] *= fade;
+#pragma unroll
+                for (int c = 0; c < kColumns; ++c) out[q][c] *= fade;
+            }
+        }
+        // ---- weights
+        u32x4 w16[QT][k16 ? kGroups / 2 : 1];
+#pragma unroll
+        for (int q = 0; q < QT; ++q) {
+            const float base = top[q] == -INFINITY ? 0.0f : E::kBias - top[q];
+            float sum = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kGroups; ++k) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[q][k][i] = exp2_of(fmaf(s[q][k][i], g.factor, base));
+                    sum += s[q][k][i];
+                }
+                if constexpr (k16) {
+                    typedef __attribute__((ext_vector_type(4))) typename E::T x4;
+                    x4 r;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) r[i] = static_cast<typename E::T>(s[q][k][i]);
+                    const uint2 p = __builtin_bit_cast(uint2, r);
+                    w16[q][k / 2][(k & 1) * 2] = p.x;
+                    w16[q][k / 2][(k & 1) * 2 + 1] = p.y;
+                }
+            }
+            weight[q] += sum;
+        }
+        // ---- their sum over the values
+#pragma unroll
+        for (int c = 0; c < kColumns; ++c) {
+            if constexpr (k16) {
+#pragma unroll
+                for (int k = 0; k < kGroups / 2; ++k) {
+                    const u32x4 v = column16(values, k, c);
+#pragma unroll
+                    for (int q = 0; q < QT; ++q) out[q][c] = E::mfma(v, w16[q][k], out[q][c]);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < kGroups; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float v = column32(values, k * 16 + quad * 4 + i, c);
+#pragma unroll
+                        for (int q = 0; q < QT; ++q) out[q][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[q][k][i], out[q][c], 0, 0, 0);
+                    }
+            }
+        }
+    }
+
+    // Keys 32 k + 4 quad .. + 3 and 32 k + 16 + 4 quad .. + 3 of column 16 c + l16.
+    __device__ __forceinline__ u32x4 column16(const char* values, int k, int c) const {
+        u32x4 v;
+        const int row = quad * 4 + (l16 >> 2);
+        const int in_row = ((c * 2 + ((l16 & 3) >> 1)) ^ swizzle(row)) * 16 + (l16 & 1) * 8;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            typedef __attribute__((address_space(3))) i16x4 lds_x4;
+            const char* from = values + (k * 32 + h * 16 + row) * kChunks * 16 + in_row;
+            const uint2 r = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_x4*)from));
+            v[2 * h] = r.x;
+            v[2 * h + 1] = r.y;
+        }
+        return v;
+    }
+    __device__ __forceinline__ float column32(const char* values, int row, int c) const {
+        return *reinterpret_cast<const float*>(values + (row * kChunks + ((c * 4 + (l16 >> 2)) ^ swizzle(row))) * 16 + (l16 & 3) * 4);
+    }
+
+    __device__ __forceinline__ bool all_numbers(const char* values) const {
+        typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+        bool fine = true;
+        if constexpr (k16) {
+            u16x2 most = {0, 0};
+            for (int i = lane; i < kKeys * kChunks; i += 64) {
+                const u32x4 v = *reinterpret_cast<const u32x4*>(values + i * 16) & 0x7fff7fffu;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, static_cast<uint32_t>(v[j])));
+            }
+            fine = most[0] < E::kInf && most[1] < E::kInf;
+        } else {
+            uint32_t most = 0;
+            for (int i = lane; i < kKeys * kChunks; i += 64) {
+                const u32x4 v = *reinterpret_cast<const u32x4*>(values + i * 16) & 0x7fffffffu;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) most = max(most, static_cast<uint32_t>(v[j]));
+            }
+            fine = most < 0x7f800000u;
+        }
+        return __ballot(!fine) == 0;
+    }
+
+    // Values of a tile that are no numbers become 0.  (Waves that share the keys may do so at once, each for itself.)
+    __device__ __forceinline__ void only_numbers(char* values) {
+        for (int i = lane; i < kKeys * kChunks; i += 64) {
+            u32x4 v = *reinterpret_cast<u32x4*>(values + i * 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (k16) {
+                    uint32_t x = v[j];
+                    if ((x & E::kInf) == E::kInf) x &= 0xffff0000u;
+                    if ((x >> 16 & E::kInf) == E::kInf) x &= 0xffffu;
+                    v[j] = x;
+                } else {
+                    if ((v[j] & 0x7f800000u) == 0x7f800000u) v[j] = 0;
+                }
+            }
+            *reinterpret_cast<u32x4*>(values + i * 16) = v;
+        }
+    }
+
+    __device__ __forceinline__ float value_at(const char* values, int row, int column) const {
+        const int chunk = (column * E::kBytes / 16) ^ swizzle(row), in_chunk = column * E::kBytes % 16;
+        return static_cast<float>(*reinterpret_cast<const typename E::T*>(values + (row * kChunks + chunk) * 16 + in_chunk));
+    }
+
+    // Tiles in which the nodes of a tree see different keys: the tree's own, and those between the first positions of the root
+    // and of the deepest node.
+    __device__ __forceinline__ bool differs(const Tile& x) const {
+        return t.nodes > 1 && (x.tree || (g.a.window > 0 && x.base < t.context + t.nodes - g.a.window && x.base + TILE > g.a.sinks));
+    }
+    __device__ __forceinline__ bool sees(const Tile& x, int key, int q) const {
+        int place = x.base + key;
+        bool yes = true;
+        if (x.tree) {
+            const int node = place & 63;
+            yes = (line[q] >> node) & 1;
+            place = t.context + __popcll(line[q] & ((1ull << node) - 1));
+        }
+        return yes && (place >= low[q] || place < g.a.sinks);
+    }
+
+    // A tile whose nodes see different keys held values that are no numbers: they were left out of the sums, and the rows that see
+    // them get them now.  The tiles in question are brought in again.
+    __device__ __forceinline__ void spoil(int first, int last) {
+        for (int i = first; i < last; ++i) {
+            const Tile x = tile_at(i);
+            if (!differs(x)) continue;
+            have_table(x);
+            ask(x, 0);
+            arrive(false);
+            const char* values = sh.values[0] + wk * kKeys * kChunks * 16;
+#pragma unroll
+            for (int q = 0; q < QT; ++q) {
+                uint32_t up[4] = {}, down[4] = {};                 // by column group: an infinity of either sign is seen (NaN: both)
+                for (int key = 0; key < kKeys; ++key) {
+                    if (!sh.seen[0][wk * kKeys + key] || !sees(x, wk * kKeys + key, q)) continue;
+                    for (int c = 0; c < kColumns; ++c)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float v = value_at(values, key, c * 16 + quad * 4 + j);
+                            up[j] |= static_cast<uint32_t>(!(v < INFINITY)) << c;
+                            down[j] |= static_cast<uint32_t>(!(v > -INFINITY)) << c;
+                        }
+                }
+#pragma unroll
+                for (int c = 0; c < kColumns; ++c)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (up[j] >> c & 1) out[q][c][j] += INFINITY;
+                        if (down[j] >> c & 1) out[q][c][j] -= INFINITY;
+                    }
+            }
+            leave();
+        }
+    }
+
+    // The unit's part [first, last) of its tiles.
+    __device__ __forceinline__ void run(int block, int first, int last) {
+        table_first = -1;
+        Tile now = tile_at(first);
+        if (threadIdx.x == 0) sh.spoiled = 0;                      // (read by all before the last barrier of the unit before)
+        have_table(now);
+        ask(now, 0);
+        begin(block);
+        for (int i = first, stage = 0; i < last; ++i, stage ^= 1) {
+            const bool ahead = i + 1 < last;
+            Tile next = now;
+            if (ahead) {
+                next = tile_at(i + 1);
+                have_table(next);
+                ask(next, stage ^ 1);
+            }
+            arrive(ahead);
+            work(now, stage);
+            leave();
+            now = next;
+        }
+        if (__builtin_amdgcn_readfirstlane(sh.spoiled)) spoil(first, last);
+        __syncthreads();
+        // ---- the lanes and the waves that share rows put their sums together
+#pragma unroll
+        for (int q = 0; q < QT; ++q) {
+            weight[q] += __shfl_xor(weight[q], 16);
+            weight[q] += __shfl_xor(weight[q], 32);
+        }
+        if constexpr (WK > 1) {
+            constexpr int kFloats = QT * (kColumns * 4 + 2) * 64;          // of a wave
+            static_assert(kFloats * 4 * WQ <= 4 * kTileBytes, "room for the waves' sums");
+            float* mine = reinterpret_cast<float*>(&sh) + wq * kFloats;
+            for (int other = 1; other < WK; ++other) {
+                if (wk == other) {
+#pragma unroll
+                    for (int q = 0; q < QT; ++q) {
+#pragma unroll
+                        for (int c = 0; c < kColumns; ++c) *reinterpret_cast<f32x4*>(mine + ((q * kColumns + c) * 64 + lane) * 4) = out[q][c];
+                        mine[QT * kColumns * 256 + q * 128 + lane] = top[q];
+                        mine[QT * kColumns * 256 + q * 128 + 64 + lane] = weight[q];
+                    }
+                }
+                __syncthreads();
+                if (wk == 0) {
+#pragma unroll
+                    for (int q = 0; q < QT; ++q) {
+                        const float their_top = mine[QT * kColumns * 256 + q * 128 + lane];
+                        const float now_top = fmaxf(top[q], their_top), base = now_top == -INFINITY ? 0.0f : now_top;
+                        const float fade = exp2_of(top[q] - base), theirs = exp2_of(their_top - base);
+                        top[q] = now_top;
+                        weight[q] = weight[q] * fade + mine[QT * kColumns * 256 + q * 128 + 64 + lane] * theirs;
+#pragma unroll
+                        for (int c = 0; c < kColumns; ++c)
+                            out[q][c] = out[q][c] * fade + *reinterpret_cast<const f32x4*>(mine + ((q * kColumns + c) * 64 + lane) * 4) * theirs;
+                    }
+                }
+                __syncthreads();
+            }
+        }
+    }
+
+    // Whole rows of the output.
+    __device__ __forceinline__ void finish(int block) {
+        if (wk != 0) return;
+        const int group = g.a.heads / g.a.kv_heads;
+#pragma unroll
+        for (int q = 0; q < QT; ++q) {
+            const int row = block * kRows + (wq * QT + q) * 16 + l16;
+            const int node = row / group;
+            if (node >= t.nodes) continue;
+            const float whole = 1.0f / weight[q];
+            char* to = static_cast<char*>(g.b.out) +
+                ((static_cast<int64_t>(b) * g.a.N + node) * g.a.out_stride + static_cast<int64_t>(kv * group + row - node * group) * g.a.head_dim) * E::kBytes;
+#pragma unroll
+            for (int c = 0; c < kColumns; ++c)
+                if (c * 16 + quad * 4 < g.a.head_dim) E::put4(to + (c * 16 + quad * 4) * E::kBytes, out[q][c] * whole);
+        }
+    }
+
+    __device__ __forceinline__ void keep(int slot) {
+        if (wk != 0) return;
+#pragma unroll
+        for (int q = 0; q < QT; ++q) {
+            const int64_t row = static_cast<int64_t>(slot) * kRows + (wq * QT + q) * 16 + l16;
+            if (quad == 0) g.partial_stats[row] = make_float2(top[q], weight[q]);
+#pragma unroll
+            for (int c = 0; c < kColumns; ++c) *reinterpret_cast<f32x4*>(g.partial + row * DP + c * 16 + quad * 4) = out[q][c];
+        }
+    }
+
+    // Sum over the workgroup; *before: of the threads before this one.
+    __device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* before) {
+        int64_t upto = v;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t o = static_cast<int64_t>(shfl64(static_cast<unsigned long long>(upto), max(lane - d, 0)));
+            if (lane >= d) upto += o;
+        }
+        __syncthreads();
+        if (lane == 63) sh.sum[wave] = upto;
+        __syncthreads();
+        int64_t all = 0;
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) upto += sh.sum[w];
+            all += sh.sum[w];
+        }
+        *before = upto - v;
+        return all;
+    }
+
+    __device__ __forceinline__ int64_t tiles_of(int tree) const {
+        if (tree >= g.a.B) return 0;
+        const TreeWork w = tree_work<TILE, kRows>(g, tree);
+        return static_cast<int64_t>(w.tiles) * w.blocks * g.a.kv_heads;
+    }
+
+    __device__ __forceinline__ void all() {
+        // workgroups of one chiplet (blockIdx % 8) take neighbouring parts of the list: the row blocks of a unit read the same keys
+        const int most = g.workgroups;
+        const int me = most % 8 == 0 ? (blockIdx.x % 8) * (most / 8) + blockIdx.x / 8 : blockIdx.x;
+        int64_t total = 0, before;
+        for (int base = 0; base < g.a.B; base += kThreads) total += block_sum(tiles_of(base + threadIdx.x), &before);
+        const int W = static_cast<int>(min(static_cast<int64_t>(most), total));      // every one of them has a tile at least
+        if (threadIdx.x == 0) g.split[me] = make_int4(-1, 0, 0, 0);
+        if (me >= W) return;
+        const int64_t begin_at = total * me / W, end_at = total * (me + 1) / W;
+        // the tree of the first tile
+        int64_t start = 0;
+        int first_tree = 0;
+        for (int base = 0;; base += kThreads) {
+            const int64_t mine = tiles_of(base + threadIdx.x);
+            const int64_t sum = block_sum(mine, &before);
+            if (begin_at < start + sum) {
+                const bool here = begin_at >= start + before && begin_at < start + before + mine;
+                __syncthreads();
+                if (here) { sh.sum[0] = start + before; sh.table[0] = base + threadIdx.x; }
+                __syncthreads();
+                start = sh.sum[0];
+                first_tree = sh.table[0];
+                __syncthreads();
+                break;
+            }
+            start += sum;
+        }
+        b = __builtin_amdgcn_readfirstlane(first_tree);
+        int64_t at = begin_at;
+        while (at < end_at) {
+            t = tree_work<TILE, kRows>(g, b);
+            const int64_t units = static_cast<int64_t>(t.blocks) * g.a.kv_heads;
+            const int64_t tiles = t.nodes > 0 ? t.tiles : 0;
+            while (at < min(end_at, start + units * tiles)) {
+                const int unit = static_cast<int>((at - start) / tiles);
+                const int64_t unit_start = start + unit * tiles;
+                kv = unit / t.blocks;
+                const int block = unit - kv * t.blocks;
+                const int first = static_cast<int>(at - unit_start);
+                const int last = static_cast<int>(min(tiles, end_at - unit_start));
+                run(block, first, last);
+                if (first == 0 && last == tiles) {
+                    finish(block);
+                } else {
+                    keep(me * 2 + (first > 0 ? 0 : 1));
+                    if (first == 0 && threadIdx.x == 0) {
+                        const int64_t end = unit_start + tiles;              // the workgroup of the unit's last tile
+                        g.split[me] = make_int4(b, kv, block, static_cast<int>((end * W - 1) / total));
+                    }
+                }
+                at = unit_start + last;
+            }
+            start += units * tiles;
+            ++b;
+        }
+    }
+};
+
+template <class A>
+__global__ __launch_bounds__(A::kThreads) __attribute__((amdgpu_waves_per_eu(2))) void attention_kernel(AttentionArgs g) {
+    extern __shared__ __align__(16) char memory[];
+    A a(g, *reinterpret_cast<typename A::Shared*>(memory));
+    a.all();
+}
+
+// Puts the shared units together: a wave per row of a unit that begins in workgroup blockIdx.x's part of the list.
+template <int DTYPE, int DP, int ROWS>
+__global__ __launch_bounds__(256) void combine_kernel(AttentionArgs g) {
+    typedef Elem<DTYPE> E;
+    const int first = blockIdx.x;
+    const int4 s = g.split[first];
+    if (s.x < 0) return;
+    const int lane = threadIdx.x & 63, local = blockIdx.y * 4 + (threadIdx.x >> 6);
+    const int b = s.x, kv = s.y, last = s.w, group = g.a.heads / g.a.kv_heads;
+    const int row = s.z * ROWS + local, node = row / group;
+    const int nodes = g.b.num_nodes ? min(max(g.b.num_nodes[b], 0), g.a.N) : g.a.N;
+    if (node >= nodes) return;
+    // part p of the unit: the second slot of workgroup `first`, the first slot of those after it
+    auto at = [&](int p) { return (static_cast<int64_t>(first + p) * 2 + (p == 0 ? 1 : 0)) * ROWS + local; };
+    const int parts = last - first + 1;
+    float top = -INFINITY;
+    for (int p = lane; p < parts; p += 64) top = fmaxf(top, g.partial_stats[at(p)].x);
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const float base = top == -INFINITY ? 0.0f : top;
+    constexpr int kLanes = DP / 4, kAtOnce = 64 / kLanes;          // lanes of a row, rows at a time
+    const int column = lane % kLanes * 4;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    float weight = 0.0f;
+#pragma unroll 4
+    for (int p = lane / kLanes; p < parts; p += kAtOnce) {
+        const float2 stats = g.partial_stats[at(p)];
+        const float f = exp2_of(stats.x - base);
+        weight += f * stats.y;
+        sum += *reinterpret_cast<const f32x4*>(g.partial + at(p) * DP + column) * f;
+    }
+    for (int d = kLanes; d < 64; d <<= 1) {
+        weight += __shfl_xor(weight, d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor(sum[i], d);
+    }
+    if (lane >= kLanes || column >= g.a.head_dim) return;
+    char* to = static_cast<char*>(g.b.out) +
+        ((static_cast<int64_t>(b) * g.a.N + node) * g.a.out_stride + static_cast<int64_t>(kv * group + row - node * group) * g.a.head_dim + column) * E::kBytes;
+    E::put4(to, sum * (1.0f / weight));
+}
+
+// ------------------------------------------------------------------ host side
+
+// Workgroups of a call: two a compute unit, which is what the tiles in LDS leave room for.
+constexpr int kMaxWorkgroups = 512;
+
+// The tile and the waves' shares for a type and a row length.  A tile of keys is 16 KB (two stages of keys and values: 64 KB).
+template <int DTYPE, int DP>
+struct Family {
+    static constexpr int kTile = 16384 / (DP * Elem<DTYPE>::kBytes);
+    static constexpr int kMostWK = kTile / (Elem<DTYPE>::kBytes == 2 ? 32 : 16) < 4 ? kTile / (Elem<DTYPE>::kBytes == 2 ? 32 : 16) : 4;
+    // two 16-row groups a wave where their queries and sums leave registers for the products
+    static constexpr int kMostQT = DP * Elem<DTYPE>::kBytes <= 256 || (DTYPE == MPV_DTYPE_F32 && DP == 128) ? 2 : 1;
+};
+
+// What a call needs to know of the kernel that it gets.
+struct Choice {
+    int rows, columns, tile;
+    int64_t tiles;                         // the most that a call can have
+    int workgroups, blocks;
+};
+
+template <class A, int DP>
+static Choice choice_of(const mpv_attention* a) {
+    Choice c;
+    c.rows = A::kRows;
+    c.columns = DP;
+    c.tile = A::kTile;
+    const int64_t rows = static_cast<int64_t>(a->N) * (a->heads / a->kv_heads);
+    c.blocks = static_cast<int>((rows + c.rows - 1) / c.rows);
+    const int64_t room = static_cast<int64_t>(a->table_width) * a->page_size;
+    int64_t seen = (room + c.tile - 1) / c.tile;
+    if (a->window > 0) {
+        const int64_t near = (static_cast<int64_t>(a->window) + c.tile - 1) / c.tile + 1 + (static_cast<int64_t>(a->sinks > 0 ? a->sinks : 0) + c.tile - 1) / c.tile;
+        if (near < seen) seen = near;
+    }
+    const int64_t unit = seen + (a->N + c.tile - 1) / c.tile;
+    const int64_t units = static_cast<int64_t>(a->B) * a->kv_heads * c.blocks;
+    c.tiles = unit > (INT64_MAX >> 8) / (units > 0 ? units : 1) ? INT64_MAX >> 8 : unit * units;
+    c.workgroups = static_cast<int>(c.tiles < kMaxWorkgroups ? (c.tiles > 0 ? c.tiles : 1) : kMaxWorkgroups);
+    return c;
+}
+
+static size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// One call: the size of its workspace (g null) or its launches.
+template <class A, int DTYPE, int DP>
+static int with_kernel(const mpv_attention* a, AttentionArgs* g, void* workspace, size_t* bytes, hipStream_t s) {
+    const Choice c = choice_of<A, DP>(a);
+    const size_t stats = whole(static_cast<size_t>(c.workgroups) * 2 * c.rows * sizeof(float2));
+    const size_t split = whole(static_cast<size_t>(c.workgroups) * sizeof(int4));
+    const size_t sums = whole(static_cast<size_t>(c.workgroups) * 2 * c.rows * DP * sizeof(float));
+    *bytes = stats + split + sums;
+    if (!g) return MPV_OK;
+    char* at = static_cast<char*>(workspace);
+    g->workgroups = c.workgroups;
+    g->blocks = c.blocks;
+    g->partial_stats = reinterpret_cast<float2*>(at);
+    g->split = reinterpret_cast<int4*>(at + stats);
+    g->partial = reinterpret_cast<float*>(at + stats + split);
+    (void)hipGetLastError();
+    if (!hip_fine(hipFuncSetAttribute(reinterpret_cast<const void*>(&attention_kernel<A>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                      static_cast<int>(sizeof(typename A::Shared)))))
+        return MPV_ERR_HIP;
+    hipLaunchKernelGGL(attention_kernel<A>, dim3(static_cast<unsigned>(c.workgroups)), dim3(A::kThreads), sizeof(typename A::Shared), s, *g);
+    // a list with one tile a unit shares none
+    const int64_t units = static_cast<int64_t>(a->B) * a->kv_heads * c.blocks;
+    if (c.tiles > units)
+        hipLaunchKernelGGL((combine_kernel<DTYPE, DP, A::kRows>), dim3(static_cast<unsigned>(c.workgroups), A::kRows / 4), dim3(256), 0, s, *g);
+    return launched();
+}
+
+template <int DTYPE, int DP>
+static int with_columns(const mpv_attention* a, AttentionArgs* g, void* workspace, size_t* bytes, hipStream_t s) {
+    typedef Family<DTYPE, DP> F;
+    constexpr int T = F::kTile, WK = F::kMostWK;
+    const int64_t rows = static_cast<int64_t>(a->N) * (a->heads / a->kv_heads);
+    if (rows <= 16) return with_kernel<Attention<DTYPE, DP, 1, 1, WK, T>, DTYPE, DP>(a, g, workspace, bytes, s);
+    if constexpr (F::kMostQT == 2) {
+        if (rows <= 32) return with_kernel<Attention<DTYPE, DP, 2, 1, WK, T>, DTYPE, DP>(a, g, workspace, bytes, s);
+        if (rows <= 64) return with_kernel<Attention<DTYPE, DP, 2, 2, (WK < 2 ? WK : 2), T>, DTYPE, DP>(a, g, workspace, bytes, s);
+        // as many rows a workgroup as divide the largest tree into even blocks
+        const int64_t blocks = (rows + 127) / 128;
+        if ((rows + blocks - 1) / blocks <= 96) return with_kernel<Attention<DTYPE, DP, 2, 3, 1, T>, DTYPE, DP>(a, g, workspace, bytes, s);
+        return with_kernel<Attention<DTYPE, DP, 2, 4, 1, T>, DTYPE, DP>(a, g, workspace, bytes, s);
+    } else {
+        if (rows <= 32) return with_kernel<Attention<DTYPE, DP, 1, 2, 1, T>, DTYPE, DP>(a, g, workspace, bytes, s);
+        return with_kernel<Attention<DTYPE, DP, 1, 4, 1, T>, DTYPE, DP>(a, g, workspace, bytes, s);
+    }
+}
+
+template <int DTYPE>
+static int with_type(const mpv_attention* a, AttentionArgs* g, void* workspace, size_t* bytes, hipStream_t s) {
+    if (a->head_dim <= 64) return with_columns<DTYPE, 64>(a, g, workspace, bytes, s);
+    if (a->head_dim <= 128) return with_columns<DTYPE, 128>(a, g, workspace, bytes, s);
+    return with_columns<DTYPE, 256>(a, g, workspace, bytes, s);
+}
+
+static int attend(const mpv_attention* a, AttentionArgs* g, void* workspace, size_t* bytes, hipStream_t s) {
+    if (a->dtype == MPV_DTYPE_F32) return with_type<MPV_DTYPE_F32>(a, g, workspace, bytes, s);
+    if (a->dtype == MPV_DTYPE_BF16) return with_type<MPV_DTYPE_BF16>(a, g, workspace, bytes, s);
+    return with_type<MPV_DTYPE_F16>(a, g, workspace, bytes, s);
 }
 
 static int check_attention(const mpv_attention* a) {
@@ -126,13 +869,6 @@ static int check_attention(const mpv_attention* a) {
     return MPV_OK;
 }
 
-template <class T>
-static int launch_attention(const AttentionArgs& g, hipStream_t s) {
-    (void)hipGetLastError();
-    hipLaunchKernelGGL(tree_attention_kernel<T>, dim3(static_cast<unsigned>(g.a.N * g.a.heads), static_cast<unsigned>(g.a.B)), dim3(64), 0, s, g);
-    return launched();
-}
-
 }  // namespace mpv
 
 extern "C" {
@@ -141,8 +877,7 @@ int mpv_tree_attention_workspace_bytes(const mpv_attention* attention, size_t* o
     if (!out) return MPV_ERR_NULL;
     const int rc = mpv::check_attention(attention);
     if (rc != MPV_OK) return rc;
-    *out = 256;
-    return MPV_OK;
+    return mpv::attend(attention, nullptr, nullptr, out, nullptr);
 }
 
 int mpv_tree_attention(const mpv_attention* attention, const mpv_attention_buffers* buf, void* workspace, size_t workspace_bytes,
@@ -153,6 +888,8 @@ int mpv_tree_attention(const mpv_attention* attention, const mpv_attention_buffe
     if (!buf) return MPV_ERR_NULL;
     mpv::AttentionArgs g;
     g.a = *attention; g.b = *buf;
+    g.sign = attention->scale > 0.0f ? 1 : attention->scale < 0.0f ? -1 : 0;
+    g.factor = g.sign ? static_cast<float>(std::fabs(static_cast<double>(attention->scale)) * 1.4426950408889634) : 1.0f;
     if (!buf->tree_parent) {
         if (!attention->parent) return MPV_ERR_NULL;
         if (attention->parent[0] != -1) return MPV_ERR_BAD_TREE;
@@ -171,9 +908,7 @@ int mpv_tree_attention(const mpv_attention* attention, const mpv_attention_buffe
         return MPV_ERR_ALIGNMENT;
     if (!workspace || !mpv::aligned(workspace, 256) || workspace_bytes < need) return MPV_ERR_WORKSPACE;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    if (attention->dtype == MPV_DTYPE_F32) return mpv::launch_attention<float>(g, s);
-    if (attention->dtype == MPV_DTYPE_BF16) return mpv::launch_attention<uint16_t>(g, s);
-    return mpv::launch_attention<__half>(g, s);
+    return mpv::attend(attention, &g, workspace, &need, s);
 }
 
 }  // extern "C"
