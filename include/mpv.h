@@ -74,6 +74,7 @@ extern "C" {
 #define MPV_MAX_CHILDREN 16   /* children of one node                      */
 #define MPV_MAX_VOCAB    (1 << 21)
 #define MPV_MAX_HEAD_DIM 256  /* values of one attention head               */
+#define MPV_MAX_HEADS    1024 /* query heads                                */
 /* and B * (N + 2) <= 2^30 */
 
 #define MPV_METHOD_SPECINFER 0
@@ -378,7 +379,7 @@ typedef struct mpv_attention_buffers {    /* DEVICE, borrowed until the work has
 
 int mpv_tree_attention_workspace_bytes(const mpv_attention* attention, size_t* out);
 
-/* Errors: MPV_ERR_NULL, _BAD_SHAPE, _UNSUPPORTED (N or head_dim too large, B * heads or a stride beyond 2^31),
+/* Errors: MPV_ERR_NULL, _BAD_SHAPE, _UNSUPPORTED (N, heads, head_dim, B, a context or a stride too large),
  * _BAD_TREE, _BAD_DTYPE, _BAD_TEMPERATURE (scale not finite), _ALIGNMENT, _WORKSPACE, _HIP. */
 int mpv_tree_attention(const mpv_attention* attention, const mpv_attention_buffers* buffers,
                        void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -1,11 +1,12 @@
 // Attention of draft-tree nodes over a paged cache: device and host code.
 //
 // With s the scaled products of a query with the keys it sees, out = sum_j e^(s_j - m) v_j / sum_j e^(s_j - m), in one pass over the
-// keys with a running reference m (log2 units).  The work is cut into tiles of kTile keys; the rows (node, query head) that share a
-// cache head, kRows of them, are a unit, and a unit's tiles are its part of the sinks, of the window (or the whole context), and
-// of the tree.  All tiles of all units form one list, which is divided evenly among the workgroups, whatever the lengths
-// of the contexts: a workgroup carries on across units, and a unit that several workgroups share is put together by
-// combine_kernel from their partial sums.
+// keys with a running reference m (log2 units).  The work is cut into tiles of kTile keys; a unit is what a tree's nodes read of one
+// cache head: its tiles are those of the sinks, of the window (or the whole context), and of the tree.  All tiles of all units
+// form one list, which is divided evenly among teams of workgroups, whatever the lengths of the contexts: a team carries on across
+// units, and a unit that several teams share is put together by combine_kernel from their partial sums.  A member of a team has
+// kRows of the rows (node, query head) that read the unit; the members read the same tiles at about the same time, on the
+// same chiplet, so that only one of them waits for memory and the others find the tile in the chiplet's L2.
 //
 // A tile of keys and values goes straight from memory to LDS (16 bytes a lane), a tile ahead of the one that is worked on.
 //   products    S^T = K Q^T: keys are the rows of the matrix instruction's first operand, read from LDS; queries stay in registers
@@ -27,13 +28,13 @@ struct AttentionArgs {
     mpv_attention a;
     mpv_attention_buffers b;
     int8_t parent[MPV_MAX_NODES];          // the shared shape (without tree_parent)
-    int workgroups;
-    int blocks;                            // row blocks of the largest tree
+    int teams;
+    int blocks;                            // row blocks of the largest tree: members of a team
     float factor;                          // |scale| log2(e): products to exponents (1 where the scale is 0)
     int sign;                              // of the scale: -1, 0, 1
-    float* partial;                        // [workgroups][2][rows][columns]
-    float2* partial_stats;                 // [workgroups][2][rows]: reference, sum of weights
-    int4* split;                           // [workgroups]: tree, cache head, row block, last workgroup of a unit that begins there and
+    float* partial;                        // [teams][members][2][rows][columns]
+    float2* partial_stats;                 // [teams][members][2][rows]: reference, sum of weights
+    int4* split;                           // [teams]: tree, cache head, row blocks, last team of a unit that begins in this team's part and
                                            // is shared; x < 0: none
 };
 
@@ -634,22 +635,21 @@ struct Attention {
     __device__ __forceinline__ int64_t tiles_of(int tree) const {
         if (tree >= g.a.B) return 0;
         const TreeWork w = tree_work<TILE, kRows>(g, tree);
-        return static_cast<int64_t>(w.tiles) * w.blocks * g.a.kv_heads;
+        return w.nodes > 0 ? static_cast<int64_t>(w.tiles) * g.a.kv_heads : 0;
     }
 
     __device__ __forceinline__ void all() {
-        // workgroups of one chiplet (blockIdx % 8) take neighbouring parts of the list: the row blocks of a unit read the same keys
-        const int most = g.workgroups;
-        const int me = most % 8 == 0 ? (blockIdx.x % 8) * (most / 8) + blockIdx.x / 8 : blockIdx.x;
+        // teams of one chiplet (blockIdx % 8) take neighbouring parts of the list
+        const int most = g.teams, place = most % 8 == 0 ? blockIdx.x / 8 : blockIdx.x;
+        const int member = place % g.blocks, team = most % 8 == 0 ? (blockIdx.x % 8) * (most / 8) + place / g.blocks : place / g.blocks;
         int64_t total = 0, before;
         for (int base = 0; base < g.a.B; base += kThreads) total += block_sum(tiles_of(base + threadIdx.x), &before);
-        const int W = static_cast<int>(min(static_cast<int64_t>(most), total));      // every one of them has a tile at least
-        if (threadIdx.x == 0) g.split[me] = make_int4(-1, 0, 0, 0);
-        if (me >= W) return;
-        const int64_t begin_at = total * me / W, end_at = total * (me + 1) / W;
+        const int T = static_cast<int>(min(static_cast<int64_t>(most), total));      // every one of them has a tile at least
+        if (member == 0 && threadIdx.x == 0) g.split[team] = make_int4(-1, 0, 0, 0);
+        if (team >= T) return;
+        const int64_t begin_at = total * team / T, end_at = total * (team + 1) / T;
         // the tree of the first tile
         int64_t start = 0;
-        int first_tree = 0;
         for (int base = 0;; base += kThreads) {
             const int64_t mine = tiles_of(base + threadIdx.x);
             const int64_t sum = block_sum(mine, &before);
@@ -659,39 +659,32 @@ struct Attention {
                 if (here) { sh.sum[0] = start + before; sh.table[0] = base + threadIdx.x; }
                 __syncthreads();
                 start = sh.sum[0];
-                first_tree = sh.table[0];
+                b = __builtin_amdgcn_readfirstlane(sh.table[0]);
                 __syncthreads();
                 break;
             }
             start += sum;
         }
-        b = __builtin_amdgcn_readfirstlane(first_tree);
         int64_t at = begin_at;
-        while (at < end_at) {
+        for (; at < end_at; ++b) {
             t = tree_work<TILE, kRows>(g, b);
-            const int64_t units = static_cast<int64_t>(t.blocks) * g.a.kv_heads;
-            const int64_t tiles = t.nodes > 0 ? t.tiles : 0;
-            while (at < min(end_at, start + units * tiles)) {
-                const int unit = static_cast<int>((at - start) / tiles);
-                const int64_t unit_start = start + unit * tiles;
-                kv = unit / t.blocks;
-                const int block = unit - kv * t.blocks;
-                const int first = static_cast<int>(at - unit_start);
-                const int last = static_cast<int>(min(tiles, end_at - unit_start));
-                run(block, first, last);
-                if (first == 0 && last == tiles) {
-                    finish(block);
-                } else {
-                    keep(me * 2 + (first > 0 ? 0 : 1));
-                    if (first == 0 && threadIdx.x == 0) {
-                        const int64_t end = unit_start + tiles;              // the workgroup of the unit's last tile
-                        g.split[me] = make_int4(b, kv, block, static_cast<int>((end * W - 1) / total));
-                    }
-                }
-                at = unit_start + last;
+            if (t.nodes == 0) continue;
+            const int64_t tree_end = start + static_cast<int64_t>(t.tiles) * g.a.kv_heads;
+            while (at < min(end_at, tree_end)) {
+                kv = static_cast<int>((at - start) / t.tiles);
+                const int64_t unit = start + static_cast<int64_t>(kv) * t.tiles;
+                const int first = static_cast<int>(at - unit);
+                const int last = static_cast<int>(min(static_cast<int64_t>(t.tiles), end_at - unit));
+                at = unit + last;
+                const bool shared = first > 0 || last < t.tiles;
+                if (member == 0 && first == 0 && shared && threadIdx.x == 0)         // (the team that has the unit's last tile)
+                    g.split[team] = make_int4(b, kv, t.blocks, static_cast<int>(((unit + t.tiles) * T - 1) / total));
+                if (member >= t.blocks) continue;
+                run(member, first, last);
+                if (shared) keep((team * g.blocks + member) * 2 + (first > 0 ? 0 : 1));
+                else finish(member);
             }
-            start += units * tiles;
-            ++b;
+            start = tree_end;
         }
     }
 };
@@ -703,20 +696,21 @@ __global__ __launch_bounds__(A::kThreads) __attribute__((amdgpu_waves_per_eu(2))
     a.all();
 }
 
-// Puts the shared units together: a wave per row of a unit that begins in workgroup blockIdx.x's part of the list.
+// Puts the shared units together: a wave per row of a unit that begins in team blockIdx.x's part of the list.
 template <int DTYPE, int DP, int ROWS>
 __global__ __launch_bounds__(256) void combine_kernel(AttentionArgs g) {
     typedef Elem<DTYPE> E;
     const int first = blockIdx.x;
     const int4 s = g.split[first];
-    if (s.x < 0) return;
-    const int lane = threadIdx.x & 63, local = blockIdx.y * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, row = blockIdx.y * 4 + (threadIdx.x >> 6);
+    const int block = row / ROWS, local = row % ROWS;
+    if (s.x < 0 || block >= s.z) return;
     const int b = s.x, kv = s.y, last = s.w, group = g.a.heads / g.a.kv_heads;
-    const int row = s.z * ROWS + local, node = row / group;
+    const int node = row / group;
     const int nodes = g.b.num_nodes ? min(max(g.b.num_nodes[b], 0), g.a.N) : g.a.N;
     if (node >= nodes) return;
-    // part p of the unit: the second slot of workgroup `first`, the first slot of those after it
-    auto at = [&](int p) { return (static_cast<int64_t>(first + p) * 2 + (p == 0 ? 1 : 0)) * ROWS + local; };
+    // part p of the unit: the second slot of team `first`, the first slot of those after it
+    auto at = [&](int p) { return ((static_cast<int64_t>(first + p) * g.blocks + block) * 2 + (p == 0 ? 1 : 0)) * ROWS + local; };
     const int parts = last - first + 1;
     float top = -INFINITY;
     for (int p = lane; p < parts; p += 64) top = fmaxf(top, g.partial_stats[at(p)].x);
@@ -746,7 +740,7 @@ __global__ __launch_bounds__(256) void combine_kernel(AttentionArgs g) {
 
 // ------------------------------------------------------------------ host side
 
-// Workgroups of a call: two a compute unit, which is what the tiles in LDS leave room for.
+// Workgroups of a call: two a compute unit, which is what the tiles in LDS leave room for (more only where a team alone has more).
 constexpr int kMaxWorkgroups = 512;
 
 // The tile and the waves' shares for a type and a row length.  A tile of keys is 16 KB (two stages of keys and values: 64 KB).
@@ -762,7 +756,7 @@ struct Family {
 struct Choice {
     int rows, columns, tile;
     int64_t tiles;                         // the most that a call can have
-    int workgroups, blocks;
+    int teams, blocks;
 };
 
 template <class A, int DP>
@@ -780,9 +774,11 @@ static Choice choice_of(const mpv_attention* a) {
         if (near < seen) seen = near;
     }
     const int64_t unit = seen + (a->N + c.tile - 1) / c.tile;
-    const int64_t units = static_cast<int64_t>(a->B) * a->kv_heads * c.blocks;
-    c.tiles = unit > (INT64_MAX >> 8) / (units > 0 ? units : 1) ? INT64_MAX >> 8 : unit * units;
-    c.workgroups = static_cast<int>(c.tiles < kMaxWorkgroups ? (c.tiles > 0 ? c.tiles : 1) : kMaxWorkgroups);
+    c.tiles = unit * a->B * a->kv_heads;
+    c.teams = kMaxWorkgroups / c.blocks;
+    if (c.teams >= 8) c.teams = c.teams / 8 * 8;
+    if (c.tiles < c.teams) c.teams = static_cast<int>(c.tiles);
+    if (c.teams < 1) c.teams = 1;
     return c;
 }
 
@@ -792,26 +788,26 @@ static size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
 template <class A, int DTYPE, int DP>
 static int with_kernel(const mpv_attention* a, AttentionArgs* g, void* workspace, size_t* bytes, hipStream_t s) {
     const Choice c = choice_of<A, DP>(a);
-    const size_t stats = whole(static_cast<size_t>(c.workgroups) * 2 * c.rows * sizeof(float2));
-    const size_t split = whole(static_cast<size_t>(c.workgroups) * sizeof(int4));
-    const size_t sums = whole(static_cast<size_t>(c.workgroups) * 2 * c.rows * DP * sizeof(float));
+    const size_t stats = whole(static_cast<size_t>(c.teams) * c.blocks * 2 * c.rows * sizeof(float2));
+    const size_t split = whole(static_cast<size_t>(c.teams) * sizeof(int4));
+    const size_t sums = whole(static_cast<size_t>(c.teams) * c.blocks * 2 * c.rows * DP * sizeof(float));
     *bytes = stats + split + sums;
     if (!g) return MPV_OK;
     char* at = static_cast<char*>(workspace);
-    g->workgroups = c.workgroups;
+    g->teams = c.teams;
     g->blocks = c.blocks;
     g->partial_stats = reinterpret_cast<float2*>(at);
     g->split = reinterpret_cast<int4*>(at + stats);
     g->partial = reinterpret_cast<float*>(at + stats + split);
+    const int64_t rows = static_cast<int64_t>(a->N) * (a->heads / a->kv_heads);
     (void)hipGetLastError();
     if (!hip_fine(hipFuncSetAttribute(reinterpret_cast<const void*>(&attention_kernel<A>), hipFuncAttributeMaxDynamicSharedMemorySize,
                                       static_cast<int>(sizeof(typename A::Shared)))))
         return MPV_ERR_HIP;
-    hipLaunchKernelGGL(attention_kernel<A>, dim3(static_cast<unsigned>(c.workgroups)), dim3(A::kThreads), sizeof(typename A::Shared), s, *g);
+    hipLaunchKernelGGL(attention_kernel<A>, dim3(static_cast<unsigned>(c.teams) * c.blocks), dim3(A::kThreads), sizeof(typename A::Shared), s, *g);
     // a list with one tile a unit shares none
-    const int64_t units = static_cast<int64_t>(a->B) * a->kv_heads * c.blocks;
-    if (c.tiles > units)
-        hipLaunchKernelGGL((combine_kernel<DTYPE, DP, A::kRows>), dim3(static_cast<unsigned>(c.workgroups), A::kRows / 4), dim3(256), 0, s, *g);
+    if (c.tiles > static_cast<int64_t>(a->B) * a->kv_heads)
+        hipLaunchKernelGGL((combine_kernel<DTYPE, DP, A::kRows>), dim3(static_cast<unsigned>(c.teams), static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, s, *g);
     return launched();
 }
 
@@ -854,7 +850,7 @@ static int check_attention(const mpv_attention* a) {
         return MPV_ERR_BAD_SHAPE;
     if (!known_dtype(a->dtype)) return MPV_ERR_BAD_DTYPE;
     if (!std::isfinite(a->scale)) return MPV_ERR_BAD_TEMPERATURE;
-    if (a->N > MPV_MAX_NODES || a->head_dim > MPV_MAX_HEAD_DIM || a->heads > 65535) return MPV_ERR_UNSUPPORTED;
+    if (a->N > MPV_MAX_NODES || a->head_dim > MPV_MAX_HEAD_DIM || a->heads > MPV_MAX_HEADS) return MPV_ERR_UNSUPPORTED;
     const int64_t row = static_cast<int64_t>(a->kv_heads) * a->head_dim, wide = static_cast<int64_t>(a->heads) * a->head_dim;
     // rows of heads that do not reach into each other
     if (a->q_stride < wide || a->out_stride < wide || a->kv_stride < row || a->slot_stride < row || a->page_stride < 0) return MPV_ERR_BAD_SHAPE;
