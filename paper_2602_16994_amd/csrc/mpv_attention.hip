@@ -8,7 +8,8 @@
 // kRows of the rows (node, query head) that read the unit; the members read the same tiles at about the same time, on the
 // same chiplet, so that only one of them waits for memory and the others find the tile in the chiplet's L2.
 //
-// A tile of keys and values goes straight from memory to LDS (16 bytes a lane), a tile ahead of the one that is worked on.
+// A tile of keys and values goes straight from memory to LDS (16 bytes a lane), up to three tiles ahead of the one that is worked on;
+// so do the entries of the block table, a batch of tiles ahead: a lane then works out where one key's rows lie.
 //   products    S^T = K Q^T: keys are the rows of the matrix instruction's first operand, read from LDS; queries stay in registers
 //   weights     lane l then holds 4 consecutive keys for query l % 16: the statistics of a query lie in 4 lanes, and the weights are
 //               where the second product wants them (the order of keys within an instruction does not matter if both operands have it)
@@ -18,6 +19,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <cstddef>
 #include <cstring>
 
 #include "mpv_host.h"
@@ -84,11 +86,17 @@ template <> struct Elem<MPV_DTYPE_F16> {
     }
 };
 
-// What an invalid key's row is read from.
-__device__ const uint4 kZeros = {0u, 0u, 0u, 0u};
+// What the row of a key that nobody sees is read from.
+__device__ const uint4 kZeros[MPV_MAX_HEAD_DIM * 4 / 16] = {};
 
-__device__ __forceinline__ void to_lds(const void* from, void* to) {      // 16 bytes a lane; `to`: the wave's first lane's
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+// 16 bytes a lane to LDS, from `to` on (the wave's first lane's place) in lane order.  Written as an instruction: the compiler would
+// wait for all such loads in flight before it reads LDS through ds_read_b64_tr_b16, the next tile's among them.  Nothing but `arrive`
+// waits for them.
+__device__ __forceinline__ void to_lds(uint64_t from, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+}
+__device__ __forceinline__ void word_to_lds(uint64_t from, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory");
 }
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ unsigned long long shfl64(unsigned long long v, int lane) {
@@ -96,9 +104,15 @@ __device__ __forceinline__ unsigned long long shfl64(unsigned long long v, int l
     return static_cast<unsigned long long>(hi) << 32 | lo;
 }
 
-constexpr int kTableChunk = 1024;          // entries of a block table kept in LDS
 // The reference of a softmax moves only where a product exceeds it by more than this (log2 units): weights are at most 2^8.
 constexpr float kSlack = 8.0f;
+// x, as if it had just been read: what depends on it is worked out where it is needed and does not occupy registers across the loops.
+__device__ __forceinline__ int fresh(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+// All bits where bit `at` is set, none otherwise.  (Masks instead of conditions: those would all wait in scalar registers at once.)
+__device__ __forceinline__ uint32_t spread(uint32_t bits, int at) { return static_cast<uint32_t>(static_cast<int32_t>(bits << (31 - at)) >> 31); }
 
 // A tree's part of the list of tiles.
 struct TreeWork {
@@ -125,35 +139,40 @@ __device__ __forceinline__ TreeWork tree_work(const AttentionArgs& g, int b) {
     return t;
 }
 
-// DTYPE; DP: columns of a row in LDS (head_dim, rounded up); QT: 16-row groups of a wave; WQ: waves side by side over the rows;
-// WK: waves side by side over a tile's keys; TILE: keys.
-template <int DTYPE, int DP, int QT, int WQ, int WK, int TILE>
+// DTYPE; DP: columns of a row in LDS (head_dim, rounded up); QT: 16-row groups of a wave; WAVES; TILE: keys; STAGES: tiles in LDS.
+template <int DTYPE, int DP, int QT, int WAVES, int TILE, int STAGES>
 struct Attention {
     typedef Elem<DTYPE> E;
-    static constexpr int kWaves = WQ * WK;
-    static constexpr int kThreads = 64 * kWaves;
-    static constexpr int kRows = 16 * QT * WQ;
+    static constexpr int kWaves = WAVES;
+    static constexpr int kThreads = 64 * WAVES;
+    static constexpr int kRows = 16 * QT * WAVES;
     static constexpr int kChunks = DP * E::kBytes / 16;            // 16-byte chunks of a row
     static constexpr int kSteps = kChunks / 4;                     // of the first product: 4 chunks of every row
-    static constexpr int kKeys = TILE / WK;                        // of a wave
-    static constexpr int kGroups = kKeys / 16;
+    static constexpr int kGroups = TILE / 16;
     static constexpr int kColumns = DP / 16;                       // 16-column groups of the output
     static constexpr int kTileBytes = TILE * DP * E::kBytes;
     static constexpr int kRowsPerLoad = 64 / kChunks;              // rows that a wave's load brings
-    static constexpr int kLoads = TILE / kRowsPerLoad;             // of keys; as many of values
-    static constexpr int kMyLoads = (kLoads + kWaves - 1) / kWaves;
+    static constexpr int kMyRows = TILE / WAVES;                   // keys that a wave brings, and their values
+    static constexpr int kMyLoads = kMyRows / kRowsPerLoad;        // of keys; as many of values
+    static constexpr int kBatch = 64 / kMyRows;                    // tiles whose rows a wave's lanes look up at a time
+    static constexpr int kAheadTiles = STAGES - 1;
     static constexpr int kTile = TILE;
     static constexpr bool k16 = E::kBytes == 2;
-    static_assert(kChunks >= 8 && kChunks <= 64 && kMyLoads * kRowsPerLoad <= 64 && kKeys % (k16 ? 32 : 16) == 0 && kGroups * 4 <= 32, "tile");
+    static_assert(kChunks >= 8 && kChunks <= 64 && kMyLoads >= 1 && kMyRows % kRowsPerLoad == 0 && 64 % kMyRows == 0, "loads");
+    static_assert(TILE % (k16 ? 32 : 16) == 0 && kGroups * 4 <= 32, "tile");
+    // the entries asked for with one batch are there when the next one begins: the waits of `arrive` leave fewer tiles in flight
+    static_assert(kBatch >= kAheadTiles && kAheadTiles * kMyLoads * 2 < 60, "batch");
 
     struct Shared {
-        __align__(16) char keys[2][kTileBytes];
-        __align__(16) char values[2][kTileBytes];
-        int table[kTableChunk];
-        __align__(4) uint8_t seen[2][TILE];                        // whether anybody sees the key
-        int hidden[2][kWaves];                                     // whether a wave found one that nobody sees
+        __align__(16) char keys[STAGES][kTileBytes];
+        __align__(16) char values[STAGES][kTileBytes];
+        __align__(16) uint64_t place[2][kBatch][TILE][2];          // where a key's and its value's row lie
+        __align__(16) int pages[WAVES][64];                        // entries of the block table, a lane's each
+        __align__(4) uint8_t seen[2][kBatch][TILE];                // whether anybody sees the key
+        int hidden[2][kBatch][WAVES];                              // whether a wave found one that nobody sees
         int spoiled;                                               // whether a tile held values that are no numbers, see spoil
-        int64_t sum[kWaves];
+        int first_tree;
+        int64_t sum[WAVES];
     };
 
     // A tile: positions of the cache from `base` on, or nodes.
@@ -161,15 +180,15 @@ struct Attention {
 
     const AttentionArgs& g;
     Shared& sh;
-    const int lane, wave, l16, quad, wq, wk;
+    const uint32_t shared_at;                                      // of `sh` in LDS
+    const int lane, wave, l16, quad;
     // the unit
     int b, kv;
     TreeWork t;
-    int table_first = -1;                                          // first column of sh.table; -1: none
 
     __device__ Attention(const AttentionArgs& args, Shared& s)
-        : g(args), sh(s), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), l16(lane & 15), quad(lane >> 4),
-          wq(wave % WQ), wk(wave / WQ) {}
+        : g(args), sh(s), shared_at(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)&s)), lane(threadIdx.x & 63),
+          wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), l16(lane & 15), quad(lane >> 4) {}
 
     static __device__ __forceinline__ int swizzle(int row) { return kChunks >= 16 ? row & 15 : (row >> 1) & 7; }
 
@@ -180,70 +199,74 @@ struct Attention {
         return x;
     }
 
-    // The block table's entries that a tile of the cache needs are in LDS afterwards.  Every wave calls it.
-    __device__ __forceinline__ void have_table(const Tile& x) {
-        if (x.tree) return;
-        const int first = x.base / g.a.page_size, last = (min(x.base + TILE, t.context) - 1) / g.a.page_size;
-        if (table_first >= 0 && first >= table_first && last < table_first + kTableChunk) return;
-        __syncthreads();                                           // nobody reads the old ones any more
-        const int32_t* row = g.b.block_table + static_cast<int64_t>(b) * g.a.table_width;
-        for (int i = threadIdx.x; i < kTableChunk; i += kThreads) sh.table[i] = first + i < g.a.table_width ? row[first + i] : -1;
-        table_first = first;
-        __syncthreads();
+    // ---- a batch of tiles: lane i has row i % kMyRows of this wave's in tile i / kMyRows
+    struct Row { int key, at; bool tree, seen; };                  // place in the tile, position or node; seen: as far as lengths say
+    __device__ __forceinline__ Row row_of(int lane, int tile, int last) const {
+        const int mine = tile + lane / kMyRows;
+        const Tile x = tile_at(mine);
+        Row r;
+        r.key = wave * kMyRows + lane % kMyRows;
+        r.at = x.base + r.key;
+        r.tree = x.tree;
+        r.seen = mine < last && (x.tree ? r.at < t.nodes
+                                        : r.at < t.context && (g.a.window <= 0 || r.at > t.context - g.a.window || r.at < g.a.sinks));
+        return r;
     }
-
-    // Asks for a tile.  A key that nobody sees is read as zeros.
-    __device__ __forceinline__ void ask(const Tile& x, int stage) {
-        // lane i finds out where the i-th of this wave's rows lies
-        const int mine = (wave + kWaves * (lane / kRowsPerLoad)) * kRowsPerLoad + lane % kRowsPerLoad;
-        const int at = x.base + mine;
-        bool seen = mine < TILE && lane < kMyLoads * kRowsPerLoad;
-        int64_t offset = 0;
+    // Asks for the block table's entries of the batch that begins with `tile`.
+    __device__ __forceinline__ void ask_pages(int tile, int last) {
+        const Row r = row_of(fresh(lane), tile, last);
+        const int32_t* entry = g.b.block_table + static_cast<int64_t>(b) * g.a.table_width + r.at / g.a.page_size;
+        const uint64_t from = r.seen && !r.tree ? reinterpret_cast<uint64_t>(entry) : reinterpret_cast<uint64_t>(&kZeros);
+        word_to_lds(from, shared_at + offsetof(Shared, pages) + wave * 256);
+    }
+    // The entries are there: works out the places of the batch's rows.
+    __device__ __forceinline__ void look_up(int tile, int last, int half) {
+        const int lane = fresh(this->lane);
+        Row r = row_of(lane, tile, last);
+        int64_t offset;
         const char *keys, *values;
-        if (x.tree) {
-            seen = seen && at < t.nodes;
-            offset = (static_cast<int64_t>(b) * g.a.N + at) * g.a.kv_stride;
+        if (r.tree) {
+            offset = (static_cast<int64_t>(b) * g.a.N + r.at) * g.a.kv_stride;
             keys = static_cast<const char*>(g.b.tree_k);
             values = static_cast<const char*>(g.b.tree_v);
         } else {
-            seen = seen && at < t.context && (g.a.window <= 0 || at > t.context - g.a.window || at < g.a.sinks);
-            if (seen) {
-                const int column = at / g.a.page_size, page = sh.table[column - table_first];
-                seen = page >= 0 && page < g.a.num_pages;
-                offset = page * g.a.page_stride + (at - column * g.a.page_size) * g.a.slot_stride;
-            }
+            const int page = sh.pages[wave][lane];
+            r.seen = r.seen && page >= 0 && page < g.a.num_pages;
+            offset = page * g.a.page_stride + r.at % g.a.page_size * g.a.slot_stride;
             keys = static_cast<const char*>(g.b.cache_k);
             values = static_cast<const char*>(g.b.cache_v);
         }
-        offset = seen ? (offset + static_cast<int64_t>(kv) * g.a.head_dim) * E::kBytes : -1;
-        const bool mine_real = mine < TILE && lane < kMyLoads * kRowsPerLoad;
-        if (mine_real) sh.seen[stage][mine] = seen;
-        const bool any_hidden = __ballot(mine_real && !seen) != 0;
-        if (lane == 0) sh.hidden[stage][wave] = any_hidden;
+        offset = (offset + static_cast<int64_t>(kv) * g.a.head_dim) * E::kBytes;
+        const int sub = lane / kMyRows;
+        const uint64_t zeros = reinterpret_cast<uint64_t>(&kZeros);
+        sh.seen[half][sub][r.key] = r.seen;
+        sh.place[half][sub][r.key][0] = r.seen ? reinterpret_cast<uint64_t>(keys) + offset : zeros;
+        sh.place[half][sub][r.key][1] = r.seen ? reinterpret_cast<uint64_t>(values) + offset : zeros;
+        const unsigned long long hidden = __ballot(!r.seen) >> (sub * kMyRows % 64);
+        if (lane % kMyRows == 0) sh.hidden[half][sub][wave] = kMyRows == 64 ? hidden != 0 : (hidden & ((1ull << (kMyRows % 64)) - 1)) != 0;
+    }
+
+    // Asks for a tile whose places are known.  A key that nobody sees is read as zeros.
+    __device__ __forceinline__ void ask(int half, int sub, int stage) {
+        const uint32_t to = shared_at + stage * kTileBytes + wave * kMyLoads * 1024;
 #pragma unroll
         for (int j = 0; j < kMyLoads; ++j) {
-            const int load = wave + kWaves * j;
-            if (kLoads % kWaves == 0 || load < kLoads) {
-                const int row = load * kRowsPerLoad + lane / kChunks;
-                const int chunk = (lane % kChunks) ^ swizzle(row);
-                const int64_t from = static_cast<int64_t>(shfl64(static_cast<unsigned long long>(offset), j * kRowsPerLoad + lane / kChunks));
-                const bool real = from >= 0 && chunk * 16 < g.a.head_dim * E::kBytes;
-                const int64_t place = from + chunk * 16;
-                to_lds(real ? keys + place : reinterpret_cast<const char*>(&kZeros), sh.keys[stage] + load * 1024);
-                to_lds(real ? values + place : reinterpret_cast<const char*>(&kZeros), sh.values[stage] + load * 1024);
-            }
+            const int row = wave * kMyRows + j * kRowsPerLoad + lane / kChunks;
+            const int chunk = (lane % kChunks) ^ swizzle(row);
+            uint64_t k = sh.place[half][sub][row][0] + chunk * 16, v = sh.place[half][sub][row][1] + chunk * 16;
+            if (chunk * 16 >= g.a.head_dim * E::kBytes) k = v = reinterpret_cast<uint64_t>(&kZeros);
+            to_lds(k, to + j * 1024);
+            to_lds(v, to + STAGES * kTileBytes + j * 1024);
         }
     }
 
-    // Waits until the tile before the last one that was asked for (ahead) or the last one is there, for all waves.
-    __device__ __forceinline__ void arrive(bool ahead) {
-        if (!ahead) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        else if (kLoads % kWaves == 0 || wave < kLoads % kWaves) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kMyLoads) : "memory");
-        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kMyLoads - 2) : "memory");
+    // Waits, for all waves, for the tile that kAheadTiles - 1 others were asked for after (more: otherwise for all); all waves are
+    // done with the tile before it then.
+    __device__ __forceinline__ void arrive(bool more) {
+        if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kMyLoads * (kAheadTiles - 1)) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
-    // All waves are done with what they read.
-    __device__ __forceinline__ void leave() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
     // ---- the rows of this lane's queries
     u32x4 query[QT][kSteps];
@@ -253,6 +276,7 @@ struct Attention {
     float top[QT], weight[QT];                                     // reference; sum of weights (this lane's keys)
 
     __device__ __forceinline__ void begin(int block) {
+        const int lane = fresh(this->lane), l16 = lane & 15, quad = lane >> 4;
         const int group = g.a.heads / g.a.kv_heads;
         // ancestors of node `lane`: in each round twice as many steps up
         unsigned long long mask = 1ull << lane;
@@ -268,7 +292,7 @@ struct Attention {
         }
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
-            const int row = block * kRows + (wq * QT + q) * 16 + l16;
+            const int row = block * kRows + (wave * QT + q) * 16 + l16;
             const int node = row / group;
             const bool real = node < t.nodes;
             line[q] = shfl64(mask, real ? node : 0);
@@ -291,45 +315,61 @@ struct Attention {
     }
 
     // A tile in LDS: products, weights, and their sum over the values.
-    __device__ __forceinline__ void work(const Tile& x, int stage) {
-        const char* keys = sh.keys[stage] + wk * kKeys * kChunks * 16;
-        char* values = sh.values[stage] + wk * kKeys * kChunks * 16;
+    __device__ __forceinline__ void work(const Tile& x, int half, int sub, int stage) {
+        const char* keys = sh.keys[stage];
+        char* values = sh.values[stage];
         f32x4 s[QT][kGroups];
         const int key_swizzle = swizzle(l16);
+        // (operands are read kAhead instructions before their use, which the order of the source alone does not bring about)
+        constexpr int kAhead = 4, kFirst = kGroups * kSteps;
+        u32x4 a[kAhead];
+        auto read_key = [&](int n) {
+            const int k = n / kSteps, d = n % kSteps;
+            return *reinterpret_cast<const u32x4*>(keys + ((k * 16 + l16) * kChunks + ((d * 4 + quad) ^ key_swizzle)) * 16);
+        };
 #pragma unroll
-        for (int k = 0; k < kGroups; ++k) {
+        for (int n = 0; n < kAhead; ++n) a[n] = read_key(n);
 #pragma unroll
-            for (int q = 0; q < QT; ++q) s[q][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int n = 0; n < kFirst; ++n) {
+            const int k = n / kSteps, d = n % kSteps;
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int d = 0; d < kSteps; ++d) {
-                const u32x4 a = *reinterpret_cast<const u32x4*>(keys + ((k * 16 + l16) * kChunks + ((d * 4 + quad) ^ key_swizzle)) * 16);
+            for (int q = 0; q < QT; ++q) {
+                if (d == 0) s[q][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if constexpr (k16) {
+                    s[q][k] = E::mfma(a[n % kAhead], query[q][d], s[q][k]);
+                } else {
+                    const f32x4 fa = __builtin_bit_cast(f32x4, a[n % kAhead]), fq = __builtin_bit_cast(f32x4, query[q][d]);
 #pragma unroll
-                for (int q = 0; q < QT; ++q) {
-                    if constexpr (k16) {
-                        s[q][k] = E::mfma(a, query[q][d], s[q][k]);
-                    } else {
-                        const f32x4 fa = __builtin_bit_cast(f32x4, a), fq = __builtin_bit_cast(f32x4, query[q][d]);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) s[q][k] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[i], fq[i], s[q][k], 0, 0, 0);
-                    }
+                    for (int i = 0; i < 4; ++i) s[q][k] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[i], fq[i], s[q][k], 0, 0, 0);
                 }
             }
+            if (n + kAhead < kFirst) a[n % kAhead] = read_key(n + kAhead);
         }
+        __builtin_amdgcn_sched_barrier(0);
         // ---- what is not seen
         const bool differ = differs(x);
         bool hidden = x.tree || differ;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) hidden = hidden || sh.hidden[stage][w];
+        for (int w = 0; w < kWaves; ++w) hidden = hidden || __builtin_amdgcn_readfirstlane(sh.hidden[half][sub][w]);
         if (hidden) {
 #pragma unroll
-            for (int k = 0; k < kGroups; ++k) {
-                const int key = wk * kKeys + k * 16 + quad * 4;
-                const uint32_t there = *reinterpret_cast<const uint32_t*>(&sh.seen[stage][key]);
+            for (int q = 0; q < QT; ++q) {
+                const int quad = fresh(lane) >> 4;
+                uint32_t bits = 0;                                 // of this lane's keys, those that its query sees
+                for (int k = 0; k < kGroups; ++k) {
+                    const int key = k * 16 + quad * 4;
+                    const uint32_t there = *reinterpret_cast<const uint32_t*>(&sh.seen[half][sub][key]);
+#pragma unroll 1
+                    for (int i = 0; i < 4; ++i) bits |= static_cast<uint32_t>((there >> (8 * i) & 1) && sees(x, key + i, q)) << (k * 4 + i);
+                }
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int k = 0; k < kGroups; ++k)
 #pragma unroll
-                    for (int q = 0; q < QT; ++q)
-                        if (!(there >> (8 * i) & 1) || !sees(x, key + i, q)) s[q][k][i] = -INFINITY;
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t keep = spread(bits, k * 4 + i);
+                        s[q][k][i] = __uint_as_float((__float_as_uint(s[q][k][i]) & keep) | (0xff800000u & ~keep));
+                    }
             }
             // a value that is no number must not reach the nodes that do not see it
             if (differ && !all_numbers(values)) {
@@ -383,16 +423,22 @@ struct Attention {
             weight[q] += sum;
         }
         // ---- their sum over the values
+        if constexpr (k16) {
+            constexpr int kSecond = kColumns * (kGroups / 2);
 #pragma unroll
-        for (int c = 0; c < kColumns; ++c) {
-            if constexpr (k16) {
+            for (int n = 0; n < kAhead; ++n) a[n] = column16(values, n % (kGroups / 2), n / (kGroups / 2));
 #pragma unroll
-                for (int k = 0; k < kGroups / 2; ++k) {
-                    const u32x4 v = column16(values, k, c);
+            for (int n = 0; n < kSecond; ++n) {
+                const int k = n % (kGroups / 2), c = n / (kGroups / 2);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int q = 0; q < QT; ++q) out[q][c] = E::mfma(v, w16[q][k], out[q][c]);
-                }
-            } else {
+                for (int q = 0; q < QT; ++q) out[q][c] = E::mfma(a[n % kAhead], w16[q][k], out[q][c]);
+                if (n + kAhead < kSecond) a[n % kAhead] = column16(values, (n + kAhead) % (kGroups / 2), (n + kAhead) / (kGroups / 2));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        } else {
+#pragma unroll
+            for (int c = 0; c < kColumns; ++c) {
 #pragma unroll
                 for (int k = 0; k < kGroups; ++k)
 #pragma unroll
@@ -429,7 +475,7 @@ struct Attention {
         bool fine = true;
         if constexpr (k16) {
             u16x2 most = {0, 0};
-            for (int i = lane; i < kKeys * kChunks; i += 64) {
+            for (int i = fresh(lane); i < TILE * kChunks; i += 64) {
                 const u32x4 v = *reinterpret_cast<const u32x4*>(values + i * 16) & 0x7fff7fffu;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, static_cast<uint32_t>(v[j])));
@@ -437,7 +483,7 @@ struct Attention {
             fine = most[0] < E::kInf && most[1] < E::kInf;
         } else {
             uint32_t most = 0;
-            for (int i = lane; i < kKeys * kChunks; i += 64) {
+            for (int i = fresh(lane); i < TILE * kChunks; i += 64) {
                 const u32x4 v = *reinterpret_cast<const u32x4*>(values + i * 16) & 0x7fffffffu;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) most = max(most, static_cast<uint32_t>(v[j]));
@@ -449,7 +495,7 @@ struct Attention {
 
     // Values of a tile that are no numbers become 0.  (Waves that share the keys may do so at once, each for itself.)
     __device__ __forceinline__ void only_numbers(char* values) {
-        for (int i = lane; i < kKeys * kChunks; i += 64) {
+        for (int i = fresh(lane); i < TILE * kChunks; i += 64) {
             u32x4 v = *reinterpret_cast<u32x4*>(values + i * 16);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -477,31 +523,31 @@ struct Attention {
         return t.nodes > 1 && (x.tree || (g.a.window > 0 && x.base < t.context + t.nodes - g.a.window && x.base + TILE > g.a.sinks));
     }
     __device__ __forceinline__ bool sees(const Tile& x, int key, int q) const {
-        int place = x.base + key;
-        bool yes = true;
-        if (x.tree) {
-            const int node = place & 63;
-            yes = (line[q] >> node) & 1;
-            place = t.context + __popcll(line[q] & ((1ull << node) - 1));
-        }
-        return yes && (place >= low[q] || place < g.a.sinks);
+        const int at = x.base + key, node = at & 63;
+        const int place = x.tree ? t.context + __popcll(line[q] & ((1ull << node) - 1)) : at;
+        const int near = static_cast<int>(place >= low[q]) | static_cast<int>(place < g.a.sinks);
+        return near & (x.tree ? static_cast<int>(line[q] >> node & 1) : 1);
     }
 
     // A tile whose nodes see different keys held values that are no numbers: they were left out of the sums, and the rows that see
     // them get them now.  The tiles in question are brought in again.
     __device__ __forceinline__ void spoil(int first, int last) {
+        const int quad = fresh(lane) >> 4;
         for (int i = first; i < last; ++i) {
             const Tile x = tile_at(i);
             if (!differs(x)) continue;
-            have_table(x);
-            ask(x, 0);
+            __syncthreads();
+            ask_pages(i, i + 1);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            look_up(i, i + 1, 0);
+            ask(0, 0, 0);
             arrive(false);
-            const char* values = sh.values[0] + wk * kKeys * kChunks * 16;
+            const char* values = sh.values[0];
 #pragma unroll
             for (int q = 0; q < QT; ++q) {
                 uint32_t up[4] = {}, down[4] = {};                 // by column group: an infinity of either sign is seen (NaN: both)
-                for (int key = 0; key < kKeys; ++key) {
-                    if (!sh.seen[0][wk * kKeys + key] || !sees(x, wk * kKeys + key, q)) continue;
+                for (int key = 0; key < TILE; ++key) {
+                    if (!sh.seen[0][0][key] || !sees(x, key, q)) continue;
                     for (int c = 0; c < kColumns; ++c)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
@@ -514,83 +560,53 @@ struct Attention {
                 for (int c = 0; c < kColumns; ++c)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        if (up[j] >> c & 1) out[q][c][j] += INFINITY;
-                        if (down[j] >> c & 1) out[q][c][j] -= INFINITY;
+                        out[q][c][j] += __uint_as_float(spread(up[j], c) & 0x7f800000u);
+                        out[q][c][j] += __uint_as_float(spread(down[j], c) & 0xff800000u);
                     }
             }
-            leave();
         }
     }
 
     // The unit's part [first, last) of its tiles.
     __device__ __forceinline__ void run(int block, int first, int last) {
-        table_first = -1;
-        Tile now = tile_at(first);
         if (threadIdx.x == 0) sh.spoiled = 0;                      // (read by all before the last barrier of the unit before)
-        have_table(now);
-        ask(now, 0);
+        ask_pages(first, last);
         begin(block);
-        for (int i = first, stage = 0; i < last; ++i, stage ^= 1) {
-            const bool ahead = i + 1 < last;
-            Tile next = now;
-            if (ahead) {
-                next = tile_at(i + 1);
-                have_table(next);
-                ask(next, stage ^ 1);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        // turn n asks for tile first + n and works on the tile kAheadTiles before it
+        const int count = last - first;
+#pragma unroll 1
+        for (int n = 0; n < count + kAheadTiles; ++n) {
+            const int mine = n - kAheadTiles;
+            if (mine >= 0) arrive(n <= count);
+            if (n < count) {
+                const int sub = n % kBatch, half = n / kBatch & 1;
+                if (sub == 0) {
+                    look_up(first + n, last, half);
+                    if (n + kBatch < count) ask_pages(first + n + kBatch, last);
+                }
+                ask(half, sub, n % STAGES);
             }
-            arrive(ahead);
-            work(now, stage);
-            leave();
-            now = next;
+            if (mine >= 0) work(tile_at(first + mine), mine / kBatch & 1, mine % kBatch, mine % STAGES);
         }
+        __syncthreads();
         if (__builtin_amdgcn_readfirstlane(sh.spoiled)) spoil(first, last);
         __syncthreads();
-        // ---- the lanes and the waves that share rows put their sums together
+        // ---- the lanes that share rows put their sums together
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
             weight[q] += __shfl_xor(weight[q], 16);
             weight[q] += __shfl_xor(weight[q], 32);
         }
-        if constexpr (WK > 1) {
-            constexpr int kFloats = QT * (kColumns * 4 + 2) * 64;          // of a wave
-            static_assert(kFloats * 4 * WQ <= 4 * kTileBytes, "room for the waves' sums");
-            float* mine = reinterpret_cast<float*>(&sh) + wq * kFloats;
-            for (int other = 1; other < WK; ++other) {
-                if (wk == other) {
-#pragma unroll
-                    for (int q = 0; q < QT; ++q) {
-#pragma unroll
-                        for (int c = 0; c < kColumns; ++c) *reinterpret_cast<f32x4*>(mine + ((q * kColumns + c) * 64 + lane) * 4) = out[q][c];
-                        mine[QT * kColumns * 256 + q * 128 + lane] = top[q];
-                        mine[QT * kColumns * 256 + q * 128 + 64 + lane] = weight[q];
-                    }
-                }
-                __syncthreads();
-                if (wk == 0) {
-#pragma unroll
-                    for (int q = 0; q < QT; ++q) {
-                        const float their_top = mine[QT * kColumns * 256 + q * 128 + lane];
-                        const float now_top = fmaxf(top[q], their_top), base = now_top == -INFINITY ? 0.0f : now_top;
-                        const float fade = exp2_of(top[q] - base), theirs = exp2_of(their_top - base);
-                        top[q] = now_top;
-                        weight[q] = weight[q] * fade + mine[QT * kColumns * 256 + q * 128 + 64 + lane] * theirs;
-#pragma unroll
-                        for (int c = 0; c < kColumns; ++c)
-                            out[q][c] = out[q][c] * fade + *reinterpret_cast<const f32x4*>(mine + ((q * kColumns + c) * 64 + lane) * 4) * theirs;
-                    }
-                }
-                __syncthreads();
-            }
-        }
     }
 
     // Whole rows of the output.
     __device__ __forceinline__ void finish(int block) {
-        if (wk != 0) return;
+        const int lane = fresh(this->lane), l16 = lane & 15, quad = lane >> 4;
         const int group = g.a.heads / g.a.kv_heads;
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
-            const int row = block * kRows + (wq * QT + q) * 16 + l16;
+            const int row = block * kRows + (wave * QT + q) * 16 + l16;
             const int node = row / group;
             if (node >= t.nodes) continue;
             const float whole = 1.0f / weight[q];
@@ -603,10 +619,10 @@ struct Attention {
     }
 
     __device__ __forceinline__ void keep(int slot) {
-        if (wk != 0) return;
+        const int lane = fresh(this->lane), l16 = lane & 15, quad = lane >> 4;
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
-            const int64_t row = static_cast<int64_t>(slot) * kRows + (wq * QT + q) * 16 + l16;
+            const int64_t row = static_cast<int64_t>(slot) * kRows + (wave * QT + q) * 16 + l16;
             if (quad == 0) g.partial_stats[row] = make_float2(top[q], weight[q]);
 #pragma unroll
             for (int c = 0; c < kColumns; ++c) *reinterpret_cast<f32x4*>(g.partial + row * DP + c * 16 + quad * 4) = out[q][c];
@@ -656,10 +672,10 @@ struct Attention {
             if (begin_at < start + sum) {
                 const bool here = begin_at >= start + before && begin_at < start + before + mine;
                 __syncthreads();
-                if (here) { sh.sum[0] = start + before; sh.table[0] = base + threadIdx.x; }
+                if (here) { sh.sum[0] = start + before; sh.first_tree = base + threadIdx.x; }
                 __syncthreads();
                 start = sh.sum[0];
-                b = __builtin_amdgcn_readfirstlane(sh.table[0]);
+                b = __builtin_amdgcn_readfirstlane(sh.first_tree);
                 __syncthreads();
                 break;
             }
@@ -740,16 +756,19 @@ __global__ __launch_bounds__(256) void combine_kernel(AttentionArgs g) {
 
 // ------------------------------------------------------------------ host side
 
-// Workgroups of a call: two a compute unit, which is what the tiles in LDS leave room for (more only where a team alone has more).
-constexpr int kMaxWorkgroups = 512;
+// Workgroups of a call: two or three a compute unit, which is what the tiles in LDS leave room for (more only where a team alone has more).
+template <class A>
+constexpr int kMaxWorkgroups = 256 * (160 * 1024 / sizeof(typename A::Shared) < 3 ? 2 : 3);
 
-// The tile and the waves' shares for a type and a row length.  A tile of keys is 16 KB (two stages of keys and values: 64 KB).
-template <int DTYPE, int DP>
+// The tile for a type and a row length: 8 KB of keys (16 for the longest rows) and as many of values, in four stages of 16 KB or two
+// of 32 KB.
+template <int DTYPE, int DP, int WAVES>
 struct Family {
-    static constexpr int kTile = 16384 / (DP * Elem<DTYPE>::kBytes);
-    static constexpr int kMostWK = kTile / (Elem<DTYPE>::kBytes == 2 ? 32 : 16) < 4 ? kTile / (Elem<DTYPE>::kBytes == 2 ? 32 : 16) : 4;
-    // two 16-row groups a wave where their queries and sums leave registers for the products
-    static constexpr int kMostQT = DP * Elem<DTYPE>::kBytes <= 256 || (DTYPE == MPV_DTYPE_F32 && DP == 128) ? 2 : 1;
+    static constexpr int kBytes = DP * Elem<DTYPE>::kBytes;
+    static constexpr int kLeast = DTYPE == MPV_DTYPE_F32 ? 16 : 32;
+    static constexpr int kMost = 8192 / kBytes < 16 * WAVES ? 8192 / kBytes : 16 * WAVES;      // (a lane looks up a row of some tiles ahead)
+    static constexpr int kTile = kMost < kLeast ? kLeast : kMost;
+    static constexpr int kStages = kTile * kBytes > 8192 ? 2 : WAVES == 1 ? 3 : 4;
 };
 
 // What a call needs to know of the kernel that it gets.
@@ -775,7 +794,7 @@ static Choice choice_of(const mpv_attention* a) {
     }
     const int64_t unit = seen + (a->N + c.tile - 1) / c.tile;
     c.tiles = unit * a->B * a->kv_heads;
-    c.teams = kMaxWorkgroups / c.blocks;
+    c.teams = kMaxWorkgroups<A> / c.blocks;
     if (c.teams >= 8) c.teams = c.teams / 8 * 8;
     if (c.tiles < c.teams) c.teams = static_cast<int>(c.tiles);
     if (c.teams < 1) c.teams = 1;
@@ -811,23 +830,23 @@ static int with_kernel(const mpv_attention* a, AttentionArgs* g, void* workspace
     return launched();
 }
 
+template <int DTYPE, int DP, int QT, int WAVES>
+using Kernel = Attention<DTYPE, DP, QT, WAVES, Family<DTYPE, DP, WAVES>::kTile, Family<DTYPE, DP, WAVES>::kStages>;
+
 template <int DTYPE, int DP>
 static int with_columns(const mpv_attention* a, AttentionArgs* g, void* workspace, size_t* bytes, hipStream_t s) {
-    typedef Family<DTYPE, DP> F;
-    constexpr int T = F::kTile, WK = F::kMostWK;
     const int64_t rows = static_cast<int64_t>(a->N) * (a->heads / a->kv_heads);
-    if (rows <= 16) return with_kernel<Attention<DTYPE, DP, 1, 1, WK, T>, DTYPE, DP>(a, g, workspace, bytes, s);
-    if constexpr (F::kMostQT == 2) {
-        if (rows <= 32) return with_kernel<Attention<DTYPE, DP, 2, 1, WK, T>, DTYPE, DP>(a, g, workspace, bytes, s);
-        if (rows <= 64) return with_kernel<Attention<DTYPE, DP, 2, 2, (WK < 2 ? WK : 2), T>, DTYPE, DP>(a, g, workspace, bytes, s);
-        // as many rows a workgroup as divide the largest tree into even blocks
-        const int64_t blocks = (rows + 127) / 128;
-        if ((rows + blocks - 1) / blocks <= 96) return with_kernel<Attention<DTYPE, DP, 2, 3, 1, T>, DTYPE, DP>(a, g, workspace, bytes, s);
-        return with_kernel<Attention<DTYPE, DP, 2, 4, 1, T>, DTYPE, DP>(a, g, workspace, bytes, s);
-    } else {
-        if (rows <= 32) return with_kernel<Attention<DTYPE, DP, 1, 2, 1, T>, DTYPE, DP>(a, g, workspace, bytes, s);
-        return with_kernel<Attention<DTYPE, DP, 1, 4, 1, T>, DTYPE, DP>(a, g, workspace, bytes, s);
-    }
+    if (rows <= 16) return with_kernel<Kernel<DTYPE, DP, 1, 1>, DTYPE, DP>(a, g, workspace, bytes, s);
+    if (rows <= 32) return with_kernel<Kernel<DTYPE, DP, 1, 2>, DTYPE, DP>(a, g, workspace, bytes, s);
+    if (rows <= 64) return with_kernel<Kernel<DTYPE, DP, 1, 4>, DTYPE, DP>(a, g, workspace, bytes, s);
+    // the most groups a wave that leave its registers room for the products; as many as divide the rows into even blocks
+    constexpr int kMost = DP * Elem<DTYPE>::kBytes <= 256 ? 3 : DP == 128 ? 2 : 1;
+    const int64_t blocks = (rows + 64 * kMost - 1) / (64 * kMost), groups = (rows + 64 * blocks - 1) / (64 * blocks);
+    if constexpr (kMost >= 3)
+        if (groups > 2) return with_kernel<Kernel<DTYPE, DP, 3, 4>, DTYPE, DP>(a, g, workspace, bytes, s);
+    if constexpr (kMost >= 2)
+        if (groups > 1) return with_kernel<Kernel<DTYPE, DP, 2, 4>, DTYPE, DP>(a, g, workspace, bytes, s);
+    return with_kernel<Kernel<DTYPE, DP, 1, 4>, DTYPE, DP>(a, g, workspace, bytes, s);
 }
 
 template <int DTYPE>
