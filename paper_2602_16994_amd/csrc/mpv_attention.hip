@@ -18,6 +18,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstddef>
 #include <cstring>
@@ -58,7 +59,7 @@ template <> struct Elem<MPV_DTYPE_BF16> {
     typedef bf16x8 Vec;
     static constexpr int kBytes = 2;
     static constexpr float kBias = 0.0f;
-    static constexpr uint32_t kInf = 0x7f80;
+    static constexpr uint32_t kInf = 0x7f80, kOnes = 0x3f803f80;
     static __device__ __forceinline__ f32x4 mfma(const u32x4& a, const u32x4& b, const f32x4& c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     }
@@ -74,7 +75,7 @@ template <> struct Elem<MPV_DTYPE_F16> {
     typedef f16x8 Vec;
     static constexpr int kBytes = 2;
     static constexpr float kBias = 6.0f;   // weights are kept 2^6 times as large, so that the small ones stay normal numbers
-    static constexpr uint32_t kInf = 0x7c00;
+    static constexpr uint32_t kInf = 0x7c00, kOnes = 0x3c003c00;
     static __device__ __forceinline__ f32x4 mfma(const u32x4& a, const u32x4& b, const f32x4& c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
     }
@@ -169,7 +170,7 @@ struct Attention {
         __align__(16) uint64_t place[2][kBatch][TILE][2];          // where a key's and its value's row lie
         __align__(16) int pages[WAVES][64];                        // entries of the block table, a lane's each
         __align__(4) uint8_t seen[2][kBatch][TILE];                // whether anybody sees the key
-        int hidden[2][kBatch][WAVES];                              // whether a wave found one that nobody sees
+        __align__(4) uint8_t special[2][kBatch][4];                // whether a wave found a key that not every node sees
         int spoiled;                                               // whether a tile held values that are no numbers, see spoil
         int first_tree;
         int64_t sum[WAVES];
@@ -242,18 +243,26 @@ struct Attention {
         sh.seen[half][sub][r.key] = r.seen;
         sh.place[half][sub][r.key][0] = r.seen ? reinterpret_cast<uint64_t>(keys) + offset : zeros;
         sh.place[half][sub][r.key][1] = r.seen ? reinterpret_cast<uint64_t>(values) + offset : zeros;
-        const unsigned long long hidden = __ballot(!r.seen) >> (sub * kMyRows % 64);
-        if (lane % kMyRows == 0) sh.hidden[half][sub][wave] = kMyRows == 64 ? hidden != 0 : (hidden & ((1ull << (kMyRows % 64)) - 1)) != 0;
+        const unsigned long long mask = kMyRows == 64 ? ~0ull : (1ull << (kMyRows % 64)) - 1;
+        const bool hidden = (__ballot(!r.seen) >> (sub * kMyRows % 64) & mask) != 0;
+        // (a wave of several writes its own byte, one of two writes two)
+        if (lane % kMyRows < 4 / WAVES)
+            sh.special[half][sub][wave + lane % kMyRows * WAVES] = hidden || r.tree || differs(tile_at(tile + sub));
     }
 
     // Asks for a tile whose places are known.  A key that nobody sees is read as zeros.
     __device__ __forceinline__ void ask(int half, int sub, int stage) {
         const uint32_t to = shared_at + stage * kTileBytes + wave * kMyLoads * 1024;
+        typedef __attribute__((ext_vector_type(2))) uint64_t u64x2;
+        u64x2 place[kMyLoads];
+#pragma unroll
+        for (int j = 0; j < kMyLoads; ++j)
+            place[j] = *reinterpret_cast<const u64x2*>(sh.place[half][sub][wave * kMyRows + j * kRowsPerLoad + lane / kChunks]);
 #pragma unroll
         for (int j = 0; j < kMyLoads; ++j) {
             const int row = wave * kMyRows + j * kRowsPerLoad + lane / kChunks;
             const int chunk = (lane % kChunks) ^ swizzle(row);
-            uint64_t k = sh.place[half][sub][row][0] + chunk * 16, v = sh.place[half][sub][row][1] + chunk * 16;
+            uint64_t k = place[j][0] + chunk * 16, v = place[j][1] + chunk * 16;
             if (chunk * 16 >= g.a.head_dim * E::kBytes) k = v = reinterpret_cast<uint64_t>(&kZeros);
             to_lds(k, to + j * 1024);
             to_lds(v, to + STAGES * kTileBytes + j * 1024);
@@ -273,7 +282,8 @@ struct Attention {
     unsigned long long line[QT];                                   // the node and its ancestors
     int low[QT];                                                   // first position seen (but for the sinks)
     f32x4 out[QT][kColumns];
-    float top[QT], weight[QT];                                     // reference; sum of weights (this lane's keys)
+    float top[QT], base[QT];                                       // reference; what is added to an exponent
+    f32x4 weight[QT];                                              // sum of weights: in all four, or (float32) of this lane's keys in the first
 
     __device__ __forceinline__ void begin(int block) {
         const int lane = fresh(this->lane), l16 = lane & 15, quad = lane >> 4;
@@ -308,7 +318,8 @@ struct Attention {
                 query[q][s] = v;
             }
             top[q] = -INFINITY;
-            weight[q] = 0.0f;
+            base[q] = 0.0f;
+            weight[q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < kColumns; ++c) out[q][c] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
@@ -318,6 +329,7 @@ struct Attention {
     __device__ __forceinline__ void work(const Tile& x, int half, int sub, int stage) {
         const char* keys = sh.keys[stage];
         char* values = sh.values[stage];
+        const uint32_t special = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint32_t*>(sh.special[half][sub]));
         f32x4 s[QT][kGroups];
         const int key_swizzle = swizzle(l16);
         // (operands are read kAhead instructions before their use, which the order of the source alone does not bring about)
@@ -348,11 +360,7 @@ struct Attention {
         }
         __builtin_amdgcn_sched_barrier(0);
         // ---- what is not seen
-        const bool differ = differs(x);
-        bool hidden = x.tree || differ;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) hidden = hidden || __builtin_amdgcn_readfirstlane(sh.hidden[half][sub][w]);
-        if (hidden) {
+        if (special) {
 #pragma unroll
             for (int q = 0; q < QT; ++q) {
                 const int quad = fresh(lane) >> 4;
@@ -372,7 +380,7 @@ struct Attention {
                     }
             }
             // a value that is no number must not reach the nodes that do not see it
-            if (differ && !all_numbers(values)) {
+            if (differs(x) && !all_numbers(values)) {
                 only_numbers(values);
                 sh.spoiled = 1;
             }
@@ -392,6 +400,7 @@ struct Attention {
                 const float now = fmaxf(top[q], most);
                 const float fade = now == -INFINITY ? 1.0f : exp2_of(top[q] - now);
                 top[q] = now;
+                base[q] = now == -INFINITY ? 0.0f : E::kBias - now;
                 weight[q] *= fade;
 #pragma unroll
                 for (int c = 0; c < kColumns; ++c) out[q][c] *= fade;
@@ -401,14 +410,12 @@ struct Attention {
         u32x4 w16[QT][k16 ? kGroups / 2 : 1];
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
-            const float base = top[q] == -INFINITY ? 0.0f : E::kBias - top[q];
-            float sum = 0.0f;
 #pragma unroll
             for (int k = 0; k < kGroups; ++k) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    s[q][k][i] = exp2_of(fmaf(s[q][k][i], g.factor, base));
-                    sum += s[q][k][i];
+                    s[q][k][i] = exp2_of(fmaf(s[q][k][i], g.factor, base[q]));
+                    if constexpr (!k16) weight[q][0] += s[q][k][i];
                 }
                 if constexpr (k16) {
                     typedef __attribute__((ext_vector_type(4))) typename E::T x4;
@@ -420,7 +427,10 @@ struct Attention {
                     w16[q][k / 2][(k & 1) * 2 + 1] = p.y;
                 }
             }
-            weight[q] += sum;
+            // (a product with ones adds up the rounded weights, those that meet the values)
+            if constexpr (k16)
+#pragma unroll
+                for (int k = 0; k < kGroups / 2; ++k) weight[q] = E::mfma(u32x4{E::kOnes, E::kOnes, E::kOnes, E::kOnes}, w16[q][k], weight[q]);
         }
         // ---- their sum over the values
         if constexpr (k16) {
@@ -593,11 +603,12 @@ struct Attention {
         if (__builtin_amdgcn_readfirstlane(sh.spoiled)) spoil(first, last);
         __syncthreads();
         // ---- the lanes that share rows put their sums together
+        if constexpr (!k16)
 #pragma unroll
-        for (int q = 0; q < QT; ++q) {
-            weight[q] += __shfl_xor(weight[q], 16);
-            weight[q] += __shfl_xor(weight[q], 32);
-        }
+            for (int q = 0; q < QT; ++q) {
+                weight[q][0] += __shfl_xor(weight[q][0], 16);
+                weight[q][0] += __shfl_xor(weight[q][0], 32);
+            }
     }
 
     // Whole rows of the output.
@@ -609,7 +620,7 @@ struct Attention {
             const int row = block * kRows + (wave * QT + q) * 16 + l16;
             const int node = row / group;
             if (node >= t.nodes) continue;
-            const float whole = 1.0f / weight[q];
+            const float whole = 1.0f / weight[q][0];
             char* to = static_cast<char*>(g.b.out) +
                 ((static_cast<int64_t>(b) * g.a.N + node) * g.a.out_stride + static_cast<int64_t>(kv * group + row - node * group) * g.a.head_dim) * E::kBytes;
 #pragma unroll
@@ -618,12 +629,14 @@ struct Attention {
         }
     }
 
-    __device__ __forceinline__ void keep(int slot) {
+    __device__ __forceinline__ void keep(int block, int slot) {
         const int lane = fresh(this->lane), l16 = lane & 15, quad = lane >> 4;
+        const int rows = t.nodes * (g.a.heads / g.a.kv_heads) - block * kRows;
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
+            if ((wave * QT + q) * 16 + l16 >= rows) continue;
             const int64_t row = static_cast<int64_t>(slot) * kRows + (wave * QT + q) * 16 + l16;
-            if (quad == 0) g.partial_stats[row] = make_float2(top[q], weight[q]);
+            if (quad == 0) g.partial_stats[row] = make_float2(top[q], weight[q][0]);
 #pragma unroll
             for (int c = 0; c < kColumns; ++c) *reinterpret_cast<f32x4*>(g.partial + row * DP + c * 16 + quad * 4) = out[q][c];
         }
@@ -697,7 +710,7 @@ struct Attention {
                     g.split[team] = make_int4(b, kv, t.blocks, static_cast<int>(((unit + t.tiles) * T - 1) / total));
                 if (member >= t.blocks) continue;
                 run(member, first, last);
-                if (shared) keep((team * g.blocks + member) * 2 + (first > 0 ? 0 : 1));
+                if (shared) keep(member, (team * g.blocks + member) * 2 + (first > 0 ? 0 : 1));
                 else finish(member);
             }
             start = tree_end;
@@ -712,46 +725,86 @@ __global__ __launch_bounds__(A::kThreads) __attribute__((amdgpu_waves_per_eu(2))
     a.all();
 }
 
-// Puts the shared units together: a wave per row of a unit that begins in team blockIdx.x's part of the list.
+// Puts the shared units together.  kLanes lanes have a row (4 columns each).  Few parts, as in large batches: a wave has as many rows
+// as it has such groups of lanes, four times over.  Many: the groups of a wave share the parts of one row.
+constexpr int kFewParts = 4;
+
 template <int DTYPE, int DP, int ROWS>
 __global__ __launch_bounds__(256) void combine_kernel(AttentionArgs g) {
     typedef Elem<DTYPE> E;
+    constexpr int kLanes = DP / 4, kGroups = 64 / kLanes;
     const int first = blockIdx.x;
     const int4 s = g.split[first];
-    const int lane = threadIdx.x & 63, row = blockIdx.y * 4 + (threadIdx.x >> 6);
-    const int block = row / ROWS, local = row % ROWS;
-    if (s.x < 0 || block >= s.z) return;
+    if (s.x < 0) return;
+    const int lane = threadIdx.x & 63, column = lane % kLanes * 4, mine = lane / kLanes;
     const int b = s.x, kv = s.y, last = s.w, group = g.a.heads / g.a.kv_heads;
-    const int node = row / group;
-    const int nodes = g.b.num_nodes ? min(max(g.b.num_nodes[b], 0), g.a.N) : g.a.N;
-    if (node >= nodes) return;
-    // part p of the unit: the second slot of team `first`, the first slot of those after it
-    auto at = [&](int p) { return ((static_cast<int64_t>(first + p) * g.blocks + block) * 2 + (p == 0 ? 1 : 0)) * ROWS + local; };
     const int parts = last - first + 1;
-    float top = -INFINITY;
-    for (int p = lane; p < parts; p += 64) top = fmaxf(top, g.partial_stats[at(p)].x);
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    const float base = top == -INFINITY ? 0.0f : top;
-    constexpr int kLanes = DP / 4, kAtOnce = 64 / kLanes;          // lanes of a row, rows at a time
-    const int column = lane % kLanes * 4;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    float weight = 0.0f;
-#pragma unroll 4
-    for (int p = lane / kLanes; p < parts; p += kAtOnce) {
-        const float2 stats = g.partial_stats[at(p)];
-        const float f = exp2_of(stats.x - base);
-        weight += f * stats.y;
-        sum += *reinterpret_cast<const f32x4*>(g.partial + at(p) * DP + column) * f;
-    }
-    for (int d = kLanes; d < 64; d <<= 1) {
-        weight += __shfl_xor(weight, d);
+    const int nodes = g.b.num_nodes ? min(max(g.b.num_nodes[b], 0), g.a.N) : g.a.N;
+    const int rows = nodes * group, wave = blockIdx.y * 4 + (threadIdx.x >> 6);
+    // part p of a row: the second slot of team `first`, the first slot of those after it
+    auto at = [&](int row, int p) {
+        return ((static_cast<int64_t>(first + p) * g.blocks + row / ROWS) * 2 + (p == 0 ? 1 : 0)) * ROWS + row % ROWS;
+    };
+    auto put = [&](int row, const f32x4& sum, float weight) {
+        const int node = row / group;
+        char* to = static_cast<char*>(g.b.out) +
+            ((static_cast<int64_t>(b) * g.a.N + node) * g.a.out_stride + static_cast<int64_t>(kv * group + row - node * group) * g.a.head_dim + column) * E::kBytes;
+        if (row < rows && column < g.a.head_dim) E::put4(to, sum * (1.0f / weight));
+    };
+    if (parts <= kFewParts) {
+        const int row0 = wave * kGroups * 4;
+        if (row0 >= rows) return;
+        float2 stats[4][kFewParts];
+        f32x4 part[4][kFewParts];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor(sum[i], d);
+        for (int r = 0; r < 4; ++r) {
+            const int row = min(row0 + r * kGroups + mine, rows - 1);
+#pragma unroll
+            for (int p = 0; p < kFewParts; ++p) {
+                if (p >= parts) break;
+                stats[r][p] = g.partial_stats[at(row, p)];
+                part[r][p] = *reinterpret_cast<const f32x4*>(g.partial + at(row, p) * DP + column);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float top = stats[r][0].x, weight = 0.0f;
+#pragma unroll
+            for (int p = 1; p < kFewParts; ++p) if (p < parts) top = fmaxf(top, stats[r][p].x);
+            const float base = top == -INFINITY ? 0.0f : top;
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int p = 0; p < kFewParts; ++p)
+                if (p < parts) {
+                    const float f = exp2_of(stats[r][p].x - base);
+                    weight += f * stats[r][p].y;
+                    sum += part[r][p] * f;
+                }
+            put(row0 + r * kGroups + mine, sum, weight);
+        }
+        return;
     }
-    if (lane >= kLanes || column >= g.a.head_dim) return;
-    char* to = static_cast<char*>(g.b.out) +
-        ((static_cast<int64_t>(b) * g.a.N + node) * g.a.out_stride + static_cast<int64_t>(kv * group + row - node * group) * g.a.head_dim + column) * E::kBytes;
-    E::put4(to, sum * (1.0f / weight));
+    for (int row = wave; row < rows; row += gridDim.y * 4) {
+        float top = -INFINITY;
+        for (int p = lane; p < parts; p += 64) top = fmaxf(top, g.partial_stats[at(row, p)].x);
+        for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+        const float base = top == -INFINITY ? 0.0f : top;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        float weight = 0.0f;
+#pragma unroll 4
+        for (int p = mine; p < parts; p += kGroups) {
+            const float2 stats = g.partial_stats[at(row, p)];
+            const float f = exp2_of(stats.x - base);
+            weight += f * stats.y;
+            sum += *reinterpret_cast<const f32x4*>(g.partial + at(row, p) * DP + column) * f;
+        }
+        for (int d = kLanes; d < 64; d <<= 1) {
+            weight += __shfl_xor(weight, d);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor(sum[i], d);
+        }
+        if (mine == 0) put(row, sum, weight);
+    }
 }
 
 // ------------------------------------------------------------------ host side
@@ -824,9 +877,12 @@ static int with_kernel(const mpv_attention* a, AttentionArgs* g, void* workspace
                                       static_cast<int>(sizeof(typename A::Shared)))))
         return MPV_ERR_HIP;
     hipLaunchKernelGGL(attention_kernel<A>, dim3(static_cast<unsigned>(c.teams) * c.blocks), dim3(A::kThreads), sizeof(typename A::Shared), s, *g);
-    // a list with one tile a unit shares none
+    // a list with one tile a unit shares none.  Few parts a unit: 16 groups of lanes' rows a workgroup; many: a row a wave, as long as
+    // there are not that many workgroups anyway.
+    constexpr int kCombined = 4 * 4 * (64 / (DP / 4));
+    const int64_t few = (rows + kCombined - 1) / kCombined, each = (rows + 3) / 4, most = 2048 / c.teams;
     if (c.tiles > static_cast<int64_t>(a->B) * a->kv_heads)
-        hipLaunchKernelGGL((combine_kernel<DTYPE, DP, A::kRows>), dim3(static_cast<unsigned>(c.teams), static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, s, *g);
+        hipLaunchKernelGGL((combine_kernel<DTYPE, DP, A::kRows>), dim3(static_cast<unsigned>(c.teams), static_cast<unsigned>(std::max(few, std::min(each, most)))), dim3(256), 0, s, *g);
     return launched();
 }
 
