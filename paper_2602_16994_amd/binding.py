@@ -545,7 +545,7 @@ def _dtype_of(t):
 
 
 def _ptr(t):
-    return t.data_ptr() if t is not None else 0
+    return None if t is None else t.data_ptr()
 
 
 def _on_device(dev, **tensors):
@@ -605,20 +605,53 @@ def _cache_strides(k, v, shape):
     return strides[0]
 
 
-def _call(name, shape, bufs, out, dev, stream):
-    """A call with a workspace, which is kept in out.workspace."""
+class _Plan:
+    """What a call derives from the shapes, strides and types of its tensors: checked once, used again for tensors that agree in them."""
+
+    def __init__(self, name, device, shape):
+        self.name, self.device, self.shape = name, device, shape
+        lib = load_library()
+        self.call = getattr(lib, name)
+        self.address = ctypes.byref(shape)
+        self.need = None
+        if name != "mpv_append_paths":
+            need = ctypes.c_size_t(0)
+            rc = getattr(lib, name + "_workspace_bytes")(self.address, ctypes.byref(need))
+            if rc != 0:
+                raise MpvError(rc, name + "_workspace_bytes")
+            self.need = max(need.value, 256)
+
+
+_plans = {}
+
+
+def _kept(key, plan):
+    if len(_plans) >= 1024:                  # sizes that change without end: start again
+        _plans.clear()
+    _plans[key] = plan
+    return plan
+
+
+def _like(t):
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
+
+
+def _launch(plan, bufs, out, stream):
+    """The call on its tensors' device; its workspace, if it has one, is kept in out.workspace."""
     import torch
-    lib = load_library()
-    need = ctypes.c_size_t(0)
-    rc = getattr(lib, name + "_workspace_bytes")(ctypes.byref(shape), ctypes.byref(need))
+    if torch.cuda.current_device() != plan.device:
+        with torch.cuda.device(plan.device):
+            return _launch(plan, bufs, out, stream)
+    raw = torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream
+    if plan.need is None:
+        rc = plan.call(plan.address, ctypes.byref(bufs), raw)
+    else:
+        ws = out.workspace
+        if ws is None or ws.numel() < plan.need or ws.get_device() != plan.device:
+            ws = out.workspace = torch.empty(plan.need, dtype=torch.uint8, device=torch.device("cuda", plan.device))
+        rc = plan.call(plan.address, ctypes.byref(bufs), ws.data_ptr(), ws.numel(), raw)
     if rc != 0:
-        raise MpvError(rc, name + "_workspace_bytes")
-    if out.workspace is None or out.workspace.numel() < need.value or out.workspace.device != dev:
-        out.workspace = torch.empty(max(need.value, 256), dtype=torch.uint8, device=dev)
-    with torch.cuda.device(dev):
-        rc = getattr(lib, name)(ctypes.byref(shape), ctypes.byref(bufs), out.workspace.data_ptr(), out.workspace.numel(), _stream_ptr(stream))
-    if rc != 0:
-        raise MpvError(rc, name)
+        raise MpvError(rc, plan.name)
     return out
 
 
@@ -640,6 +673,22 @@ def mpv_tree_attention(parent, q, tree_k, tree_v, cache_k, cache_v, block_table,
     so many nodes of a tree exist (rows of `out` behind them are left as they were).  tree_parent int32 [B,N], on the device: a
     parent array per tree, in the place of `parent`.  `out` may be a previous TreeAttentionResult whose buffers are reused."""
     import torch
+    key = ("attention", None if tree_parent is not None else tuple(parent), scale, window, sinks, _like(q), _like(tree_k), _like(tree_v),
+           _like(cache_k), _like(cache_v), _like(block_table), _like(context_len), _like(num_nodes), _like(tree_parent),
+           None if out is None else _like(out.out))
+    plan = _plans.get(key)
+    if plan is None:
+        plan = _kept(key, _attention_plan(parent, q, tree_k, tree_v, cache_k, cache_v, block_table, context_len, scale, window, sinks,
+                                          num_nodes, tree_parent, out))
+    if out is None:
+        out = TreeAttentionResult(out=torch.empty(q.shape, dtype=q.dtype, device=q.device))
+    bufs = _AttentionBuffers(q.data_ptr(), tree_k.data_ptr(), tree_v.data_ptr(), cache_k.data_ptr(), cache_v.data_ptr(), block_table.data_ptr(),
+                             context_len.data_ptr(), _ptr(num_nodes), _ptr(tree_parent), out.out.data_ptr())
+    return _launch(plan, bufs, out, stream)
+
+
+def _attention_plan(parent, q, tree_k, tree_v, cache_k, cache_v, block_table, context_len, scale, window, sinks, num_nodes, tree_parent, out):
+    import torch
     if q.dim() != 4 or tree_k.dim() != 4 or cache_k.dim() != 4 or block_table.dim() != 2:
         raise ValueError("q, tree_k, tree_v, cache_k and cache_v must have 4 dimensions, block_table 2")
     B, N, heads, head_dim = q.shape
@@ -658,18 +707,17 @@ def mpv_tree_attention(parent, q, tree_k, tree_v, cache_k, cache_v, block_table,
            tree_parent=(tree_parent, (B, N)))
     if tree_parent is None and len(parent) != N:
         raise ValueError("parent must have as many entries as a tree has nodes")
-    if out is None:
-        out = TreeAttentionResult(out=torch.empty(B, N, heads, head_dim, dtype=q.dtype, device=dev))
-    _on_device(dev, out=out.out)
-    if out.out.dtype != q.dtype:
-        raise TypeError("out must have the dtype of q")
+    out_stride = heads * head_dim
+    if out is not None:
+        _on_device(dev, out=out.out)
+        if out.out.dtype != q.dtype:
+            raise TypeError("out must have the dtype of q")
+        out_stride = _row_stride("out", out.out, (B, N), (heads, head_dim))
     arr = (ctypes.c_int32 * N)(*[int(x) for x in parent]) if tree_parent is None else None
-    shape = _Attention(B, N, heads, kv_heads, head_dim, dtype, num_pages, page_size, width, int(window), int(sinks),
-                       float(head_dim ** -0.5 if scale is None else scale), _row_stride("q", q, (B, N), (heads, head_dim)), kv_stride,
-                       _row_stride("out", out.out, (B, N), (heads, head_dim)), page_stride, slot_stride, arr)
-    bufs = _AttentionBuffers(_ptr(q), _ptr(tree_k), _ptr(tree_v), _ptr(cache_k), _ptr(cache_v), _ptr(block_table), _ptr(context_len),
-                             _ptr(num_nodes), _ptr(tree_parent), _ptr(out.out))
-    return _call("mpv_tree_attention", shape, bufs, out, dev, stream)
+    return _Plan("mpv_tree_attention", dev.index, _Attention(
+        B, N, heads, kv_heads, head_dim, dtype, num_pages, page_size, width, int(window), int(sinks),
+        float(head_dim ** -0.5 if scale is None else scale), _row_stride("q", q, (B, N), (heads, head_dim)), kv_stride, out_stride,
+        page_stride, slot_stride, arr))
 
 
 def mpv_verify_chains(tokens, target_probs, draft_probs, uniforms, num_nodes=None, max_depth=None, out=None, stream=None):
@@ -679,6 +727,26 @@ def mpv_verify_chains(tokens, target_probs, draft_probs, uniforms, num_nodes=Non
     tokens int32 [B,N], uniforms float32 [B,N], target_probs and draft_probs [B,N,V] (float32, bfloat16 or float16; rows may lie
     further apart than V): CUDA tensors.  draft_probs=None: the drafts are certain (looked up, or greedy).  num_nodes int32 [B]: rows
     of each chain, one more than its drafted tokens.  `out` may be a previous VerifyResult whose buffers are reused."""
+    import torch
+    if max_depth is None:
+        max_depth = out.path_nodes.shape[1] if out is not None else max(1, target_probs.shape[1] - 1)
+    key = ("chains", max_depth, _like(tokens), _like(target_probs), _like(draft_probs), _like(uniforms), _like(num_nodes),
+           None if out is None else (_like(out.accept_len), _like(out.path_nodes), _like(out.path_tokens), _like(out.bonus_token),
+                                     _like(out.counters)))
+    plan = _plans.get(key)
+    if plan is None:
+        plan = _kept(key, _chains_plan(tokens, target_probs, draft_probs, uniforms, num_nodes, max_depth, out))
+    if out is None:
+        B, i32 = target_probs.shape[0], dict(dtype=torch.int32, device=target_probs.device)
+        out = VerifyResult(accept_len=torch.empty(B, **i32), path_nodes=torch.empty(B, max_depth, **i32),
+                           path_tokens=torch.empty(B, max_depth, **i32), bonus_token=torch.empty(B, **i32), counters=torch.empty(8, **i32))
+    bufs = _ChainBuffers(target_probs.data_ptr(), _ptr(draft_probs), tokens.data_ptr(), uniforms.data_ptr(), _ptr(num_nodes),
+                         out.accept_len.data_ptr(), out.path_nodes.data_ptr(), out.path_tokens.data_ptr(), out.bonus_token.data_ptr(),
+                         out.counters.data_ptr())
+    return _launch(plan, bufs, out, stream)
+
+
+def _chains_plan(tokens, target_probs, draft_probs, uniforms, num_nodes, max_depth, out):
     import torch
     if target_probs.dim() != 3:
         raise ValueError("target_probs must be [B,N,V]")
@@ -690,19 +758,12 @@ def mpv_verify_chains(tokens, target_probs, draft_probs, uniforms, num_nodes=Non
     dtype = _dtype_of(target_probs)
     _whole(dev, torch.int32, tokens=(tokens, (B, N)), num_nodes=(num_nodes, (B,)))
     _whole(dev, torch.float32, uniforms=(uniforms, (B, N)))
-    if max_depth is None:
-        max_depth = out.path_nodes.shape[1] if out is not None else max(1, N - 1)
-    i32 = dict(dtype=torch.int32, device=dev)
-    if out is None:
-        out = VerifyResult(accept_len=torch.empty(B, **i32), path_nodes=torch.empty(B, max_depth, **i32),
-                           path_tokens=torch.empty(B, max_depth, **i32), bonus_token=torch.empty(B, **i32), counters=torch.empty(8, **i32))
-    _whole(dev, torch.int32, accept_len=(out.accept_len, (B,)), path_nodes=(out.path_nodes, (B, max_depth)),
-           path_tokens=(out.path_tokens, (B, max_depth)), bonus_token=(out.bonus_token, (B,)), counters=(out.counters, (8,)))
-    shape = _Chains(B, N, V, dtype, max_depth, _row_stride("target_probs", target_probs, (B, N), (V,)),
-                    _row_stride("draft_probs", draft_probs, (B, N), (V,)) if draft_probs is not None else 0)
-    bufs = _ChainBuffers(_ptr(target_probs), _ptr(draft_probs), _ptr(tokens), _ptr(uniforms), _ptr(num_nodes), _ptr(out.accept_len),
-                         _ptr(out.path_nodes), _ptr(out.path_tokens), _ptr(out.bonus_token), _ptr(out.counters))
-    return _call("mpv_verify_chains", shape, bufs, out, dev, stream)
+    if out is not None:
+        _whole(dev, torch.int32, accept_len=(out.accept_len, (B,)), path_nodes=(out.path_nodes, (B, max_depth)),
+               path_tokens=(out.path_tokens, (B, max_depth)), bonus_token=(out.bonus_token, (B,)), counters=(out.counters, (8,)))
+    return _Plan("mpv_verify_chains", dev.index, _Chains(
+        B, N, V, dtype, max_depth, _row_stride("target_probs", target_probs, (B, N), (V,)),
+        _row_stride("draft_probs", draft_probs, (B, N), (V,)) if draft_probs is not None else 0))
 
 
 @dataclass
@@ -725,6 +786,27 @@ def mpv_extend_tables(block_table, context_len, new_len, free_pages, free_count,
     place beside `extra`, negative for a finished request.  slot_map int64: [B,n] for a row of slots per request, [n] for all of them
     packed.  `out` may be a previous TablesResult whose buffers are reused."""
     import torch
+    if inplace and out is not None:
+        out.context_len, out.free_count = context_len, free_count
+    key = ("tables", page_size, extra, _like(block_table), _like(context_len), _like(new_len), _like(free_pages), _like(free_count),
+           _like(slot_map), None if out is None else (_like(out.context_len), _like(out.free_count), _like(out.granted), _like(out.offsets)))
+    plan = _plans.get(key)
+    if plan is None:
+        plan = _kept(key, _tables_plan(block_table, context_len, new_len, free_pages, free_count, page_size, slot_map, extra, out))
+    if out is None:
+        B, i32 = block_table.shape[0], dict(dtype=torch.int32, device=block_table.device)
+        out = TablesResult(context_len=context_len if inplace else torch.empty(B, **i32),
+                           free_count=free_count if inplace else torch.empty(1, **i32), granted=torch.empty(B, **i32), slot_map=slot_map,
+                           offsets=torch.empty(B + 1, **i32))
+    out.slot_map = slot_map
+    bufs = _TableBuffers(new_len.data_ptr(), context_len.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
+                         out.context_len.data_ptr(), out.free_count.data_ptr(), slot_map.data_ptr(), out.granted.data_ptr(),
+                         out.offsets.data_ptr())
+    return _launch(plan, bufs, out, stream)
+
+
+def _tables_plan(block_table, context_len, new_len, free_pages, free_count, page_size, slot_map, extra, out):
+    import torch
     if block_table.dim() != 2 or free_pages.dim() != 1 or slot_map.dim() not in (1, 2):
         raise ValueError("block_table must be [B,table_width], free_pages [num_pages], slot_map [B,n] or [n]")
     B, width = block_table.shape
@@ -733,20 +815,10 @@ def mpv_extend_tables(block_table, context_len, new_len, free_pages, free_count,
     _whole(dev, torch.int32, block_table=(block_table, (B, width)), context_len=(context_len, (B,)), new_len=(new_len, (B,)),
            free_pages=(free_pages, (pages,)), free_count=(free_count, (1,)))
     _whole(dev, torch.int64, slot_map=(slot_map, tuple(slot_map.shape) if packed else (B, slot_map.shape[1])))
-    i32 = dict(dtype=torch.int32, device=dev)
-    if out is None:
-        out = TablesResult(context_len=context_len if inplace else torch.empty(B, **i32),
-                           free_count=free_count if inplace else torch.empty(1, **i32), granted=torch.empty(B, **i32), slot_map=slot_map,
-                           offsets=torch.empty(B + 1, **i32))
-    elif inplace:
-        out.context_len, out.free_count = context_len, free_count
-    out.slot_map = slot_map
-    _whole(dev, torch.int32, context_len=(out.context_len, (B,)), free_count=(out.free_count, (1,)), granted=(out.granted, (B,)),
-           offsets=(out.offsets, (B + 1,)))
-    shape = _Tables(B, int(page_size), width, pages, int(extra), int(packed), slot_map.shape[-1])
-    bufs = _TableBuffers(_ptr(new_len), _ptr(context_len), _ptr(block_table), _ptr(free_pages), _ptr(free_count), _ptr(out.context_len),
-                         _ptr(out.free_count), _ptr(slot_map), _ptr(out.granted), _ptr(out.offsets))
-    return _call("mpv_extend_tables", shape, bufs, out, dev, stream)
+    if out is not None:
+        _whole(dev, torch.int32, context_len=(out.context_len, (B,)), free_count=(out.free_count, (1,)), granted=(out.granted, (B,)),
+               offsets=(out.offsets, (B + 1,)))
+    return _Plan("mpv_extend_tables", dev.index, _Tables(B, int(page_size), width, pages, int(extra), int(packed), slot_map.shape[-1]))
 
 
 def mpv_append_paths(tree_k, tree_v, cache_k, cache_v, slot_map, accept_len, path_nodes=None, stream=None):
@@ -756,6 +828,16 @@ def mpv_append_paths(tree_k, tree_v, cache_k, cache_v, slot_map, accept_len, pat
     tree_k / tree_v [layers,B,N,kv_heads,head_dim] and cache_k / cache_v [layers,num_pages,page_size,kv_heads,head_dim], or all four
     without the first dimension for one layer; slot_map int64 [B,n]; accept_len int32 [B] and path_nodes int32 [B,max_depth] as a
     verification writes them (path_nodes=None: chains, nodes 1, 2, ...)."""
+    key = ("append", _like(tree_k), _like(tree_v), _like(cache_k), _like(cache_v), _like(slot_map), _like(accept_len), _like(path_nodes))
+    plan = _plans.get(key)
+    if plan is None:
+        plan = _kept(key, _append_plan(tree_k, tree_v, cache_k, cache_v, slot_map, accept_len, path_nodes))
+    bufs = _AppendBuffers(tree_k.data_ptr(), tree_v.data_ptr(), cache_k.data_ptr(), cache_v.data_ptr(), slot_map.data_ptr(),
+                          accept_len.data_ptr(), _ptr(path_nodes))
+    _launch(plan, bufs, None, stream)
+
+
+def _append_plan(tree_k, tree_v, cache_k, cache_v, slot_map, accept_len, path_nodes):
     import torch
     if tree_k.dim() == 4 and cache_k.dim() == 4:
         tree_k, tree_v, cache_k, cache_v = (t.unsqueeze(0) for t in (tree_k, tree_v, cache_k, cache_v))
@@ -773,21 +855,16 @@ def mpv_append_paths(tree_k, tree_v, cache_k, cache_v, slot_map, accept_len, pat
     deep = path_nodes.shape[1] if path_nodes is not None and path_nodes.dim() == 2 else 0
     _whole(dev, torch.int64, slot_map=(slot_map, (B, slot_map.shape[1])))
     _whole(dev, torch.int32, accept_len=(accept_len, (B,)), path_nodes=(path_nodes, (B, deep)))
-    if layers == 0 or B == 0:
-        return
-    tree_stride = _row_stride("tree_k", tree_k[0], (B, N), (kv_heads, head_dim))
-    page_stride, slot_stride = _cache_strides(cache_k[0], cache_v[0], (num_pages, page_size, kv_heads, head_dim))
-    tree_layer, cache_layer = (t.stride(0) if layers > 1 else 0 for t in (tree_k, cache_k))
-    if (_row_stride("tree_v", tree_v[0], (B, N), (kv_heads, head_dim)) != tree_stride
-            or (layers > 1 and (tree_v.stride(0) != tree_layer or cache_v.stride(0) != cache_layer))):
-        raise ValueError("keys and values must have the same strides")
-    shape = _Append(layers, B, N, dtype, kv_heads * head_dim, deep, slot_map.shape[1], num_pages, page_size, tree_layer, tree_stride,
-                    cache_layer, page_stride, slot_stride)
-    bufs = _AppendBuffers(_ptr(tree_k), _ptr(tree_v), _ptr(cache_k), _ptr(cache_v), _ptr(slot_map), _ptr(accept_len), _ptr(path_nodes))
-    with torch.cuda.device(dev):
-        rc = load_library().mpv_append_paths(ctypes.byref(shape), ctypes.byref(bufs), _stream_ptr(stream))
-    if rc != 0:
-        raise MpvError(rc, "mpv_append_paths")
+    shape = _Append(layers, B, N, dtype, kv_heads * head_dim, deep, slot_map.shape[1], num_pages, page_size, 0, 0, 0, 0, 0)
+    if layers and B:
+        shape.tree_stride = _row_stride("tree_k", tree_k[0], (B, N), (kv_heads, head_dim))
+        shape.page_stride, shape.slot_stride = _cache_strides(cache_k[0], cache_v[0], (num_pages, page_size, kv_heads, head_dim))
+        if layers > 1:
+            shape.tree_layer_stride, shape.cache_layer_stride = tree_k.stride(0), cache_k.stride(0)
+        if (_row_stride("tree_v", tree_v[0], (B, N), (kv_heads, head_dim)) != shape.tree_stride
+                or (layers > 1 and (tree_v.stride(0) != tree_k.stride(0) or cache_v.stride(0) != cache_k.stride(0)))):
+            raise ValueError("keys and values must have the same strides")
+    return _Plan("mpv_append_paths", dev.index, shape)
 
 
 MPV_KERNEL_NAMES = {0: "init", 1: "node_task", 2: "debug_stats"}
