@@ -614,6 +614,10 @@ class _Plan:
         self.call = getattr(lib, name)
         self.address = ctypes.byref(shape)
         self.need = None
+        global _raw_stream
+        if _raw_stream is None:              # the current stream's handle without a Stream object around it (2 us a call), where torch has it
+            import torch
+            _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         if name != "mpv_append_paths":
             need = ctypes.c_size_t(0)
             rc = getattr(lib, name + "_workspace_bytes")(self.address, ctypes.byref(need))
@@ -623,6 +627,7 @@ class _Plan:
 
 
 _plans = {}
+_raw_stream = None
 
 
 def _kept(key, plan):
@@ -642,7 +647,12 @@ def _launch(plan, bufs, out, stream):
     if torch.cuda.current_device() != plan.device:
         with torch.cuda.device(plan.device):
             return _launch(plan, bufs, out, stream)
-    raw = torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream
+    if stream is not None:
+        raw = stream.cuda_stream
+    elif _raw_stream is not None:
+        raw = _raw_stream(plan.device)
+    else:
+        raw = torch.cuda.current_stream().cuda_stream
     if plan.need is None:
         rc = plan.call(plan.address, ctypes.byref(bufs), raw)
     else:

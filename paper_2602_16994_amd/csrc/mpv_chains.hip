@@ -7,18 +7,36 @@
 
 namespace mpv {
 
+// The tests cost a few dependent loads; what is read in earnest is one row of p (and of q) a chain, for the sum of its masses, and a
+// small part of it again, where the drawn point lies.  Masses are taken and added in double: the differences of two rows are exact
+// and a border of the cumulative mass lies where it does in the definition, but for sums' rounding (2^-53).
+//
+// One workgroup a chain (chain_kernel) where that is enough; with fewer chains than compute units and long rows the sums are
+// made by `parts` workgroups a chain (part_kernel), and draw_kernel goes on from there.
+
 constexpr int kChainBlock = 1024;
+constexpr int kPartBlock = 256;
 
 struct ChainArgs {
     mpv_chains c;
     mpv_chain_buffers b;
+    int parts, part;                       // workgroups a chain, elements of each
+    double* sums;                          // [B][parts]
 };
 
 // A probability as a double; what is not positive counts as 0.
 __device__ __forceinline__ double mass_of(float v) { return v > 0.0f ? static_cast<double>(v) : 0.0; }
-__device__ __forceinline__ float prob(const float* p, int64_t i) { return p[i]; }
-__device__ __forceinline__ float prob(const uint16_t* p, int64_t i) { return __uint_as_float(static_cast<uint32_t>(p[i]) << 16); }
-__device__ __forceinline__ float prob(const __half* p, int64_t i) { return __half2float(p[i]); }
+__device__ __forceinline__ float prob(float p) { return p; }
+__device__ __forceinline__ float prob(uint16_t p) { return __uint_as_float(static_cast<uint32_t>(p) << 16); }
+__device__ __forceinline__ float prob(__half p) { return __half2float(p); }
+
+// 16 bytes of a row, at any element's address
+template <class T>
+struct Vector {
+    static constexpr int N = 16 / sizeof(T);
+    T v[N];
+    __device__ __forceinline__ void load(const T* from) { __builtin_memcpy(v, from, 16); }
+};
 
 // What the bonus token is drawn from: token t has the mass (p_t - q_t)_+, p_t without a draft row, nothing where t is `without`.
 template <class T>
@@ -26,10 +44,26 @@ struct Rest {
     const T* p;
     const T* q;
     int without;
-    __device__ __forceinline__ double operator()(int t) const {
-        double m = mass_of(prob(p, t));
-        if (q) m -= mass_of(prob(q, t));
+    __device__ __forceinline__ double of(T pt, T qt, int t) const {
+        const double m = mass_of(prob(pt)) - (q ? mass_of(prob(qt)) : 0.0);
         return m > 0.0 && t != without ? m : 0.0;
+    }
+    __device__ __forceinline__ double operator()(int t) const { return of(p[t], q ? q[t] : T(), t); }
+    // mass of the tokens from + lane * N .. of every 64 * N, below `to`
+    __device__ __forceinline__ double lane_sum(int from, int to, int lane, int lanes) const {
+        constexpr int N = Vector<T>::N;
+        double s = 0.0;
+        int t = from + lane * N;
+#pragma unroll 4
+        for (; t + N <= to; t += lanes * N) {
+            Vector<T> a, d;
+            a.load(p + t);
+            if (q) d.load(q + t);
+#pragma unroll
+            for (int i = 0; i < N; ++i) s += of(a.v[i], q ? d.v[i] : T(), t + i);
+        }
+        for (; t < to; ++t) s += (*this)(t);                // (only the lane at the end has some left)
+        return s;
     }
 };
 
@@ -38,132 +72,220 @@ __device__ __forceinline__ double wave_sum(double v) {
     return v;
 }
 
-// A workgroup per chain: the tests (a lane each), then the draw.  The row is divided among the waves, the part in which the
-// cumulative mass passes the drawn point is divided again, and one wave walks through what is left.
+// A chain's rows.
 template <class T>
-__global__ __launch_bounds__(kChainBlock) void chains_kernel(ChainArgs a) {
-    constexpr int kWaves = kChainBlock / 64;
-    __shared__ double part[kWaves];
-    __shared__ int stop;
-    const int b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int N = a.c.N, V = a.c.V;
-    const int nodes = a.b.num_nodes ? min(max(a.b.num_nodes[b], 1), N) : N;
-    const int32_t* tokens = a.b.tokens + static_cast<int64_t>(b) * N;
-    const float* u = a.b.uniforms + static_cast<int64_t>(b) * N;
-    const T* target = static_cast<const T*>(a.b.target_probs) + static_cast<int64_t>(b) * N * a.c.target_stride;
-    const T* draft = a.b.draft_probs ? static_cast<const T*>(a.b.draft_probs) + static_cast<int64_t>(b) * N * a.c.draft_stride : nullptr;
-    if (wave == 0) {
+struct Chain {
+    const int32_t* tokens;
+    const float* u;
+    const T* target;
+    const T* draft;
+    int nodes;
+    __device__ __forceinline__ Chain(const ChainArgs& a, int b) {
+        const int N = a.c.N;
+        nodes = a.b.num_nodes ? min(max(a.b.num_nodes[b], 1), N) : N;
+        tokens = a.b.tokens + static_cast<int64_t>(b) * N;
+        u = a.b.uniforms + static_cast<int64_t>(b) * N;
+        target = static_cast<const T*>(a.b.target_probs) + static_cast<int64_t>(b) * N * a.c.target_stride;
+        draft = a.b.draft_probs ? static_cast<const T*>(a.b.draft_probs) + static_cast<int64_t>(b) * N * a.c.draft_stride : nullptr;
+    }
+    // Accepted tokens: lane n - 1 tests token n.  A whole wave calls it.
+    __device__ __forceinline__ int test(const ChainArgs& a, int lane) const {
         const int n = lane + 1;
         bool passed = false;
         if (n < nodes) {
             const int x = tokens[n];
-            if (x >= 0 && x < V) {
-                const double p = mass_of(prob(target + (n - 1) * a.c.target_stride, x));
-                const double q = draft ? mass_of(prob(draft + (n - 1) * a.c.draft_stride, x)) : 1.0;
+            if (x >= 0 && x < a.c.V) {
+                const double p = mass_of(prob(target[(n - 1) * a.c.target_stride + x]));
+                const double q = draft ? mass_of(prob(draft[(n - 1) * a.c.draft_stride + x])) : 1.0;
                 passed = static_cast<double>(u[n]) * q < p;
             }
         }
-        const int length = __ffsll(~static_cast<unsigned long long>(__ballot(passed))) - 1;
-        if (lane < a.c.max_depth) {
-            const int64_t at = static_cast<int64_t>(b) * a.c.max_depth + lane;
-            a.b.path_nodes[at] = lane < length ? n : -1;
-            a.b.path_tokens[at] = lane < length ? tokens[n] : -1;
-        }
-        for (int i = 64 + lane; i < a.c.max_depth; i += 64) {
-            const int64_t at = static_cast<int64_t>(b) * a.c.max_depth + i;
-            a.b.path_nodes[at] = -1;
-            a.b.path_tokens[at] = -1;
-        }
-        if (lane == 0) {
-            a.b.accept_len[b] = length;
-            stop = length;
-        }
+        return __ffsll(~static_cast<unsigned long long>(__ballot(passed))) - 1;
     }
-    __syncthreads();
-    const int length = stop;
-    const bool rejected = length + 1 < nodes;
-    const int x = rejected ? tokens[length + 1] : -1;
-    const bool bad = rejected && (x < 0 || x >= V);
-    Rest<T> rest;
-    rest.p = target + length * a.c.target_stride;
-    rest.q = rejected && draft ? draft + length * a.c.draft_stride : nullptr;
-    rest.without = rejected && !draft && !bad ? x : -1;
-    if (threadIdx.x == 0 && bad) atomicAdd(&a.b.counters[MPV_COUNTER_BAD_TOKEN], 1u);
+    __device__ __forceinline__ Rest<T> rest(const ChainArgs& a, int length, bool* bad) const {
+        const bool rejected = length + 1 < nodes;
+        const int x = rejected ? tokens[length + 1] : -1;
+        *bad = rejected && (x < 0 || x >= a.c.V);
+        Rest<T> r;
+        r.p = target + length * a.c.target_stride;
+        r.q = rejected && draft ? draft + length * a.c.draft_stride : nullptr;
+        r.without = rejected && !draft && !*bad ? x : -1;
+        return r;
+    }
+    __device__ __forceinline__ void write_path(const ChainArgs& a, int b, int length, int lane) const {
+        for (int i = lane; i < a.c.max_depth; i += 64) {
+            const int64_t at = static_cast<int64_t>(b) * a.c.max_depth + i;
+            a.b.path_nodes[at] = i < length ? i + 1 : -1;
+            a.b.path_tokens[at] = i < length ? tokens[i + 1] : -1;
+        }
+        if (lane == 0) a.b.accept_len[b] = length;
+    }
+};
 
-    // sums of the waves' parts [w * step, (w + 1) * step) of [from, to)
-    auto parts = [&](int from, int to, int step) {
-        double s = 0.0;
-        const int end = min(from + (wave + 1) * step, to);
-        for (int t = from + wave * step + lane; t < end; t += 64) s += rest(t);
-        s = wave_sum(s);
+// The workgroup's share of the draw: `part` holds the sums of kWaves equal parts (of `step` tokens) of a range.
+struct Draw {
+    static constexpr int kWaves = kChainBlock / 64;
+    double* part;                          // LDS
+    int lane, wave;
+
+    // sums of the waves' parts [from + w * step, from + (w + 1) * step) below `to`; returns their total
+    template <class T>
+    __device__ __forceinline__ double parts(const Rest<T>& rest, int from, int to, int step) {
+        const int begin = from + wave * step;
+        const double s = wave_sum(rest.lane_sum(min(begin, to), min(begin + step, to), lane, 64));
         __syncthreads();
         if (lane == 0) part[wave] = s;
         __syncthreads();
-    };
-    auto total_of = [&]() {
+        double all = 0.0;
+        for (int w = 0; w < kWaves; ++w) all += part[w];
+        return all;
+    }
+    // The first of n sums that passes the point, or the last with mass; *before: the sums ahead of it.
+    static __device__ __forceinline__ int pick(const double* sums, int n, double point, double* before) {
         double s = 0.0;
-        for (int w = 0; w < kWaves; ++w) s += part[w];
-        return s;
-    };
-    int from = 0, to = V, step = (V + kWaves - 1) / kWaves;
-    parts(from, to, step);
-    double total = total_of();
+        int at = 0;
+        *before = 0.0;
+        for (int w = 0; w < n; ++w) {
+            if (sums[w] > 0.0) {
+                at = w;
+                *before = s;
+                if (s + sums[w] > point) break;
+            }
+            s += sums[w];
+        }
+        return at;
+    }
+    // The token of [from, to) in which the cumulative mass passes `point` (the last one with mass if none does).  part: the sums of
+    // its kWaves parts of `step` tokens.  The first wave's lanes have the answer.
+    template <class T>
+    __device__ __forceinline__ int token(const Rest<T>& rest, int from, int to, int step, double point) {
+        double before;
+        for (int level = 0; level < 2; ++level) {
+            from += pick(part, kWaves, point, &before) * step;
+            point -= before;
+            to = min(from + step, to);
+            step = (to - from + kWaves - 1) / kWaves;
+            if (step < 64) break;
+            if (level == 0) parts(rest, from, to, step);
+        }
+        if (wave != 0) return 0;
+        before = 0.0;
+        int last = from;
+        for (int base = from; base < to; base += 64) {
+            const int t = base + lane;
+            const double m = t < to ? rest(t) : 0.0;
+            double s = m;
+            for (int d = 1; d < 64; d <<= 1) {
+                const double o = __shfl_up(s, d);
+                if (lane >= d) s += o;
+            }
+            const unsigned long long some = __ballot(m > 0.0);
+            const unsigned long long past = __ballot(m > 0.0 && before + s > point);
+            if (past) return base + __ffsll(past) - 1;
+            if (some) last = base + 63 - __clzll(static_cast<long long>(some));
+            before += __shfl(s, 63);
+        }
+        return last;
+    }
+};
+
+// The draw over the whole row.
+template <class T>
+__device__ __forceinline__ void draw_row(const ChainArgs& a, int b, const Chain<T>& chain, Rest<T> rest, Draw& draw) {
+    const int V = a.c.V, step = (V + Draw::kWaves - 1) / Draw::kWaves;
+    double total = draw.parts(rest, 0, V, step);
     if (!(total > 0.0)) {
         if (threadIdx.x == 0) atomicAdd(&a.b.counters[MPV_COUNTER_ZERO_MASS], 1u);
         rest.q = nullptr;
         rest.without = -1;
-        parts(from, to, step);
-        total = total_of();
+        total = draw.parts(rest, 0, V, step);
     }
+    const int token = total > 0.0 ? draw.token(rest, 0, V, step, static_cast<double>(chain.u[0]) * total) : 0;
+    if (threadIdx.x == 0) a.b.bonus_token[b] = token;
+}
+
+template <class T>
+__global__ __launch_bounds__(kChainBlock) void chain_kernel(ChainArgs a) {
+    __shared__ double part[Draw::kWaves];
+    __shared__ int stop;
+    const int b = blockIdx.x;
+    Draw draw{part, static_cast<int>(threadIdx.x & 63), static_cast<int>(threadIdx.x >> 6)};
+    const Chain<T> chain(a, b);
+    if (draw.wave == 0) {
+        const int length = chain.test(a, draw.lane);
+        chain.write_path(a, b, length, draw.lane);
+        if (draw.lane == 0) stop = length;
+    }
+    __syncthreads();
+    bool bad;
+    const Rest<T> rest = chain.rest(a, stop, &bad);
+    if (threadIdx.x == 0 && bad) atomicAdd(&a.b.counters[MPV_COUNTER_BAD_TOKEN], 1u);
+    draw_row(a, b, chain, rest, draw);
+}
+
+// A part's sum.  Every workgroup of a chain tests its tokens for itself.
+template <class T>
+__global__ __launch_bounds__(kPartBlock) void part_kernel(ChainArgs a) {
+    __shared__ double part[kPartBlock / 64];
+    const int b = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Chain<T> chain(a, b);
+    const int length = chain.test(a, lane);
+    bool bad;
+    const Rest<T> rest = chain.rest(a, length, &bad);
+    const int from = blockIdx.x * a.part, to = min(from + a.part, a.c.V);
+    const double s = wave_sum(rest.lane_sum(from, to, threadIdx.x, kPartBlock));
+    if (lane == 0) part[wave] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) a.sums[static_cast<int64_t>(b) * a.parts + blockIdx.x] = part[0] + part[1] + part[2] + part[3];
+    if (blockIdx.x == 0 && wave == 1) chain.write_path(a, b, length, lane);
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < MPV_COUNTER_COUNT) a.b.counters[threadIdx.x] = 0;
+}
+
+template <class T>
+__global__ __launch_bounds__(kChainBlock) void draw_kernel(ChainArgs a) {
+    __shared__ double part[Draw::kWaves];
+    const int b = blockIdx.x;
+    Draw draw{part, static_cast<int>(threadIdx.x & 63), static_cast<int>(threadIdx.x >> 6)};
+    const Chain<T> chain(a, b);
+    bool bad;
+    const Rest<T> rest = chain.rest(a, a.b.accept_len[b], &bad);
+    if (threadIdx.x == 0 && bad) atomicAdd(&a.b.counters[MPV_COUNTER_BAD_TOKEN], 1u);
+    const double* sums = a.sums + static_cast<int64_t>(b) * a.parts;
+    double total = 0.0;
+    for (int w = 0; w < a.parts; ++w) total += sums[w];
     if (!(total > 0.0)) {
-        if (threadIdx.x == 0) a.b.bonus_token[b] = 0;
+        draw_row(a, b, chain, rest, draw);
         return;
     }
-    double point = static_cast<double>(u[0]) * total;      // the token sought is the first with more than that up to it
-    for (int level = 0; level < 2; ++level) {
-        // the first part that passes the point, or the last with mass
-        double before = 0.0, at = 0.0;
-        int pick = -1;
-        for (int w = 0; w < kWaves; ++w) {
-            if (part[w] > 0.0) {
-                pick = w;
-                at = before;
-                if (before + part[w] > point) break;
-            }
-            before += part[w];
-        }
-        if (pick < 0) pick = 0;                              // (cannot be: the range has mass)
-        point -= at;
-        from += pick * step;
-        to = min(from + step, to);
-        step = (to - from + kWaves - 1) / kWaves;
-        if (level == 0) parts(from, to, step);
-    }
-    if (wave != 0) return;
-    double before = 0.0;
-    int last = from;
-    for (int base = from; base < to; base += 64) {
-        const int t = base + lane;
-        const double m = t < to ? rest(t) : 0.0;
-        double s = m;
-        for (int d = 1; d < 64; d <<= 1) {
-            const double o = __shfl_up(s, d);
-            if (lane >= d) s += o;
-        }
-        const unsigned long long some = __ballot(m > 0.0);
-        const unsigned long long past = __ballot(m > 0.0 && before + s > point);
-        if (past) {
-            last = base + __ffsll(past) - 1;
-            break;
-        }
-        if (some) last = base + 63 - __clzll(static_cast<long long>(some));
-        before += __shfl(s, 63);
-    }
-    if (lane == 0) a.b.bonus_token[b] = last;
+    double before;
+    const double point = static_cast<double>(chain.u[0]) * total;
+    const int from = Draw::pick(sums, a.parts, point, &before) * a.part, to = min(from + a.part, a.c.V);
+    const int step = (to - from + Draw::kWaves - 1) / Draw::kWaves;
+    draw.parts(rest, from, to, step);
+    const int token = draw.token(rest, from, to, step, point - before);
+    if (threadIdx.x == 0) a.b.bonus_token[b] = token;
 }
 
 __global__ void clear_counters_kernel(uint32_t* counters) {
     if (threadIdx.x < MPV_COUNTER_COUNT) counters[threadIdx.x] = 0;
+}
+
+// Workgroups a chain: as many as fill the device, none with fewer than 4096 tokens.
+static int parts_of(const mpv_chains* c) {
+    const int most = (c->V + 4095) / 4096, wanted = c->B > 0 ? (2048 + c->B - 1) / c->B : 1;
+    return most < wanted ? most : wanted;
+}
+
+template <class T>
+static void launch_chains(ChainArgs& a, hipStream_t s) {
+    const dim3 chains(static_cast<unsigned>(a.c.B));
+    if (a.parts > 1) {
+        hipLaunchKernelGGL(part_kernel<T>, dim3(static_cast<unsigned>(a.parts), chains.x), dim3(kPartBlock), 0, s, a);
+        hipLaunchKernelGGL(draw_kernel<T>, chains, dim3(kChainBlock), 0, s, a);
+    } else {
+        hipLaunchKernelGGL(clear_counters_kernel, dim3(1), dim3(64), 0, s, a.b.counters);
+        hipLaunchKernelGGL(chain_kernel<T>, chains, dim3(kChainBlock), 0, s, a);
+    }
 }
 
 static int check_chains(const mpv_chains* c) {
@@ -185,7 +307,8 @@ int mpv_verify_chains_workspace_bytes(const mpv_chains* chains, size_t* out) {
     if (!out) return MPV_ERR_NULL;
     const int rc = mpv::check_chains(chains);
     if (rc != MPV_OK) return rc;
-    *out = 256;
+    const size_t sums = static_cast<size_t>(chains->B) * mpv::parts_of(chains) * sizeof(double);
+    *out = (sums + 255) / 256 * 256 + 256;
     return MPV_OK;
 }
 
@@ -205,13 +328,15 @@ int mpv_verify_chains(const mpv_chains* chains, const mpv_chain_buffers* buf, vo
     if (!workspace || !mpv::aligned(workspace, 256) || workspace_bytes < need) return MPV_ERR_WORKSPACE;
     mpv::ChainArgs a;
     a.c = *chains; a.b = *buf;
+    a.parts = mpv::parts_of(chains);
+    a.part = (chains->V + a.parts - 1) / a.parts;
+    a.part = (a.part + 7) / 8 * 8;
+    a.sums = static_cast<double*>(workspace);
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();
-    hipLaunchKernelGGL(mpv::clear_counters_kernel, dim3(1), dim3(64), 0, s, buf->counters);
-    const dim3 grid(static_cast<unsigned>(chains->B)), block(mpv::kChainBlock);
-    if (chains->dtype == MPV_DTYPE_F32) hipLaunchKernelGGL(mpv::chains_kernel<float>, grid, block, 0, s, a);
-    else if (chains->dtype == MPV_DTYPE_BF16) hipLaunchKernelGGL(mpv::chains_kernel<uint16_t>, grid, block, 0, s, a);
-    else hipLaunchKernelGGL(mpv::chains_kernel<__half>, grid, block, 0, s, a);
+    if (chains->dtype == MPV_DTYPE_F32) mpv::launch_chains<float>(a, s);
+    else if (chains->dtype == MPV_DTYPE_BF16) mpv::launch_chains<uint16_t>(a, s);
+    else mpv::launch_chains<__half>(a, s);
     return mpv::launched();
 }
 
