@@ -9,7 +9,7 @@ namespace mpv {
 constexpr int kPlanBlock = 1024;
 constexpr int kFillBlock = 256;
 constexpr int kFillSlots = 2048;           // slots of one workgroup of the fill kernel
-// Up to so many slots the plan's workgroup fills them itself, in one launch.
+// Up to so many slots (of requests that take one round of the plan's workgroup) that workgroup fills them itself, in one launch.
 constexpr int64_t kFillAtOnce = 4096;
 
 struct PlanEntry {                         // what the fill needs of a request
@@ -24,23 +24,22 @@ struct TableArgs {
     PlanEntry* plan;                       // [B]
 };
 
-// Inclusive sum over the workgroup; *total gets the sum of all.  `part`: LDS of a value per wave.
-__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* part, int64_t* total) {
+// Inclusive sums of two numbers over the workgroup, the sums of all in total[2].  `part`: LDS, two values a wave.
+__device__ __forceinline__ void block_scan(int64_t (&v)[2], int64_t (&total)[2], int64_t (*part)[2]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     for (int d = 1; d < 64; d <<= 1) {
-        const int64_t o = __shfl_up(v, d);
-        if (lane >= d) v += o;
+        const int64_t a = __shfl_up(v[0], d), b = __shfl_up(v[1], d);
+        if (lane >= d) { v[0] += a; v[1] += b; }
     }
     __syncthreads();
-    if (lane == 63) part[wave] = v;
+    if (lane == 63) { part[wave][0] = v[0]; part[wave][1] = v[1]; }
     __syncthreads();
-    int64_t before = 0, all = 0;
+    total[0] = total[1] = 0;
     for (int w = 0; w < waves; ++w) {
-        if (w < wave) before += part[w];
-        all += part[w];
+        if (w == wave) { v[0] += total[0]; v[1] += total[1]; }
+        total[0] += part[w][0];
+        total[1] += part[w][1];
     }
-    *total = all;
-    return v + before;
 }
 
 __device__ __forceinline__ void fill_slot(const TableArgs& a, int b, const PlanEntry& e, int i, int64_t* to) {
@@ -63,19 +62,23 @@ __device__ __forceinline__ void fill_slot(const TableArgs& a, int b, const PlanE
 
 // One workgroup: who gets what (sums over the requests in their order), and the pages of finished requests.
 __global__ __launch_bounds__(kPlanBlock) void plan_tables_kernel(TableArgs a, int fill) {
-    __shared__ int64_t part[kPlanBlock / 64];
-    const int B = a.t.B, lane = threadIdx.x & 63;
+    __shared__ int64_t part[kPlanBlock / 64][2];
+    __shared__ PlanEntry plan[kPlanBlock];                          // with fill: of the only round
+    const int B = a.t.B, lane = threadIdx.x & 63, threads = blockDim.x;
     const int64_t page_size = a.t.page_size, width = a.t.table_width;
-    const int count0 = min(max(a.b.free_count[0], 0), a.t.num_pages);
-    int64_t count = count0;
-    for (int base = 0; base < B; base += kPlanBlock) {
+    int64_t count = min(max(a.b.free_count[0], 0), a.t.num_pages);
+    int64_t v[2], total[2];
+    for (int base = 0; base < B; base += threads) {
         const int b = base + threadIdx.x;
         int64_t back = 0;
         if (b < B && a.b.new_len[b] < 0)
             back = min((max(a.b.context_len[b], 0) + page_size - 1) / page_size, width);
-        int64_t total;
-        const int64_t begin = count + block_scan(back, part, &total) - back;
-        count += total;
+        if (!__syncthreads_or(back > 0)) continue;
+        v[0] = back;
+        v[1] = 0;
+        block_scan(v, total, part);
+        const int64_t begin = count + v[0] - back;
+        count += total[0];
         for (uint64_t m = __ballot(back > 0); m; m &= m - 1) {
             const int l = __ffsll(static_cast<unsigned long long>(m)) - 1;
             const int64_t pages = __shfl(back, l), to = __shfl(begin, l);
@@ -86,7 +89,7 @@ __global__ __launch_bounds__(kPlanBlock) void plan_tables_kernel(TableArgs a, in
     }
     count = min(count, static_cast<int64_t>(a.t.num_pages));
     int64_t asked = 0, tokens = 0, placed = 0, taken = 0;          // sums over the requests before this round's
-    for (int base = 0; base < B; base += kPlanBlock) {
+    for (int base = 0; base < B; base += threads) {
         const int b = base + threadIdx.x;
         int64_t old = 0, n = 0, have = 0, need = 0;
         bool done = false, never = true;
@@ -100,27 +103,30 @@ __global__ __launch_bounds__(kPlanBlock) void plan_tables_kernel(TableArgs a, in
             never = done || want > width || (!a.t.packed && n > a.t.slot_width);
             need = never ? 0 : want - have;
         }
-        int64_t total;
-        const int64_t upto = asked + block_scan(need, part, &total);
-        asked += total;
-        const int64_t token = tokens + block_scan(never ? 0 : n, part, &total);
-        tokens += total;
+        v[0] = need;
+        v[1] = never ? 0 : n;
+        block_scan(v, total, part);
+        const int64_t upto = asked + v[0], token = tokens + v[1];
+        asked += total[0];
+        tokens += total[1];
         const bool fits = !never && (need == 0 || upto <= count) && (!a.t.packed || n == 0 || token <= a.t.slot_width);
         const int64_t given = fits ? n : 0;
-        const int64_t end = placed + block_scan(given, part, &total);
-        placed += total;
-        (void)block_scan(fits ? need : 0, part, &total);
-        taken += total;
+        v[0] = given;
+        v[1] = fits ? need : 0;
+        block_scan(v, total, part);
+        const int64_t begin = placed + v[0] - given;
+        placed += total[0];
+        taken += total[1];
         if (b < B) {
             a.b.granted[b] = static_cast<int32_t>(fits ? n : done ? 0 : -1);
             a.b.context_len_out[b] = static_cast<int32_t>(done ? 0 : old + given);
-            if (a.b.offsets) a.b.offsets[b] = static_cast<int32_t>(end - given);
+            if (a.b.offsets) a.b.offsets[b] = static_cast<int32_t>(begin);
             PlanEntry e;
             e.old = static_cast<int32_t>(old);
             e.given = static_cast<int32_t>(given);
             e.have = static_cast<int32_t>(have);
             e.top = static_cast<int32_t>(count - 1 - (upto - need));
-            a.plan[b] = e;
+            if (fill) plan[threadIdx.x] = e; else a.plan[b] = e;
         }
     }
     if (threadIdx.x == 0) {
@@ -130,16 +136,16 @@ __global__ __launch_bounds__(kPlanBlock) void plan_tables_kernel(TableArgs a, in
     if (!fill) return;
     __syncthreads();
     if (a.t.packed) {
-        for (int b = threadIdx.x >> 6; b < B; b += kPlanBlock / 64) {
-            const PlanEntry e = a.plan[b];
+        for (int b = threadIdx.x >> 6; b < B; b += threads / 64) {
+            const PlanEntry e = plan[b];
             const int64_t begin = a.b.offsets[b];
             for (int i = lane; i < e.given; i += 64) fill_slot(a, b, e, i, a.b.slot_map + begin + i);
         }
     } else {
         const int slot_width = static_cast<int>(a.t.slot_width);
-        for (int x = threadIdx.x; x < B * slot_width; x += kPlanBlock) {
+        for (int x = threadIdx.x; x < B * slot_width; x += threads) {
             const int b = x / slot_width;
-            fill_slot(a, b, a.plan[b], x - b * slot_width, a.b.slot_map + x);
+            fill_slot(a, b, plan[b], x - b * slot_width, a.b.slot_map + x);
         }
     }
 }
@@ -257,9 +263,11 @@ int mpv_extend_tables(const mpv_tables* tables, const mpv_table_buffers* buf, vo
     a.t = *tables; a.b = *buf; a.plan = static_cast<mpv::PlanEntry*>(workspace);
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const int64_t slots = tables->slot_width * (tables->packed ? 1 : tables->B);
-    const int fill = slots <= mpv::kFillAtOnce;
+    // a wave for 64 requests, four at least (they fill the slots, too)
+    const int threads = tables->B >= mpv::kPlanBlock ? mpv::kPlanBlock : tables->B <= 256 ? 256 : (tables->B + 63) / 64 * 64;
+    const int fill = slots <= mpv::kFillAtOnce && tables->B <= threads;
     (void)hipGetLastError();
-    hipLaunchKernelGGL(mpv::plan_tables_kernel, dim3(1), dim3(mpv::kPlanBlock), 0, s, a, fill);
+    hipLaunchKernelGGL(mpv::plan_tables_kernel, dim3(1), dim3(threads), 0, s, a, fill);
     if (!fill) {
         const dim3 grid(static_cast<unsigned>((slots + mpv::kFillSlots - 1) / mpv::kFillSlots));
         if (tables->packed) hipLaunchKernelGGL(mpv::fill_packed_kernel, grid, dim3(mpv::kFillBlock), 0, s, a);

@@ -24,8 +24,8 @@ struct ChainArgs {
     double* sums;                          // [B][parts]
 };
 
-// A probability as a double; what is not positive counts as 0.
-__device__ __forceinline__ double mass_of(float v) { return v > 0.0f ? static_cast<double>(v) : 0.0; }
+// A probability as a double; what is not positive counts as 0 (fmax: NaN too).
+__device__ __forceinline__ double mass_of(float v) { return static_cast<double>(fmaxf(v, 0.0f)); }
 __device__ __forceinline__ float prob(float p) { return p; }
 __device__ __forceinline__ float prob(uint16_t p) { return __uint_as_float(static_cast<uint32_t>(p) << 16); }
 __device__ __forceinline__ float prob(__half p) { return __half2float(p); }
@@ -44,13 +44,14 @@ struct Rest {
     const T* p;
     const T* q;
     int without;
-    __device__ __forceinline__ double of(T pt, T qt, int t) const {
-        const double m = mass_of(prob(pt)) - (q ? mass_of(prob(qt)) : 0.0);
-        return m > 0.0 && t != without ? m : 0.0;
+    __device__ __forceinline__ double operator()(int t) const {
+        if (t == without) return 0.0;
+        const double m = mass_of(prob(p[t]));
+        return q ? fmax(m - mass_of(prob(q[t])), 0.0) : m;
     }
-    __device__ __forceinline__ double operator()(int t) const { return of(p[t], q ? q[t] : T(), t); }
-    // mass of the tokens from + lane * N .. of every 64 * N, below `to`
-    __device__ __forceinline__ double lane_sum(int from, int to, int lane, int lanes) const {
+    // Mass of the 16-byte groups lane, lane + lanes, .. of [from, to).  The token left out is looked for a group at a time.
+    template <bool Q>
+    __device__ __forceinline__ double lane_sum_of(int from, int to, int lane, int lanes) const {
         constexpr int N = Vector<T>::N;
         double s = 0.0;
         int t = from + lane * N;
@@ -58,12 +59,22 @@ struct Rest {
         for (; t + N <= to; t += lanes * N) {
             Vector<T> a, d;
             a.load(p + t);
-            if (q) d.load(q + t);
+            if constexpr (Q) d.load(q + t);
+            if (!Q && static_cast<unsigned>(without - t) < static_cast<unsigned>(N)) {
+                for (int i = 0; i < N; ++i) s += (*this)(t + i);
+            } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) s += of(a.v[i], q ? d.v[i] : T(), t + i);
+                for (int i = 0; i < N; ++i) {
+                    if constexpr (Q) s += fmax(mass_of(prob(a.v[i])) - mass_of(prob(d.v[i])), 0.0);
+                    else s += mass_of(prob(a.v[i]));
+                }
+            }
         }
         for (; t < to; ++t) s += (*this)(t);                // (only the lane at the end has some left)
         return s;
+    }
+    __device__ __forceinline__ double lane_sum(int from, int to, int lane, int lanes) const {
+        return q ? lane_sum_of<true>(from, to, lane, lanes) : lane_sum_of<false>(from, to, lane, lanes);
     }
 };
 
@@ -169,22 +180,28 @@ struct Draw {
             if (level == 0) parts(rest, from, to, step);
         }
         if (wave != 0) return 0;
-        before = 0.0;
-        int last = from;
-        for (int base = from; base < to; base += 64) {
-            const int t = base + lane;
-            const double m = t < to ? rest(t) : 0.0;
-            double s = m;
-            for (int d = 1; d < 64; d <<= 1) {
-                const double o = __shfl_up(s, d);
-                if (lane >= d) s += o;
-            }
-            const unsigned long long some = __ballot(m > 0.0);
-            const unsigned long long past = __ballot(m > 0.0 && before + s > point);
-            if (past) return base + __ffsll(past) - 1;
-            if (some) last = base + 63 - __clzll(static_cast<long long>(some));
-            before += __shfl(s, 63);
+        // at most 1024 tokens: neighbouring ones to a lane
+        const int mine = (to - from + 63) / 64, begin = from + lane * mine, end = min(begin + mine, to);
+        double sum = 0.0;
+        for (int t = begin; t < end; ++t) sum += rest(t);
+        double upto = sum;
+        for (int d = 1; d < 64; d <<= 1) {
+            const double o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
         }
+        const unsigned long long some = __ballot(sum > 0.0), past = __ballot(sum > 0.0 && upto > point);
+        const int at = past ? __ffsll(past) - 1 : some ? 63 - __clzll(static_cast<long long>(some)) : 0;
+        int last = begin;
+        if (lane == at) {
+            double run = upto - sum;
+            for (int t = begin; t < end; ++t) {
+                const double m = rest(t);
+                if (m > 0.0) last = t;
+                run += m;
+                if (m > 0.0 && run > point) break;
+            }
+        }
+        last = __shfl(last, at);
         return last;
     }
 };
