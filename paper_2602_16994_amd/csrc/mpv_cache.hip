@@ -179,8 +179,12 @@ __global__ __launch_bounds__(kFillBlock) void fill_packed_kernel(TableArgs a) {
     for (int d = 32; d; d >>= 1) { lo += __shfl_xor(lo, d); hi += __shfl_xor(hi, d); }
     if ((threadIdx.x & 63) == 0) { atomicAdd(&lo_hi[0], lo); atomicAdd(&lo_hi[1], hi); }
     __syncthreads();
-    for (int64_t x = first + threadIdx.x; x <= last; x += kFillBlock) {
-        int l = lo_hi[0], h = lo_hi[1];                     // the request lies in [l, h]
+    const int first_request = lo_hi[0], last_request = lo_hi[1];
+#pragma unroll
+    for (int j = 0; j < kFillSlots / kFillBlock; ++j) {
+        const int64_t x = first + j * kFillBlock + threadIdx.x;
+        if (x > last) break;
+        int l = first_request, h = last_request;            // the request lies in [l, h]
         while (l < h) {
             const int m = (l + h) >> 1;
             if (a.b.offsets[m + 1] <= x) l = m + 1; else h = m;

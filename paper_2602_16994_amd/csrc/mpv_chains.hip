@@ -101,15 +101,15 @@ struct Chain {
     }
     // Accepted tokens: lane n - 1 tests token n.  A whole wave calls it.
     __device__ __forceinline__ int test(const ChainArgs& a, int lane) const {
+        // (what does not depend on the chain's length is asked for together with it)
         const int n = lane + 1;
+        const int x = n < a.c.N ? tokens[n] : -1;
+        const float un = n < a.c.N ? u[n] : 0.0f;
         bool passed = false;
-        if (n < nodes) {
-            const int x = tokens[n];
-            if (x >= 0 && x < a.c.V) {
-                const double p = mass_of(prob(target[(n - 1) * a.c.target_stride + x]));
-                const double q = draft ? mass_of(prob(draft[(n - 1) * a.c.draft_stride + x])) : 1.0;
-                passed = static_cast<double>(u[n]) * q < p;
-            }
+        if (n < nodes && x >= 0 && x < a.c.V) {
+            const double p = mass_of(prob(target[(n - 1) * a.c.target_stride + x]));
+            const double q = draft ? mass_of(prob(draft[(n - 1) * a.c.draft_stride + x])) : 1.0;
+            passed = static_cast<double>(un) * q < p;
         }
         return __ffsll(~static_cast<unsigned long long>(__ballot(passed))) - 1;
     }
@@ -133,76 +133,102 @@ struct Chain {
     }
 };
 
-// The workgroup's share of the draw: `part` holds the sums of kWaves equal parts (of `step` tokens) of a range.
+// A workgroup's share of a draw.
 struct Draw {
     static constexpr int kWaves = kChainBlock / 64;
-    double* part;                          // LDS
-    int lane, wave;
+    struct Shared {
+        double part[kWaves];
+        int first, last;
+        int token;
+    };
+    Shared& sh;
+    const int lane, wave;
 
-    // sums of the waves' parts [from + w * step, from + (w + 1) * step) below `to`; returns their total
+    // sums of the waves' parts [from + w * step, from + (w + 1) * step) below `to` in sh.part; returns their total
     template <class T>
     __device__ __forceinline__ double parts(const Rest<T>& rest, int from, int to, int step) {
         const int begin = from + wave * step;
         const double s = wave_sum(rest.lane_sum(min(begin, to), min(begin + step, to), lane, 64));
         __syncthreads();
-        if (lane == 0) part[wave] = s;
+        if (lane == 0) sh.part[wave] = s;
         __syncthreads();
         double all = 0.0;
-        for (int w = 0; w < kWaves; ++w) all += part[w];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) all += sh.part[w];
         return all;
     }
-    // The first of n sums that passes the point, or the last with mass; *before: the sums ahead of it.
-    static __device__ __forceinline__ int pick(const double* sums, int n, double point, double* before) {
+    static __device__ __forceinline__ double upto(double s, int lane) {
+        for (int d = 1; d < 64; d <<= 1) {
+            const double o = __shfl_up(s, d);
+            if (lane >= d) s += o;
+        }
+        return s;
+    }
+    // The sum of n sums.  A whole wave calls it.
+    static __device__ __forceinline__ double total_of(const double* sums, int n, int lane) {
         double s = 0.0;
+        for (int w = lane; w < n; w += 64) s += sums[w];
+        return wave_sum(s);
+    }
+    // The first of n sums that passes the point, or the last with mass; *before: the sums ahead of it.  A whole wave calls it.
+    static __device__ __forceinline__ int pick(const double* sums, int n, double point, int lane, double* before) {
+        double ahead = 0.0;
         int at = 0;
         *before = 0.0;
-        for (int w = 0; w < n; ++w) {
-            if (sums[w] > 0.0) {
-                at = w;
-                *before = s;
-                if (s + sums[w] > point) break;
+        for (int base = 0; base < n; base += 64) {
+            const double mine = base + lane < n ? sums[base + lane] : 0.0;
+            const double to = ahead + upto(mine, lane);
+            const unsigned long long some = __ballot(mine > 0.0), past = __ballot(mine > 0.0 && to > point);
+            if (some) {
+                const int l = past ? __ffsll(past) - 1 : 63 - __clzll(static_cast<long long>(some));
+                at = base + l;
+                *before = __shfl(to - mine, l);
             }
-            s += sums[w];
+            if (past) break;
+            ahead = __shfl(to, 63);
         }
         return at;
     }
-    // The token of [from, to) in which the cumulative mass passes `point` (the last one with mass if none does).  part: the sums of
-    // its kWaves parts of `step` tokens.  The first wave's lanes have the answer.
+    // The token of [from, to) in which the cumulative mass passes `point`, the last one with mass if none does: neighbouring tokens
+    // to a lane, whole 16-byte groups.  Thread 0 has the answer.
     template <class T>
-    __device__ __forceinline__ int token(const Rest<T>& rest, int from, int to, int step, double point) {
-        double before;
-        for (int level = 0; level < 2; ++level) {
-            from += pick(part, kWaves, point, &before) * step;
-            point -= before;
-            to = min(from + step, to);
-            step = (to - from + kWaves - 1) / kWaves;
-            if (step < 64) break;
-            if (level == 0) parts(rest, from, to, step);
-        }
-        if (wave != 0) return 0;
-        // at most 1024 tokens: neighbouring ones to a lane
-        const int mine = (to - from + 63) / 64, begin = from + lane * mine, end = min(begin + mine, to);
-        double sum = 0.0;
-        for (int t = begin; t < end; ++t) sum += rest(t);
-        double upto = sum;
-        for (int d = 1; d < 64; d <<= 1) {
-            const double o = __shfl_up(upto, d);
-            if (lane >= d) upto += o;
-        }
-        const unsigned long long some = __ballot(sum > 0.0), past = __ballot(sum > 0.0 && upto > point);
-        const int at = past ? __ffsll(past) - 1 : some ? 63 - __clzll(static_cast<long long>(some)) : 0;
-        int last = begin;
-        if (lane == at) {
-            double run = upto - sum;
-            for (int t = begin; t < end; ++t) {
-                const double m = rest(t);
-                if (m > 0.0) last = t;
-                run += m;
-                if (m > 0.0 && run > point) break;
+    __device__ __forceinline__ int token(const Rest<T>& rest, int from, int to, double point) {
+        constexpr int N = Vector<T>::N;
+        const int mine = (to - from + kChainBlock * N - 1) / (kChainBlock * N) * N;
+        const int begin = min(from + static_cast<int>(threadIdx.x) * mine, to), end = min(begin + mine, to);
+        const double sum = rest.lane_sum(begin, end, 0, 1);
+        double end_at = upto(sum, lane);
+        __syncthreads();
+        if (lane == 63) sh.part[wave] = end_at;
+        if (threadIdx.x == 0) { sh.first = kChainBlock; sh.last = 0; sh.token = from; }
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) end_at += sh.part[w];
+        const unsigned long long some = __ballot(sum > 0.0), past = __ballot(sum > 0.0 && end_at > point);
+        if (lane == 0 && past) atomicMin(&sh.first, wave * 64 + __ffsll(past) - 1);
+        if (lane == 0 && some) atomicMax(&sh.last, wave * 64 + 63 - __clzll(static_cast<long long>(some)));
+        __syncthreads();
+        if (static_cast<int>(threadIdx.x) == (sh.first < kChainBlock ? sh.first : sh.last)) {
+            double run = end_at - sum;
+            int last = begin;
+            bool found = false;
+            for (int t = begin; t < end && !found; t += N) {
+                double m[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) m[i] = t + i < end ? rest(t + i) : 0.0;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    if (found) continue;
+                    run += m[i];
+                    if (m[i] > 0.0) {
+                        last = t + i;
+                        found = run > point;
+                    }
+                }
             }
+            sh.token = last;
         }
-        last = __shfl(last, at);
-        return last;
+        __syncthreads();
+        return sh.token;
     }
 };
 
@@ -217,16 +243,22 @@ __device__ __forceinline__ void draw_row(const ChainArgs& a, int b, const Chain<
         rest.without = -1;
         total = draw.parts(rest, 0, V, step);
     }
-    const int token = total > 0.0 ? draw.token(rest, 0, V, step, static_cast<double>(chain.u[0]) * total) : 0;
+    int token = 0;
+    if (total > 0.0) {
+        double before;
+        const double point = static_cast<double>(chain.u[0]) * total;
+        const int from = Draw::pick(draw.sh.part, Draw::kWaves, point, draw.lane, &before) * step;
+        token = draw.token(rest, from, min(from + step, V), point - before);
+    }
     if (threadIdx.x == 0) a.b.bonus_token[b] = token;
 }
 
 template <class T>
 __global__ __launch_bounds__(kChainBlock) void chain_kernel(ChainArgs a) {
-    __shared__ double part[Draw::kWaves];
+    __shared__ Draw::Shared shared;
     __shared__ int stop;
     const int b = blockIdx.x;
-    Draw draw{part, static_cast<int>(threadIdx.x & 63), static_cast<int>(threadIdx.x >> 6)};
+    Draw draw{shared, static_cast<int>(threadIdx.x & 63), static_cast<int>(threadIdx.x >> 6)};
     const Chain<T> chain(a, b);
     if (draw.wave == 0) {
         const int length = chain.test(a, draw.lane);
@@ -260,26 +292,23 @@ __global__ __launch_bounds__(kPartBlock) void part_kernel(ChainArgs a) {
 
 template <class T>
 __global__ __launch_bounds__(kChainBlock) void draw_kernel(ChainArgs a) {
-    __shared__ double part[Draw::kWaves];
+    __shared__ Draw::Shared shared;
     const int b = blockIdx.x;
-    Draw draw{part, static_cast<int>(threadIdx.x & 63), static_cast<int>(threadIdx.x >> 6)};
+    Draw draw{shared, static_cast<int>(threadIdx.x & 63), static_cast<int>(threadIdx.x >> 6)};
     const Chain<T> chain(a, b);
     bool bad;
     const Rest<T> rest = chain.rest(a, a.b.accept_len[b], &bad);
     if (threadIdx.x == 0 && bad) atomicAdd(&a.b.counters[MPV_COUNTER_BAD_TOKEN], 1u);
     const double* sums = a.sums + static_cast<int64_t>(b) * a.parts;
-    double total = 0.0;
-    for (int w = 0; w < a.parts; ++w) total += sums[w];
+    const double total = Draw::total_of(sums, a.parts, draw.lane);
     if (!(total > 0.0)) {
         draw_row(a, b, chain, rest, draw);
         return;
     }
     double before;
     const double point = static_cast<double>(chain.u[0]) * total;
-    const int from = Draw::pick(sums, a.parts, point, &before) * a.part, to = min(from + a.part, a.c.V);
-    const int step = (to - from + Draw::kWaves - 1) / Draw::kWaves;
-    draw.parts(rest, from, to, step);
-    const int token = draw.token(rest, from, to, step, point - before);
+    const int from = Draw::pick(sums, a.parts, point, draw.lane, &before) * a.part;
+    const int token = draw.token(rest, from, min(from + a.part, a.c.V), point - before);
     if (threadIdx.x == 0) a.b.bonus_token[b] = token;
 }
 
