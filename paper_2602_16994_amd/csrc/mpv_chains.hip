@@ -49,26 +49,53 @@ struct Rest {
         const double m = mass_of(prob(p[t]));
         return q ? fmax(m - mass_of(prob(q[t])), 0.0) : m;
     }
-    // Mass of the 16-byte groups lane, lane + lanes, .. of [from, to).  The token left out is looked for a group at a time.
+    // Mass of N tokens from t on.  The token left out is looked for a group at a time.
+    template <bool Q>
+    __device__ __forceinline__ double group_sum(const Vector<T>& a, const Vector<T>& d, int t) const {
+        constexpr int N = Vector<T>::N;
+        double s[2] = {};
+        if (!Q && static_cast<unsigned>(without - t) < static_cast<unsigned>(N)) {
+            for (int i = 0; i < N; ++i) s[0] += (*this)(t + i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if constexpr (Q) s[i & 1] += fmax(mass_of(prob(a.v[i])) - mass_of(prob(d.v[i])), 0.0);
+                else s[i & 1] += mass_of(prob(a.v[i]));
+            }
+        }
+        return s[0] + s[1];
+    }
+    // Mass of the 16-byte groups lane, lane + lanes, .. of [from, to), four of them asked for at a time.
     template <bool Q>
     __device__ __forceinline__ double lane_sum_of(int from, int to, int lane, int lanes) const {
-        constexpr int N = Vector<T>::N;
+        constexpr int N = Vector<T>::N, kAtOnce = 4;
         double s = 0.0;
         int t = from + lane * N;
-#pragma unroll 4
-        for (; t + N <= to; t += lanes * N) {
-            Vector<T> a, d;
-            a.load(p + t);
-            if constexpr (Q) d.load(q + t);
-            if (!Q && static_cast<unsigned>(without - t) < static_cast<unsigned>(N)) {
-                for (int i = 0; i < N; ++i) s += (*this)(t + i);
-            } else {
+        const int step = lanes * N;
+        for (; t + (kAtOnce - 1) * step + N <= to; t += kAtOnce * step) {
+            Vector<T> a[kAtOnce], d[kAtOnce];
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    if constexpr (Q) s += fmax(mass_of(prob(a.v[i])) - mass_of(prob(d.v[i])), 0.0);
-                    else s += mass_of(prob(a.v[i]));
-                }
+            for (int j = 0; j < kAtOnce; ++j) {
+                a[j].load(p + t + j * step);
+                if constexpr (Q) d[j].load(q + t + j * step);
             }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) s += group_sum<Q>(a[j], d[j], t + j * step);
+        }
+        {
+            Vector<T> a[kAtOnce - 1], d[kAtOnce - 1];
+#pragma unroll
+            for (int j = 0; j < kAtOnce - 1; ++j)
+                if (t + j * step + N <= to) {
+                    a[j].load(p + t + j * step);
+                    if constexpr (Q) d[j].load(q + t + j * step);
+                }
+#pragma unroll
+            for (int j = 0; j < kAtOnce - 1; ++j)
+                if (t + N <= to) {
+                    s += group_sum<Q>(a[j], d[j], t);
+                    t += step;
+                }
         }
         for (; t < to; ++t) s += (*this)(t);                // (only the lane at the end has some left)
         return s;
@@ -213,8 +240,20 @@ struct Draw {
             bool found = false;
             for (int t = begin; t < end && !found; t += N) {
                 double m[N];
+                if (t + N <= end) {
+                    Vector<T> a, d;
+                    a.load(rest.p + t);
+                    if (rest.q) d.load(rest.q + t);
 #pragma unroll
-                for (int i = 0; i < N; ++i) m[i] = t + i < end ? rest(t + i) : 0.0;
+                    for (int i = 0; i < N; ++i) {
+                        m[i] = mass_of(prob(a.v[i]));
+                        if (rest.q) m[i] = fmax(m[i] - mass_of(prob(d.v[i])), 0.0);
+                        if (t + i == rest.without) m[i] = 0.0;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) m[i] = t + i < end ? rest(t + i) : 0.0;
+                }
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     if (found) continue;
