@@ -107,6 +107,10 @@ __device__ __forceinline__ unsigned long long shfl64(unsigned long long v, int l
 
 // The reference of a softmax moves only where a product exceeds it by more than this (log2 units): weights are at most 2^8.
 constexpr float kSlack = 8.0f;
+__device__ __forceinline__ int64_t uniform64(unsigned long long v) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v >> 32));
+    return static_cast<int64_t>(static_cast<unsigned long long>(hi) << 32 | lo);
+}
 // x, as if it had just been read: what depends on it is worked out where it is needed and does not occupy registers across the loops.
 __device__ __forceinline__ int fresh(int x) {
     asm volatile("" : "+v"(x));
@@ -140,8 +144,9 @@ __device__ __forceinline__ TreeWork tree_work(const AttentionArgs& g, int b) {
     return t;
 }
 
-// DTYPE; DP: columns of a row in LDS (head_dim, rounded up); QT: 16-row groups of a wave; WAVES; TILE: keys; STAGES: tiles in LDS.
-template <int DTYPE, int DP, int QT, int WAVES, int TILE, int STAGES>
+// DTYPE; DP: columns of a row in LDS (head_dim, rounded up); QT: 16-row groups of a wave; WAVES; TILE: keys; STAGES: tiles in LDS;
+// SHARE: workgroups that a compute unit holds.
+template <int DTYPE, int DP, int QT, int WAVES, int TILE, int STAGES, int SHARE>
 struct Attention {
     typedef Elem<DTYPE> E;
     static constexpr int kWaves = WAVES;
@@ -158,6 +163,7 @@ struct Attention {
     static constexpr int kBatch = 64 / kMyRows;                    // tiles whose rows a wave's lanes look up at a time
     static constexpr int kAheadTiles = STAGES - 1;
     static constexpr int kTile = TILE;
+    static constexpr int kShare = SHARE;
     static constexpr bool k16 = E::kBytes == 2;
     static_assert(kChunks >= 8 && kChunks <= 64 && kMyLoads >= 1 && kMyRows % kRowsPerLoad == 0 && 64 % kMyRows == 0, "loads");
     static_assert(TILE % (k16 ? 32 : 16) == 0 && kGroups * 4 <= 32, "tile");
@@ -170,10 +176,8 @@ struct Attention {
         __align__(16) uint64_t place[2][kBatch][TILE][2];          // where a key's and its value's row lie
         __align__(16) int pages[WAVES][64];                        // entries of the block table, a lane's each
         __align__(4) uint8_t seen[2][kBatch][TILE];                // whether anybody sees the key
-        __align__(4) uint8_t special[2][kBatch][4];                // whether a wave found a key that not every node sees
+        __align__(8) uint8_t special[2][kBatch][8];                // whether a wave found a key that not every node sees
         int spoiled;                                               // whether a tile held values that are no numbers, see spoil
-        int first_tree;
-        int64_t sum[WAVES];
     };
 
     // A tile: positions of the cache from `base` on, or nodes.
@@ -245,9 +249,7 @@ struct Attention {
         sh.place[half][sub][r.key][1] = r.seen ? reinterpret_cast<uint64_t>(values) + offset : zeros;
         const unsigned long long mask = kMyRows == 64 ? ~0ull : (1ull << (kMyRows % 64)) - 1;
         const bool hidden = (__ballot(!r.seen) >> (sub * kMyRows % 64) & mask) != 0;
-        // (a wave of several writes its own byte, one of two writes two)
-        if (lane % kMyRows < 4 / WAVES)
-            sh.special[half][sub][wave + lane % kMyRows * WAVES] = hidden || r.tree || differs(tile_at(tile + sub));
+        if (lane % kMyRows == 0) sh.special[half][sub][wave] = hidden || r.tree || differs(tile_at(tile + sub));
     }
 
     // Asks for a tile whose places are known.  A key that nobody sees is read as zeros.
@@ -329,7 +331,8 @@ struct Attention {
     __device__ __forceinline__ void work(const Tile& x, int half, int sub, int stage) {
         const char* keys = sh.keys[stage];
         char* values = sh.values[stage];
-        const uint32_t special = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint32_t*>(sh.special[half][sub]));
+        constexpr unsigned long long kBytesOfWaves = WAVES == 8 ? ~0ull : (1ull << (8 * (WAVES % 8))) - 1;
+        const bool special = uniform64(*reinterpret_cast<const unsigned long long*>(sh.special[half][sub]) & kBytesOfWaves) != 0;
         f32x4 s[QT][kGroups];
         const int key_swizzle = swizzle(l16);
         // (operands are read kAhead instructions before their use, which the order of the source alone does not bring about)
@@ -447,17 +450,23 @@ struct Attention {
             }
             __builtin_amdgcn_sched_barrier(0);
         } else {
+            constexpr int kSecond = kColumns * kGroups * 4, kAhead32 = 8;
+            float v[kAhead32];
+            auto read_value = [&](int n) {
+                const int i = n % 4, k = n / 4 % kGroups, c = n / (4 * kGroups);
+                return column32(values, k * 16 + quad * 4 + i, c);
+            };
 #pragma unroll
-            for (int c = 0; c < kColumns; ++c) {
+            for (int n = 0; n < kAhead32; ++n) v[n] = read_value(n);
 #pragma unroll
-                for (int k = 0; k < kGroups; ++k)
+            for (int n = 0; n < kSecond; ++n) {
+                const int i = n % 4, k = n / 4 % kGroups, c = n / (4 * kGroups);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float v = column32(values, k * 16 + quad * 4 + i, c);
-#pragma unroll
-                        for (int q = 0; q < QT; ++q) out[q][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[q][k][i], out[q][c], 0, 0, 0);
-                    }
+                for (int q = 0; q < QT; ++q) out[q][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[n % kAhead32], s[q][k][i], out[q][c], 0, 0, 0);
+                if (n + kAhead32 < kSecond) v[n % kAhead32] = read_value(n + kAhead32);
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 
@@ -642,23 +651,13 @@ struct Attention {
         }
     }
 
-    // Sum over the workgroup; *before: of the threads before this one.
-    __device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* before) {
-        int64_t upto = v;
+    // Inclusive sum over the wave.
+    __device__ __forceinline__ int64_t wave_scan(int64_t v) const {
         for (int d = 1; d < 64; d <<= 1) {
-            const int64_t o = static_cast<int64_t>(shfl64(static_cast<unsigned long long>(upto), max(lane - d, 0)));
-            if (lane >= d) upto += o;
+            const int64_t o = static_cast<int64_t>(shfl64(static_cast<unsigned long long>(v), max(lane - d, 0)));
+            if (lane >= d) v += o;
         }
-        __syncthreads();
-        if (lane == 63) sh.sum[wave] = upto;
-        __syncthreads();
-        int64_t all = 0;
-        for (int w = 0; w < kWaves; ++w) {
-            if (w < wave) upto += sh.sum[w];
-            all += sh.sum[w];
-        }
-        *before = upto - v;
-        return all;
+        return v;
     }
 
     __device__ __forceinline__ int64_t tiles_of(int tree) const {
@@ -671,28 +670,35 @@ struct Attention {
         // teams of one chiplet (blockIdx % 8) take neighbouring parts of the list
         const int most = g.teams, place = most % 8 == 0 ? blockIdx.x / 8 : blockIdx.x;
         const int member = place % g.blocks, team = most % 8 == 0 ? (blockIdx.x % 8) * (most / 8) + place / g.blocks : place / g.blocks;
-        int64_t total = 0, before;
-        for (int base = 0; base < g.a.B; base += kThreads) total += block_sum(tiles_of(base + threadIdx.x), &before);
+        // every wave adds the trees' tiles up for itself, 64 trees at a time
+        const int trees = g.a.B;
+        int64_t mine = tiles_of(lane), total = mine;
+        for (int base = 64; base < trees; base += 64) total += tiles_of(base + lane);
+        int64_t upto = wave_scan(mine);
+        if (trees > 64) total = wave_scan(total); else total = upto;
+        total = uniform64(shfl64(total, 63));
         const int T = static_cast<int>(min(static_cast<int64_t>(most), total));      // every one of them has a tile at least
         if (member == 0 && threadIdx.x == 0) g.split[team] = make_int4(-1, 0, 0, 0);
         if (team >= T) return;
-        const int64_t begin_at = total * team / T, end_at = total * (team + 1) / T;
+        // the first `longer` teams have one tile more than the others
+        const int64_t share = total <= UINT32_MAX ? static_cast<int64_t>(static_cast<uint32_t>(total) / static_cast<uint32_t>(T)) : total / T;
+        const int64_t longer = total - share * T;
+        const int64_t begin_at = share * team + min(static_cast<int64_t>(team), longer), end_at = begin_at + share + (team < longer);
         // the tree of the first tile
         int64_t start = 0;
-        for (int base = 0;; base += kThreads) {
-            const int64_t mine = tiles_of(base + threadIdx.x);
-            const int64_t sum = block_sum(mine, &before);
-            if (begin_at < start + sum) {
-                const bool here = begin_at >= start + before && begin_at < start + before + mine;
-                __syncthreads();
-                if (here) { sh.sum[0] = start + before; sh.first_tree = base + threadIdx.x; }
-                __syncthreads();
-                start = sh.sum[0];
-                b = __builtin_amdgcn_readfirstlane(sh.first_tree);
-                __syncthreads();
+        b = 0;
+        for (int base = 0;;) {
+            const int64_t chunk = uniform64(shfl64(upto, 63));
+            if (begin_at < start + chunk) {
+                const int l = __ffsll(static_cast<unsigned long long>(__ballot(begin_at < start + upto))) - 1;
+                start += uniform64(shfl64(upto - mine, l));
+                b = __builtin_amdgcn_readfirstlane(base + l);
                 break;
             }
-            start += sum;
+            start += chunk;
+            base += 64;
+            mine = tiles_of(base + lane);
+            upto = wave_scan(mine);
         }
         int64_t at = begin_at;
         for (; at < end_at; ++b) {
@@ -700,14 +706,20 @@ struct Attention {
             if (t.nodes == 0) continue;
             const int64_t tree_end = start + static_cast<int64_t>(t.tiles) * g.a.kv_heads;
             while (at < min(end_at, tree_end)) {
-                kv = static_cast<int>((at - start) / t.tiles);
+                // (the tiles of a tree's heads may be more than 32 bits hold, but hardly ever are)
+                const int64_t into = at - start;
+                kv = static_cast<int>(into <= UINT32_MAX ? static_cast<uint32_t>(into) / static_cast<uint32_t>(t.tiles) : into / t.tiles);
                 const int64_t unit = start + static_cast<int64_t>(kv) * t.tiles;
                 const int first = static_cast<int>(at - unit);
                 const int last = static_cast<int>(min(static_cast<int64_t>(t.tiles), end_at - unit));
                 at = unit + last;
                 const bool shared = first > 0 || last < t.tiles;
                 if (member == 0 && first == 0 && shared && threadIdx.x == 0)         // (the team that has the unit's last tile)
-                    g.split[team] = make_int4(b, kv, t.blocks, static_cast<int>(((unit + t.tiles) * T - 1) / total));
+                {
+                    const int64_t x = unit + t.tiles - 1, ahead = longer * (share + 1);
+                    const int64_t whose = x < ahead ? x / (share + 1) : longer + (x - ahead) / share;
+                    g.split[team] = make_int4(b, kv, t.blocks, static_cast<int>(whose));
+                }
                 if (member >= t.blocks) continue;
                 run(member, first, last);
                 if (shared) keep(member, (team * g.blocks + member) * 2 + (first > 0 ? 0 : 1));
@@ -809,19 +821,20 @@ __global__ __launch_bounds__(256) void combine_kernel(AttentionArgs g) {
 
 // ------------------------------------------------------------------ host side
 
-// Workgroups of a call: two or three a compute unit, which is what the tiles in LDS leave room for (more only where a team alone has more).
+// Workgroups of a call: as many as 256 compute units hold at a time (more only where a team alone has more).
 template <class A>
-constexpr int kMaxWorkgroups = 256 * (160 * 1024 / sizeof(typename A::Shared) < 3 ? 2 : 3);
+constexpr int kMaxWorkgroups = 256 * A::kShare;
 
-// The tile for a type and a row length: 8 KB of keys (16 for the longest rows) and as many of values, in four stages of 16 KB or two
-// of 32 KB.
+// The tile for a type and a row length: 8 KB of keys (16 for the longest rows) and as many of values.  Two workgroups share a compute
+// unit, with four stages of 16 KB or two of 32 KB each; those of one wave are three; and one of eight waves has the unit for itself.
 template <int DTYPE, int DP, int WAVES>
 struct Family {
     static constexpr int kBytes = DP * Elem<DTYPE>::kBytes;
     static constexpr int kLeast = DTYPE == MPV_DTYPE_F32 ? 16 : 32;
     static constexpr int kMost = 8192 / kBytes < 16 * WAVES ? 8192 / kBytes : 16 * WAVES;      // (a lane looks up a row of some tiles ahead)
     static constexpr int kTile = kMost < kLeast ? kLeast : kMost;
-    static constexpr int kStages = kTile * kBytes > 8192 ? 2 : WAVES == 1 ? 3 : 4;
+    static constexpr int kShare = WAVES == 1 && kTile * kBytes <= 8192 ? 3 : WAVES == 8 ? 1 : 2;
+    static constexpr int kStages = kTile * kBytes > 8192 ? (kShare == 1 ? 4 : 2) : WAVES == 1 ? 3 : 4;
 };
 
 // What a call needs to know of the kernel that it gets.
@@ -887,7 +900,8 @@ static int with_kernel(const mpv_attention* a, AttentionArgs* g, void* workspace
 }
 
 template <int DTYPE, int DP, int QT, int WAVES>
-using Kernel = Attention<DTYPE, DP, QT, WAVES, Family<DTYPE, DP, WAVES>::kTile, Family<DTYPE, DP, WAVES>::kStages>;
+using Kernel = Attention<DTYPE, DP, QT, WAVES, Family<DTYPE, DP, WAVES>::kTile, Family<DTYPE, DP, WAVES>::kStages,
+                         Family<DTYPE, DP, WAVES>::kShare>;
 
 template <int DTYPE, int DP>
 static int with_columns(const mpv_attention* a, AttentionArgs* g, void* workspace, size_t* bytes, hipStream_t s) {
@@ -895,14 +909,15 @@ static int with_columns(const mpv_attention* a, AttentionArgs* g, void* workspac
     if (rows <= 16) return with_kernel<Kernel<DTYPE, DP, 1, 1>, DTYPE, DP>(a, g, workspace, bytes, s);
     if (rows <= 32) return with_kernel<Kernel<DTYPE, DP, 1, 2>, DTYPE, DP>(a, g, workspace, bytes, s);
     if (rows <= 64) return with_kernel<Kernel<DTYPE, DP, 1, 4>, DTYPE, DP>(a, g, workspace, bytes, s);
-    // the most groups a wave that leave its registers room for the products; as many as divide the rows into even blocks
-    constexpr int kMost = DP * Elem<DTYPE>::kBytes <= 256 ? 3 : DP == 128 ? 2 : 1;
-    const int64_t blocks = (rows + 64 * kMost - 1) / (64 * kMost), groups = (rows + 64 * blocks - 1) / (64 * blocks);
-    if constexpr (kMost >= 3)
+    if constexpr (DP * Elem<DTYPE>::kBytes > 256) {
+        // (two groups a wave of such long rows do not fit its registers)
+        return with_kernel<Kernel<DTYPE, DP, 1, 8>, DTYPE, DP>(a, g, workspace, bytes, s);
+    } else {
+        // as many groups a wave as divide the rows into even blocks
+        const int64_t blocks = (rows + 191) / 192, groups = (rows + 64 * blocks - 1) / (64 * blocks);
         if (groups > 2) return with_kernel<Kernel<DTYPE, DP, 3, 4>, DTYPE, DP>(a, g, workspace, bytes, s);
-    if constexpr (kMost >= 2)
-        if (groups > 1) return with_kernel<Kernel<DTYPE, DP, 2, 4>, DTYPE, DP>(a, g, workspace, bytes, s);
-    return with_kernel<Kernel<DTYPE, DP, 1, 4>, DTYPE, DP>(a, g, workspace, bytes, s);
+        return with_kernel<Kernel<DTYPE, DP, 2, 4>, DTYPE, DP>(a, g, workspace, bytes, s);
+    }
 }
 
 template <int DTYPE>
