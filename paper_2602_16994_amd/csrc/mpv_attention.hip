@@ -27,18 +27,38 @@
 
 namespace mpv {
 
+// Division of numbers below 2^31 by one that the host knows (Granlund and Montgomery, Division by invariant integers using
+// multiplication, 1994, figure 4.1).
+struct Divisor {
+    uint32_t d, factor, shift1, shift2;
+    __host__ void set(uint32_t by) {
+        int log = 0;
+        while ((1ull << log) < by) ++log;
+        d = by;
+        factor = static_cast<uint32_t>(((1ull << 32) * ((1ull << log) - by)) / by + 1);
+        shift1 = log < 1 ? log : 1;
+        shift2 = log < 1 ? 0 : log - 1;
+    }
+    __device__ __forceinline__ int of(int n) const {
+        const uint32_t x = static_cast<uint32_t>(n), high = __umulhi(factor, x);
+        return static_cast<int>((high + ((x - high) >> shift1)) >> shift2);
+    }
+};
+
 struct AttentionArgs {
     mpv_attention a;
     mpv_attention_buffers b;
     int8_t parent[MPV_MAX_NODES];          // the shared shape (without tree_parent)
     int teams;
     int blocks;                            // row blocks of the largest tree: members of a team
+    int group;                             // query heads of a cache head
+    Divisor by_group, by_page;
     float factor;                          // |scale| log2(e): products to exponents (1 where the scale is 0)
     int sign;                              // of the scale: -1, 0, 1
     float* partial;                        // [teams][members][2][rows][columns]
     float2* partial_stats;                 // [teams][members][2][rows]: reference, sum of weights
-    int4* split;                           // [teams]: tree, cache head, row blocks, last team of a unit that begins in this team's part and
-                                           // is shared; x < 0: none
+    int4* split;                           // shared units (tree, cache head, first and last team; x < 0: none), by unit or by the first team
+    int by_unit;
 };
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
@@ -140,7 +160,7 @@ __device__ __forceinline__ TreeWork tree_work(const AttentionArgs& g, int b) {
     }
     t.context_tiles = (t.context - t.low + TILE - 1) / TILE;
     t.tiles = t.sink_tiles + t.context_tiles + (t.nodes + TILE - 1) / TILE;
-    t.blocks = (t.nodes * (a.heads / a.kv_heads) + ROWS - 1) / ROWS;
+    t.blocks = (t.nodes * g.group + ROWS - 1) / ROWS;
     return t;
 }
 
@@ -220,7 +240,7 @@ struct Attention {
     // Asks for the block table's entries of the batch that begins with `tile`.
     __device__ __forceinline__ void ask_pages(int tile, int last) {
         const Row r = row_of(fresh(lane), tile, last);
-        const int32_t* entry = g.b.block_table + static_cast<int64_t>(b) * g.a.table_width + r.at / g.a.page_size;
+        const int32_t* entry = g.b.block_table + static_cast<int64_t>(b) * g.a.table_width + g.by_page.of(r.at);
         const uint64_t from = r.seen && !r.tree ? reinterpret_cast<uint64_t>(entry) : reinterpret_cast<uint64_t>(&kZeros);
         word_to_lds(from, shared_at + offsetof(Shared, pages) + wave * 256);
     }
@@ -237,7 +257,7 @@ struct Attention {
         } else {
             const int page = sh.pages[wave][lane];
             r.seen = r.seen && page >= 0 && page < g.a.num_pages;
-            offset = page * g.a.page_stride + r.at % g.a.page_size * g.a.slot_stride;
+            offset = page * g.a.page_stride + (r.at - g.by_page.of(r.at) * g.a.page_size) * g.a.slot_stride;
             keys = static_cast<const char*>(g.b.cache_k);
             values = static_cast<const char*>(g.b.cache_v);
         }
@@ -289,7 +309,7 @@ struct Attention {
 
     __device__ __forceinline__ void begin(int block) {
         const int lane = fresh(this->lane), l16 = lane & 15, quad = lane >> 4;
-        const int group = g.a.heads / g.a.kv_heads;
+        const int group = g.group;
         // ancestors of node `lane`: in each round twice as many steps up
         unsigned long long mask = 1ull << lane;
         int up = -1;
@@ -305,7 +325,7 @@ struct Attention {
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
             const int row = block * kRows + (wave * QT + q) * 16 + l16;
-            const int node = row / group;
+            const int node = g.by_group.of(row);
             const bool real = node < t.nodes;
             line[q] = shfl64(mask, real ? node : 0);
             low[q] = g.a.window > 0 ? t.context + __popcll(line[q]) - g.a.window : INT32_MIN;
@@ -623,11 +643,11 @@ struct Attention {
     // Whole rows of the output.
     __device__ __forceinline__ void finish(int block) {
         const int lane = fresh(this->lane), l16 = lane & 15, quad = lane >> 4;
-        const int group = g.a.heads / g.a.kv_heads;
+        const int group = g.group;
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
             const int row = block * kRows + (wave * QT + q) * 16 + l16;
-            const int node = row / group;
+            const int node = g.by_group.of(row);
             if (node >= t.nodes) continue;
             const float whole = 1.0f / weight[q][0];
             char* to = static_cast<char*>(g.b.out) +
@@ -640,7 +660,7 @@ struct Attention {
 
     __device__ __forceinline__ void keep(int block, int slot) {
         const int lane = fresh(this->lane), l16 = lane & 15, quad = lane >> 4;
-        const int rows = t.nodes * (g.a.heads / g.a.kv_heads) - block * kRows;
+        const int rows = t.nodes * g.group - block * kRows;
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
             if ((wave * QT + q) * 16 + l16 >= rows) continue;
@@ -677,8 +697,8 @@ struct Attention {
         int64_t upto = wave_scan(mine);
         if (trees > 64) total = wave_scan(total); else total = upto;
         total = uniform64(shfl64(total, 63));
-        const int T = static_cast<int>(min(static_cast<int64_t>(most), total));      // every one of them has a tile at least
-        if (member == 0 && threadIdx.x == 0) g.split[team] = make_int4(-1, 0, 0, 0);
+        const int T = static_cast<int>(min(static_cast<int64_t>(most), total));      // every team has a tile at least
+        if (member == 0 && threadIdx.x == 0 && !g.by_unit) g.split[team] = make_int4(-1, 0, 0, 0);
         if (team >= T) return;
         // the first `longer` teams have one tile more than the others
         const int64_t share = total <= UINT32_MAX ? static_cast<int64_t>(static_cast<uint32_t>(total) / static_cast<uint32_t>(T)) : total / T;
@@ -714,11 +734,10 @@ struct Attention {
                 const int last = static_cast<int>(min(static_cast<int64_t>(t.tiles), end_at - unit));
                 at = unit + last;
                 const bool shared = first > 0 || last < t.tiles;
-                if (member == 0 && first == 0 && shared && threadIdx.x == 0)         // (the team that has the unit's last tile)
-                {
-                    const int64_t x = unit + t.tiles - 1, ahead = longer * (share + 1);
+                if (member == 0 && first == 0 && threadIdx.x == 0 && (shared || g.by_unit)) {
+                    const int64_t x = unit + t.tiles - 1, ahead = longer * (share + 1);      // the unit's last tile, and whose it is
                     const int64_t whose = x < ahead ? x / (share + 1) : longer + (x - ahead) / share;
-                    g.split[team] = make_int4(b, kv, t.blocks, static_cast<int>(whose));
+                    g.split[g.by_unit ? b * g.a.kv_heads + kv : team] = make_int4(shared ? b : -1, kv, team, static_cast<int>(whose));
                 }
                 if (member >= t.blocks) continue;
                 run(member, first, last);
@@ -738,18 +757,19 @@ __global__ __launch_bounds__(A::kThreads) __attribute__((amdgpu_waves_per_eu(2))
 }
 
 // Puts the shared units together.  kLanes lanes have a row (4 columns each).  Few parts, as in large batches: a wave has as many rows
-// as it has such groups of lanes, four times over.  Many: the groups of a wave share the parts of one row.
-constexpr int kFewParts = 4;
+// as it has such groups of lanes, twice over.  Many: the groups of a workgroup share the parts of one row.
+constexpr int kFewParts = 8, kFewRows = 2;
 
 template <int DTYPE, int DP, int ROWS>
 __global__ __launch_bounds__(256) void combine_kernel(AttentionArgs g) {
     typedef Elem<DTYPE> E;
     constexpr int kLanes = DP / 4, kGroups = 64 / kLanes;
-    const int first = blockIdx.x;
-    const int4 s = g.split[first];
+    const int nodes_of_unit = g.by_unit && g.b.num_nodes ? g.b.num_nodes[blockIdx.x / g.a.kv_heads] : 1;
+    if (nodes_of_unit <= 0) return;                                // (nobody wrote its entry)
+    const int4 s = g.split[blockIdx.x];
     if (s.x < 0) return;
     const int lane = threadIdx.x & 63, column = lane % kLanes * 4, mine = lane / kLanes;
-    const int b = s.x, kv = s.y, last = s.w, group = g.a.heads / g.a.kv_heads;
+    const int b = s.x, kv = s.y, first = s.z, last = s.w, group = g.group;
     const int parts = last - first + 1;
     const int nodes = g.b.num_nodes ? min(max(g.b.num_nodes[b], 0), g.a.N) : g.a.N;
     const int rows = nodes * group, wave = blockIdx.y * 4 + (threadIdx.x >> 6);
@@ -758,28 +778,28 @@ __global__ __launch_bounds__(256) void combine_kernel(AttentionArgs g) {
         return ((static_cast<int64_t>(first + p) * g.blocks + row / ROWS) * 2 + (p == 0 ? 1 : 0)) * ROWS + row % ROWS;
     };
     auto put = [&](int row, const f32x4& sum, float weight) {
-        const int node = row / group;
+        const int node = g.by_group.of(row);
         char* to = static_cast<char*>(g.b.out) +
             ((static_cast<int64_t>(b) * g.a.N + node) * g.a.out_stride + static_cast<int64_t>(kv * group + row - node * group) * g.a.head_dim + column) * E::kBytes;
         if (row < rows && column < g.a.head_dim) E::put4(to, sum * (1.0f / weight));
     };
     if (parts <= kFewParts) {
-        const int row0 = wave * kGroups * 4;
+        const int row0 = wave * kGroups * kFewRows;
         if (row0 >= rows) return;
-        float2 stats[4][kFewParts];
-        f32x4 part[4][kFewParts];
+        float2 stats[kFewRows][kFewParts];
+        f32x4 part[kFewRows][kFewParts];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
+        for (int r = 0; r < kFewRows; ++r) {
             const int row = min(row0 + r * kGroups + mine, rows - 1);
 #pragma unroll
             for (int p = 0; p < kFewParts; ++p) {
-                if (p >= parts) break;
+                if (p >= parts) continue;
                 stats[r][p] = g.partial_stats[at(row, p)];
                 part[r][p] = *reinterpret_cast<const f32x4*>(g.partial + at(row, p) * DP + column);
             }
         }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
+        for (int r = 0; r < kFewRows; ++r) {
             float top = stats[r][0].x, weight = 0.0f;
 #pragma unroll
             for (int p = 1; p < kFewParts; ++p) if (p < parts) top = fmaxf(top, stats[r][p].x);
@@ -796,26 +816,66 @@ __global__ __launch_bounds__(256) void combine_kernel(AttentionArgs g) {
         }
         return;
     }
-    for (int row = wave; row < rows; row += gridDim.y * 4) {
-        float top = -INFINITY;
-        for (int p = lane; p < parts; p += 64) top = fmaxf(top, g.partial_stats[at(row, p)].x);
-        for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-        const float base = top == -INFINITY ? 0.0f : top;
+    __shared__ float tops[4], weights[4];
+    __shared__ f32x4 sums[4][kLanes];
+    const int own = threadIdx.x >> 6;
+    for (int row = blockIdx.y; row < rows; row += gridDim.y) {
+        // (statistics and sums are asked for together, four parts a group at a time)
+        float top = -INFINITY, weight = 0.0f;
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-        float weight = 0.0f;
-#pragma unroll 4
-        for (int p = mine; p < parts; p += kGroups) {
-            const float2 stats = g.partial_stats[at(row, p)];
-            const float f = exp2_of(stats.x - base);
-            weight += f * stats.y;
-            sum += *reinterpret_cast<const f32x4*>(g.partial + at(row, p) * DP + column) * f;
+        for (int p = own * kGroups + mine; p < parts; p += 16 * kGroups) {
+            float2 stats[4];
+            f32x4 part[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t from = at(row, min(p + j * 4 * kGroups, parts - 1));
+                stats[j] = g.partial_stats[from];
+                part[j] = *reinterpret_cast<const f32x4*>(g.partial + from * DP + column);
+            }
+            float now = top;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (p + j * 4 * kGroups < parts) now = fmaxf(now, stats[j].x);
+            const float base = now == -INFINITY ? 0.0f : now, fade = exp2_of(top - base);
+            weight *= fade;
+            sum *= fade;
+            top = now;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (p + j * 4 * kGroups < parts) {
+                    const float f = exp2_of(stats[j].x - base);
+                    weight += f * stats[j].y;
+                    sum += part[j] * f;
+                }
         }
+        float now = top;
+        for (int d = kLanes; d < 64; d <<= 1) now = fmaxf(now, __shfl_xor(now, d));
+        const float fade = exp2_of(top - (now == -INFINITY ? 0.0f : now));
+        weight *= fade;
+        sum *= fade;
         for (int d = kLanes; d < 64; d <<= 1) {
             weight += __shfl_xor(weight, d);
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor(sum[i], d);
         }
-        if (mine == 0) put(row, sum, weight);
+        __syncthreads();
+        if (lane == 0) { tops[own] = now; weights[own] = weight; }
+        if (mine == 0) sums[own][lane] = sum;
+        __syncthreads();
+        if (own == 0 && mine == 0) {
+            float most = tops[0];
+#pragma unroll
+            for (int w = 1; w < 4; ++w) most = fmaxf(most, tops[w]);
+            const float base = most == -INFINITY ? 0.0f : most;
+            weight = 0.0f;
+            sum = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float f = exp2_of(tops[w] - base);
+                weight += weights[w] * f;
+                sum += sums[w][lane] * f;
+            }
+            put(row, sum, weight);
+        }
     }
 }
 
@@ -881,6 +941,10 @@ static int with_kernel(const mpv_attention* a, AttentionArgs* g, void* workspace
     char* at = static_cast<char*>(workspace);
     g->teams = c.teams;
     g->blocks = c.blocks;
+    g->by_unit = static_cast<int64_t>(a->B) * a->kv_heads < c.teams;
+    g->group = a->heads / a->kv_heads;
+    g->by_group.set(static_cast<uint32_t>(g->group));
+    g->by_page.set(static_cast<uint32_t>(a->page_size));
     g->partial_stats = reinterpret_cast<float2*>(at);
     g->split = reinterpret_cast<int4*>(at + stats);
     g->partial = reinterpret_cast<float*>(at + stats + split);
@@ -890,12 +954,14 @@ static int with_kernel(const mpv_attention* a, AttentionArgs* g, void* workspace
                                       static_cast<int>(sizeof(typename A::Shared)))))
         return MPV_ERR_HIP;
     hipLaunchKernelGGL(attention_kernel<A>, dim3(static_cast<unsigned>(c.teams) * c.blocks), dim3(A::kThreads), sizeof(typename A::Shared), s, *g);
-    // a list with one tile a unit shares none.  Few parts a unit: 16 groups of lanes' rows a workgroup; many: a row a wave, as long as
-    // there are not that many workgroups anyway.
-    constexpr int kCombined = 4 * 4 * (64 / (DP / 4));
-    const int64_t few = (rows + kCombined - 1) / kCombined, each = (rows + 3) / 4, most = 2048 / c.teams;
-    if (c.tiles > static_cast<int64_t>(a->B) * a->kv_heads)
-        hipLaunchKernelGGL((combine_kernel<DTYPE, DP, A::kRows>), dim3(static_cast<unsigned>(c.teams), static_cast<unsigned>(std::max(few, std::min(each, most)))), dim3(256), 0, s, *g);
+    // a list with one tile a unit shares none.  Few parts a unit: `some` rows a workgroup; many, which only units that are fewer than
+    // the teams can have: a row, up to 4096 workgroups.
+    constexpr int kSome = kFewRows * 4 * (64 / (DP / 4));
+    const int64_t units = static_cast<int64_t>(a->B) * a->kv_heads, few = (rows + kSome - 1) / kSome;
+    const int64_t entries = g->by_unit ? units : c.teams;
+    if (c.tiles > units)
+        hipLaunchKernelGGL((combine_kernel<DTYPE, DP, A::kRows>), dim3(static_cast<unsigned>(entries), static_cast<unsigned>(std::max(few, std::min(rows, 4096 / entries)))),
+                           dim3(256), 0, s, *g);
     return launched();
 }
 
