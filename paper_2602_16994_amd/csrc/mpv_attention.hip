@@ -136,6 +136,8 @@ __device__ __forceinline__ int fresh(int x) {
     asm volatile("" : "+v"(x));
     return x;
 }
+// What beginning and ending a unit takes, in tiles: workgroups with many short units would end last otherwise.
+constexpr int kUnitCost = 8;
 // All bits where bit `at` is set, none otherwise.  (Masks instead of conditions: those would all wait in scalar registers at once.)
 __device__ __forceinline__ uint32_t spread(uint32_t bits, int at) { return static_cast<uint32_t>(static_cast<int32_t>(bits << (31 - at)) >> 31); }
 
@@ -272,19 +274,23 @@ struct Attention {
         if (lane % kMyRows == 0) sh.special[half][sub][wave] = hidden || r.tree || differs(tile_at(tile + sub));
     }
 
-    // Asks for a tile whose places are known.  A key that nobody sees is read as zeros.
-    __device__ __forceinline__ void ask(int half, int sub, int stage) {
-        const uint32_t to = shared_at + stage * kTileBytes + wave * kMyLoads * 1024;
-        typedef __attribute__((ext_vector_type(2))) uint64_t u64x2;
-        u64x2 place[kMyLoads];
+    // Asks for a tile whose places are known: reads them, and later sends for the rows.  A key that nobody sees is read as zeros.
+    typedef __attribute__((ext_vector_type(2))) uint64_t u64x2;
+    struct Places { u64x2 of[kMyLoads]; };
+    __device__ __forceinline__ Places places(int half, int sub) const {
+        Places p;
 #pragma unroll
         for (int j = 0; j < kMyLoads; ++j)
-            place[j] = *reinterpret_cast<const u64x2*>(sh.place[half][sub][wave * kMyRows + j * kRowsPerLoad + lane / kChunks]);
+            p.of[j] = *reinterpret_cast<const u64x2*>(sh.place[half][sub][wave * kMyRows + j * kRowsPerLoad + lane / kChunks]);
+        return p;
+    }
+    __device__ __forceinline__ void ask(const Places& p, int stage) {
+        const uint32_t to = shared_at + stage * kTileBytes + wave * kMyLoads * 1024;
 #pragma unroll
         for (int j = 0; j < kMyLoads; ++j) {
             const int row = wave * kMyRows + j * kRowsPerLoad + lane / kChunks;
             const int chunk = (lane % kChunks) ^ swizzle(row);
-            uint64_t k = place[j][0] + chunk * 16, v = place[j][1] + chunk * 16;
+            uint64_t k = p.of[j][0] + chunk * 16, v = p.of[j][1] + chunk * 16;
             if (chunk * 16 >= g.a.head_dim * E::kBytes) k = v = reinterpret_cast<uint64_t>(&kZeros);
             to_lds(k, to + j * 1024);
             to_lds(v, to + STAGES * kTileBytes + j * 1024);
@@ -301,7 +307,7 @@ struct Attention {
 
     // ---- the rows of this lane's queries
     u32x4 query[QT][kSteps];
-    unsigned long long line[QT];                                   // the node and its ancestors
+    unsigned long long line[QT];                                   // the node and its ancestors, those that it sees
     int low[QT];                                                   // first position seen (but for the sinks)
     f32x4 out[QT][kColumns];
     float top[QT], base[QT];                                       // reference; what is added to an exponent
@@ -328,7 +334,19 @@ struct Attention {
             const int node = g.by_group.of(row);
             const bool real = node < t.nodes;
             line[q] = shfl64(mask, real ? node : 0);
-            low[q] = g.a.window > 0 ? t.context + __popcll(line[q]) - g.a.window : INT32_MIN;
+            low[q] = 0;
+            if (g.a.window > 0) {
+                const int depth = __popcll(line[q]) - 1, first = depth + 1 - g.a.window;
+                low[q] = t.context + first;
+                // ancestors before the window that are no sinks are not seen: those from the `sinks - context`-th to the `first`-th
+                if (first > 0) {
+                    unsigned long long rest = line[q];
+                    for (int d = 0; d < first; ++d) {
+                        if (t.context + d >= g.a.sinks) line[q] &= ~(rest & -rest);
+                        rest &= rest - 1;
+                    }
+                }
+            }
             const char* from = static_cast<const char*>(g.b.q) +
                 ((static_cast<int64_t>(b) * g.a.N + node) * g.a.q_stride + static_cast<int64_t>(kv * group + row - node * group) * g.a.head_dim) * E::kBytes;
 #pragma unroll
@@ -347,23 +365,31 @@ struct Attention {
         }
     }
 
-    // A tile in LDS: products, weights, and their sum over the values.
-    __device__ __forceinline__ void work(const Tile& x, int half, int sub, int stage) {
+    // ---- a tile in LDS: products, weights, and their sum over the values.
+    // Operands of the products are read kAhead instructions before their use, which the order of the source alone does not bring about.
+    static constexpr int kAhead = 4;
+    struct First { u32x4 keys[kAhead]; unsigned long long special; };
+    __device__ __forceinline__ u32x4 read_key(const char* keys, int n) const {
+        const int k = n / kSteps, d = n % kSteps;
+        return *reinterpret_cast<const u32x4*>(keys + ((k * 16 + l16) * kChunks + ((d * 4 + quad) ^ swizzle(l16))) * 16);
+    }
+    __device__ __forceinline__ First read_first(int half, int sub, int stage) const {
+        constexpr unsigned long long kBytesOfWaves = WAVES == 8 ? ~0ull : (1ull << (8 * (WAVES % 8))) - 1;
+        First f;
+#pragma unroll
+        for (int n = 0; n < kAhead; ++n) f.keys[n] = read_key(sh.keys[stage], n);
+        f.special = *reinterpret_cast<const unsigned long long*>(sh.special[half][sub]) & kBytesOfWaves;
+        return f;
+    }
+    __device__ __forceinline__ void work(int index, int half, int sub, int stage, const First& f) {
         const char* keys = sh.keys[stage];
         char* values = sh.values[stage];
-        constexpr unsigned long long kBytesOfWaves = WAVES == 8 ? ~0ull : (1ull << (8 * (WAVES % 8))) - 1;
-        const bool special = uniform64(*reinterpret_cast<const unsigned long long*>(sh.special[half][sub]) & kBytesOfWaves) != 0;
         f32x4 s[QT][kGroups];
-        const int key_swizzle = swizzle(l16);
-        // (operands are read kAhead instructions before their use, which the order of the source alone does not bring about)
-        constexpr int kAhead = 4, kFirst = kGroups * kSteps;
+        constexpr int kFirst = kGroups * kSteps;
         u32x4 a[kAhead];
-        auto read_key = [&](int n) {
-            const int k = n / kSteps, d = n % kSteps;
-            return *reinterpret_cast<const u32x4*>(keys + ((k * 16 + l16) * kChunks + ((d * 4 + quad) ^ key_swizzle)) * 16);
-        };
 #pragma unroll
-        for (int n = 0; n < kAhead; ++n) a[n] = read_key(n);
+        for (int n = 0; n < kAhead; ++n) a[n] = f.keys[n];
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int n = 0; n < kFirst; ++n) {
             const int k = n / kSteps, d = n % kSteps;
@@ -379,20 +405,23 @@ struct Attention {
                     for (int i = 0; i < 4; ++i) s[q][k] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[i], fq[i], s[q][k], 0, 0, 0);
                 }
             }
-            if (n + kAhead < kFirst) a[n % kAhead] = read_key(n + kAhead);
+            if (n + kAhead < kFirst) a[n % kAhead] = read_key(keys, n + kAhead);
         }
         __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(0);
         // ---- what is not seen
-        if (special) {
+        if (uniform64(f.special) != 0) {
+            const Tile x = tile_at(index);
 #pragma unroll
             for (int q = 0; q < QT; ++q) {
                 const int quad = fresh(lane) >> 4;
                 uint32_t bits = 0;                                 // of this lane's keys, those that its query sees
+#pragma unroll
                 for (int k = 0; k < kGroups; ++k) {
                     const int key = k * 16 + quad * 4;
-                    const uint32_t there = *reinterpret_cast<const uint32_t*>(&sh.seen[half][sub][key]);
-#pragma unroll 1
-                    for (int i = 0; i < 4; ++i) bits |= static_cast<uint32_t>((there >> (8 * i) & 1) && sees(x, key + i, q)) << (k * 4 + i);
+                    uint32_t there = *reinterpret_cast<const uint32_t*>(&sh.seen[half][sub][key]);      // a byte each, 0 or 1
+                    there = (there | there >> 7 | there >> 14 | there >> 21) & 15u;
+                    bits |= (there & sees4(x, key, q)) << (k * 4);
                 }
 #pragma unroll
                 for (int k = 0; k < kGroups; ++k)
@@ -456,6 +485,7 @@ struct Attention {
                 for (int k = 0; k < kGroups / 2; ++k) weight[q] = E::mfma(u32x4{E::kOnes, E::kOnes, E::kOnes, E::kOnes}, w16[q][k], weight[q]);
         }
         // ---- their sum over the values
+        __builtin_amdgcn_s_setprio(1);
         if constexpr (k16) {
             constexpr int kSecond = kColumns * (kGroups / 2);
 #pragma unroll
@@ -488,6 +518,7 @@ struct Attention {
             }
             __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_s_setprio(0);
     }
 
     // Keys 32 k + 4 quad .. + 3 and 32 k + 16 + 4 quad .. + 3 of column 16 c + l16.
@@ -514,6 +545,7 @@ struct Attention {
         bool fine = true;
         if constexpr (k16) {
             u16x2 most = {0, 0};
+#pragma unroll 4
             for (int i = fresh(lane); i < TILE * kChunks; i += 64) {
                 const u32x4 v = *reinterpret_cast<const u32x4*>(values + i * 16) & 0x7fff7fffu;
 #pragma unroll
@@ -522,6 +554,7 @@ struct Attention {
             fine = most[0] < E::kInf && most[1] < E::kInf;
         } else {
             uint32_t most = 0;
+#pragma unroll 4
             for (int i = fresh(lane); i < TILE * kChunks; i += 64) {
                 const u32x4 v = *reinterpret_cast<const u32x4*>(values + i * 16) & 0x7fffffffu;
 #pragma unroll
@@ -561,11 +594,12 @@ struct Attention {
     __device__ __forceinline__ bool differs(const Tile& x) const {
         return t.nodes > 1 && (x.tree || (g.a.window > 0 && x.base < t.context + t.nodes - g.a.window && x.base + TILE > g.a.sinks));
     }
-    __device__ __forceinline__ bool sees(const Tile& x, int key, int q) const {
-        const int at = x.base + key, node = at & 63;
-        const int place = x.tree ? t.context + __popcll(line[q] & ((1ull << node) - 1)) : at;
-        const int near = static_cast<int>(place >= low[q]) | static_cast<int>(place < g.a.sinks);
-        return near & (x.tree ? static_cast<int>(line[q] >> node & 1) : 1);
+    // Which of the four keys from `key` on the lane's query q sees, as far as tree, window and sinks say.
+    __device__ __forceinline__ uint32_t sees4(const Tile& x, int key, int q) const {
+        const int at = x.base + key;
+        if (x.tree) return static_cast<uint32_t>(line[q] >> (at & 63)) & 15u;
+        const int before = min(max(low[q] - at, 0), 4), sinks = min(max(g.a.sinks - at, 0), 4);
+        return (15u << before & 15u) | ((1u << sinks) - 1);
     }
 
     // A tile whose nodes see different keys held values that are no numbers: they were left out of the sums, and the rows that see
@@ -579,14 +613,14 @@ struct Attention {
             ask_pages(i, i + 1);
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             look_up(i, i + 1, 0);
-            ask(0, 0, 0);
+            ask(places(0, 0), 0);
             arrive(false);
             const char* values = sh.values[0];
 #pragma unroll
             for (int q = 0; q < QT; ++q) {
                 uint32_t up[4] = {}, down[4] = {};                 // by column group: an infinity of either sign is seen (NaN: both)
                 for (int key = 0; key < TILE; ++key) {
-                    if (!sh.seen[0][0][key] || !sees(x, key, q)) continue;
+                    if (!sh.seen[0][0][key] || !(sees4(x, key, q) & 1)) continue;
                     for (int c = 0; c < kColumns; ++c)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
@@ -624,9 +658,13 @@ struct Attention {
                     look_up(first + n, last, half);
                     if (n + kBatch < count) ask_pages(first + n + kBatch, last);
                 }
-                ask(half, sub, n % STAGES);
             }
-            if (mine >= 0) work(tile_at(first + mine), mine / kBatch & 1, mine % kBatch, mine % STAGES);
+            // (what is read of LDS first is asked for at once, needed or not)
+            const unsigned past = static_cast<unsigned>(mine + 2 * kBatch * STAGES);
+            const Places p = places(n / kBatch & 1, n % kBatch);
+            const First f = read_first(past / kBatch & 1, past % kBatch, past % STAGES);
+            if (n < count) ask(p, n % STAGES);
+            if (mine >= 0) work(first + mine, past / kBatch & 1, past % kBatch, past % STAGES, f);
         }
         __syncthreads();
         if (__builtin_amdgcn_readfirstlane(sh.spoiled)) spoil(first, last);
@@ -680,10 +718,13 @@ struct Attention {
         return v;
     }
 
-    __device__ __forceinline__ int64_t tiles_of(int tree) const {
-        if (tree >= g.a.B) return 0;
+    // A tree's tiles and units.
+    struct Count { int64_t tiles; int units; };
+    __device__ __forceinline__ Count count_of(int tree) const {
+        if (tree >= g.a.B) return {0, 0};
         const TreeWork w = tree_work<TILE, kRows>(g, tree);
-        return w.nodes > 0 ? static_cast<int64_t>(w.tiles) * g.a.kv_heads : 0;
+        if (w.nodes == 0) return {0, 0};
+        return {static_cast<int64_t>(w.tiles) * g.a.kv_heads, g.a.kv_heads};
     }
 
     __device__ __forceinline__ void all() {
@@ -692,12 +733,21 @@ struct Attention {
         const int member = place % g.blocks, team = most % 8 == 0 ? (blockIdx.x % 8) * (most / 8) + place / g.blocks : place / g.blocks;
         // every wave adds the trees' tiles up for itself, 64 trees at a time
         const int trees = g.a.B;
-        int64_t mine = tiles_of(lane), total = mine;
-        for (int base = 64; base < trees; base += 64) total += tiles_of(base + lane);
-        int64_t upto = wave_scan(mine);
-        if (trees > 64) total = wave_scan(total); else total = upto;
-        total = uniform64(shfl64(total, 63));
-        const int T = static_cast<int>(min(static_cast<int64_t>(most), total));      // every team has a tile at least
+        Count mine = count_of(lane);
+        int64_t tiles = mine.tiles, units = mine.units;
+        for (int base = 64; base < trees; base += 64) {
+            const Count c = count_of(base + lane);
+            tiles += c.tiles;
+            units += c.units;
+        }
+        for (int d = 32; d; d >>= 1) {
+            tiles += static_cast<int64_t>(shfl64(static_cast<unsigned long long>(tiles), lane ^ d));
+            units += static_cast<int64_t>(shfl64(static_cast<unsigned long long>(units), lane ^ d));
+        }
+        // a unit counts as `extra` tiles more than it has, all of them before its first
+        const int extra = static_cast<int>(min(static_cast<int64_t>(kUnitCost), uniform64(tiles) / (2 * most)));
+        const int64_t total = uniform64(tiles) + extra * uniform64(units);
+        const int T = static_cast<int>(min(static_cast<int64_t>(most), total));
         if (member == 0 && threadIdx.x == 0 && !g.by_unit) g.split[team] = make_int4(-1, 0, 0, 0);
         if (team >= T) return;
         // the first `longer` teams have one tile more than the others
@@ -708,34 +758,35 @@ struct Attention {
         int64_t start = 0;
         b = 0;
         for (int base = 0;;) {
-            const int64_t chunk = uniform64(shfl64(upto, 63));
+            const int64_t weight = mine.tiles + extra * mine.units, upto = wave_scan(weight), chunk = uniform64(shfl64(upto, 63));
             if (begin_at < start + chunk) {
                 const int l = __ffsll(static_cast<unsigned long long>(__ballot(begin_at < start + upto))) - 1;
-                start += uniform64(shfl64(upto - mine, l));
+                start += uniform64(shfl64(upto - weight, l));
                 b = __builtin_amdgcn_readfirstlane(base + l);
                 break;
             }
             start += chunk;
             base += 64;
-            mine = tiles_of(base + lane);
-            upto = wave_scan(mine);
+            mine = count_of(base + lane);
         }
         int64_t at = begin_at;
         for (; at < end_at; ++b) {
             t = tree_work<TILE, kRows>(g, b);
             if (t.nodes == 0) continue;
-            const int64_t tree_end = start + static_cast<int64_t>(t.tiles) * g.a.kv_heads;
+            const int length = t.tiles + extra;
+            const int64_t tree_end = start + static_cast<int64_t>(length) * g.a.kv_heads;
             while (at < min(end_at, tree_end)) {
                 // (the tiles of a tree's heads may be more than 32 bits hold, but hardly ever are)
                 const int64_t into = at - start;
-                kv = static_cast<int>(into <= UINT32_MAX ? static_cast<uint32_t>(into) / static_cast<uint32_t>(t.tiles) : into / t.tiles);
-                const int64_t unit = start + static_cast<int64_t>(kv) * t.tiles;
-                const int first = static_cast<int>(at - unit);
-                const int last = static_cast<int>(min(static_cast<int64_t>(t.tiles), end_at - unit));
-                at = unit + last;
+                kv = static_cast<int>(into <= UINT32_MAX ? static_cast<uint32_t>(into) / static_cast<uint32_t>(length) : into / length);
+                const int64_t unit = start + static_cast<int64_t>(kv) * length;
+                const int first = max(static_cast<int>(at - unit) - extra, 0);
+                const int last = static_cast<int>(min(static_cast<int64_t>(length), end_at - unit)) - extra;
+                at = min(unit + length, end_at);
                 const bool shared = first > 0 || last < t.tiles;
+                if (last <= first) continue;
                 if (member == 0 && first == 0 && threadIdx.x == 0 && (shared || g.by_unit)) {
-                    const int64_t x = unit + t.tiles - 1, ahead = longer * (share + 1);      // the unit's last tile, and whose it is
+                    const int64_t x = unit + length - 1, ahead = longer * (share + 1);       // the unit's last tile, and whose it is
                     const int64_t whose = x < ahead ? x / (share + 1) : longer + (x - ahead) / share;
                     g.split[g.by_unit ? b * g.a.kv_heads + kv : team] = make_int4(shared ? b : -1, kv, team, static_cast<int>(whose));
                 }
@@ -1040,6 +1091,7 @@ int mpv_tree_attention(const mpv_attention* attention, const mpv_attention_buffe
     if (!buf) return MPV_ERR_NULL;
     mpv::AttentionArgs g;
     g.a = *attention; g.b = *buf;
+    g.a.sinks = attention->sinks > 0 ? attention->sinks : 0;
     g.sign = attention->scale > 0.0f ? 1 : attention->scale < 0.0f ? -1 : 0;
     g.factor = g.sign ? static_cast<float>(std::fabs(static_cast<double>(attention->scale)) * 1.4426950408889634) : 1.0f;
     if (!buf->tree_parent) {
