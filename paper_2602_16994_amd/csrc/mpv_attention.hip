@@ -199,7 +199,7 @@ struct Attention {
         __align__(16) int pages[WAVES][64];                        // entries of the block table, a lane's each
         __align__(4) uint8_t seen[2][kBatch][TILE];                // whether anybody sees the key
         __align__(8) uint8_t special[2][kBatch][8];                // whether a wave found a key that not every node sees
-        int spoiled;                                               // whether a tile held values that are no numbers, see spoil
+        int spoiled;                                               // whether a sum is no number, see run
     };
 
     // A tile: positions of the cache from `base` on, or nodes.
@@ -381,7 +381,7 @@ struct Attention {
         f.special = *reinterpret_cast<const unsigned long long*>(sh.special[half][sub]) & kBytesOfWaves;
         return f;
     }
-    __device__ __forceinline__ void work(int index, int half, int sub, int stage, const First& f) {
+    __device__ __forceinline__ void work(int index, int half, int sub, int stage, const First& f, bool careful) {
         const char* keys = sh.keys[stage];
         char* values = sh.values[stage];
         f32x4 s[QT][kGroups];
@@ -432,10 +432,7 @@ struct Attention {
                     }
             }
             // a value that is no number must not reach the nodes that do not see it
-            if (differs(x) && !all_numbers(values)) {
-                only_numbers(values);
-                sh.spoiled = 1;
-            }
+            if (careful && differs(x) && !all_numbers(values)) only_numbers(values);
         }
         // ---- references
 #pragma unroll
@@ -602,8 +599,8 @@ struct Attention {
         return (15u << before & 15u) | ((1u << sinks) - 1);
     }
 
-    // A tile whose nodes see different keys held values that are no numbers: they were left out of the sums, and the rows that see
-    // them get them now.  The tiles in question are brought in again.
+    // Where the nodes of a tree see different keys, values that are no numbers were left out of the sums: the rows that see them get
+    // them now.  The tiles in question are brought in again.
     __device__ __forceinline__ void spoil(int first, int last) {
         const int quad = fresh(lane) >> 4;
         for (int i = first; i < last; ++i) {
@@ -640,35 +637,53 @@ struct Attention {
         }
     }
 
-    // The unit's part [first, last) of its tiles.
+    // The unit's part [first, last) of its tiles.  A value that is no number spoils the sums of all nodes, those that do not see it
+    // too (their weights of it are 0).  Nobody looks for one; but if a sum is no number in the end, all is done again, with care.
     __device__ __forceinline__ void run(int block, int first, int last) {
-        if (threadIdx.x == 0) sh.spoiled = 0;                      // (read by all before the last barrier of the unit before)
-        ask_pages(first, last);
-        begin(block);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        // turn n asks for tile first + n and works on the tile kAheadTiles before it
         const int count = last - first;
+        bool careful = false;
+        for (;; careful = true) {
+            if (threadIdx.x == 0) sh.spoiled = 0;                  // (read by all before the last barrier)
+            ask_pages(first, last);
+            begin(block);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            // turn n asks for tile first + n and works on the tile kAheadTiles before it
 #pragma unroll 1
-        for (int n = 0; n < count + kAheadTiles; ++n) {
-            const int mine = n - kAheadTiles;
-            if (mine >= 0) arrive(n <= count);
-            if (n < count) {
-                const int sub = n % kBatch, half = n / kBatch & 1;
-                if (sub == 0) {
-                    look_up(first + n, last, half);
-                    if (n + kBatch < count) ask_pages(first + n + kBatch, last);
+            for (int n = 0; n < count + kAheadTiles; ++n) {
+                const int mine = n - kAheadTiles;
+                if (mine >= 0) arrive(n <= count);
+                if (n < count) {
+                    const int sub = n % kBatch, half = n / kBatch & 1;
+                    if (sub == 0) {
+                        look_up(first + n, last, half);
+                        if (n + kBatch < count) ask_pages(first + n + kBatch, last);
+                    }
                 }
+                // (what is read of LDS first is asked for at once, needed or not)
+                const unsigned past = static_cast<unsigned>(mine + 2 * kBatch * STAGES);
+                const Places p = places(n / kBatch & 1, n % kBatch);
+                const First f = read_first(past / kBatch & 1, past % kBatch, past % STAGES);
+                if (n < count) ask(p, n % STAGES);
+                if (mine >= 0) work(first + mine, past / kBatch & 1, past % kBatch, past % STAGES, f, careful);
             }
-            // (what is read of LDS first is asked for at once, needed or not)
-            const unsigned past = static_cast<unsigned>(mine + 2 * kBatch * STAGES);
-            const Places p = places(n / kBatch & 1, n % kBatch);
-            const First f = read_first(past / kBatch & 1, past % kBatch, past % STAGES);
-            if (n < count) ask(p, n % STAGES);
-            if (mine >= 0) work(first + mine, past / kBatch & 1, past % kBatch, past % STAGES, f);
+            if (careful || t.nodes == 1) break;
+            // a spoiled column is spoiled in every row, so one group of rows will do
+            float zero = 0.0f;
+#pragma unroll
+            for (int c = 0; c < kColumns; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) zero = fmaf(out[0][c][i], 0.0f, zero);
+            if (__ballot(zero != 0.0f) && lane == 0) sh.spoiled = 1;
+            __syncthreads();
+            const bool again = __builtin_amdgcn_readfirstlane(sh.spoiled) != 0;
+            __syncthreads();
+            if (!again) break;
         }
         __syncthreads();
-        if (__builtin_amdgcn_readfirstlane(sh.spoiled)) spoil(first, last);
-        __syncthreads();
+        if (careful) {
+            spoil(first, last);
+            __syncthreads();
+        }
         // ---- the lanes that share rows put their sums together
         if constexpr (!k16)
 #pragma unroll
@@ -678,21 +693,36 @@ struct Attention {
             }
     }
 
-    // Whole rows of the output.
+    // Rows of the output, 16 at a time: through the part of LDS that only this wave's loads fill (whole rows of its keys and values in
+    // each stage), from where a row leaves in one piece.  (Written from the registers, 8 bytes a lane, it took 6 us a unit.)
+    __device__ __forceinline__ char* own_row(int row) const {
+        const int piece = row / kMyRows;
+        static_assert(16 / kMyRows <= 2 * STAGES, "room for 16 rows");
+        char* at = piece < STAGES ? sh.keys[piece] : sh.values[piece - STAGES];
+        return at + (wave * kMyRows + row % kMyRows) * kChunks * 16;
+    }
     __device__ __forceinline__ void finish(int block) {
         const int lane = fresh(this->lane), l16 = lane & 15, quad = lane >> 4;
         const int group = g.group;
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
-            const int row = block * kRows + (wave * QT + q) * 16 + l16;
-            const int node = g.by_group.of(row);
-            if (node >= t.nodes) continue;
             const float whole = 1.0f / weight[q][0];
-            char* to = static_cast<char*>(g.b.out) +
-                ((static_cast<int64_t>(b) * g.a.N + node) * g.a.out_stride + static_cast<int64_t>(kv * group + row - node * group) * g.a.head_dim) * E::kBytes;
+            char* mine = own_row(l16);
 #pragma unroll
-            for (int c = 0; c < kColumns; ++c)
-                if (c * 16 + quad * 4 < g.a.head_dim) E::put4(to + (c * 16 + quad * 4) * E::kBytes, out[q][c] * whole);
+            for (int c = 0; c < kColumns; ++c) {
+                const int byte = (c * 16 + quad * 4) * E::kBytes;
+                E::put4(mine + ((byte / 16) ^ swizzle(l16)) * 16 + byte % 16, out[q][c] * whole);
+            }
+#pragma unroll
+            for (int j = 0; j < 16 / kRowsPerLoad; ++j) {
+                const int local = j * kRowsPerLoad + lane / kChunks, chunk = lane % kChunks;
+                const u32x4 v = *reinterpret_cast<const u32x4*>(own_row(local) + (chunk ^ swizzle(local)) * 16);
+                const int row = block * kRows + (wave * QT + q) * 16 + local;
+                const int node = g.by_group.of(row);
+                char* to = static_cast<char*>(g.b.out) +
+                    ((static_cast<int64_t>(b) * g.a.N + node) * g.a.out_stride + static_cast<int64_t>(kv * group + row - node * group) * g.a.head_dim) * E::kBytes;
+                if (node < t.nodes && chunk * 16 < g.a.head_dim * E::kBytes) *reinterpret_cast<u32x4*>(to + chunk * 16) = v;
+            }
         }
     }
 
