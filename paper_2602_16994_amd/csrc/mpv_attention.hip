@@ -499,9 +499,11 @@ struct Attention {
         } else {
             constexpr int kSecond = kColumns * kGroups * 4, kAhead32 = 8;
             float v[kAhead32];
+            // (the places of a lane's values differ in every column and row: they are worked out again for every tile, beside the products)
+            const int lane = fresh(this->lane), l16 = lane & 15, quad = lane >> 4;
             auto read_value = [&](int n) {
-                const int i = n % 4, k = n / 4 % kGroups, c = n / (4 * kGroups);
-                return column32(values, k * 16 + quad * 4 + i, c);
+                const int i = n % 4, k = n / 4 % kGroups, c = n / (4 * kGroups), row = k * 16 + quad * 4 + i;
+                return *reinterpret_cast<const float*>(values + (row * kChunks + ((c * 4 + (l16 >> 2)) ^ swizzle(row))) * 16 + (l16 & 3) * 4);
             };
 #pragma unroll
             for (int n = 0; n < kAhead32; ++n) v[n] = read_value(n);
@@ -533,10 +535,6 @@ struct Attention {
         }
         return v;
     }
-    __device__ __forceinline__ float column32(const char* values, int row, int c) const {
-        return *reinterpret_cast<const float*>(values + (row * kChunks + ((c * 4 + (l16 >> 2)) ^ swizzle(row))) * 16 + (l16 & 3) * 4);
-    }
-
     __device__ __forceinline__ bool all_numbers(const char* values) const {
         typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
         bool fine = true;
@@ -1135,7 +1133,7 @@ int mpv_tree_attention(const mpv_attention* attention, const mpv_attention_buffe
     }
     if (attention->B == 0) return MPV_OK;
     if (!buf->q || !buf->tree_k || !buf->tree_v || !buf->context_len || !buf->out ||
-        (attention->table_width > 0 && (!buf->block_table || !buf->cache_k || !buf->cache_v)))
+        (attention->table_width > 0 && (!buf->block_table || (attention->num_pages > 0 && (!buf->cache_k || !buf->cache_v)))))
         return MPV_ERR_NULL;
     if (!mpv::aligned(buf->q, 16) || !mpv::aligned(buf->tree_k, 16) || !mpv::aligned(buf->tree_v, 16) || !mpv::aligned(buf->cache_k, 16) ||
         !mpv::aligned(buf->cache_v, 16) || !mpv::aligned(buf->out, 16))

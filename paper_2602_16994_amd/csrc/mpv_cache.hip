@@ -296,7 +296,7 @@ int mpv_append_paths(const mpv_append* p, const mpv_append_buffers* buf, void* h
         p->page_stride < 0)
         return MPV_ERR_BAD_SHAPE;
     const int64_t layers = (p->layers + mpv::kAppendLayers - 1) / mpv::kAppendLayers;
-    if (layers > 65535 || static_cast<int64_t>(p->B) * a.rows > INT32_MAX || mpv::span(0, p->num_pages, p->page_size) == INT64_MAX ||
+    if (layers > 65535 || static_cast<int64_t>(p->B) * a.rows >= (1 << 24) || mpv::span(0, p->num_pages, p->page_size) == INT64_MAX ||
         mpv::span(0, mpv::span(mpv::span(0, p->layers, p->tree_layer_stride), static_cast<int64_t>(p->B) * p->N, p->tree_stride), 4) == INT64_MAX ||
         mpv::span(0, mpv::span(mpv::span(mpv::span(0, p->layers, p->cache_layer_stride), p->num_pages, p->page_stride), p->page_size, p->slot_stride), 4) == INT64_MAX)
         return MPV_ERR_UNSUPPORTED;

@@ -377,7 +377,7 @@ static int check_chains(const mpv_chains* c) {
     if (!c) return MPV_ERR_NULL;
     if (c->B < 0 || c->N < 1 || c->V < 1 || c->max_depth < 1 || c->max_depth < c->N - 1) return MPV_ERR_BAD_SHAPE;
     if (!known_dtype(c->dtype)) return MPV_ERR_BAD_DTYPE;
-    if (c->N > MPV_MAX_NODES || c->V > MPV_MAX_VOCAB || c->B > (1 << 24) || c->max_depth > (1 << 20)) return MPV_ERR_UNSUPPORTED;
+    if (c->N > MPV_MAX_NODES || c->V > MPV_MAX_VOCAB || c->B > (1 << 21) || c->max_depth > (1 << 20)) return MPV_ERR_UNSUPPORTED;
     if (c->target_stride < c->V || c->draft_stride < 0) return MPV_ERR_BAD_SHAPE;
     const int64_t rows = static_cast<int64_t>(c->B) * c->N;
     if (span(0, span(0, rows, c->target_stride), 4) == INT64_MAX || span(0, span(0, rows, c->draft_stride), 4) == INT64_MAX) return MPV_ERR_UNSUPPORTED;

@@ -283,3 +283,86 @@ def test_a_cache_whose_offsets_pass_32_bits():
                                   torch.tensor([[0, 1, 2]], dtype=torch.int32, device="cuda"), context).out
     torch.cuda.synchronize()
     assert torch.equal(far, near)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("N,H,KV", [(5, 3, 1), (10, 3, 1), (20, 3, 1), (33, 3, 1), (52, 3, 1), (43, 9, 1)])
+def test_numbers_of_rows(N, H, KV, D, dtype):
+    """15, 30, 60, 99, 156 and 387 rows a cache head, none of them a whole number of 16: every number of waves and of blocks."""
+    print("[case] rows", N, H, KV, D, dtype, flush=True)
+    rng = np.random.default_rng(N)
+    parent = [-1] + [int(rng.integers(max(0, n - 4), n)) for n in range(1, N)]
+    Case(2, parent, H, KV, D, dtype, [150, 77], 16, window=100, sinks=2, seed=N + D).check()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("B,KV", [(70, 1), (150, 8), (333, 2)])
+def test_many_trees(B, KV, dtype):
+    """More trees than a wave has lanes, more units than there are workgroups; empty trees among them."""
+    print("[case] many trees", B, KV, dtype, flush=True)
+    rng = np.random.default_rng(B)
+    context = rng.integers(0, 90, B).tolist()
+    context[B // 2] = 1500
+    nodes = rng.integers(0, 4, B).tolist()
+    case = Case(B, CHAIN3, KV, KV, 32, dtype, context, 16, nodes=nodes, seed=B)
+    case.out = mpv.TreeAttentionResult(out=torch.full_like(case.q, 7.0))
+    got = case.check(case.run(out=case.out).out)
+    for b, n in enumerate(nodes):
+        assert (got[b, n:] == 7.0).all()
+
+
+def test_no_tree_has_a_node():
+    print("[case] all empty", flush=True)
+    case = Case(5, CHAIN3, 4, 2, 64, torch.bfloat16, [90, 0, 3, 64, 700], 16, nodes=[0, 0, -1, 0, 0], seed=22)
+    out = mpv.TreeAttentionResult(out=torch.full_like(case.q, 7.0))
+    assert (case.run(out=out).out == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1.0])
+def test_scales(scale, dtype):
+    print("[case] scale", scale, dtype, flush=True)
+    Case(2, TREE7, 4, 2, 64, dtype, [300, 40], 16, seed=23, scale=scale, gain=0.3).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("fill", [float("nan"), float("inf"), -float("inf")])
+def test_what_all_see_reaches_all(dtype, fill):
+    """A value in the context that is no number spoils its column in every node of its tree, and nothing else."""
+    print("[case] seen by all", dtype, fill, flush=True)
+    case = Case(2, TREE7, 4, 2, 64, dtype, [500, 90], 16, seed=24)
+    clean = case.run().out.clone()
+    case.cv[case.table[0, 3], 5, 1, 9] = fill
+    got = case.run().out
+    spoiled = torch.zeros_like(got, dtype=torch.bool)
+    spoiled[0, :, 2:, 9] = True
+    assert torch.equal(got[~spoiled], clean[~spoiled])
+    assert not torch.isfinite(got[spoiled]).any() and (fill == fill or torch.isnan(got[spoiled]).all())
+
+
+def test_a_key_of_minus_infinity_has_no_weight():
+    print("[case] infinite key", flush=True)
+    case = Case(1, TREE7, 2, 2, 64, torch.float32, [70], 16, seed=25)
+    case.q.abs_()
+    case.tk[0, 1] = -float("inf")                 # its products are -inf: seen by nodes 1, 2 and 3, without weight
+    got = case.run().out.clone()
+    assert torch.isfinite(got).all()
+    case.tv[0, 1] += 5.0
+    assert torch.equal(case.run().out, got)
+
+
+def test_pages_of_one_slot_and_of_many():
+    """The same context in pages of other sizes: the same results, bit by bit."""
+    print("[case] page sizes", flush=True)
+    first = Case(1, TREE7, 4, 2, 64, torch.bfloat16, [900], 1, seed=26)
+    k, v = torch.randn(2, 900, 2, 64, device="cuda").to(torch.bfloat16)
+    at = torch.arange(900, device="cuda")
+    outs = []
+    for page in (1, 3, 16, 1000):
+        case = Case(1, TREE7, 4, 2, 64, torch.bfloat16, [900], page, seed=26)
+        case.q, case.tk, case.tv = first.q, first.tk, first.tv
+        case.ck[case.table[0, at // page].long(), at % page] = k
+        case.cv[case.table[0, at // page].long(), at % page] = v
+        outs.append(case.run().out)
+    assert all(torch.equal(o, outs[0]) for o in outs)
