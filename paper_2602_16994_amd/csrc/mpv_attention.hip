@@ -27,24 +27,6 @@
 
 namespace mpv {
 
-// Division of numbers below 2^31 by one that the host knows (Granlund and Montgomery, Division by invariant integers using
-// multiplication, 1994, figure 4.1).
-struct Divisor {
-    uint32_t d, factor, shift1, shift2;
-    __host__ void set(uint32_t by) {
-        int log = 0;
-        while ((1ull << log) < by) ++log;
-        d = by;
-        factor = static_cast<uint32_t>(((1ull << 32) * ((1ull << log) - by)) / by + 1);
-        shift1 = log < 1 ? log : 1;
-        shift2 = log < 1 ? 0 : log - 1;
-    }
-    __device__ __forceinline__ int of(int n) const {
-        const uint32_t x = static_cast<uint32_t>(n), high = __umulhi(factor, x);
-        return static_cast<int>((high + ((x - high) >> shift1)) >> shift2);
-    }
-};
-
 struct AttentionArgs {
     mpv_attention a;
     mpv_attention_buffers b;

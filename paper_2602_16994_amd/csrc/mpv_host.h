@@ -1,4 +1,4 @@
-// Host-side helpers shared by the translation units of the library.
+// Helpers shared by the translation units of the library.
 
 #pragma once
 
@@ -31,5 +31,23 @@ inline int64_t span(int64_t a, int64_t b, int64_t c) {
     if (__builtin_mul_overflow(b, c, &r) || __builtin_add_overflow(a, r, &r)) return INT64_MAX;
     return r;
 }
+
+// Division of numbers below 2^31 by one that the host knows (Granlund and Montgomery, Division by invariant integers using
+// multiplication, 1994, figure 4.1).
+struct Divisor {
+    uint32_t d, factor, shift1, shift2;
+    __host__ void set(uint32_t by) {
+        int log = 0;
+        while ((1ull << log) < by) ++log;
+        d = by;
+        factor = static_cast<uint32_t>(((1ull << 32) * ((1ull << log) - by)) / by + 1);
+        shift1 = log < 1 ? log : 1;
+        shift2 = log < 1 ? 0 : log - 1;
+    }
+    __device__ __forceinline__ int of(int n) const {
+        const uint32_t x = static_cast<uint32_t>(n), high = __umulhi(factor, x);
+        return static_cast<int>((high + ((x - high) >> shift1)) >> shift2);
+    }
+};
 
 }  // namespace mpv
