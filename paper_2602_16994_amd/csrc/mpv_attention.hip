@@ -94,13 +94,15 @@ __device__ const uint4 kZeros[MPV_MAX_HEAD_DIM * 4 / 16] = {};
 
 // 16 bytes a lane to LDS, from `to` on (the wave's first lane's place) in lane order.  Written as an instruction: the compiler would
 // wait for all such loads in flight before it reads LDS through ds_read_b64_tr_b16, the next tile's among them.  Nothing but `arrive`
-// waits for them.
+// waits for them.  (A load that goes to LDS may follow a write of m0 after one wait state.)
 __device__ __forceinline__ void to_lds(uint64_t from, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
 }
 __device__ __forceinline__ void word_to_lds(uint64_t from, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory");
 }
+// What a wave's lanes wrote to LDS is there for its other lanes (LDS serves a wave in order; the compiler must keep that order).
+__device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local"); }
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ unsigned long long shfl64(unsigned long long v, int lane) {
     const uint32_t lo = __shfl(static_cast<uint32_t>(v), lane), hi = __shfl(static_cast<uint32_t>(v >> 32), lane);
@@ -254,6 +256,7 @@ struct Attention {
         const unsigned long long mask = kMyRows == 64 ? ~0ull : (1ull << (kMyRows % 64)) - 1;
         const bool hidden = (__ballot(!r.seen) >> (sub * kMyRows % 64) & mask) != 0;
         if (lane % kMyRows == 0) sh.special[half][sub][wave] = hidden || r.tree || differs(tile_at(tile + sub));
+        wave_order();
     }
 
     // Asks for a tile whose places are known: reads them, and later sends for the rows.  A key that nobody sees is read as zeros.
@@ -441,12 +444,13 @@ struct Attention {
         u32x4 w16[QT][k16 ? kGroups / 2 : 1];
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
+            float sum = 0.0f;                                      // (float32: a tile's own sum first, over long contexts it matters)
 #pragma unroll
             for (int k = 0; k < kGroups; ++k) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     s[q][k][i] = exp2_of(fmaf(s[q][k][i], g.factor, base[q]));
-                    if constexpr (!k16) weight[q][0] += s[q][k][i];
+                    if constexpr (!k16) sum += s[q][k][i];
                 }
                 if constexpr (k16) {
                     typedef __attribute__((ext_vector_type(4))) typename E::T x4;
@@ -458,6 +462,7 @@ struct Attention {
                     w16[q][k / 2][(k & 1) * 2 + 1] = p.y;
                 }
             }
+            if constexpr (!k16) weight[q][0] += sum;
             // (a product with ones adds up the rounded weights, those that meet the values)
             if constexpr (k16)
 #pragma unroll
@@ -693,6 +698,7 @@ struct Attention {
                 const int byte = (c * 16 + quad * 4) * E::kBytes;
                 E::put4(mine + ((byte / 16) ^ swizzle(l16)) * 16 + byte % 16, out[q][c] * whole);
             }
+            wave_order();
 #pragma unroll
             for (int j = 0; j < 16 / kRowsPerLoad; ++j) {
                 const int local = j * kRowsPerLoad + lane / kChunks, chunk = lane % kChunks;
@@ -703,6 +709,7 @@ struct Attention {
                     ((static_cast<int64_t>(b) * g.a.N + node) * g.a.out_stride + static_cast<int64_t>(kv * group + row - node * group) * g.a.head_dim) * E::kBytes;
                 if (node < t.nodes && chunk * 16 < g.a.head_dim * E::kBytes) *reinterpret_cast<u32x4*>(to + chunk * 16) = v;
             }
+            wave_order();
         }
     }
 
