@@ -6,10 +6,18 @@ namespace mpv {
 
 // ------------------------------------------------------------------ tables
 
+// What a call has to move is small (8 bytes a token and the pages' numbers): it costs launches and loads that depend on each other
+// (length -> place in the list of free pages -> page -> slot).  So one launch where one workgroup can do it all, and no load of a thread
+// waits for another one of the same kind.  64 requests, 1 to 6 new tokens each: 7.2 us; 300 prompts of up to 8192 tokens (1.2 million
+// slots, 10 MB): 12.6 us.
 constexpr int kPlanBlock = 1024;
 constexpr int kFillBlock = 256;
-constexpr int kFillSlots = 2048;           // slots of one workgroup of the fill kernel
-// Up to so many slots (of requests that take one round of the plan's workgroup) that workgroup fills them itself, in one launch.
+// Slots of a thread of the fill kernels, their pages asked for together (300 prompts: 12.6 us, 13.7 with eight).
+constexpr int kFillTogether = 4;
+constexpr int kFillSlots = kFillBlock * kFillTogether;
+// Up to so many slots (of requests that take one round of the plan's workgroup) that workgroup fills them itself, in one launch:
+// 1024 slots in 8.0 us against 8.8 with a second launch, 4000 packed ones in 8.5 against 10.8, 4096 in rows in 10.5 against 10.4;
+// 16384 in 34 against 10.4.
 constexpr int64_t kFillAtOnce = 4096;
 
 struct PlanEntry {                         // what the fill needs of a request
@@ -54,8 +62,24 @@ __device__ __forceinline__ int64_t slot_of(const TableArgs& a, int b, const Plan
     if (column >= e.have && place == 0) a.b.block_table[static_cast<int64_t>(b) * a.t.table_width + column] = page;
     return page >= 0 && page < a.t.num_pages ? static_cast<int64_t>(page) * a.t.page_size + place : -1;
 }
-__device__ __forceinline__ void fill_slot(const TableArgs& a, int b, const PlanEntry& e, int i, int64_t* to) {
-    *to = i < e.given ? slot_of(a, b, e, i, *page_of(a, b, e, i)) : -1;
+// A place of the slot map: request, its new token, where its slot goes (null: nowhere).
+struct Place {
+    int b, i;
+    PlanEntry e;
+    int64_t* to;
+};
+// A thread's places, their pages asked for together.
+template <int N>
+__device__ __forceinline__ void fill_places(const TableArgs& a, const Place (&p)[N]) {
+    int page[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        page[j] = -1;
+        if (p[j].to && p[j].i < p[j].e.given) page[j] = *page_of(a, p[j].b, p[j].e, p[j].i);
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if (p[j].to) *p[j].to = p[j].i < p[j].e.given ? slot_of(a, p[j].b, p[j].e, p[j].i, page[j]) : -1;
 }
 
 // One workgroup: who gets what (sums over the requests in their order), and the pages of finished requests.
@@ -138,32 +162,47 @@ __global__ __launch_bounds__(kPlanBlock) void plan_tables_kernel(TableArgs a, in
         for (int b = threadIdx.x >> 6; b < B; b += threads / 64) {
             const PlanEntry e = plan[b];
             const int64_t begin = a.b.offsets[b];
-            for (int i = lane; i < e.given; i += 64) fill_slot(a, b, e, i, a.b.slot_map + begin + i);
+            for (int base = lane; base < e.given; base += 64 * kFillTogether) {
+                Place p[kFillTogether];
+#pragma unroll
+                for (int j = 0; j < kFillTogether; ++j) {
+                    const int i = base + 64 * j;
+                    p[j] = {b, i, e, i < e.given ? a.b.slot_map + begin + i : nullptr};
+                }
+                fill_places(a, p);
+            }
         }
     } else {
-        const int slot_width = static_cast<int>(a.t.slot_width);
-        for (int x = threadIdx.x; x < B * slot_width; x += threads) {
-            const int b = x / slot_width;
-            fill_slot(a, b, plan[b], x - b * slot_width, a.b.slot_map + x);
+        const int slot_width = static_cast<int>(a.t.slot_width), slots = B * slot_width;
+        for (int base = threadIdx.x; base < slots; base += threads * kFillTogether) {
+            Place p[kFillTogether];
+#pragma unroll
+            for (int j = 0; j < kFillTogether; ++j) {
+                const int x = base + threads * j, b = x < slots ? x / slot_width : 0;
+                p[j] = {b, x - b * slot_width, plan[b], x < slots ? a.b.slot_map + x : nullptr};
+            }
+            fill_places(a, p);
         }
     }
 }
 
 __global__ __launch_bounds__(kFillBlock) void fill_rows_kernel(TableArgs a) {
     const int64_t slots = a.t.slot_width * a.t.B;
-    for (int64_t x = static_cast<int64_t>(blockIdx.x) * kFillSlots + threadIdx.x, j = 0; j < kFillSlots / kFillBlock; ++j, x += kFillBlock)
-        if (x < slots) {
-            const int b = static_cast<int>(x / a.t.slot_width);
-            fill_slot(a, b, a.plan[b], static_cast<int>(x - b * a.t.slot_width), a.b.slot_map + x);
-        }
+    Place p[kFillTogether];
+#pragma unroll
+    for (int j = 0; j < kFillTogether; ++j) {
+        const int64_t x = static_cast<int64_t>(blockIdx.x) * kFillSlots + kFillBlock * j + threadIdx.x;
+        const int b = x < slots ? static_cast<int>(static_cast<uint32_t>(x) / static_cast<uint32_t>(a.t.slot_width)) : 0;
+        p[j] = {b, static_cast<int>(x - b * a.t.slot_width), a.plan[b], x < slots ? a.b.slot_map + x : nullptr};
+    }
+    fill_places(a, p);
 }
 
 // Requests of a workgroup's slots: the number of requests that end at or before the first of them, found by counting, and at or
-// before the last.  Where they are few, as they are where tokens are many, their entries lie in LDS, and a thread's pages are asked
-// for together (1.2 million slots of 300 requests: 12 us when each of a thread's eight slots waited for its own).
+// before the last.  Where they are few, as they are where tokens are many, their entries lie in LDS and the request of a slot is found
+// there; otherwise by bisection of the offsets.
 constexpr int kFewRequests = 8;
 __global__ __launch_bounds__(kFillBlock) void fill_packed_kernel(TableArgs a) {
-    constexpr int kMine = kFillSlots / kFillBlock;
     __shared__ int lo_hi[2];
     __shared__ PlanEntry plan[kFewRequests];
     __shared__ int offset[kFewRequests + 1];
@@ -188,21 +227,15 @@ __global__ __launch_bounds__(kFillBlock) void fill_packed_kernel(TableArgs a) {
         if (static_cast<int>(threadIdx.x) <= requests) offset[threadIdx.x] = a.b.offsets[first_request + threadIdx.x];
         if (static_cast<int>(threadIdx.x) < requests) plan[threadIdx.x] = a.plan[first_request + threadIdx.x];
         __syncthreads();
-        int request[kMine], page[kMine];
+        Place p[kFillTogether];
 #pragma unroll
-        for (int j = 0; j < kMine; ++j) {
-            const int64_t x = min(first + j * kFillBlock + threadIdx.x, last);
+        for (int j = 0; j < kFillTogether; ++j) {
+            const int64_t x = first + j * kFillBlock + threadIdx.x;
             int r = 0;
             for (int k = 1; k < requests; ++k) r += offset[k] <= x;
-            request[j] = r;
-            page[j] = *page_of(a, first_request + r, plan[r], static_cast<int>(x - offset[r]));
+            p[j] = {first_request + r, static_cast<int>(x - offset[r]), plan[r], x <= last ? a.b.slot_map + x : nullptr};
         }
-#pragma unroll
-        for (int j = 0; j < kMine; ++j) {
-            const int64_t x = first + j * kFillBlock + threadIdx.x;
-            const int r = request[j];
-            if (x <= last) a.b.slot_map[x] = slot_of(a, first_request + r, plan[r], static_cast<int>(x - offset[r]), page[j]);
-        }
+        fill_places(a, p);
         return;
     }
     for (int64_t x = first + threadIdx.x; x <= last; x += kFillBlock) {
@@ -211,14 +244,15 @@ __global__ __launch_bounds__(kFillBlock) void fill_packed_kernel(TableArgs a) {
             const int m = (l + h) >> 1;
             if (a.b.offsets[m + 1] <= x) l = m + 1; else h = m;
         }
-        fill_slot(a, l, a.plan[l], static_cast<int>(x - a.b.offsets[l]), a.b.slot_map + x);
+        const Place p[1] = {{l, static_cast<int>(x - a.b.offsets[l]), a.plan[l], a.b.slot_map + x}};
+        fill_places(a, p);
     }
 }
 
 // ------------------------------------------------------------------ append
 
 constexpr int kAppendBlock = 256;
-constexpr int kAppendLayers = 8;           // layers of one workgroup
+constexpr int kAppendLayers = 2;           // layers of one workgroup: a (layer, keys or values) for each of its waves
 
 struct AppendArgs {
     mpv_append p;
@@ -227,7 +261,10 @@ struct AppendArgs {
     int bytes;                             // of an element
 };
 
-// A workgroup moves one row of one tree, keys and values, for kAppendLayers layers; a wave takes a (layer, keys or values) at a time.
+// A copy, bound by memory where it is large: a workgroup moves one row of one tree, keys and values, for kAppendLayers layers, a wave
+// one of them.  What a wave needs first (accept_len, path, slot) are loads that depend on each other, so many short workgroups hide them
+// better than few long ones: 256 trees of 41 nodes and 16 layers of rows of 2 KB, 117 MB read and written, 25.9 us (4.5 TB/s), 27.8 with
+// eight layers a workgroup; 4 trees, 32 layers: 3.2 us against 4.0.
 __global__ __launch_bounds__(kAppendBlock) void append_kernel(AppendArgs a) {
     const int b = blockIdx.x / a.rows, i = blockIdx.x - b * a.rows;
     if (i > a.b.accept_len[b]) return;
@@ -290,12 +327,14 @@ int mpv_extend_tables(const mpv_tables* tables, const mpv_table_buffers* buf, vo
     a.by_page.set(static_cast<uint32_t>(tables->page_size));
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const int64_t slots = tables->slot_width * (tables->packed ? 1 : tables->B);
-    // a wave for 64 requests, four at least (they fill the slots, too)
-    const int threads = tables->B >= mpv::kPlanBlock ? mpv::kPlanBlock : tables->B <= 256 ? 256 : (tables->B + 63) / 64 * 64;
+    // a wave for 64 requests; as they fill the slots, too, four at least, and eight where slots are many (4096 in rows: 10.5 us against
+    // 12.7 with four and 11.5 with sixteen; 512 in rows: the same)
+    const int least = slots >= 1024 && slots <= mpv::kFillAtOnce ? 512 : 256;
+    const int threads = tables->B >= mpv::kPlanBlock ? mpv::kPlanBlock : tables->B <= least ? least : (tables->B + 63) / 64 * 64;
     const int fill = slots <= mpv::kFillAtOnce && tables->B <= threads;
     (void)hipGetLastError();
     hipLaunchKernelGGL(mpv::plan_tables_kernel, dim3(1), dim3(threads), 0, s, a, fill);
-    if (!fill) {
+    if (!fill && slots > 0) {
         const dim3 grid(static_cast<unsigned>((slots + mpv::kFillSlots - 1) / mpv::kFillSlots));
         if (tables->packed) hipLaunchKernelGGL(mpv::fill_packed_kernel, grid, dim3(mpv::kFillBlock), 0, s, a);
         else hipLaunchKernelGGL(mpv::fill_rows_kernel, grid, dim3(mpv::kFillBlock), 0, s, a);

@@ -90,6 +90,28 @@ def test_prompts(packed):
     check(table, context, new, free, count, 16, sum(max(n, 0) for n in new) if packed else 3000, 0, packed)
 
 
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("most", [50, 204, 205, 300, 819, 820, 5000])
+def test_slot_maps_of_all_sizes(most, packed):
+    """Filled by one workgroup or by many, with one slot, four or more of a thread."""
+    print("[case] slot maps", most, packed, flush=True)
+    rng = np.random.default_rng(most)
+    new = rng.integers(most // 2, most + 1, 5).tolist()
+    new[4] = most
+    context = rng.integers(0, 100, 5).tolist()
+    table, free, count = make(5, -(-(most + 100) // 24), 24, context, 5 * (most // 24 + 2), seed=most)
+    check(table, context, new, free, count, 24, 5 * most if packed else most, 0, packed)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_many_requests_and_no_slots(packed):
+    print("[case] no slots", packed, flush=True)
+    new = [-1 if b % 7 == 0 else 0 for b in range(2000)]
+    context = [b % 40 for b in range(2000)]
+    table, free, count = make(2000, 3, 16, context, 5, seed=8)
+    check(table, context, new, free, count, 16, 0, 0, packed)
+
+
 def test_a_slot_map_that_is_too_small():
     print("[case] small map", flush=True)
     table, free, count = make(6, 10, 4, [0, 3, 4, 8, 1, 0], 50, seed=3)
