@@ -662,6 +662,11 @@ def _launch(plan, bufs, out, stream):
         rc = plan.call(plan.address, ctypes.byref(bufs), ws.data_ptr(), ws.numel(), raw)
     if rc != 0:
         raise MpvError(rc, plan.name)
+    if stream is not None and out is not None and raw != torch.cuda.current_stream().cuda_stream:
+        # what was allocated for the current stream is in use on another one: it must not be given away before that is done
+        for t in vars(out).values():
+            if isinstance(t, torch.Tensor) and t.is_cuda:
+                t.record_stream(stream)
     return out
 
 

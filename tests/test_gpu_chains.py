@@ -147,3 +147,25 @@ def test_captured_and_replayed():
         for name in ("accept_len", "path_nodes", "path_tokens", "bonus_token", "counters"):
             assert torch.equal(getattr(kept, name), getattr(eager, name)), name
         check(tokens, p, q, u, res=kept)
+
+
+def test_what_is_used_on_another_stream_is_not_given_away_before_it_is_done():
+    print("[case] another stream", flush=True)
+    tokens, p, q, u = make(4, 5, 32000, torch.float32)
+    want = check(tokens, p, q, u)
+    side = torch.cuda.Stream()
+    busy = torch.zeros(64 << 20, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(600):                       # some 60 ms, in which the allocator has to wait
+            busy += 1.0
+    res = mpv.mpv_verify_chains(tokens, p, q, u, stream=side)
+    places = {t.data_ptr() for t in (res.workspace, res.path_nodes, res.bonus_token)}
+    sizes = res.workspace.numel()
+    assert len(places) == 3 and not side.query()
+    held = res.bonus_token
+    del res
+    new = [torch.empty(sizes, dtype=torch.uint8, device="cuda") for _ in range(8)] + [torch.empty_like(want.path_nodes) for _ in range(8)]
+    assert not side.query() and not places & {t.data_ptr() for t in new}
+    torch.cuda.synchronize()
+    assert torch.equal(held, want.bonus_token)
