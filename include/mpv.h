@@ -416,8 +416,8 @@ typedef struct mpv_chain_buffers {         /* DEVICE */
 
 int mpv_verify_chains_workspace_bytes(const mpv_chains* chains, size_t* out);
 
-/* Errors: MPV_ERR_NULL, _BAD_SHAPE, _UNSUPPORTED (N or V too large), _BAD_DTYPE, _ALIGNMENT (a pointer is no multiple of
- * its element's size), _WORKSPACE, _HIP. */
+/* Errors: MPV_ERR_NULL, _BAD_SHAPE, _UNSUPPORTED (N, V, B, max_depth or a stride too large), _BAD_DTYPE, _ALIGNMENT (a pointer
+ * is no multiple of its element's size), _WORKSPACE, _HIP. */
 int mpv_verify_chains(const mpv_chains* chains, const mpv_chain_buffers* buffers,
                       void* workspace, size_t workspace_bytes, void* hip_stream);
 
@@ -484,7 +484,7 @@ typedef struct mpv_append_buffers {        /* DEVICE */
     const int32_t* path_nodes;    /* [B,max_depth] or NULL                                                    */
 } mpv_append_buffers;
 
-/* Errors: MPV_ERR_NULL, _BAD_SHAPE, _UNSUPPORTED, _BAD_DTYPE, _ALIGNMENT, _HIP. */
+/* Errors: MPV_ERR_NULL, _BAD_SHAPE, _UNSUPPORTED (N, row, B, layers or a stride too large), _BAD_DTYPE, _ALIGNMENT, _HIP. */
 int mpv_append_paths(const mpv_append* append, const mpv_append_buffers* buffers, void* hip_stream);
 
 /* Per-launch timing for benchmarks (process-wide state, not thread-safe).
