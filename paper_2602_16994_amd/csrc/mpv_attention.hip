@@ -23,7 +23,7 @@
 //   256 trees of 41 nodes, contexts of 512 to 4096: 164 rows read every key, 611 us, 2.6 GB at 4.3 TB/s and 645 TFLOP/s (the floor of
 //     either alone: 520 us, 360 us).  Loads, the exponents' vector instructions and matrix instructions take turns in a wave, and two
 //     workgroups a compute unit do not fill all of the gaps.  With all pages the same (no memory): 12 % less.
-//   8 single tokens, contexts of 20 000 to 131 072: 505 us, 5.3 TB/s: memory.
+//   8 single tokens, contexts of 20 000 to 131 072: 505 us for 2.9 GB, 5.8 TB/s: memory.
 //   one tree of 7 nodes, a context of 900: 11.3 us, two launches and the loads that depend on each other (lengths, page, key).
 // Contexts of medium size that many teams share are bound by their partial sums as much as by the cache: 32 trees with a window of 1024
 // keys of 4 heads of 256 float16 values, 54 us for 144 MB.  float32 is bound by its matrix instruction (154 TFLOP/s at most; 16x16x4).
