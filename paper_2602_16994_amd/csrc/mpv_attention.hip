@@ -113,6 +113,13 @@ __device__ __forceinline__ void to_lds(uint64_t from, uint32_t to) {
 __device__ __forceinline__ void word_to_lds(uint64_t from, uint32_t to) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory");
 }
+// A place in LDS.  (The pass for the host, which never runs it, has pointers of 64 bits.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Wint-to-pointer-cast"
+__device__ __forceinline__ __attribute__((address_space(3))) char* lds_place(uint32_t at) {
+    return reinterpret_cast<__attribute__((address_space(3))) char*>(at);
+}
+#pragma clang diagnostic pop
 // What a wave's lanes wrote to LDS is there for its other lanes (LDS serves a wave in order; the compiler must keep that order).
 __device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local"); }
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -190,8 +197,8 @@ struct Attention {
     static_assert(kBatch >= kAheadTiles && kAheadTiles * kMyLoads * 2 < 60, "batch");
 
     struct Shared {
-        __align__(16) char keys[STAGES][kTileBytes];
-        __align__(16) char values[STAGES][kTileBytes];
+        __align__(1024) char keys[STAGES][kTileBytes];
+        __align__(1024) char values[STAGES][kTileBytes];
         __align__(16) uint64_t place[2][kBatch][TILE][2];          // where a key's and its value's row lie
         __align__(16) int pages[WAVES][64];                        // entries of the block table, a lane's each
         __align__(4) uint8_t seen[2][kBatch][TILE];                // whether anybody sees the key
@@ -367,20 +374,27 @@ struct Attention {
     // Operands of the products are read kAhead instructions before their use, which the order of the source alone does not bring about.
     static constexpr int kAhead = 4;
     struct First { u32x4 keys[kAhead]; unsigned long long special; };
-    __device__ __forceinline__ u32x4 read_key(const char* keys, int n) const {
+    // (Rows begin at multiples of their length, so exchanged chunks are reached by exclusive or of a place in the first one of them.)
+    template <class V> static __device__ __forceinline__ V lds(uint32_t at) {
+        return *reinterpret_cast<const __attribute__((address_space(3))) V*>(lds_place(at));
+    }
+    __device__ __forceinline__ uint32_t keys_at(int stage) const {
+        return shared_at + stage * kTileBytes + (l16 * kChunks + (quad ^ swizzle(l16))) * 16;
+    }
+    static __device__ __forceinline__ u32x4 read_key(uint32_t keys, int n) {
         const int k = n / kSteps, d = n % kSteps;
-        return *reinterpret_cast<const u32x4*>(keys + ((k * 16 + l16) * kChunks + ((d * 4 + quad) ^ swizzle(l16))) * 16);
+        return lds<u32x4>((keys ^ (d * 64)) + k * 16 * kChunks * 16);
     }
     __device__ __forceinline__ First read_first(int half, int sub, int stage) const {
         constexpr unsigned long long kBytesOfWaves = WAVES == 8 ? ~0ull : (1ull << (8 * (WAVES % 8))) - 1;
         First f;
 #pragma unroll
-        for (int n = 0; n < kAhead; ++n) f.keys[n] = read_key(sh.keys[stage], n);
+        for (int n = 0; n < kAhead; ++n) f.keys[n] = read_key(keys_at(stage), n);
         f.special = *reinterpret_cast<const unsigned long long*>(sh.special[half][sub]) & kBytesOfWaves;
         return f;
     }
     __device__ __forceinline__ void work(int index, int half, int sub, int stage, const First& f, bool careful) {
-        const char* keys = sh.keys[stage];
+        const uint32_t keys = keys_at(stage);
         char* values = sh.values[stage];
         f32x4 s[QT][kGroups];
         constexpr int kFirst = kGroups * kSteps;
@@ -442,8 +456,9 @@ struct Attention {
                 for (int i = 0; i < 4; ++i) most = fmaxf(most, s[q][k][i]);
             most *= g.factor;
             if (__ballot(most > top[q] + kSlack)) {
-                most = fmaxf(most, __shfl_xor(most, 16));
-                most = fmaxf(most, __shfl_xor(most, 32));
+                const int other = fresh(lane);
+                most = fmaxf(most, __shfl(most, other ^ 16));
+                most = fmaxf(most, __shfl(most, other ^ 32));
                 const float now = fmaxf(top[q], most);
                 const float fade = now == -INFINITY ? 1.0f : exp2_of(top[q] - now);
                 top[q] = now;
@@ -485,15 +500,16 @@ struct Attention {
         __builtin_amdgcn_s_setprio(1);
         if constexpr (k16) {
             constexpr int kSecond = kColumns * (kGroups / 2);
+            const uint32_t columns = values_at(stage);
 #pragma unroll
-            for (int n = 0; n < kAhead; ++n) a[n] = column16(values, n % (kGroups / 2), n / (kGroups / 2));
+            for (int n = 0; n < kAhead; ++n) a[n] = column16(columns, n % (kGroups / 2), n / (kGroups / 2));
 #pragma unroll
             for (int n = 0; n < kSecond; ++n) {
                 const int k = n % (kGroups / 2), c = n / (kGroups / 2);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int q = 0; q < QT; ++q) out[q][c] = E::mfma(a[n % kAhead], w16[q][k], out[q][c]);
-                if (n + kAhead < kSecond) a[n % kAhead] = column16(values, (n + kAhead) % (kGroups / 2), (n + kAhead) / (kGroups / 2));
+                if (n + kAhead < kSecond) a[n % kAhead] = column16(columns, (n + kAhead) % (kGroups / 2), (n + kAhead) / (kGroups / 2));
             }
             __builtin_amdgcn_sched_barrier(0);
         } else {
@@ -521,15 +537,17 @@ struct Attention {
     }
 
     // Keys 32 k + 4 quad .. + 3 and 32 k + 16 + 4 quad .. + 3 of column 16 c + l16.
-    __device__ __forceinline__ u32x4 column16(const char* values, int k, int c) const {
-        u32x4 v;
+    __device__ __forceinline__ uint32_t values_at(int stage) const {
         const int row = quad * 4 + (l16 >> 2);
-        const int in_row = ((c * 2 + ((l16 & 3) >> 1)) ^ swizzle(row)) * 16 + (l16 & 1) * 8;
+        return shared_at + (STAGES + stage) * kTileBytes + row * kChunks * 16 + (((l16 & 3) >> 1) ^ swizzle(row)) * 16 + (l16 & 1) * 8;
+    }
+    static __device__ __forceinline__ u32x4 column16(uint32_t values, int k, int c) {
+        u32x4 v;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             typedef __attribute__((address_space(3))) i16x4 lds_x4;
-            const char* from = values + (k * 32 + h * 16 + row) * kChunks * 16 + in_row;
-            const uint2 r = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_x4*)from));
+            const uint32_t from = (values ^ (c * 32)) + (k * 32 + h * 16) * kChunks * 16;
+            const uint2 r = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_x4*)lds_place(from)));
             v[2 * h] = r.x;
             v[2 * h + 1] = r.y;
         }
@@ -832,7 +850,7 @@ struct Attention {
 
 template <class A>
 __global__ __launch_bounds__(A::kThreads) __attribute__((amdgpu_waves_per_eu(2))) void attention_kernel(AttentionArgs g) {
-    extern __shared__ __align__(16) char memory[];
+    extern __shared__ __align__(1024) char memory[];
     A a(g, *reinterpret_cast<typename A::Shared*>(memory));
     a.all();
 }
