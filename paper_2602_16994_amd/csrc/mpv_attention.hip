@@ -20,13 +20,13 @@
 // ones, so that a common factor of their errors falls out.  Everything else (products, references, both sums) is float32.
 //
 // What bounds it, with 32 query heads on 8 cache heads of 128 bfloat16 values:
-//   256 trees of 41 nodes, contexts of 512 to 4096: 164 rows read every key, 611 us, 2.6 GB at 4.3 TB/s and 645 TFLOP/s (the floor of
-//     either alone: 520 us, 360 us).  Loads, the exponents' vector instructions and matrix instructions take turns in a wave, and two
+//   256 trees of 41 nodes, contexts of 512 to 4096: 164 rows read every key, 613 us, 2.6 GB at 4.2 TB/s and 645 TFLOP/s (the floor of
+//     either alone: 540 us, 350 us).  Loads, the exponents' vector instructions and matrix instructions take turns in a wave, and two
 //     workgroups a compute unit do not fill all of the gaps.  With all pages the same (no memory): 12 % less.
 //   8 single tokens, contexts of 20 000 to 131 072: 505 us for 2.9 GB, 5.8 TB/s: memory.
-//   one tree of 7 nodes, a context of 900: 11.3 us, two launches and the loads that depend on each other (lengths, page, key).
+//   one tree of 7 nodes, a context of 900: 11.2 us, two launches and the loads that depend on each other (lengths, page, key).
 // Contexts of medium size that many teams share are bound by their partial sums as much as by the cache: 32 trees with a window of 1024
-// keys of 4 heads of 256 float16 values, 54 us for 144 MB.  float32 is bound by its matrix instruction (154 TFLOP/s at most; 16x16x4).
+// keys of 4 heads of 256 float16 values, 52 us for 144 MB.  float32 is bound by its matrix instruction (154 TFLOP/s at most; 16x16x4).
 
 #include <hip/hip_runtime.h>
 
@@ -140,7 +140,7 @@ __device__ __forceinline__ int fresh(int x) {
     return x;
 }
 // What beginning and ending a unit takes, in tiles: workgroups with many short units would end last otherwise.  256 trees of 8 nodes,
-// contexts of 16 to 256: 68 us, 90 without; the benchmark's trees 611 us, 640 without; contexts of one length: the same.
+// contexts of 16 to 256: 66 us, 91 without; the benchmark's trees 613 us, 637 without; contexts of one length: the same.
 constexpr int kUnitCost = 8;
 // All bits where bit `at` is set, none otherwise.  (Masks instead of conditions: those would all wait in scalar registers at once.)
 __device__ __forceinline__ uint32_t spread(uint32_t bits, int at) { return static_cast<uint32_t>(static_cast<int32_t>(bits << (31 - at)) >> 31); }
@@ -857,7 +857,7 @@ __global__ __launch_bounds__(A::kThreads) __attribute__((amdgpu_waves_per_eu(2))
 
 // Puts the shared units together.  kLanes lanes have a row (4 columns each).  Few parts, as in large batches: a wave has as many rows
 // as it has such groups of lanes, twice over.  Many: the groups of a workgroup share the parts of one row.
-// (Few: a workgroup a row takes 651 us instead of 611 for the benchmark's trees, 58 instead of 54 for 32 trees with a window of 1024.)
+// (Few: a workgroup a row takes 651 us instead of 613 for the benchmark's trees, 56 instead of 52 for 32 trees with a window of 1024.)
 constexpr int kFewParts = 8, kFewRows = 2;
 
 template <int DTYPE, int DP, int ROWS>
@@ -1042,7 +1042,7 @@ static int with_kernel(const mpv_attention* a, AttentionArgs* g, void* workspace
     char* at = static_cast<char*>(workspace);
     g->teams = c.teams;
     g->blocks = c.blocks;
-    // (units that are fewer than the teams are joined by unit: 15.0 us by team instead of 11.3 for one tree, 37 instead of 30 in float32)
+    // (units that are fewer than the teams are joined by unit: 14.6 us by team instead of 11.2 for one tree, 37 instead of 30 in float32)
     g->by_unit = static_cast<int64_t>(a->B) * a->kv_heads < c.teams;
     g->group = a->heads / a->kv_heads;
     g->by_group.set(static_cast<uint32_t>(g->group));
@@ -1075,7 +1075,7 @@ template <int DTYPE, int DP>
 static int with_columns(const mpv_attention* a, AttentionArgs* g, void* workspace, size_t* bytes, hipStream_t s) {
     const int64_t rows = static_cast<int64_t>(a->N) * (a->heads / a->kv_heads);
     // as few waves as hold the rows: a wave reads all of a tile from LDS, whatever it has to do with it.  (16 rows and less on two waves:
-    // 536 us instead of 505 for 8 long contexts, 44 instead of 30 in float32; 32 rows on four: 224 instead of 217 for 64 trees of 8 nodes.)
+    // 538 us instead of 505 for 8 long contexts, 44 instead of 30 in float32; 32 rows on four: 223 instead of 217 for 64 trees of 8 nodes.)
     if (rows <= 16) return with_kernel<Kernel<DTYPE, DP, 1, 1>, DTYPE, DP>(a, g, workspace, bytes, s);
     if (rows <= 32) return with_kernel<Kernel<DTYPE, DP, 1, 2>, DTYPE, DP>(a, g, workspace, bytes, s);
     if (rows <= 64) return with_kernel<Kernel<DTYPE, DP, 1, 4>, DTYPE, DP>(a, g, workspace, bytes, s);
@@ -1084,7 +1084,7 @@ static int with_columns(const mpv_attention* a, AttentionArgs* g, void* workspac
         return with_kernel<Kernel<DTYPE, DP, 1, 8>, DTYPE, DP>(a, g, workspace, bytes, s);
     } else {
         // as many groups a wave as divide the rows into even blocks: every block reads the tiles again, from the chiplet's cache.  (Two
-        // groups for the benchmark's 164 rows: 881 us instead of 611.)
+        // groups for the benchmark's 164 rows: 870 us instead of 613.)
         const int64_t blocks = (rows + 191) / 192, groups = (rows + 64 * blocks - 1) / (64 * blocks);
         if (groups > 2) return with_kernel<Kernel<DTYPE, DP, 3, 4>, DTYPE, DP>(a, g, workspace, bytes, s);
         return with_kernel<Kernel<DTYPE, DP, 2, 4>, DTYPE, DP>(a, g, workspace, bytes, s);
