@@ -6,6 +6,7 @@ the computation runs in the library's kernels.  There is no CPU fallback: if the
 library is missing, loading raises.
 """
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -641,6 +642,18 @@ def _like(t):
     return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
 
 
+_nothing = contextlib.nullcontext()
+
+
+def _allocating(stream):
+    """What a call allocates, its results and workspace, is allocated on the stream that it runs on: memory that was given back on
+    another one may still be in use by work that was enqueued there before, and the call's stream does not wait for that."""
+    if stream is None:
+        return _nothing
+    import torch
+    return torch.cuda.stream(stream)
+
+
 def _launch(plan, bufs, out, stream):
     """The call on its tensors' device; its workspace, if it has one, is kept in out.workspace."""
     import torch
@@ -658,15 +671,24 @@ def _launch(plan, bufs, out, stream):
     else:
         ws = out.workspace
         if ws is None or ws.numel() < plan.need or ws.get_device() != plan.device:
-            ws = out.workspace = torch.empty(plan.need, dtype=torch.uint8, device=torch.device("cuda", plan.device))
+            with _allocating(stream):
+                ws = out.workspace = torch.empty(plan.need, dtype=torch.uint8, device=torch.device("cuda", plan.device))
+            out._workspace_stream = raw
+        elif getattr(out, "_workspace_stream", None) != raw:       # it is used on another stream than the one before
+            ws.record_stream(torch.cuda.current_stream() if stream is None else stream)
+            out._workspace_stream = raw
         rc = plan.call(plan.address, ctypes.byref(bufs), ws.data_ptr(), ws.numel(), raw)
     if rc != 0:
         raise MpvError(rc, plan.name)
     if stream is not None and out is not None and raw != torch.cuda.current_stream().cuda_stream:
-        # what was allocated for the current stream is in use on another one: it must not be given away before that is done
+        # what was allocated elsewhere is in use on this stream, and results that were allocated on it are used on the current one next:
+        # neither must be given away before that is done
+        current = torch.cuda.current_stream()
         for t in vars(out).values():
             if isinstance(t, torch.Tensor) and t.is_cuda:
                 t.record_stream(stream)
+                if t is not out.workspace:
+                    t.record_stream(current)
     return out
 
 
@@ -696,7 +718,8 @@ def mpv_tree_attention(parent, q, tree_k, tree_v, cache_k, cache_v, block_table,
         plan = _kept(key, _attention_plan(parent, q, tree_k, tree_v, cache_k, cache_v, block_table, context_len, scale, window, sinks,
                                           num_nodes, tree_parent, out))
     if out is None:
-        out = TreeAttentionResult(out=torch.empty(q.shape, dtype=q.dtype, device=q.device))
+        with _allocating(stream):
+            out = TreeAttentionResult(out=torch.empty(q.shape, dtype=q.dtype, device=q.device))
     bufs = _AttentionBuffers(q.data_ptr(), tree_k.data_ptr(), tree_v.data_ptr(), cache_k.data_ptr(), cache_v.data_ptr(), block_table.data_ptr(),
                              context_len.data_ptr(), _ptr(num_nodes), _ptr(tree_parent), out.out.data_ptr())
     return _launch(plan, bufs, out, stream)
@@ -753,8 +776,9 @@ def mpv_verify_chains(tokens, target_probs, draft_probs, uniforms, num_nodes=Non
         plan = _kept(key, _chains_plan(tokens, target_probs, draft_probs, uniforms, num_nodes, max_depth, out))
     if out is None:
         B, i32 = target_probs.shape[0], dict(dtype=torch.int32, device=target_probs.device)
-        out = VerifyResult(accept_len=torch.empty(B, **i32), path_nodes=torch.empty(B, max_depth, **i32),
-                           path_tokens=torch.empty(B, max_depth, **i32), bonus_token=torch.empty(B, **i32), counters=torch.empty(8, **i32))
+        with _allocating(stream):
+            out = VerifyResult(accept_len=torch.empty(B, **i32), path_nodes=torch.empty(B, max_depth, **i32),
+                               path_tokens=torch.empty(B, max_depth, **i32), bonus_token=torch.empty(B, **i32), counters=torch.empty(8, **i32))
     bufs = _ChainBuffers(target_probs.data_ptr(), _ptr(draft_probs), tokens.data_ptr(), uniforms.data_ptr(), _ptr(num_nodes),
                          out.accept_len.data_ptr(), out.path_nodes.data_ptr(), out.path_tokens.data_ptr(), out.bonus_token.data_ptr(),
                          out.counters.data_ptr())
@@ -810,9 +834,10 @@ def mpv_extend_tables(block_table, context_len, new_len, free_pages, free_count,
         plan = _kept(key, _tables_plan(block_table, context_len, new_len, free_pages, free_count, page_size, slot_map, extra, out))
     if out is None:
         B, i32 = block_table.shape[0], dict(dtype=torch.int32, device=block_table.device)
-        out = TablesResult(context_len=context_len if inplace else torch.empty(B, **i32),
-                           free_count=free_count if inplace else torch.empty(1, **i32), granted=torch.empty(B, **i32), slot_map=slot_map,
-                           offsets=torch.empty(B + 1, **i32))
+        with _allocating(stream):
+            out = TablesResult(context_len=context_len if inplace else torch.empty(B, **i32),
+                               free_count=free_count if inplace else torch.empty(1, **i32), granted=torch.empty(B, **i32), slot_map=slot_map,
+                               offsets=torch.empty(B + 1, **i32))
     out.slot_map = slot_map
     bufs = _TableBuffers(new_len.data_ptr(), context_len.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
                          out.context_len.data_ptr(), out.free_count.data_ptr(), slot_map.data_ptr(), out.granted.data_ptr(),
