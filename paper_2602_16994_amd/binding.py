@@ -813,6 +813,7 @@ class TablesResult:
     slot_map: "object"          # int64, the tensor that was passed
     offsets: "object"           # int32 [B+1]  exclusive sums of the tokens placed
     workspace: Optional["object"] = None
+    inplace: bool = False       # context_len and free_count are the tensors that were passed
 
 
 def mpv_extend_tables(block_table, context_len, new_len, free_pages, free_count, page_size, slot_map, extra=0, inplace=False, out=None,
@@ -823,29 +824,36 @@ def mpv_extend_tables(block_table, context_len, new_len, free_pages, free_count,
     block_table int32 [B,table_width] and free_pages int32 [num_pages] are changed in place; context_len int32 [B] and
     free_count int32 [1] are, too, with inplace=True, otherwise their new values are in the result alone.  new_len int32 [B]: tokens to
     place beside `extra`, negative for a finished request.  slot_map int64: [B,n] for a row of slots per request, [n] for all of them
-    packed.  `out` may be a previous TablesResult whose buffers are reused."""
+    packed.  `out` may be a previous TablesResult whose buffers are reused (without inplace=True, not those that a caller passed).
+    """
     import torch
-    if inplace and out is not None:
-        out.context_len, out.free_count = context_len, free_count
+    # a result's lengths and count are written again unless they are a caller's tensors: those of a call in place, or this call's inputs
+    after, left = (None, None) if out is None else (out.context_len, out.free_count)
+    if inplace:
+        after, left = context_len, free_count
+    elif out is not None and (out.inplace or after.data_ptr() == context_len.data_ptr() or left.data_ptr() == free_count.data_ptr()):
+        after = left = None
     key = ("tables", page_size, extra, _like(block_table), _like(context_len), _like(new_len), _like(free_pages), _like(free_count),
-           _like(slot_map), None if out is None else (_like(out.context_len), _like(out.free_count), _like(out.granted), _like(out.offsets)))
+           _like(slot_map), _like(after), _like(left), None if out is None else (_like(out.granted), _like(out.offsets)))
     plan = _plans.get(key)
     if plan is None:
-        plan = _kept(key, _tables_plan(block_table, context_len, new_len, free_pages, free_count, page_size, slot_map, extra, out))
-    if out is None:
+        plan = _kept(key, _tables_plan(block_table, context_len, new_len, free_pages, free_count, page_size, slot_map, extra, after, left, out))
+    if out is None or after is None:
         B, i32 = block_table.shape[0], dict(dtype=torch.int32, device=block_table.device)
         with _allocating(stream):
-            out = TablesResult(context_len=context_len if inplace else torch.empty(B, **i32),
-                               free_count=free_count if inplace else torch.empty(1, **i32), granted=torch.empty(B, **i32), slot_map=slot_map,
-                               offsets=torch.empty(B + 1, **i32))
-    out.slot_map = slot_map
+            if after is None:
+                after, left = torch.empty(B, **i32), torch.empty(1, **i32)
+            if out is None:
+                out = TablesResult(context_len=after, free_count=left, granted=torch.empty(B, **i32), slot_map=slot_map,
+                                   offsets=torch.empty(B + 1, **i32))
+    out.context_len, out.free_count, out.slot_map, out.inplace = after, left, slot_map, inplace
     bufs = _TableBuffers(new_len.data_ptr(), context_len.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
                          out.context_len.data_ptr(), out.free_count.data_ptr(), slot_map.data_ptr(), out.granted.data_ptr(),
                          out.offsets.data_ptr())
     return _launch(plan, bufs, out, stream)
 
 
-def _tables_plan(block_table, context_len, new_len, free_pages, free_count, page_size, slot_map, extra, out):
+def _tables_plan(block_table, context_len, new_len, free_pages, free_count, page_size, slot_map, extra, after, left, out):
     import torch
     if block_table.dim() != 2 or free_pages.dim() != 1 or slot_map.dim() not in (1, 2):
         raise ValueError("block_table must be [B,table_width], free_pages [num_pages], slot_map [B,n] or [n]")
@@ -855,9 +863,9 @@ def _tables_plan(block_table, context_len, new_len, free_pages, free_count, page
     _whole(dev, torch.int32, block_table=(block_table, (B, width)), context_len=(context_len, (B,)), new_len=(new_len, (B,)),
            free_pages=(free_pages, (pages,)), free_count=(free_count, (1,)))
     _whole(dev, torch.int64, slot_map=(slot_map, tuple(slot_map.shape) if packed else (B, slot_map.shape[1])))
+    _whole(dev, torch.int32, **{"the result's context_len": (after, (B,)), "the result's free_count": (left, (1,))})
     if out is not None:
-        _whole(dev, torch.int32, context_len=(out.context_len, (B,)), free_count=(out.free_count, (1,)), granted=(out.granted, (B,)),
-               offsets=(out.offsets, (B + 1,)))
+        _whole(dev, torch.int32, granted=(out.granted, (B,)), offsets=(out.offsets, (B + 1,)))
     return _Plan("mpv_extend_tables", dev.index, _Tables(B, int(page_size), width, pages, int(extra), int(packed), slot_map.shape[-1]))
 
 
