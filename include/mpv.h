@@ -335,7 +335,8 @@ int mpv_fill_uniforms(uint64_t seed, int64_t count, float* d_u, void* hip_stream
  *   mpv_append_paths: their keys and values, of all layers, enter the cache;
  *   the bonus token is the root of the next step's trees.
  * The cache holds accepted tokens only: what was drafted in vain never enters it.  All calls work on lengths
- * that live on the device, allocate nothing, do not synchronise and can be captured in a graph.
+ * that live on the device, allocate nothing, do not synchronise and can be captured in a graph.  A call with B = 0 succeeds and writes
+ * nothing at all (its counters, free_count_out and offsets among what it leaves as it was).
  * --------------------------------------------------------------------------------------------- */
 
 /* Attention of the nodes of B draft trees over a paged cache and over their own tree.

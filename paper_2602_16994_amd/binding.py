@@ -782,7 +782,11 @@ def mpv_verify_chains(tokens, target_probs, draft_probs, uniforms, num_nodes=Non
     bufs = _ChainBuffers(target_probs.data_ptr(), _ptr(draft_probs), tokens.data_ptr(), uniforms.data_ptr(), _ptr(num_nodes),
                          out.accept_len.data_ptr(), out.path_nodes.data_ptr(), out.path_tokens.data_ptr(), out.bonus_token.data_ptr(),
                          out.counters.data_ptr())
-    return _launch(plan, bufs, out, stream)
+    _launch(plan, bufs, out, stream)
+    if not target_probs.shape[0]:                  # the library writes nothing then
+        with _allocating(stream):
+            out.counters.zero_()
+    return out
 
 
 def _chains_plan(tokens, target_probs, draft_probs, uniforms, num_nodes, max_depth, out):
@@ -850,7 +854,12 @@ def mpv_extend_tables(block_table, context_len, new_len, free_pages, free_count,
     bufs = _TableBuffers(new_len.data_ptr(), context_len.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
                          out.context_len.data_ptr(), out.free_count.data_ptr(), slot_map.data_ptr(), out.granted.data_ptr(),
                          out.offsets.data_ptr())
-    return _launch(plan, bufs, out, stream)
+    _launch(plan, bufs, out, stream)
+    if not block_table.shape[0]:                   # the library writes nothing then
+        with _allocating(stream):
+            left.copy_(free_count.clamp(0, free_pages.shape[0]))
+            out.offsets.zero_()
+    return out
 
 
 def _tables_plan(block_table, context_len, new_len, free_pages, free_count, page_size, slot_map, extra, after, left, out):

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2602_16994_amd as mpv
+from tests.test_gpu_chains import make as make_chains
 from tests.test_gpu_serving_streams import i32, tables
 
 pytestmark = pytest.mark.gpu
@@ -52,3 +53,30 @@ def test_a_refused_call_leaves_the_result_as_it_was():
     with pytest.raises(TypeError):
         mpv.mpv_extend_tables(**b, inplace=True, out=res)
     assert res.context_len is kept[0] and res.free_count is kept[1]
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_no_requests(packed):
+    print("[case] no requests", packed, flush=True)
+    a = tables()
+    for name in ("block_table", "context_len", "new_len"):
+        a[name] = a[name][:0]
+    a["slot_map"] = torch.full((4,), -7, dtype=torch.int64, device="cuda") if packed else a["slot_map"][:0]
+    old = mpv.TablesResult(context_len=i32([]), free_count=i32([99]), granted=i32([]), slot_map=a["slot_map"], offsets=i32([99]))
+    res = mpv.mpv_extend_tables(**a, out=old)
+    assert res.free_count.tolist() == [4] and res.offsets.tolist() == [0] and res.context_len.numel() == 0
+    assert a["free_count"].tolist() == [4] and a["free_pages"].tolist() == [0, 1, 2, 3, -1, -1] and (a["slot_map"] == -7).all()
+    a["free_count"] = i32([10 ** 6])               # taken within [0, num_pages]
+    res = mpv.mpv_extend_tables(**a, inplace=True)
+    assert a["free_count"].tolist() == [6] and res.free_count is a["free_count"]
+
+
+def test_no_chains():
+    print("[case] no chains", flush=True)
+    tokens, p, q, u = make_chains(2, 3, 10, torch.float32)
+    old = mpv.mpv_verify_chains(tokens, p, q, u)
+    for name in ("accept_len", "path_nodes", "path_tokens", "bonus_token"):
+        setattr(old, name, getattr(old, name)[:0])
+    old.counters.fill_(5)
+    res = mpv.mpv_verify_chains(tokens[:0], p[:0], q[:0], u[:0], out=old)
+    assert res.counters.tolist() == [0] * 8 and res.accept_len.numel() == 0
