@@ -426,7 +426,8 @@ int mpv_verify_chains(const mpv_chains* chains, const mpv_chain_buffers* buffers
  * gets room for n = new_len[b] + extra more: the pages it needs are taken from the end of the list of free pages (in
  * request order, ascending position), entered into its row of the block table, and the slots of its new tokens
  * (page * page_size + place in it) are written.  new_len[b] < 0: the request is finished; its pages go to the end of the
- * list (before any are taken, in request order) and its context becomes empty.
+ * list (before any are taken, in request order; what num_pages entries do not hold, which takes a free_count that was wrong, is
+ * dropped) and its context becomes empty.
  * Requests are served in order.  One that cannot fit its row of the block table or (slot rows) whose n exceeds the row
  * is refused; so is every request that needs a page from the first one on whose pages, with those asked for before it, exceed
  * the free ones, and (packed slots) every request with n > 0 from the first one on whose tokens, with those asked for before it, exceed

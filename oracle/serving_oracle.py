@@ -94,7 +94,8 @@ def verify_chain(tokens, target, draft, uniforms):
 
 def extend_tables(table, context, new_len, free, free_count, size, slot_width, extra, packed):
     """Returns (table, context, free, free_count, granted, slots, offsets): new arrays; packed slots hold only the tokens placed."""
-    table, free = table.copy(), list(int(x) for x in free[:max(0, min(int(free_count), len(free)))])
+    pages = len(free)
+    table, free = table.copy(), list(int(x) for x in free[:max(0, min(int(free_count), pages))])
     B, width = table.shape
     context = np.maximum(np.asarray(context, dtype=np.int64), 0)
     after = context.copy()
@@ -103,6 +104,7 @@ def extend_tables(table, context, new_len, free, free_count, size, slot_width, e
         if new_len[b] < 0:
             free += [int(x) for x in table[b, :min(-(-int(context[b]) // size), width)]]
             after[b] = 0
+    free = free[:pages]                            # the list holds no more
     top, asked, tokens, taken, placed = len(free), 0, 0, 0, 0
     rows, offsets = [], [0]
     for b in range(B):
