@@ -567,6 +567,13 @@ def _whole(dev, dtype, **tensors):
             raise ValueError(f"{name} must be a contiguous tensor {list(shape)}, got {list(t.shape)} with strides {list(t.stride())}")
 
 
+def _int32(**numbers):
+    """Numbers that the library takes in 32 bits: ctypes would cut others off without a word."""
+    for name, x in numbers.items():
+        if not -2 ** 31 <= x < 2 ** 31:
+            raise ValueError(f"{name} must fit 32 bits, got {x}")
+
+
 def _row_stride(name, t, lead, inner):
     """Elements between the rows of a tensor [*lead, *inner] whose rows (the inner dimensions) are contiguous and whose leading
     dimensions follow each other."""
@@ -727,6 +734,10 @@ def mpv_tree_attention(parent, q, tree_k, tree_v, cache_k, cache_v, block_table,
 
 def _attention_plan(parent, q, tree_k, tree_v, cache_k, cache_v, block_table, context_len, scale, window, sinks, num_nodes, tree_parent, out):
     import torch
+    _int32(window=window, sinks=sinks)
+    if tree_parent is None:
+        for n, up in enumerate(parent):
+            _int32(**{f"parent[{n}]": up})
     if q.dim() != 4 or tree_k.dim() != 4 or cache_k.dim() != 4 or block_table.dim() != 2:
         raise ValueError("q, tree_k, tree_v, cache_k and cache_v must have 4 dimensions, block_table 2")
     B, N, heads, head_dim = q.shape
@@ -791,6 +802,7 @@ def mpv_verify_chains(tokens, target_probs, draft_probs, uniforms, num_nodes=Non
 
 def _chains_plan(tokens, target_probs, draft_probs, uniforms, num_nodes, max_depth, out):
     import torch
+    _int32(max_depth=max_depth)
     if target_probs.dim() != 3:
         raise ValueError("target_probs must be [B,N,V]")
     B, N, V = target_probs.shape
@@ -864,6 +876,7 @@ def mpv_extend_tables(block_table, context_len, new_len, free_pages, free_count,
 
 def _tables_plan(block_table, context_len, new_len, free_pages, free_count, page_size, slot_map, extra, after, left, out):
     import torch
+    _int32(page_size=page_size, extra=extra)
     if block_table.dim() != 2 or free_pages.dim() != 1 or slot_map.dim() not in (1, 2):
         raise ValueError("block_table must be [B,table_width], free_pages [num_pages], slot_map [B,n] or [n]")
     B, width = block_table.shape
