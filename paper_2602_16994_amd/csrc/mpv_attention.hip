@@ -108,10 +108,10 @@ __device__ const uint4 kZeros[MPV_MAX_HEAD_DIM * 4 / 16] = {};
 // wait for all such loads in flight before it reads LDS through ds_read_b64_tr_b16, the next tile's among them.  Nothing but `arrive`
 // waits for them.  (A load that goes to LDS may follow a write of m0 after one wait state.)
 __device__ __forceinline__ void to_lds(uint64_t from, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory", "m0");
 }
 __device__ __forceinline__ void word_to_lds(uint64_t from, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory", "m0");
 }
 // A place in LDS.  (The pass for the host, which never runs it, has pointers of 64 bits.)
 #pragma clang diagnostic push
