@@ -359,13 +359,19 @@ __global__ void clear_counters_kernel(uint32_t* counters) {
     if (threadIdx.x < MPV_COUNTER_COUNT) counters[threadIdx.x] = 0;
 }
 
-// Workgroups a chain.  One (of 1024 threads) where the chains alone nearly fill the device: 256 chains of 151 937 bfloat16 tokens
-// take 24.4 us, 30.0 with eight parts each; 200 of them 20.7 against 24.1; but 128 of 128 256 float32 tokens with a draft 38.6 against
-// 32.2, and one of 151 937 tokens 22.2 against 9.4.  Otherwise 2048 in all (half as many: 64 chains of 128 256 tokens in 19.3 us against
-// 18.7), none with fewer than 2048 tokens (4096: 16 chains of 32 000 tokens in 10.4 us against 9.5; 1024: 9.2, but 9.8 against 9.4 for
-// one of 151 937, whose sums the draw then has to add up).
-static int parts_of(const mpv_chains* c) {
-    if (c->B >= 192) return 1;
+// Workgroups a chain.  One (of 1024 threads) where the chains alone nearly fill the device; more of them are needed where a chain has two
+// long rows to read, so that those of the compute units that would have none are missed.  us with one / with parts, rows of 128 256 tokens
+// (in brackets: of 32 000),
+//   with a draft     float32: 128 chains 38.6 / 32.2, 192: 35.6 / 32.7 (15.4 / 15.4), 239: 40.3 / 39.5 (16.5 / 17.7), 256: 41.9 / 41.8 (17.0 / 17.8)
+//                    bfloat16: 192 chains 28.0 / 23.8 (15.0 / 15.4), 239: 29.8 / 27.4 (15.8 / 16.5), 256: 30.3 / 29.5 (16.2 / 16.2)
+//                    (of 262 144 tokens, float32: 208 chains 74.1 / 74.8, 240: 77.4 / 83.4; bfloat16: 43.1 / 40.2, 46.2 / 45.2)
+//   without          float32: 96 chains 18.7 / 18.5 (11.5 / 10.7), 144: 21.2 / 22.4 (12.2 / 13.1), 256: 29.8 / 33.4 (14.5 / 16.0)
+//                    bfloat16: 96 chains 18.1 / 16.8 (11.8 / 11.5), 144: 18.8 / 19.6 (12.1 / 13.4), 256: 21.5 / 25.4 (12.5 / 15.4)
+// One of 151 937 tokens takes 22.2 us with one, 9.4 with parts.  Otherwise 2048 workgroups in all (half as many: 64 chains of 128 256 tokens in
+// 19.3 us against 18.7), none with fewer than 2048 tokens (4096: 16 chains of 32 000 tokens in 10.4 us against 9.5; 1024: 9.2, but 9.8
+// against 9.4 for one of 151 937, whose sums the draw then has to add up).
+static int parts_of(const mpv_chains* c, bool draft) {
+    if (c->B >= (!draft ? 144 : c->V < 65536 ? 192 : 240)) return 1;
     const int most = (c->V + 2047) / 2048, wanted = c->B > 0 ? (2048 + c->B - 1) / c->B : 1;
     return most < wanted ? most : wanted;
 }
@@ -401,7 +407,7 @@ int mpv_verify_chains_workspace_bytes(const mpv_chains* chains, size_t* out) {
     if (!out) return MPV_ERR_NULL;
     const int rc = mpv::check_chains(chains);
     if (rc != MPV_OK) return rc;
-    const size_t sums = static_cast<size_t>(chains->B) * mpv::parts_of(chains) * sizeof(double);
+    const size_t sums = static_cast<size_t>(chains->B) * mpv::parts_of(chains, true) * sizeof(double);      // (without a draft: no more)
     *out = (sums + 255) / 256 * 256 + 256;
     return MPV_OK;
 }
@@ -422,7 +428,7 @@ int mpv_verify_chains(const mpv_chains* chains, const mpv_chain_buffers* buf, vo
     if (!workspace || !mpv::aligned(workspace, 256) || workspace_bytes < need) return MPV_ERR_WORKSPACE;
     mpv::ChainArgs a;
     a.c = *chains; a.b = *buf;
-    a.parts = mpv::parts_of(chains);
+    a.parts = mpv::parts_of(chains, buf->draft_probs != nullptr);
     a.part = (chains->V + a.parts - 1) / a.parts;
     a.part = (a.part + 7) / 8 * 8;
     a.sums = static_cast<double*>(workspace);

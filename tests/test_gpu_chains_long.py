@@ -9,10 +9,10 @@ from tests.test_gpu_chains import TYPES, check, make
 
 pytestmark = pytest.mark.gpu
 
-# One workgroup a chain: a wave's share of a row takes several rounds of four loads a lane (20 011: some lanes one, most two), and the
-# share that is drawn from several groups of 16 bytes a lane (from 65 536 tokens of 4 bytes, 131 072 of 2 on).  Several a chain: parts of
-# 8016 and of 10 853 tokens, of which the same holds.
-SIZES = [(192, 3, 20011), (192, 2, 151937), (128, 2, 128256), (150, 2, 151937)]
+# One workgroup a chain (without a draft from 144 chains on, with one from 192, or 240 of long rows): a wave's share of a row takes several
+# rounds of four loads a lane (20 011: some lanes one, most two), and the share that is drawn from several groups of 16 bytes a lane (from
+# 65 536 tokens of 4 bytes, 131 072 of 2 on).  Several a chain: parts of 8016 and of 10 856 tokens, of which the same holds.
+SIZES = [(192, 3, 20011), (192, 2, 151937), (128, 2, 128256), (150, 2, 151937), (240, 3, 20011), (241, 2, 151937)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -25,7 +25,7 @@ def test_long_rows(B, N, V, draft, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("draft", [True, False])
-@pytest.mark.parametrize("B", [9, 195])
+@pytest.mark.parametrize("B", [9, 143, 144, 195, 239, 240])
 def test_long_rows_apart_and_ragged_chains(B, draft, dtype):
     print("[case] long and ragged", B, draft, dtype, flush=True)
     tokens, p, q, u = make(B, 4, 9001, dtype, draft, seed=B, pad=5)
@@ -34,7 +34,7 @@ def test_long_rows_apart_and_ragged_chains(B, draft, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("draft", [True, False])
-@pytest.mark.parametrize("B,V", [(6, 8191), (6, 32001), (192, 9001)])
+@pytest.mark.parametrize("B,V", [(6, 8191), (6, 32001), (192, 9001), (250, 9001)])
 def test_tokens_out_of_range_and_long_rows_without_mass(B, V, draft, dtype):
     print("[case] long bad rows", B, V, draft, dtype, flush=True)
     tokens, p, q, u = make(B, 4, V, dtype, draft, seed=4)
@@ -50,7 +50,7 @@ def test_tokens_out_of_range_and_long_rows_without_mass(B, V, draft, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("u0", [0.0, 1.0 - 2.0 ** -24])
-@pytest.mark.parametrize("B,V", [(6, 8191), (6, 32001), (192, 9001)])
+@pytest.mark.parametrize("B,V", [(6, 8191), (6, 32001), (192, 9001), (250, 9001)])
 def test_long_rows_and_uniforms_at_the_ends(B, V, u0, dtype):
     print("[case] long ends", B, V, u0, dtype, flush=True)
     tokens, p, q, u = make(B, 3, V, dtype, True, seed=3)
@@ -60,7 +60,7 @@ def test_long_rows_and_uniforms_at_the_ends(B, V, u0, dtype):
     check(tokens, p, q, u)
 
 
-@pytest.mark.parametrize("B,V", [(6, 32001), (192, 9001)])
+@pytest.mark.parametrize("B,V", [(6, 32001), (192, 9001), (250, 9001)])
 def test_a_row_whose_mass_is_one_token(B, V):
     print("[case] one token", B, V, flush=True)
     tokens, p, q, u = make(B, 2, V, torch.float32, False, seed=5)
