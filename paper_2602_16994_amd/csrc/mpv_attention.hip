@@ -1056,13 +1056,19 @@ static int with_kernel(const mpv_attention* a, AttentionArgs* g, void* workspace
                                       static_cast<int>(sizeof(typename A::Shared)))))
         return MPV_ERR_HIP;
     hipLaunchKernelGGL(attention_kernel<A>, dim3(static_cast<unsigned>(c.teams) * c.blocks), dim3(A::kThreads), sizeof(typename A::Shared), s, *g);
-    // a list with one tile a unit shares none.  Few parts a unit: `some` rows a workgroup; many, which only units that are fewer than
-    // the teams can have: a row, up to 4096 workgroups.
+    // A list with one tile a unit shares none.  Few parts a unit: `some` rows a workgroup, and that is all where no unit has more tiles than
+    // that.  Many, as a unit can have that is one of few or much longer than the others: a row, up to 4096 workgroups, or 16 384 where units are
+    // not fewer than the teams and the block table has room for long ones (300 trees of 41 nodes on 2 heads, one context of 131 072 and 299 of
+    // 100: 106 us, 136 with 4096; 100 trees of 7 nodes on 8 heads with one such: 142, 144; the benchmark's trees: the same, 65 536 workgroups
+    // cost them 2 %; 256 trees of 8 nodes, contexts of 16 to 256 in a table with room for 320: 62.2 with 4096, 65.7 with 16 384).
+    constexpr int kLongTiles = 64;
     constexpr int kSome = kFewRows * 4 * (64 / (DP / 4));
     const int64_t units = static_cast<int64_t>(a->B) * a->kv_heads, few = (rows + kSome - 1) / kSome;
     const int64_t entries = g->by_unit ? units : c.teams;
+    const int64_t workgroups = g->by_unit || c.tiles <= units * kLongTiles ? 4096 : 16384;
+    const int64_t most = c.tiles > units * kFewParts ? std::min(rows, workgroups / entries) : 0;
     if (c.tiles > units)
-        hipLaunchKernelGGL((combine_kernel<DTYPE, DP, A::kRows>), dim3(static_cast<unsigned>(entries), static_cast<unsigned>(std::max(few, std::min(rows, 4096 / entries)))),
+        hipLaunchKernelGGL((combine_kernel<DTYPE, DP, A::kRows>), dim3(static_cast<unsigned>(entries), static_cast<unsigned>(std::max(few, most))),
                            dim3(256), 0, s, *g);
     return launched();
 }
