@@ -347,6 +347,8 @@ int mpv_fill_uniforms(uint64_t seed, int64_t count, float* d_u, void* hip_stream
  * Position j of tree b lies in page block_table[b, j / page_size], slot j % page_size; a page outside
  * [0, num_pages) is not seen, context_len is taken within [0, table_width * page_size].
  * What a node does not see does not reach its output, whatever it holds (NaN included).
+ * An infinite value or NaN that it does see makes that column of its output infinite or NaN; which of them an infinity makes whose
+ * weight is too small for float32 (or, rounded, for `dtype`) depends on where the tree's tiles end.
  * Sums and softmax statistics are float32; weights are rounded to `dtype` before they meet the values (F32: not). */
 typedef struct mpv_attention {
     int32_t B, N;            /* trees; nodes per tree (<= MPV_MAX_NODES); N = 1: single tokens               */
