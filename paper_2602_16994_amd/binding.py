@@ -214,6 +214,47 @@ def _stream_ptr(stream):
     return ctypes.c_void_p(stream.cuda_stream)
 
 
+_nothing = contextlib.nullcontext()
+
+
+def _allocating(stream):
+    """What a call allocates, its results and workspace, is allocated on the stream that it runs on: memory that was given back on
+    another one may still be in use by work that was enqueued there before, and the call's stream does not wait for that."""
+    if stream is None:
+        return _nothing
+    import torch
+    return torch.cuda.stream(stream)
+
+
+def _workspace(out, need, device, stream, raw):
+    """out.workspace, of at least `need` bytes, for a call on `stream` (handle `raw`)."""
+    import torch
+    ws = out.workspace
+    if ws is None or ws.numel() < need or ws.get_device() != device:
+        with _allocating(stream):
+            ws = out.workspace = torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", device))
+    elif getattr(out, "_workspace_stream", None) != raw:           # it is used on another stream than the one before
+        ws.record_stream(torch.cuda.current_stream() if stream is None else stream)
+    out._workspace_stream = raw
+    return ws
+
+
+def _used_on(stream, out, workspace=None):
+    """Tells the allocator of a call on `stream`: what was allocated elsewhere is in use there, and results that were allocated on it are
+    used on the current one next; neither must be given away before that is done."""
+    import torch
+    if stream is None:
+        return
+    current = torch.cuda.current_stream()
+    if stream.cuda_stream == current.cuda_stream:
+        return
+    for t in out:
+        if isinstance(t, torch.Tensor) and t.is_cuda:
+            t.record_stream(stream)
+            if t is not workspace:
+                t.record_stream(current)
+
+
 def _dtype_id(t):
     import torch
     if t.dtype == torch.float32:
@@ -310,21 +351,22 @@ def mpv_verify(parent, tokens, target_logits, draft_logits, temperature, uniform
     prob = _make_problem(B, N, V, method, _dtype_id(target_logits), temperature, max_depth, parent)
     if out is None:
         i32 = dict(dtype=torch.int32, device=dev)
-        out = VerifyResult(
-            accept_len=torch.empty(B, **i32),
-            path_nodes=torch.empty(B, max_depth, **i32),
-            path_tokens=torch.empty(B, max_depth, **i32),
-            bonus_token=torch.empty(B, **i32),
-            counters=torch.empty(8, dtype=torch.int32, device=dev),
-        )
-        if debug:
-            f32 = dict(dtype=torch.float32, device=dev)
-            if method in (MPV_METHOD_SPECINFER, MPV_METHOD_TRAVERSAL):
-                out.stats = torch.empty(B, N, 4, **f32)
-                out.edge_probs = torch.empty(B, N, 2, **f32)
-            out.accept_prob = torch.empty(B, N, **f32)
-            out.final_residual = torch.empty(B, V, **f32)
-    lib = load_library()
+        with _allocating(stream):
+            out = VerifyResult(
+                accept_len=torch.empty(B, **i32),
+                path_nodes=torch.empty(B, max_depth, **i32),
+                path_tokens=torch.empty(B, max_depth, **i32),
+                bonus_token=torch.empty(B, **i32),
+                counters=torch.empty(8, dtype=torch.int32, device=dev),
+            )
+            if debug:
+                f32 = dict(dtype=torch.float32, device=dev)
+                if method in (MPV_METHOD_SPECINFER, MPV_METHOD_TRAVERSAL):
+                    out.stats = torch.empty(B, N, 4, **f32)
+                    out.edge_probs = torch.empty(B, N, 2, **f32)
+                out.accept_prob = torch.empty(B, N, **f32)
+                out.final_residual = torch.empty(B, V, **f32)
+    lib, on = load_library(), _stream_ptr(stream)
 
     def ptr(t):
         return ctypes.c_void_p(t.data_ptr()) if t is not None else ctypes.c_void_p(0)
@@ -334,11 +376,9 @@ def mpv_verify(parent, tokens, target_logits, draft_logits, temperature, uniform
         rc = lib.mpv_workspace_bytes(ctypes.byref(prob), ctypes.byref(need))
         if rc != 0:
             raise MpvError(rc, "mpv_workspace_bytes")
-        if workspace is None:
-            workspace = out.workspace
-        if workspace is None or workspace.numel() < need.value:
-            workspace = torch.empty(max(need.value, 256), dtype=torch.uint8, device=dev)
-        out.workspace = workspace
+        if workspace is not None and workspace is not out.workspace:
+            out.workspace, out._workspace_stream = workspace, None
+        workspace = _workspace(out, max(need.value, 256), target_logits.get_device(), stream, on.value)
 
     bufs = _Buffers(ptr(target_logits), ptr(draft_logits), ptr(tokens), ptr(uniforms),
                     ptr(out.accept_len), ptr(out.path_nodes), ptr(out.path_tokens),
@@ -354,17 +394,19 @@ def mpv_verify(parent, tokens, target_logits, draft_logits, temperature, uniform
                                          or context_node.dtype != torch.int32 or tuple(context_node.shape) != (B, N)):
             raise ValueError("context_node must be a contiguous int32 CUDA tensor [B,N]")
         rc = lib.mpv_verify_merged(ctypes.byref(prob), rows.ctypes.data, ptr(context_node), ctypes.byref(bufs),
-                                   ptr(workspace), ctypes.c_size_t(workspace.numel()), _stream_ptr(stream))
+                                   ptr(workspace), ctypes.c_size_t(workspace.numel()), on)
         if rc != 0:
             raise MpvError(rc, "mpv_verify_merged")
+        _used_on(stream, vars(out).values(), workspace)
         return out
     if static_scratch:
-        rc = lib.mpv_verify_static(ctypes.byref(prob), ctypes.byref(bufs), _stream_ptr(stream))
+        rc = lib.mpv_verify_static(ctypes.byref(prob), ctypes.byref(bufs), on)
     else:
         rc = lib.mpv_verify(ctypes.byref(prob), ctypes.byref(bufs), ptr(workspace),
-                            ctypes.c_size_t(workspace.numel()), _stream_ptr(stream))
+                            ctypes.c_size_t(workspace.numel()), on)
     if rc != 0:
         raise MpvError(rc, "mpv_verify_static" if static_scratch else "mpv_verify")
+    _used_on(stream, vars(out).values(), workspace)
     return out
 
 
@@ -400,18 +442,18 @@ def mpv_block_efficiency(parent, tokens, target_logits, draft_logits, temperatur
     dev = target_logits.device
     max_depth = max(1, tree_depth(list(parent)) if len(parent) == N and N > 0 else 1)
     prob = _make_problem(B, N, V, method, _dtype_id(target_logits), temperature, max_depth, parent)
-    lib = load_library()
+    lib, on = load_library(), _stream_ptr(stream)
     need = ctypes.c_size_t(0)
     rc = lib.mpv_workspace_bytes(ctypes.byref(prob), ctypes.byref(need))
     if rc != 0:
         raise MpvError(rc, "mpv_workspace_bytes")
     if out is None:
-        out = BlockEfficiencyResult(
-            expected=torch.empty(B, dtype=torch.float32, device=dev),
-            reach_prob=torch.empty(B, N, dtype=torch.float32, device=dev),
-            counters=torch.empty(8, dtype=torch.int32, device=dev))
-    if out.workspace is None or out.workspace.numel() < need.value:
-        out.workspace = torch.empty(max(need.value, 256), dtype=torch.uint8, device=dev)
+        with _allocating(stream):
+            out = BlockEfficiencyResult(
+                expected=torch.empty(B, dtype=torch.float32, device=dev),
+                reach_prob=torch.empty(B, N, dtype=torch.float32, device=dev),
+                counters=torch.empty(8, dtype=torch.int32, device=dev))
+    _workspace(out, max(need.value, 256), target_logits.get_device(), stream, on.value)
 
     def ptr(t):
         return ctypes.c_void_p(t.data_ptr()) if t is not None else ctypes.c_void_p(0)
@@ -426,15 +468,17 @@ def mpv_block_efficiency(parent, tokens, target_logits, draft_logits, temperatur
             raise ValueError("context_node must be a contiguous int32 CUDA tensor [B,N]")
         rc = lib.mpv_block_efficiency_merged(ctypes.byref(prob), rows.ctypes.data, ptr(context_node), ptr(target_logits), ptr(draft_logits),
                                              ptr(tokens), ptr(out.workspace), ctypes.c_size_t(out.workspace.numel()),
-                                             ptr(out.reach_prob), ptr(out.expected), ptr(out.counters), _stream_ptr(stream))
+                                             ptr(out.reach_prob), ptr(out.expected), ptr(out.counters), on)
         if rc != 0:
             raise MpvError(rc, "mpv_block_efficiency_merged")
+        _used_on(stream, vars(out).values(), out.workspace)
         return out
     rc = lib.mpv_block_efficiency(ctypes.byref(prob), ptr(target_logits), ptr(draft_logits), ptr(tokens),
                                   ptr(out.workspace), ctypes.c_size_t(out.workspace.numel()),
-                                  ptr(out.reach_prob), ptr(out.expected), ptr(out.counters), _stream_ptr(stream))
+                                  ptr(out.reach_prob), ptr(out.expected), ptr(out.counters), on)
     if rc != 0:
         raise MpvError(rc, "mpv_block_efficiency")
+    _used_on(stream, vars(out).values(), out.workspace)
     return out
 
 
@@ -458,9 +502,10 @@ def mpv_acceptance_rates(parent, target_logits, draft_logits, temperature, metho
     rc = lib.mpv_workspace_bytes(ctypes.byref(prob), ctypes.byref(need))
     if rc != 0:
         raise MpvError(rc, "mpv_workspace_bytes")
-    workspace = torch.empty(max(need.value, 256), dtype=torch.uint8, device=dev)
-    alpha = torch.empty(B, N, dtype=torch.float32, device=dev)
-    counters = torch.empty(8, dtype=torch.int32, device=dev)
+    with _allocating(stream):
+        workspace = torch.empty(max(need.value, 256), dtype=torch.uint8, device=dev)
+        alpha = torch.empty(B, N, dtype=torch.float32, device=dev)
+        counters = torch.empty(8, dtype=torch.int32, device=dev)
     if merged_parent is not None:
         import numpy as np
         rows = np.ascontiguousarray(np.asarray(merged_parent), dtype=np.int32)
@@ -472,6 +517,7 @@ def mpv_acceptance_rates(parent, target_logits, draft_logits, temperature, metho
                                              ctypes.c_void_p(counters.data_ptr()), _stream_ptr(stream))
         if rc != 0:
             raise MpvError(rc, "mpv_acceptance_rates_merged")
+        _used_on(stream, (alpha, counters))
         return alpha, counters
     rc = lib.mpv_acceptance_rates(ctypes.byref(prob), ctypes.c_void_p(target_logits.data_ptr()),
                                   ctypes.c_void_p(draft_logits.data_ptr()), ctypes.c_void_p(workspace.data_ptr()),
@@ -479,6 +525,7 @@ def mpv_acceptance_rates(parent, target_logits, draft_logits, temperature, metho
                                   ctypes.c_void_p(counters.data_ptr()), _stream_ptr(stream))
     if rc != 0:
         raise MpvError(rc, "mpv_acceptance_rates")
+    _used_on(stream, (alpha, counters))
     return alpha, counters
 
 
@@ -491,19 +538,21 @@ def mpv_nucleus_mask(logits, temperature, top_p, out=None, inplace=False, stream
         raise ValueError("logits must be a contiguous CUDA tensor")
     V = logits.shape[-1]
     rows = logits.numel() // V if V else 0
-    if inplace:
-        out = logits
-    elif out is None:
-        out = torch.empty_like(logits)
     lead = tuple(logits.shape[:-1])
-    thr = torch.empty(lead, dtype=torch.float32, device=logits.device)
-    kept = torch.empty(lead, dtype=torch.int32, device=logits.device)
+    with _allocating(stream):
+        if inplace:
+            out = logits
+        elif out is None:
+            out = torch.empty_like(logits)
+        thr = torch.empty(lead, dtype=torch.float32, device=logits.device)
+        kept = torch.empty(lead, dtype=torch.int32, device=logits.device)
     rc = load_library().mpv_nucleus_mask(ctypes.c_void_p(logits.data_ptr()), ctypes.c_void_p(out.data_ptr()),
                                          _dtype_id(logits), rows, V, float(temperature), float(top_p),
                                          ctypes.c_void_p(thr.data_ptr()), ctypes.c_void_p(kept.data_ptr()),
                                          _stream_ptr(stream))
     if rc != 0:
         raise MpvError(rc, "mpv_nucleus_mask")
+    _used_on(stream, (out, thr, kept))
     return out, thr, kept
 
 
@@ -514,11 +563,13 @@ def mpv_row_stats(logits, temperature, out=None, stream=None):
         raise ValueError("logits must be a contiguous 2-D CUDA tensor")
     rows, V = logits.shape
     if out is None:
-        out = torch.empty(rows, 2, dtype=torch.float32, device=logits.device)
+        with _allocating(stream):
+            out = torch.empty(rows, 2, dtype=torch.float32, device=logits.device)
     rc = load_library().mpv_row_stats(ctypes.c_void_p(logits.data_ptr()), _dtype_id(logits), rows, V,
                                       float(temperature), ctypes.c_void_p(out.data_ptr()), _stream_ptr(stream))
     if rc != 0:
         raise MpvError(rc, "mpv_row_stats")
+    _used_on(stream, (out,))
     return out
 
 
@@ -526,11 +577,13 @@ def mpv_fill_uniforms(seed, count, out=None, device="cuda", stream=None):
     """count counter-based uniforms in [0,1) from `seed` (see include/mpv.h)."""
     import torch
     if out is None:
-        out = torch.empty(count, dtype=torch.float32, device=device)
+        with _allocating(stream):
+            out = torch.empty(count, dtype=torch.float32, device=device)
     rc = load_library().mpv_fill_uniforms(ctypes.c_uint64(seed & (2 ** 64 - 1)), int(count),
                                           ctypes.c_void_p(out.data_ptr()), _stream_ptr(stream))
     if rc != 0:
         raise MpvError(rc, "mpv_fill_uniforms")
+    _used_on(stream, (out,))
     return out
 
 
@@ -649,18 +702,6 @@ def _like(t):
     return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
 
 
-_nothing = contextlib.nullcontext()
-
-
-def _allocating(stream):
-    """What a call allocates, its results and workspace, is allocated on the stream that it runs on: memory that was given back on
-    another one may still be in use by work that was enqueued there before, and the call's stream does not wait for that."""
-    if stream is None:
-        return _nothing
-    import torch
-    return torch.cuda.stream(stream)
-
-
 def _launch(plan, bufs, out, stream):
     """The call on its tensors' device; its workspace, if it has one, is kept in out.workspace."""
     import torch
@@ -676,26 +717,12 @@ def _launch(plan, bufs, out, stream):
     if plan.need is None:
         rc = plan.call(plan.address, ctypes.byref(bufs), raw)
     else:
-        ws = out.workspace
-        if ws is None or ws.numel() < plan.need or ws.get_device() != plan.device:
-            with _allocating(stream):
-                ws = out.workspace = torch.empty(plan.need, dtype=torch.uint8, device=torch.device("cuda", plan.device))
-            out._workspace_stream = raw
-        elif getattr(out, "_workspace_stream", None) != raw:       # it is used on another stream than the one before
-            ws.record_stream(torch.cuda.current_stream() if stream is None else stream)
-            out._workspace_stream = raw
+        ws = _workspace(out, plan.need, plan.device, stream, raw)
         rc = plan.call(plan.address, ctypes.byref(bufs), ws.data_ptr(), ws.numel(), raw)
     if rc != 0:
         raise MpvError(rc, plan.name)
-    if stream is not None and out is not None and raw != torch.cuda.current_stream().cuda_stream:
-        # what was allocated elsewhere is in use on this stream, and results that were allocated on it are used on the current one next:
-        # neither must be given away before that is done
-        current = torch.cuda.current_stream()
-        for t in vars(out).values():
-            if isinstance(t, torch.Tensor) and t.is_cuda:
-                t.record_stream(stream)
-                if t is not out.workspace:
-                    t.record_stream(current)
+    if stream is not None and out is not None:
+        _used_on(stream, vars(out).values(), out.workspace)
     return out
 
 
