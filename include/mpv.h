@@ -440,7 +440,8 @@ typedef struct mpv_tables {
     int32_t extra;                /* >= 0, added to every new_len that is not negative                       */
     int32_t packed;               /* 0: slot_map[b * slot_width + i], -1 behind a request's tokens;
                                      1: slot_map[offsets[b] + i], `slot_width` slots in all, what lies behind the last
-                                     token is left as it was                                                  */
+                                     token is left as it was: for a pass over prompts, one row a token, that writes its keys and values
+                                     itself (mpv_append_paths takes rows of slots)                            */
     int64_t slot_width;
 } mpv_tables;
 

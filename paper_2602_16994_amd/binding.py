@@ -871,17 +871,18 @@ def mpv_extend_tables(block_table, context_len, new_len, free_pages, free_count,
     """
     import torch
     # a result's lengths and count are written again unless they are a caller's tensors: those of a call in place, or this call's inputs
-    after, left = (None, None) if out is None else (out.context_len, out.free_count)
+    lengths, count = context_len.data_ptr(), free_count.data_ptr()
+    after = left = None
     if inplace:
         after, left = context_len, free_count
-    elif out is not None and (out.inplace or after.data_ptr() == context_len.data_ptr() or left.data_ptr() == free_count.data_ptr()):
-        after = left = None
+    elif out is not None and not out.inplace and out.context_len.data_ptr() != lengths and out.free_count.data_ptr() != count:
+        after, left = out.context_len, out.free_count
     key = ("tables", page_size, extra, _like(block_table), _like(context_len), _like(new_len), _like(free_pages), _like(free_count),
            _like(slot_map), _like(after), _like(left), None if out is None else (_like(out.granted), _like(out.offsets)))
     plan = _plans.get(key)
     if plan is None:
         plan = _kept(key, _tables_plan(block_table, context_len, new_len, free_pages, free_count, page_size, slot_map, extra, after, left, out))
-    if out is None or after is None:
+    if after is None or out is None:
         B, i32 = block_table.shape[0], dict(dtype=torch.int32, device=block_table.device)
         with _allocating(stream):
             if after is None:
@@ -890,9 +891,8 @@ def mpv_extend_tables(block_table, context_len, new_len, free_pages, free_count,
                 out = TablesResult(context_len=after, free_count=left, granted=torch.empty(B, **i32), slot_map=slot_map,
                                    offsets=torch.empty(B + 1, **i32))
     out.context_len, out.free_count, out.slot_map, out.inplace = after, left, slot_map, inplace
-    bufs = _TableBuffers(new_len.data_ptr(), context_len.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
-                         out.context_len.data_ptr(), out.free_count.data_ptr(), slot_map.data_ptr(), out.granted.data_ptr(),
-                         out.offsets.data_ptr())
+    bufs = _TableBuffers(new_len.data_ptr(), lengths, block_table.data_ptr(), free_pages.data_ptr(), count, after.data_ptr(), left.data_ptr(),
+                         slot_map.data_ptr(), out.granted.data_ptr(), out.offsets.data_ptr())
     _launch(plan, bufs, out, stream)
     if not block_table.shape[0]:                   # the library writes nothing then
         with _allocating(stream):
