@@ -1059,9 +1059,8 @@ static int with_kernel(const mpv_attention* a, AttentionArgs* g, void* workspace
     // A list with one tile a unit shares none.  Few parts a unit: `some` rows a workgroup, and that is all where no unit has more tiles than
     // that.  Many, as a unit can have that is one of few or much longer than the others: a row, up to 4096 workgroups, or 16 384 where units are
     // not fewer than the teams and the block table has room for long ones (300 trees of 41 nodes on 2 heads, one context of 131 072 and 299 of
-    // 100: 106 us, 136 with 4096; 100 trees of 7 nodes on 8 heads with one such: 142, 144; the benchmark's trees, which need none of them: 21.5 us
-    // of some 610 for this launch, 19 with 4096, and with 65 536 the whole takes 2 % more; 256 trees of 8 nodes, contexts of 16 to 256 in a table
-    // with room for 320: 62.2 with 4096, 65.7 with 16 384).
+    // 100: 106 us, 118 with 8192, 135 with 4096; 100 trees of 7 nodes on 8 heads with one such: 142, 141, 143; the benchmark's trees, which need none
+    // of them: 616 with each, 2 % more with 65 536; 256 trees of 8 nodes, contexts of 16 to 256 in a table with room for 320: 65.7, 63.5, 62.2).
     constexpr int kLongTiles = 64;
     constexpr int kSome = kFewRows * 4 * (64 / (DP / 4));
     const int64_t units = static_cast<int64_t>(a->B) * a->kv_heads, few = (rows + kSome - 1) / kSome;
