@@ -255,6 +255,12 @@ def _used_on(stream, out, workspace=None):
                 t.record_stream(current)
 
 
+def _no_counts(stream, counters):
+    """The counters of a batch of none: the library writes nothing then."""
+    with _allocating(stream):
+        counters.zero_()
+
+
 def _dtype_id(t):
     import torch
     if t.dtype == torch.float32:
@@ -366,6 +372,8 @@ def mpv_verify(parent, tokens, target_logits, draft_logits, temperature, uniform
                     out.edge_probs = torch.empty(B, N, 2, **f32)
                 out.accept_prob = torch.empty(B, N, **f32)
                 out.final_residual = torch.empty(B, V, **f32)
+    if not B:
+        _no_counts(stream, out.counters)
     lib, on = load_library(), _stream_ptr(stream)
 
     def ptr(t):
@@ -454,6 +462,8 @@ def mpv_block_efficiency(parent, tokens, target_logits, draft_logits, temperatur
                 reach_prob=torch.empty(B, N, dtype=torch.float32, device=dev),
                 counters=torch.empty(8, dtype=torch.int32, device=dev))
     _workspace(out, max(need.value, 256), target_logits.get_device(), stream, on.value)
+    if not B:
+        _no_counts(stream, out.counters)
 
     def ptr(t):
         return ctypes.c_void_p(t.data_ptr()) if t is not None else ctypes.c_void_p(0)
@@ -506,6 +516,8 @@ def mpv_acceptance_rates(parent, target_logits, draft_logits, temperature, metho
         workspace = torch.empty(max(need.value, 256), dtype=torch.uint8, device=dev)
         alpha = torch.empty(B, N, dtype=torch.float32, device=dev)
         counters = torch.empty(8, dtype=torch.int32, device=dev)
+    if not B:
+        _no_counts(stream, counters)
     if merged_parent is not None:
         import numpy as np
         rows = np.ascontiguousarray(np.asarray(merged_parent), dtype=np.int32)
@@ -821,9 +833,8 @@ def mpv_verify_chains(tokens, target_probs, draft_probs, uniforms, num_nodes=Non
                          out.accept_len.data_ptr(), out.path_nodes.data_ptr(), out.path_tokens.data_ptr(), out.bonus_token.data_ptr(),
                          out.counters.data_ptr())
     _launch(plan, bufs, out, stream)
-    if not target_probs.shape[0]:                  # the library writes nothing then
-        with _allocating(stream):
-            out.counters.zero_()
+    if not target_probs.shape[0]:
+        _no_counts(stream, out.counters)
     return out
 
 

@@ -39,7 +39,7 @@ def calls():
 
 def keep_busy(stream, buffer):
     with torch.cuda.stream(stream):
-        for _ in range(600):                       # some 60 ms
+        for _ in range(1500):                      # some 160 ms
             buffer += 1.0
 
 
