@@ -387,6 +387,34 @@ int mpv_tree_attention_workspace_bytes(const mpv_attention* attention, size_t* o
 int mpv_tree_attention(const mpv_attention* attention, const mpv_attention_buffers* buffers,
                        void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* The same behind prefixes that requests share (a system prompt, a document): tree b's positions begin with those of prefix
+ * prefix_of[b], the positions of its own context follow, then its nodes: node n is at prefix_len + context_len[b] + depth(n), and window
+ * and sinks count from the prefix's first position.  Position j of prefix p lies in page prefix_table[p, j / page_size] of the same cache,
+ * slot j % page_size (a prefix need not fill its last page; a tree's context begins with a page of its own); prefix_len is taken within
+ * [0, prefix_width * page_size].  Trees without a prefix have a prefix_of outside [0, prefixes).
+ * A prefix is read once for up to 64 trees that follow each other with the same prefix_of (at indices that agree in b / 64), whatever the
+ * others have: order the trees by their prefix; any other order gives the same results and reads more.
+ * lse[b,n,h] = ln of the sum of e^s over what node n sees, for query head h; float32, of weights as they are before they are rounded.
+ * Without prefixes it is mpv_tree_attention with lse.  Results may differ from that call's in the last bits. */
+typedef struct mpv_prefixed {
+    mpv_attention attention;
+    int32_t prefixes, prefix_width;   /* rows of prefix_table, pages in a row                                */
+} mpv_prefixed;
+
+typedef struct mpv_prefixed_buffers {     /* DEVICE, borrowed until the work has run */
+    mpv_attention_buffers attention;
+    const int32_t* prefix_of;     /* [B] or NULL: no tree has a prefix                                       */
+    const int32_t* prefix_table;  /* [prefixes,prefix_width]                                                 */
+    const int32_t* prefix_len;    /* [prefixes]                                                              */
+    float* lse;                   /* [B,N,heads] or NULL; rows behind num_nodes[b] are left as they were     */
+} mpv_prefixed_buffers;
+
+int mpv_prefix_attention_workspace_bytes(const mpv_prefixed* prefixed, size_t* out);
+
+/* Errors as those of mpv_tree_attention; _UNSUPPORTED also where prefix, context and tree together are too long. */
+int mpv_prefix_attention(const mpv_prefixed* prefixed, const mpv_prefixed_buffers* buffers,
+                         void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Verification of B chains of drafted tokens against the target's probabilities, from given random numbers
  * (Sec. 3.2 on a tree of one path, with probabilities in the place of logits).  Row n of a chain belongs to the context
  * that ends with its n-th drafted token (row 0: the current context); tokens[b,n], n >= 1, was drafted from draft row

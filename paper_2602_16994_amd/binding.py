@@ -73,6 +73,14 @@ class _AttentionBuffers(ctypes.Structure):
                                                "tree_parent", "out")]
 
 
+class _Prefixed(ctypes.Structure):
+    _fields_ = [("attention", _Attention), ("prefixes", ctypes.c_int32), ("prefix_width", ctypes.c_int32)]
+
+
+class _PrefixedBuffers(ctypes.Structure):
+    _fields_ = [("attention", _AttentionBuffers)] + [(n, ctypes.c_void_p) for n in ("prefix_of", "prefix_table", "prefix_len", "lse")]
+
+
 class _Chains(ctypes.Structure):
     _fields_ = ([(n, ctypes.c_int32) for n in ("B", "N", "V", "dtype", "max_depth")]
                 + [(n, ctypes.c_int64) for n in ("target_stride", "draft_stride")])
@@ -161,8 +169,8 @@ def load_library(path=None):
                                   ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p]
     lib.mpv_fill_uniforms.restype = ctypes.c_int
     lib.mpv_fill_uniforms.argtypes = [ctypes.c_uint64, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p]
-    for name, shape, bufs in (("mpv_tree_attention", _Attention, _AttentionBuffers), ("mpv_verify_chains", _Chains, _ChainBuffers),
-                              ("mpv_extend_tables", _Tables, _TableBuffers)):
+    for name, shape, bufs in (("mpv_tree_attention", _Attention, _AttentionBuffers), ("mpv_prefix_attention", _Prefixed, _PrefixedBuffers),
+                              ("mpv_verify_chains", _Chains, _ChainBuffers), ("mpv_extend_tables", _Tables, _TableBuffers)):
         call, size = getattr(lib, name), getattr(lib, name + "_workspace_bytes")
         call.restype = size.restype = ctypes.c_int
         call.argtypes = [ctypes.POINTER(shape), ctypes.POINTER(bufs), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
@@ -771,7 +779,12 @@ def mpv_tree_attention(parent, q, tree_k, tree_v, cache_k, cache_v, block_table,
     return _launch(plan, bufs, out, stream)
 
 
-def _attention_plan(parent, q, tree_k, tree_v, cache_k, cache_v, block_table, context_len, scale, window, sinks, num_nodes, tree_parent, out):
+def _attention_plan(*args):
+    dev, shape = _attention_shape(*args)
+    return _Plan("mpv_tree_attention", dev.index, shape)
+
+
+def _attention_shape(parent, q, tree_k, tree_v, cache_k, cache_v, block_table, context_len, scale, window, sinks, num_nodes, tree_parent, out):
     import torch
     _int32(window=window, sinks=sinks)
     if tree_parent is None:
@@ -802,10 +815,63 @@ def _attention_plan(parent, q, tree_k, tree_v, cache_k, cache_v, block_table, co
             raise TypeError("out must have the dtype of q")
         out_stride = _row_stride("out", out.out, (B, N), (heads, head_dim))
     arr = (ctypes.c_int32 * N)(*[int(x) for x in parent]) if tree_parent is None else None
-    return _Plan("mpv_tree_attention", dev.index, _Attention(
+    return dev, _Attention(
         B, N, heads, kv_heads, head_dim, dtype, num_pages, page_size, width, int(window), int(sinks),
         float(head_dim ** -0.5 if scale is None else scale), _row_stride("q", q, (B, N), (heads, head_dim)), kv_stride, out_stride,
-        page_stride, slot_stride, arr))
+        page_stride, slot_stride, arr)
+
+
+@dataclass
+class PrefixAttentionResult:
+    out: "object"               # [B,N,heads,head_dim]
+    lse: Optional["object"] = None      # float32 [B,N,heads]
+    workspace: Optional["object"] = None
+
+
+def mpv_prefix_attention(parent, q, tree_k, tree_v, cache_k, cache_v, block_table, context_len, prefix_of=None, prefix_table=None,
+                         prefix_len=None, scale=None, window=0, sinks=0, num_nodes=None, tree_parent=None, lse=False, out=None, stream=None):
+    """mpv_tree_attention of trees behind prefixes that requests share, each read once for up to 64 trees that follow each other (see
+    include/mpv.h); returns a PrefixAttentionResult.
+
+    prefix_of int32 [B]: the prefix of a tree, negative for none; prefix_table int32 [prefixes,prefix_width], pages of the same cache;
+    prefix_len int32 [prefixes]; all three None: no prefixes.  lse=True: the logarithms of the sums, too (as mpv_score_positions takes them).
+    `out` may be a previous PrefixAttentionResult whose buffers are reused (its lse is written if it has one).  The other arguments
+    are those of mpv_tree_attention."""
+    import torch
+    key = ("prefixed", None if tree_parent is not None else tuple(parent), scale, window, sinks, _like(q), _like(tree_k), _like(tree_v),
+           _like(cache_k), _like(cache_v), _like(block_table), _like(context_len), _like(num_nodes), _like(tree_parent), _like(prefix_of),
+           _like(prefix_table), _like(prefix_len), None if out is None else (_like(out.out), _like(out.lse)))
+    plan = _plans.get(key)
+    if plan is None:
+        plan = _kept(key, _prefixed_plan(parent, q, tree_k, tree_v, cache_k, cache_v, block_table, context_len, scale, window, sinks,
+                                         num_nodes, tree_parent, prefix_of, prefix_table, prefix_len, out))
+    if out is None:
+        with _allocating(stream):
+            out = PrefixAttentionResult(out=torch.empty(q.shape, dtype=q.dtype, device=q.device),
+                                        lse=torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if lse else None)
+    bufs = _PrefixedBuffers((q.data_ptr(), tree_k.data_ptr(), tree_v.data_ptr(), cache_k.data_ptr(), cache_v.data_ptr(), block_table.data_ptr(),
+                             context_len.data_ptr(), _ptr(num_nodes), _ptr(tree_parent), out.out.data_ptr()),
+                            _ptr(prefix_of), _ptr(prefix_table), _ptr(prefix_len), _ptr(out.lse))
+    return _launch(plan, bufs, out, stream)
+
+
+def _prefixed_plan(parent, q, tree_k, tree_v, cache_k, cache_v, block_table, context_len, scale, window, sinks, num_nodes, tree_parent,
+                   prefix_of, prefix_table, prefix_len, out):
+    import torch
+    dev, shape = _attention_shape(parent, q, tree_k, tree_v, cache_k, cache_v, block_table, context_len, scale, window, sinks, num_nodes,
+                                  tree_parent, out)
+    given = [x is not None for x in (prefix_of, prefix_table, prefix_len)]
+    if any(given) and not all(given):
+        raise ValueError("prefix_of, prefix_table and prefix_len belong together")
+    prefixes = width = 0
+    if all(given):
+        if prefix_table.dim() != 2:
+            raise ValueError("prefix_table must be [prefixes,prefix_width]")
+        prefixes, width = prefix_table.shape
+        _whole(dev, torch.int32, prefix_of=(prefix_of, (shape.B,)), prefix_table=(prefix_table, (prefixes, width)), prefix_len=(prefix_len, (prefixes,)))
+    if out is not None:
+        _whole(dev, torch.float32, lse=(out.lse, (shape.B, shape.N, shape.heads)))
+    return _Plan("mpv_prefix_attention", dev.index, _Prefixed(shape, prefixes, width))
 
 
 def mpv_verify_chains(tokens, target_probs, draft_probs, uniforms, num_nodes=None, max_depth=None, out=None, stream=None):

@@ -29,6 +29,8 @@ UNITS = {
     "mpv.hip": ["-mllvm", "-disable-machine-licm"],
     # (so are the paths of a tile that few tiles take; -Winline-asm says that m0 is reserved wherever an instruction names it as written)
     "mpv_attention.hip": ["-mllvm", "-disable-machine-licm", "-Wno-inline-asm"],
+    "mpv_prefix.hip": ["-mllvm", "-disable-machine-licm", "-Wno-inline-asm"],
+    "mpv_behind.hip": ["-mllvm", "-disable-machine-licm", "-Wno-inline-asm"],
     "mpv_chains.hip": [],
     "mpv_cache.hip": [],
 }

@@ -1,0 +1,155 @@
+// Attention of draft trees behind prefixes that requests share: the trees' own part, and the call.
+//
+// A softmax over several parts of its keys needs of each part the sum of its values' weights, the sum of the weights, and the reference of both:
+//   m = max m_i,  out = sum_i e^(m_i - m) o_i / sum_i e^(m_i - m) w_i,  ln sum_j e^(s_j) = m + ln sum_i e^(m_i - m) w_i.
+// So prefix_kernel works out the prefix's part for the nodes of all trees that share it (mpv_prefix.hip), and a row goes on from there
+// over its own context and tree as if they were the next tiles (kBehind of mpv_attention.h).  The state between the two is float32.
+
+#include "mpv_prefix.h"
+
+namespace mpv {
+
+template <class A>
+__global__ __launch_bounds__(A::kThreads) __attribute__((amdgpu_waves_per_eu(2))) void behind_kernel(PrefixArgs g) {
+    extern __shared__ __align__(1024) char memory[];
+    A a(g, *reinterpret_cast<typename A::Shared*>(memory));
+    a.all();
+}
+
+// Puts the units together that several teams share.
+template <int DTYPE, int DP, int ROWS>
+__global__ __launch_bounds__(256) void join_behind_kernel(PrefixArgs g) {
+    combine<kBehind, DTYPE, DP, ROWS>(g);
+}
+
+template <class A, int DTYPE, int DP>
+static int with_kernel(const mpv_attention* a, PrefixArgs* g, char* workspace, size_t* bytes, hipStream_t s) {
+    const Choice c = choice_of<A, DP>(a);
+    const Parts parts = Parts::of(c);
+    *bytes = parts.bytes();
+    if (!g) return MPV_OK;
+    parts.place(g, workspace);
+    g->teams = c.teams;
+    g->blocks = c.blocks;
+    g->by_unit = static_cast<int64_t>(a->B) * a->kv_heads < c.teams;
+    const int64_t rows = static_cast<int64_t>(a->N) * (a->heads / a->kv_heads);
+    (void)hipGetLastError();
+    if (!hip_fine(hipFuncSetAttribute(reinterpret_cast<const void*>(&behind_kernel<A>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                      static_cast<int>(sizeof(typename A::Shared)))))
+        return MPV_ERR_HIP;
+    hipLaunchKernelGGL(behind_kernel<A>, dim3(static_cast<unsigned>(c.teams) * c.blocks), dim3(A::kThreads), sizeof(typename A::Shared), s, *g);
+    const Second second = second_of<DP>(a, c, g->by_unit);
+    if (second.workgroups)
+        hipLaunchKernelGGL((join_behind_kernel<DTYPE, DP, A::kRows>), dim3(static_cast<unsigned>(second.entries), static_cast<unsigned>(second.workgroups)),
+                           dim3(256), 0, s, *g);
+    return launched();
+}
+
+template <int DTYPE, int DP>
+static int with_columns(const mpv_attention* a, PrefixArgs* g, char* workspace, size_t* bytes, hipStream_t s) {
+    return by_rows<kBehind, DTYPE, DP>(static_cast<int64_t>(a->N) * (a->heads / a->kv_heads), [&](auto kernel) {
+        return with_kernel<typename decltype(kernel)::T, DTYPE, DP>(a, g, workspace, bytes, s);
+    });
+}
+
+template <int DTYPE>
+static int with_type(const mpv_attention* a, PrefixArgs* g, char* workspace, size_t* bytes, hipStream_t s) {
+    if (a->head_dim <= 64) return with_columns<DTYPE, 64>(a, g, workspace, bytes, s);
+    if (a->head_dim <= 128) return with_columns<DTYPE, 128>(a, g, workspace, bytes, s);
+    return with_columns<DTYPE, 256>(a, g, workspace, bytes, s);
+}
+
+static int attend_behind(const mpv_attention* a, PrefixArgs* g, char* workspace, size_t* bytes, hipStream_t s) {
+    if (a->dtype == MPV_DTYPE_F32) return with_type<MPV_DTYPE_F32>(a, g, workspace, bytes, s);
+    if (a->dtype == MPV_DTYPE_BF16) return with_type<MPV_DTYPE_BF16>(a, g, workspace, bytes, s);
+    return with_type<MPV_DTYPE_F16>(a, g, workspace, bytes, s);
+}
+
+// Bytes of a workspace: the state of the rows (none without prefixes), and what either half needs while it runs.
+struct Room {
+    size_t state, stats, exact, parts;
+    size_t bytes() const { return state + stats + exact + parts; }
+};
+static int room_of(const mpv_prefixed* p, Room* r) {
+    const mpv_attention* a = &p->attention;
+    *r = {0, 0, 0, 0};
+    size_t behind, prefix = 0;
+    int rc = attend_behind(a, nullptr, nullptr, &behind, nullptr);
+    if (rc != MPV_OK) return rc;
+    if (a->B > 0 && p->prefixes > 0 && p->prefix_width > 0) {
+        rc = attend_prefixes(a, nullptr, nullptr, &prefix, nullptr);
+        if (rc != MPV_OK) return rc;
+        const size_t rows = static_cast<size_t>(a->B) * a->N * a->heads;
+        r->stats = whole(rows * sizeof(float2));
+        r->exact = whole(rows * sizeof(float));
+        r->state = whole(rows * columns_of(a) * sizeof(float));
+    }
+    r->parts = std::max(behind, prefix);
+    return MPV_OK;
+}
+
+static int check_prefixed(const mpv_prefixed* p) {
+    if (!p) return MPV_ERR_NULL;
+    const int rc = check_attention(&p->attention);
+    if (rc != MPV_OK) return rc;
+    if (p->prefixes < 0 || p->prefix_width < 0) return MPV_ERR_BAD_SHAPE;
+    const mpv_attention& a = p->attention;
+    // positions are counted in 32 bits
+    if (span(span(MPV_MAX_NODES, a.table_width, a.page_size), p->prefix_width, a.page_size) > INT32_MAX) return MPV_ERR_UNSUPPORTED;
+    return MPV_OK;
+}
+
+}  // namespace mpv
+
+extern "C" {
+
+int mpv_prefix_attention_workspace_bytes(const mpv_prefixed* prefixed, size_t* out) {
+    if (!out) return MPV_ERR_NULL;
+    int rc = mpv::check_prefixed(prefixed);
+    if (rc != MPV_OK) return rc;
+    mpv::Room room;
+    rc = mpv::room_of(prefixed, &room);
+    *out = room.bytes();
+    return rc;
+}
+
+int mpv_prefix_attention(const mpv_prefixed* prefixed, const mpv_prefixed_buffers* buf, void* workspace, size_t workspace_bytes,
+                         void* hip_stream) {
+    int rc = mpv::check_prefixed(prefixed);
+    if (rc != MPV_OK) return rc;
+    mpv::Room room;
+    rc = mpv::room_of(prefixed, &room);
+    if (rc != MPV_OK) return rc;
+    if (!buf) return MPV_ERR_NULL;
+    const mpv_attention* a = &prefixed->attention;
+    mpv::PrefixArgs g;
+    rc = mpv::take_arguments(a, &buf->attention, &g);
+    if (rc != MPV_OK) return rc;
+    if (a->B == 0) return MPV_OK;
+    rc = mpv::check_buffers(a, &buf->attention);
+    if (rc != MPV_OK) return rc;
+    const bool any = room.state != 0 && buf->prefix_of;
+    // (a prefix may be all that there is in the cache)
+    if (any && (!buf->prefix_table || !buf->prefix_len || (a->num_pages > 0 && (!buf->attention.cache_k || !buf->attention.cache_v)))) return MPV_ERR_NULL;
+    if (!workspace || !mpv::aligned(workspace, 256) || workspace_bytes < room.bytes()) return MPV_ERR_WORKSPACE;
+    g.prefix_of = any ? buf->prefix_of : nullptr;
+    g.prefix_table = buf->prefix_table;
+    g.prefix_len = buf->prefix_len;
+    g.prefixes = prefixed->prefixes;
+    g.prefix_width = prefixed->prefix_width;
+    g.lse = buf->lse;
+    char* at = static_cast<char*>(workspace);
+    g.state = reinterpret_cast<float*>(at);
+    g.state_stats = reinterpret_cast<float2*>(at + room.state);
+    g.state_exact = reinterpret_cast<float*>(at + room.state + room.stats);
+    at += room.state + room.stats + room.exact;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    size_t need;
+    if (any) {
+        rc = mpv::attend_prefixes(a, &g, at, &need, s);
+        if (rc != MPV_OK) return rc;
+    }
+    return mpv::attend_behind(a, &g, at, &need, s);
+}
+
+}  // extern "C"
