@@ -75,6 +75,7 @@ extern "C" {
 #define MPV_MAX_VOCAB    (1 << 21)
 #define MPV_MAX_HEAD_DIM 256  /* values of one attention head               */
 #define MPV_MAX_HEADS    1024 /* query heads                                */
+#define MPV_MAX_TOP      64   /* alternatives of a row of log probabilities  */
 /* and B * (N + 2) <= 2^30 */
 
 #define MPV_METHOD_SPECINFER 0
@@ -519,6 +520,125 @@ typedef struct mpv_append_buffers {        /* DEVICE */
 
 /* Errors: MPV_ERR_NULL, _BAD_SHAPE, _UNSUPPORTED (N, row, B, layers or a stride too large), _BAD_DTYPE, _ALIGNMENT, _HIP. */
 int mpv_append_paths(const mpv_append* append, const mpv_append_buffers* buffers, void* hip_stream);
+
+/* The attention weight that the positions of a cache gather, for mpv_evict_positions: the nodes of the path that was accepted give
+ * their weights to what they saw, in all layers at once.  For every position j < context_len[b] of the cache, and score head g,
+ *   scores[layer,b,g,j] <- decay scores[layer,b,g,j] + sum over n and h of e^(scale q.k_j - lse[layer,b,n,h]),
+ * n over the root and the accepted path (node 0, path_nodes[b, i] for i < accept_len[b]), h over the query heads of cache head g
+ * (score_heads = kv_heads) or all of them (1).  The path itself takes the positions behind the context, as mpv_append_paths puts it
+ * there: position context_len[b] + i gets what the path's nodes from the i-th on gave to the i-th, its old score is forgotten.  lse: of
+ * mpv_prefix_attention (which may have seen a prefix, too: that has no scores); of an attention without a window.
+ * Call it with the context_len of that attention, before mpv_extend_tables.  Scores of other positions are left as they were; positions
+ * whose page, or node, is out of range are given nothing.  A row whose lse is -inf gives nothing. */
+typedef struct mpv_scores {
+    int32_t layers, B, N;
+    int32_t heads, kv_heads, score_heads;     /* score_heads: 1 or kv_heads                                  */
+    int32_t head_dim;                         /* <= MPV_MAX_HEAD_DIM, a multiple of 16 bytes                 */
+    int32_t dtype;                            /* of q, tree_k and cache_k                                    */
+    int32_t max_depth;                        /* row width of path_nodes (0 without)                         */
+    int32_t num_pages, page_size, table_width;
+    float scale, decay;                       /* finite                                                      */
+    int64_t score_width;                      /* positions in a row of scores, >= table_width * page_size    */
+    int64_t q_layer_stride, q_stride;         /* elements from layer to layer, from node to node             */
+    int64_t tree_layer_stride, tree_stride;
+    int64_t cache_layer_stride, page_stride, slot_stride;
+} mpv_scores;
+
+typedef struct mpv_score_buffers {         /* DEVICE */
+    const void* q;                /* [layers,B,N,heads,head_dim]                                              */
+    const void* tree_k;           /* [layers,B,N,kv_heads,head_dim]                                           */
+    const void* cache_k;          /* [layers,num_pages,page_size,kv_heads,head_dim]                           */
+    const int32_t* block_table;   /* [B,table_width]                                                          */
+    const int32_t* context_len;   /* [B]                                                                      */
+    const float* lse;             /* [layers,B,N,heads]                                                       */
+    const int32_t* accept_len;    /* [B] or NULL: the root alone (single tokens)                              */
+    const int32_t* path_nodes;    /* [B,max_depth] or NULL: nodes 1, 2, ...                                   */
+    float* scores;                /* [layers,B,score_heads,score_width]                                       */
+} mpv_score_buffers;
+
+/* Errors: MPV_ERR_NULL, _BAD_SHAPE, _UNSUPPORTED (a size or stride too large), _BAD_DTYPE, _BAD_TEMPERATURE (scale or decay not finite),
+ * _ALIGNMENT, _HIP. */
+int mpv_score_positions(const mpv_scores* scores, const mpv_score_buffers* buffers, void* hip_stream);
+
+/* Eviction: a request with more than `trigger` cached positions keeps `budget` of them: the first `sinks`, the last `recent`,
+ * and of the others those with the largest scores, of equal ones the first (NaN counts as less than any number).  They move forward
+ * in order: position i of the cache holds what position kept[i] held, keys and values of all layers; each score head keeps positions of its
+ * own (score_heads = kv_heads), or whole slots move (1).  A window of the attention counts positions as they are then.  The pages behind
+ * ceil(budget / page_size) go to the end of the list of free pages (in request order, ascending position; what num_pages entries do not
+ * hold is dropped); the block table is not changed.  Other requests are left as they are.
+ * A row of which either slot lies in a page outside [0,num_pages) does not move.  No page of a request that is cut may appear twice, in its own row or
+ * in another's.  scores_out may be scores; otherwise what lies behind a request's positions is left as it was.  kept is -1 throughout for a
+ * request that is not cut. */
+typedef struct mpv_eviction {
+    int32_t layers, B;                     /* layers = 0: tables and lengths alone                           */
+    int32_t kv_heads, score_heads;
+    int32_t head_dim, dtype;
+    int32_t num_pages, page_size, table_width;
+    int32_t budget, trigger, sinks, recent;   /* 1 <= budget <= trigger; sinks + recent <= budget            */
+    int64_t score_width;                   /* >= table_width * page_size                                      */
+    int64_t cache_layer_stride, page_stride, slot_stride;
+} mpv_eviction;
+
+typedef struct mpv_eviction_buffers {      /* DEVICE */
+    void* cache_k;                /* [layers,num_pages,page_size,kv_heads,head_dim], in and out               */
+    void* cache_v;
+    const int32_t* block_table;   /* [B,table_width]                                                          */
+    const int32_t* context_len;   /* [B], taken within [0, table_width * page_size]                           */
+    const float* scores;          /* [layers,B,score_heads,score_width]                                       */
+    float* scores_out;            /* the same; may be scores                                                  */
+    int32_t* kept;                /* [layers,B,score_heads,budget]                                            */
+    int32_t* free_pages;          /* [num_pages], in and out                                                  */
+    const int32_t* free_count;    /* [1], taken within [0,num_pages]                                          */
+    int32_t* context_len_out;     /* [B]; may be context_len                                                  */
+    int32_t* free_count_out;      /* [1]; may be free_count                                                   */
+} mpv_eviction_buffers;
+
+int mpv_evict_positions_workspace_bytes(const mpv_eviction* eviction, size_t* out);
+
+/* Errors: MPV_ERR_NULL, _BAD_SHAPE, _UNSUPPORTED (a size or stride too large), _BAD_DTYPE, _ALIGNMENT, _WORKSPACE, _HIP. */
+int mpv_evict_positions(const mpv_eviction* eviction, const mpv_eviction_buffers* buffers,
+                        void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Log probabilities of given tokens under p = softmax(z / T), with the entropy of p and its most likely tokens.
+ * paths = 1: of what a verification emitted: output row i <= accept_len[b] of tree b is logit row 0 (i = 0) or path_nodes[b, i - 1], its
+ * token path_tokens[b, i] or, for i = accept_len[b], the bonus token; output rows [B, max_depth + 1].
+ * paths = 0: of one token for each of N rows of a request (prompts; greedy steps); output rows [B, N].
+ *   logprob = ln p(token), entropy = - sum p ln p,
+ *   rank = 1 + the number of tokens with a larger logit, or an equal one and a smaller index;
+ *   top_tokens / top_logprobs: the `top` first in that order; -1 and -inf where fewer have a logit above -inf.
+ * A token outside [0,V) has logprob -inf and rank -1.  Rows that do not exist (i > accept_len[b]; n >= num_nodes[b]; a node outside [0,N)):
+ * logprob 0, rank -1, entropy 0, tokens -1, -inf.  A row of -inf alone: logprob -inf, entropy 0, no alternatives.  NaN or +inf in a row:
+ * NaN, rank -1, tokens -1.  Sums are float32. */
+typedef struct mpv_logprobs {
+    int32_t B, N, V;
+    int32_t dtype;                /* MPV_DTYPE_*, F16 too                                                     */
+    int32_t top;                  /* 0 .. MPV_MAX_TOP                                                         */
+    int32_t paths;                /* 0 or 1                                                                   */
+    int32_t max_depth;            /* paths: row width of path_nodes and tokens, >= 1                          */
+    float   temperature;          /* finite, > 0                                                              */
+    int64_t stride;               /* elements from a logit row to the next (>= V); requests follow each other */
+} mpv_logprobs;
+
+typedef struct mpv_logprob_buffers {       /* DEVICE */
+    const void*    logits;        /* [B,N,V], at any element's address                                        */
+    const int32_t* tokens;        /* paths: path_tokens [B,max_depth]; otherwise [B,N]                        */
+    const int32_t* accept_len;    /* paths: as a verification writes them; otherwise ignored                  */
+    const int32_t* path_nodes;
+    const int32_t* bonus_token;
+    const int32_t* num_nodes;     /* [B] or NULL, rows of a request; ignored with paths                       */
+    float*   logprob;             /* a number for each output row, and so on                                  */
+    float*   entropy;
+    int32_t* rank;
+    int32_t* top_tokens;          /* [rows,top]; may be NULL with top = 0                                     */
+    float*   top_logprobs;
+} mpv_logprob_buffers;
+
+int mpv_token_logprobs_workspace_bytes(const mpv_logprobs* logprobs, size_t* out);
+
+/* Errors: MPV_ERR_NULL, _BAD_SHAPE, _UNSUPPORTED (V, top, rows or a stride too large), _BAD_DTYPE, _BAD_TEMPERATURE, _ALIGNMENT (logits are no
+ * multiple of their element's size), _WORKSPACE, _HIP. */
+int mpv_token_logprobs(const mpv_logprobs* logprobs, const mpv_logprob_buffers* buffers,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Per-launch timing for benchmarks (process-wide state, not thread-safe).
  * mpv_timing_enable(n > 0) creates n pairs of HIP events; from then on every

@@ -10,7 +10,7 @@ from .binding import (  # noqa: F401
     mpv_fill_uniforms, mpv_last_hip_error, mpv_row_stats, mpv_strerror,
     mpv_timing_enable, mpv_timing_read, mpv_verify, mpv_version, mpv_workspace_bytes, mpv_merge_duplicates,
     mpv_tree_attention, mpv_verify_chains, mpv_extend_tables, mpv_append_paths, TreeAttentionResult, TablesResult,
-    mpv_prefix_attention, PrefixAttentionResult,
+    mpv_prefix_attention, PrefixAttentionResult, mpv_score_positions, mpv_evict_positions, EvictResult, mpv_token_logprobs, LogprobsResult,
     MPV_KERNEL_NAMES,
     MPV_COUNTER_NEAR_TIE_ACCEPT, MPV_COUNTER_NEAR_TIE_BONUS, MPV_COUNTER_ZERO_MASS, MPV_COUNTER_BAD_TOKEN,
     MPV_COUNTER_DEPENDENCY_TIMEOUT, MPV_COUNTER_NODE_TASKS_RUN, MPV_COUNTER_NODE_TASKS_CANCELLED,

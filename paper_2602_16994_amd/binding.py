@@ -110,6 +110,39 @@ class _AppendBuffers(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("tree_k", "tree_v", "cache_k", "cache_v", "slot_map", "accept_len", "path_nodes")]
 
 
+class _Scores(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("layers", "B", "N", "heads", "kv_heads", "score_heads", "head_dim", "dtype", "max_depth", "num_pages",
+                                               "page_size", "table_width")]
+                + [(n, ctypes.c_float) for n in ("scale", "decay")]
+                + [(n, ctypes.c_int64) for n in ("score_width", "q_layer_stride", "q_stride", "tree_layer_stride", "tree_stride",
+                                                 "cache_layer_stride", "page_stride", "slot_stride")])
+
+
+class _ScoreBuffers(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "tree_k", "cache_k", "block_table", "context_len", "lse", "accept_len", "path_nodes", "scores")]
+
+
+class _Eviction(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("layers", "B", "kv_heads", "score_heads", "head_dim", "dtype", "num_pages", "page_size",
+                                               "table_width", "budget", "trigger", "sinks", "recent")]
+                + [(n, ctypes.c_int64) for n in ("score_width", "cache_layer_stride", "page_stride", "slot_stride")])
+
+
+class _EvictionBuffers(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("cache_k", "cache_v", "block_table", "context_len", "scores", "scores_out", "kept", "free_pages",
+                                               "free_count", "context_len_out", "free_count_out")]
+
+
+class _Logprobs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("B", "N", "V", "dtype", "top", "paths", "max_depth")]
+                + [("temperature", ctypes.c_float), ("stride", ctypes.c_int64)])
+
+
+class _LogprobBuffers(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("logits", "tokens", "accept_len", "path_nodes", "bonus_token", "num_nodes", "logprob", "entropy",
+                                               "rank", "top_tokens", "top_logprobs")]
+
+
 _lib = None
 
 
@@ -170,13 +203,16 @@ def load_library(path=None):
     lib.mpv_fill_uniforms.restype = ctypes.c_int
     lib.mpv_fill_uniforms.argtypes = [ctypes.c_uint64, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p]
     for name, shape, bufs in (("mpv_tree_attention", _Attention, _AttentionBuffers), ("mpv_prefix_attention", _Prefixed, _PrefixedBuffers),
-                              ("mpv_verify_chains", _Chains, _ChainBuffers), ("mpv_extend_tables", _Tables, _TableBuffers)):
+                              ("mpv_verify_chains", _Chains, _ChainBuffers), ("mpv_extend_tables", _Tables, _TableBuffers),
+                              ("mpv_evict_positions", _Eviction, _EvictionBuffers), ("mpv_token_logprobs", _Logprobs, _LogprobBuffers)):
         call, size = getattr(lib, name), getattr(lib, name + "_workspace_bytes")
         call.restype = size.restype = ctypes.c_int
         call.argtypes = [ctypes.POINTER(shape), ctypes.POINTER(bufs), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
         size.argtypes = [ctypes.POINTER(shape), ctypes.POINTER(ctypes.c_size_t)]
-    lib.mpv_append_paths.restype = ctypes.c_int
-    lib.mpv_append_paths.argtypes = [ctypes.POINTER(_Append), ctypes.POINTER(_AppendBuffers), ctypes.c_void_p]
+    for name, shape, bufs in (("mpv_append_paths", _Append, _AppendBuffers), ("mpv_score_positions", _Scores, _ScoreBuffers)):
+        call = getattr(lib, name)
+        call.restype = ctypes.c_int
+        call.argtypes = [ctypes.POINTER(shape), ctypes.POINTER(bufs), ctypes.c_void_p]
     lib.mpv_timing_enable.restype = ctypes.c_int
     lib.mpv_timing_enable.argtypes = [ctypes.c_int32]
     lib.mpv_timing_read.restype = ctypes.c_int
@@ -699,7 +735,7 @@ class _Plan:
         if _raw_stream is None:              # the current stream's handle without a Stream object around it (2 us a call), where torch has it
             import torch
             _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        if name != "mpv_append_paths":
+        if hasattr(lib, name + "_workspace_bytes"):
             need = ctypes.c_size_t(0)
             rc = getattr(lib, name + "_workspace_bytes")(self.address, ctypes.byref(need))
             if rc != 0:
@@ -1039,6 +1075,211 @@ def _append_plan(tree_k, tree_v, cache_k, cache_v, slot_map, accept_len, path_no
                 or (layers > 1 and (tree_v.stride(0) != tree_k.stride(0) or cache_v.stride(0) != cache_k.stride(0)))):
             raise ValueError("keys and values must have the same strides")
     return _Plan("mpv_append_paths", dev.index, shape)
+
+
+def _layers(**tensors):
+    """Tensors that all have a dimension of layers or all have none, with it: name=(tensor, dimensions)."""
+    with_it = {t.dim() == dims for t, dims in tensors.values()}
+    if len(with_it) != 1 or any(t.dim() not in (dims - 1, dims) for t, dims in tensors.values()):
+        raise ValueError(f"{', '.join(tensors)} must all have a dimension of layers or all have none")
+    return [t if with_it == {True} else t.unsqueeze(0) for t, _ in tensors.values()]
+
+
+def mpv_score_positions(q, tree_k, cache_k, block_table, context_len, lse, scores, accept_len=None, path_nodes=None, scale=None, decay=1.0,
+                        stream=None):
+    """Adds the attention weights that the accepted nodes gave to the positions of the cache, and to their own, to `scores` (see
+    include/mpv.h), enqueued on the current (or given) torch stream.
+
+    q [layers,B,N,heads,head_dim], tree_k [layers,B,N,kv_heads,head_dim], cache_k [layers,num_pages,page_size,kv_heads,head_dim], lse float32
+    [layers,B,N,heads] (of mpv_prefix_attention) and scores float32 [layers,B,kv_heads or 1,positions], or all five without the first
+    dimension for one layer; block_table int32 [B,table_width], context_len int32 [B]: as the attention had them, before
+    mpv_extend_tables.  accept_len int32 [B] and path_nodes int32 [B,max_depth] as a verification writes them (accept_len=None: the root alone,
+    as for single tokens; path_nodes=None: chains, nodes 1, 2, ...).  scale: head_dim ** -0.5 unless given.  decay multiplies the old scores."""
+    key = ("scores", scale, decay, _like(q), _like(tree_k), _like(cache_k), _like(block_table), _like(context_len), _like(lse), _like(scores),
+           _like(accept_len), _like(path_nodes))
+    plan = _plans.get(key)
+    if plan is None:
+        plan = _kept(key, _scores_plan(q, tree_k, cache_k, block_table, context_len, lse, scores, accept_len, path_nodes, scale, decay))
+    bufs = _ScoreBuffers(q.data_ptr(), tree_k.data_ptr(), cache_k.data_ptr(), block_table.data_ptr(), context_len.data_ptr(), lse.data_ptr(),
+                         _ptr(accept_len), _ptr(path_nodes), scores.data_ptr())
+    _launch(plan, bufs, None, stream)
+
+
+def _scores_plan(q, tree_k, cache_k, block_table, context_len, lse, scores, accept_len, path_nodes, scale, decay):
+    import torch
+    q, tree_k, cache_k, lse, scores = _layers(q=(q, 5), tree_k=(tree_k, 5), cache_k=(cache_k, 5), lse=(lse, 4), scores=(scores, 4))
+    layers, B, N, heads, head_dim = q.shape
+    kv_heads, num_pages, page_size, dev = tree_k.shape[3], cache_k.shape[1], cache_k.shape[2], q.device
+    _on_device(dev, q=q, tree_k=tree_k, cache_k=cache_k)
+    if any(t.dtype != q.dtype for t in (tree_k, cache_k)):
+        raise TypeError("q, tree_k and cache_k must have the same dtype")
+    dtype = _dtype_of(q)
+    if tuple(tree_k.shape[:3]) != (layers, B, N) or cache_k.shape[0] != layers or block_table.dim() != 2:
+        raise ValueError("q, tree_k and cache_k must have the same layers, q and tree_k the same trees; block_table is [B,table_width]")
+    if path_nodes is not None and (accept_len is None or path_nodes.dim() != 2):
+        raise ValueError("path_nodes is [B,max_depth], and is read with accept_len only")
+    deep, width = path_nodes.shape[1] if path_nodes is not None else 0, block_table.shape[1]
+    score_heads, positions = scores.shape[2], scores.shape[3]
+    _whole(dev, torch.float32, lse=(lse, (layers, B, N, heads)), scores=(scores, (layers, B, score_heads, positions)))
+    _whole(dev, torch.int32, block_table=(block_table, (B, width)), context_len=(context_len, (B,)), accept_len=(accept_len, (B,)),
+           path_nodes=(path_nodes, (B, deep)))
+    shape = _Scores(layers, B, N, heads, kv_heads, score_heads, head_dim, dtype, deep, num_pages, page_size, width,
+                    float(head_dim ** -0.5 if scale is None else scale), float(decay), positions, 0, heads * head_dim, 0, kv_heads * head_dim,
+                    0, 0, kv_heads * head_dim)
+    if layers and B:
+        shape.q_stride = _row_stride("q", q[0], (B, N), (heads, head_dim))
+        shape.tree_stride = _row_stride("tree_k", tree_k[0], (B, N), (kv_heads, head_dim))
+        shape.page_stride, shape.slot_stride = _cache_strides(cache_k[0], cache_k[0], (num_pages, page_size, kv_heads, head_dim))
+        if layers > 1:
+            shape.q_layer_stride, shape.tree_layer_stride, shape.cache_layer_stride = q.stride(0), tree_k.stride(0), cache_k.stride(0)
+    return _Plan("mpv_score_positions", dev.index, shape)
+
+
+@dataclass
+class EvictResult:
+    context_len: Optional["object"] = None     # int32 [B]    tokens in the cache after the call
+    free_count: Optional["object"] = None      # int32 [1]
+    scores: Optional["object"] = None          # float32 [layers,B,score_heads,positions]
+    kept: Optional["object"] = None            # int32 [layers,B,score_heads,budget]    old positions; -1: the request was not cut
+    workspace: Optional["object"] = None
+    inplace: bool = False                      # context_len, free_count and scores are the tensors that were passed
+
+
+def mpv_evict_positions(cache_k, cache_v, block_table, context_len, scores, free_pages, free_count, budget, trigger=None, sinks=0, recent=0,
+                        inplace=False, out=None, stream=None):
+    """Cuts requests with more than `trigger` cached positions (the budget unless given) down to `budget`: the first `sinks`, the last `recent`,
+    and the best by their scores (see include/mpv.h), enqueued on the current (or given) torch stream; returns an EvictResult.
+
+    cache_k / cache_v [layers,num_pages,page_size,kv_heads,head_dim] and scores float32 [layers,B,kv_heads or 1,positions], or all three
+    without the first dimension for one layer; block_table int32 [B,table_width], context_len int32 [B], free_pages int32 [num_pages],
+    free_count int32 [1].  Caches and free_pages are changed in place; context_len, free_count and scores are, too, with inplace=True, otherwise
+    their new values are in the result alone.  `out` may be a previous EvictResult whose buffers are reused (without inplace=True, not
+    those that a caller passed)."""
+    import torch
+    lengths, count, old = context_len.data_ptr(), free_count.data_ptr(), scores.data_ptr()
+    trigger = budget if trigger is None else trigger
+    after = left = new = None
+    if inplace:
+        after, left, new = context_len, free_count, scores
+    elif out is not None and not out.inplace:
+        def mine(t, passed):
+            return t if t is not None and t.data_ptr() != passed else None
+        after, left, new = mine(out.context_len, lengths), mine(out.free_count, count), mine(out.scores, old)
+    kept = None if out is None else out.kept
+    key = ("evict", budget, trigger, sinks, recent, _like(cache_k), _like(cache_v), _like(block_table), _like(context_len), _like(scores),
+           _like(free_pages), _like(free_count), _like(after), _like(left), _like(new), _like(kept))
+    plan = _plans.get(key)
+    if plan is None:
+        plan = _kept(key, _evict_plan(cache_k, cache_v, block_table, context_len, scores, free_pages, free_count, budget, trigger, sinks, recent,
+                                      after, left, new, kept))
+    with _allocating(stream):
+        i32 = dict(dtype=torch.int32, device=scores.device)
+        after = torch.empty(context_len.shape[0], **i32) if after is None else after
+        left = torch.empty(1, **i32) if left is None else left
+        new = torch.empty_like(scores) if new is None else new
+        kept = torch.empty((*scores.shape[:-1], budget), **i32) if kept is None else kept
+    out = EvictResult() if out is None else out
+    out.context_len, out.free_count, out.scores, out.kept, out.inplace = after, left, new, kept, inplace
+    bufs = _EvictionBuffers(cache_k.data_ptr(), cache_v.data_ptr(), block_table.data_ptr(), lengths, old, new.data_ptr(), kept.data_ptr(),
+                            free_pages.data_ptr(), count, after.data_ptr(), left.data_ptr())
+    _launch(plan, bufs, out, stream)
+    if not context_len.shape[0]:                   # the library writes nothing then
+        with _allocating(stream):
+            left.copy_(free_count.clamp(0, free_pages.shape[0]))
+    return out
+
+
+def _evict_plan(cache_k, cache_v, block_table, context_len, scores, free_pages, free_count, budget, trigger, sinks, recent, after, left, new, kept):
+    import torch
+    _int32(budget=budget, trigger=trigger, sinks=sinks, recent=recent)
+    lead = tuple(scores.shape[:-1])
+    if kept is not None:
+        _whole(scores.device, torch.int32, **{"the result's kept": (kept, (*lead, budget))})
+    if new is not None:
+        _whole(scores.device, torch.float32, **{"the result's scores": (new, tuple(scores.shape))})
+    cache_k, cache_v, scores = _layers(cache_k=(cache_k, 5), cache_v=(cache_v, 5), scores=(scores, 4))
+    layers, num_pages, page_size, kv_heads, head_dim = cache_k.shape
+    dev = cache_k.device
+    _on_device(dev, cache_k=cache_k, cache_v=cache_v)
+    if cache_v.dtype != cache_k.dtype:
+        raise TypeError("cache_k and cache_v must have the same dtype")
+    dtype = _dtype_of(cache_k)
+    if block_table.dim() != 2 or tuple(cache_v.shape) != tuple(cache_k.shape):
+        raise ValueError("cache_k and cache_v must have the same shapes, block_table is [B,table_width]")
+    B, width = block_table.shape
+    score_heads, positions = scores.shape[2], scores.shape[3]
+    _whole(dev, torch.float32, scores=(scores, (layers, B, score_heads, positions)))
+    _whole(dev, torch.int32, block_table=(block_table, (B, width)), context_len=(context_len, (B,)), free_pages=(free_pages, (num_pages,)),
+           free_count=(free_count, (1,)))
+    _whole(dev, torch.int32, **{"the result's context_len": (after, (B,)), "the result's free_count": (left, (1,))})
+    shape = _Eviction(layers, B, kv_heads, score_heads, head_dim, dtype, num_pages, page_size, width, budget, trigger, sinks, recent, positions,
+                      0, 0, kv_heads * head_dim)
+    if layers:
+        shape.page_stride, shape.slot_stride = _cache_strides(cache_k[0], cache_v[0], (num_pages, page_size, kv_heads, head_dim))
+        if layers > 1:
+            shape.cache_layer_stride = cache_k.stride(0)
+            if cache_v.stride(0) != cache_k.stride(0):
+                raise ValueError("cache_k and cache_v must have the same strides")
+    return _Plan("mpv_evict_positions", dev.index, shape)
+
+
+@dataclass
+class LogprobsResult:
+    logprob: "object"           # float32 [B,rows]
+    entropy: "object"           # float32 [B,rows]
+    rank: "object"              # int32 [B,rows]   1: the most likely token
+    top_tokens: "object"        # int32 [B,rows,top]
+    top_logprobs: "object"      # float32 [B,rows,top]
+    workspace: Optional["object"] = None
+
+
+def mpv_token_logprobs(logits, tokens, temperature=1.0, top=0, accept_len=None, path_nodes=None, bonus_token=None, num_nodes=None, out=None,
+                       stream=None):
+    """Log probabilities of given tokens, entropies and the `top` most likely tokens (see include/mpv.h), enqueued on the current (or
+    given) torch stream; returns a LogprobsResult.
+
+    logits [B,N,V] (float32, bfloat16 or float16; rows may lie further apart than V).  With accept_len int32 [B], path_nodes int32
+    [B,max_depth] and bonus_token int32 [B], as a verification writes them: of what it emitted, `tokens` its path_tokens int32 [B,max_depth], and
+    the results have max_depth + 1 rows.  Without: tokens int32 [B,N], one for each row, num_nodes int32 [B] rows of each request.
+    `out` may be a previous LogprobsResult whose buffers are reused."""
+    import torch
+    key = ("logprobs", temperature, top, _like(logits), _like(tokens), _like(accept_len), _like(path_nodes), _like(bonus_token), _like(num_nodes),
+           None if out is None else (_like(out.logprob), _like(out.entropy), _like(out.rank), _like(out.top_tokens), _like(out.top_logprobs)))
+    plan = _plans.get(key)
+    if plan is None:
+        plan = _kept(key, _logprobs_plan(logits, tokens, temperature, top, accept_len, path_nodes, bonus_token, num_nodes, out))
+    if out is None:
+        rows = (logits.shape[0], logits.shape[1] if accept_len is None else path_nodes.shape[1] + 1)
+        f32, i32 = dict(dtype=torch.float32, device=logits.device), dict(dtype=torch.int32, device=logits.device)
+        with _allocating(stream):
+            out = LogprobsResult(logprob=torch.empty(rows, **f32), entropy=torch.empty(rows, **f32), rank=torch.empty(rows, **i32),
+                                 top_tokens=torch.empty(*rows, top, **i32), top_logprobs=torch.empty(*rows, top, **f32))
+    bufs = _LogprobBuffers(logits.data_ptr(), tokens.data_ptr(), _ptr(accept_len), _ptr(path_nodes), _ptr(bonus_token), _ptr(num_nodes),
+                           out.logprob.data_ptr(), out.entropy.data_ptr(), out.rank.data_ptr(), out.top_tokens.data_ptr(), out.top_logprobs.data_ptr())
+    return _launch(plan, bufs, out, stream)
+
+
+def _logprobs_plan(logits, tokens, temperature, top, accept_len, path_nodes, bonus_token, num_nodes, out):
+    import torch
+    _int32(top=top)
+    if logits.dim() != 3:
+        raise ValueError("logits must be [B,N,V]")
+    B, N, V = logits.shape
+    dev = logits.device
+    _on_device(dev, logits=logits)
+    dtype = _dtype_of(logits)
+    given = [x is not None for x in (accept_len, path_nodes, bonus_token)]
+    if any(given) and (not all(given) or num_nodes is not None or path_nodes.dim() != 2):
+        raise ValueError("accept_len, path_nodes [B,max_depth] and bonus_token belong together, without num_nodes")
+    deep = path_nodes.shape[1] if all(given) else 0
+    width = deep + 1 if all(given) else N
+    _whole(dev, torch.int32, tokens=(tokens, (B, deep) if all(given) else (B, N)), accept_len=(accept_len, (B,)), path_nodes=(path_nodes, (B, deep)),
+           bonus_token=(bonus_token, (B,)), num_nodes=(num_nodes, (B,)))
+    if out is not None:
+        _whole(dev, torch.float32, logprob=(out.logprob, (B, width)), entropy=(out.entropy, (B, width)), top_logprobs=(out.top_logprobs, (B, width, top)))
+        _whole(dev, torch.int32, rank=(out.rank, (B, width)), top_tokens=(out.top_tokens, (B, width, top)))
+    return _Plan("mpv_token_logprobs", dev.index, _Logprobs(B, N, V, dtype, top, int(all(given)), deep, float(temperature),
+                                                            _row_stride("logits", logits, (B, N), (V,))))
 
 
 MPV_KERNEL_NAMES = {0: "init", 1: "node_task", 2: "debug_stats"}

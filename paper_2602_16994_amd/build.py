@@ -33,6 +33,9 @@ UNITS = {
     "mpv_behind.hip": ["-mllvm", "-disable-machine-licm", "-Wno-inline-asm"],
     "mpv_chains.hip": [],
     "mpv_cache.hip": [],
+    "mpv_scores.hip": [],
+    "mpv_evict.hip": [],
+    "mpv_logprobs.hip": [],
 }
 
 

@@ -1,0 +1,276 @@
+// Eviction of cached positions that gathered little weight: device and host code.
+//
+// select_kernel: a workgroup has one list (layer, request, score head).  The budget's worth of best scores is found a byte of their order at
+// a time; then the kept positions are written in order, and the slots that their rows lie in.
+// move_kernel: kept rows move forward in order.  The i-th kept position s_i is at least i and the s_i ascend, so that what is written to the
+// rows [c, c + n) was read with them or before: a wave that takes a slice of a list's rows, some rows at a time, all loads before the
+// stores, needs no other copy.  Different slices (of different bytes) do not meet.  Its first workgroup returns the pages.
+
+#include <algorithm>
+
+#include "mpv_host.h"
+
+namespace mpv {
+
+constexpr int kSelectBlock = 512;
+constexpr int kMoveBlock = 256;
+constexpr int kSlice = 128;                // bytes of a row that a wave moves
+constexpr int kSliceLanes = kSlice / 16, kRowsTogether = 64 / kSliceLanes, kLoads = 8;
+constexpr int kMoveRows = kRowsTogether * kLoads;
+
+struct EvictArgs {
+    mpv_eviction p;
+    mpv_eviction_buffers b;
+    int lists, slices;
+    int64_t row_bytes, lead;               // of a moved row; elements from a head's row to the next (a list's: 0 where a list has whole slots)
+    Divisor by_page;
+    int32_t* slots;                        // [lists][budget] slot of a kept row, -1: none
+    int32_t* moved;                        // [lists] first row that moves (budget: none does)
+};
+
+__device__ __forceinline__ int context_of(const EvictArgs& a, int b) { return min(max(a.b.context_len[b], 0), a.p.table_width * a.p.page_size); }
+
+// Order of the scores; NaN comes last, both zeros are the same.
+__device__ __forceinline__ uint32_t score_order(float z) {
+    const uint32_t u = __float_as_uint(z + 0.0f);
+    return z != z ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// Exclusive sums of two numbers over the workgroup, the sums of all in total[2].
+__device__ __forceinline__ void before(int (&v)[2], int (&total)[2], int (*part)[2]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int upto[2] = {v[0], v[1]};
+    for (int d = 1; d < 64; d <<= 1) {
+        const int x = __shfl_up(upto[0], d), y = __shfl_up(upto[1], d);
+        if (lane >= d) { upto[0] += x; upto[1] += y; }
+    }
+    __syncthreads();
+    if (lane == 63) { part[wave][0] = upto[0]; part[wave][1] = upto[1]; }
+    __syncthreads();
+    v[0] = upto[0] - v[0];
+    v[1] = upto[1] - v[1];
+    total[0] = total[1] = 0;
+    for (int w = 0; w < static_cast<int>(blockDim.x >> 6); ++w) {
+        if (w < wave) { v[0] += part[w][0]; v[1] += part[w][1]; }
+        total[0] += part[w][0];
+        total[1] += part[w][1];
+    }
+}
+
+__global__ __launch_bounds__(kSelectBlock) void select_kernel(EvictArgs a) {
+    const mpv_eviction& p = a.p;
+    const int list = blockIdx.x, b = list / p.score_heads % p.B;
+    const int context = context_of(a, b);
+    const float* scores = a.b.scores + static_cast<int64_t>(list) * p.score_width;
+    float* out = a.b.scores_out + static_cast<int64_t>(list) * p.score_width;
+    int32_t* kept = a.b.kept + static_cast<int64_t>(list) * p.budget;
+    if (context <= p.trigger) {
+        for (int i = threadIdx.x; i < p.budget; i += kSelectBlock) kept[i] = -1;
+        if (out != scores)
+            for (int i = threadIdx.x; i < context; i += kSelectBlock) out[i] = scores[i];
+        if (threadIdx.x == 0) a.moved[list] = p.budget;
+        return;
+    }
+    __shared__ int counts[256];
+    __shared__ int part[kSelectBlock / 64][2];
+    __shared__ int chosen_digit, chosen_above;
+    const int from = p.sinks, to = context - p.recent, want = p.budget - p.sinks - p.recent;
+    // the want-th largest; `above`: those larger than it
+    uint32_t limit = 0;
+    int above = 0;
+    for (int shift = 24; shift >= 0 && want > 0; shift -= 8) {
+        if (threadIdx.x < 256) counts[threadIdx.x] = 0;
+        __syncthreads();
+        for (int j = from + threadIdx.x; j < to; j += kSelectBlock) {
+            const uint32_t k = score_order(scores[j]);
+            if (shift == 24 || k >> (shift + 8) == limit >> (shift + 8)) atomicAdd(&counts[k >> shift & 255], 1);
+        }
+        __syncthreads();
+        int mine[2] = {threadIdx.x < 256 ? counts[255 - threadIdx.x] : 0, 0}, total[2];
+        const int count = mine[0];
+        before(mine, total, part);
+        if (above + mine[0] < want && above + mine[0] + count >= want) { chosen_digit = 255 - threadIdx.x; chosen_above = above + mine[0]; }
+        __syncthreads();
+        limit |= static_cast<uint32_t>(chosen_digit) << shift;
+        above = chosen_above;
+        __syncthreads();
+    }
+    // the kept positions in order: of equal ones the first
+    const int equal = want - above;
+    int larger_before = 0, equal_before = 0;
+    for (int i = threadIdx.x; i < p.sinks; i += kSelectBlock) kept[i] = i;
+    for (int base = from; base < to && want > 0; base += kSelectBlock) {
+        const int j = base + threadIdx.x;
+        const uint32_t k = j < to ? score_order(scores[j]) : 0u;
+        const bool is_larger = j < to && k > limit, is_equal = j < to && k == limit;
+        int at[2] = {is_larger, is_equal}, total[2];
+        before(at, total, part);
+        const int e = equal_before + at[1];
+        if (is_larger || (is_equal && e < equal)) kept[p.sinks + larger_before + at[0] + min(e, equal)] = j;
+        larger_before += total[0];
+        equal_before += total[1];
+    }
+    for (int i = threadIdx.x; i < p.recent; i += kSelectBlock) kept[p.budget - p.recent + i] = to + i;
+    __threadfence_block();
+    __syncthreads();
+    // their scores and slots
+    __shared__ int stay;
+    if (threadIdx.x == 0) stay = 0;
+    __syncthreads();
+    for (int base = 0; base < p.budget; base += kSelectBlock) {
+        const int i = base + threadIdx.x;
+        float score = 0.0f;
+        if (i < p.budget) {
+            const int j = kept[i], column = a.by_page.of(j);
+            const int page = a.b.block_table[static_cast<int64_t>(b) * p.table_width + column];
+            a.slots[static_cast<int64_t>(list) * p.budget + i] = page >= 0 && page < p.num_pages ? page * p.page_size + j - column * p.page_size : -1;
+            score = scores[j];
+            if (j == i) atomicAdd(&stay, 1);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (`out` may be `scores`)
+        __syncthreads();
+        if (i < p.budget) out[i] = score;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) a.moved[list] = stay;
+}
+
+// Pages behind the kept positions go to the end of the list of free ones, in request order.
+__device__ __forceinline__ void return_pages(const EvictArgs& a) {
+    const mpv_eviction& p = a.p;
+    __shared__ int part[kMoveBlock / 64][2];
+    int64_t count = min(max(a.b.free_count[0], 0), p.num_pages);
+    const int have = (p.budget + p.page_size - 1) / p.page_size;
+    for (int base = 0; base < p.B; base += kMoveBlock) {
+        const int b = base + threadIdx.x;
+        const int context = b < p.B ? context_of(a, b) : 0;
+        const bool cut = context > p.trigger;
+        const int pages = cut ? (context + p.page_size - 1) / p.page_size - have : 0;
+        int at[2] = {pages, 0}, total[2];
+        before(at, total, part);
+        for (int i = 0; i < pages; ++i) {
+            const int64_t place = count + at[0] + i;
+            if (place < p.num_pages) a.b.free_pages[place] = a.b.block_table[static_cast<int64_t>(b) * p.table_width + have + i];
+        }
+        if (b < p.B) a.b.context_len_out[b] = cut ? p.budget : context;
+        count += total[0];
+    }
+    if (threadIdx.x == 0) a.b.free_count_out[0] = static_cast<int32_t>(min(count, static_cast<int64_t>(p.num_pages)));
+}
+
+__global__ __launch_bounds__(kMoveBlock) void move_kernel(EvictArgs a) {
+    const mpv_eviction& p = a.p;
+    if (blockIdx.x == 0) return return_pages(a);
+    const int lane = threadIdx.x & 63, part = lane % kSliceLanes, mine = lane / kSliceLanes;
+    const int64_t wave = (static_cast<int64_t>(blockIdx.x) - 1) * (kMoveBlock / 64) + (threadIdx.x >> 6);
+    const int64_t number = wave / 2;
+    const int list = static_cast<int>(number / a.slices), slice = static_cast<int>(number - static_cast<int64_t>(list) * a.slices);
+    if (list >= a.lists) return;
+    const int head = list % p.score_heads, b = list / p.score_heads % p.B, layer = list / p.score_heads / p.B;
+    const int bytes = p.dtype == MPV_DTYPE_F32 ? 4 : 2;
+    char* cache = static_cast<char*>(wave & 1 ? a.b.cache_v : a.b.cache_k) + (layer * p.cache_layer_stride + head * a.lead) * bytes;
+    const int64_t byte = static_cast<int64_t>(slice) * kSlice + part * 16;
+    const bool mine_too = byte < a.row_bytes;
+    cache += byte;
+    auto row = [&](int slot) {
+        const int page = a.by_page.of(slot);
+        return cache + (page * p.page_stride + (slot - page * p.page_size) * p.slot_stride) * bytes;
+    };
+    const int32_t* slots = a.slots + static_cast<int64_t>(list) * p.budget;
+    for (int first = a.moved[list]; first < p.budget; first += kMoveRows) {
+        uint4 v[kLoads];
+        int from[kLoads], to[kLoads];
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int i = first + j * kRowsTogether + mine;
+            from[j] = to[j] = -1;
+            if (i < p.budget && mine_too) {
+                const int column = a.by_page.of(i), page = a.b.block_table[static_cast<int64_t>(b) * p.table_width + column];
+                from[j] = slots[i];
+                if (page >= 0 && page < p.num_pages) to[j] = page * p.page_size + i - column * p.page_size;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j)
+            if (from[j] >= 0 && to[j] >= 0) v[j] = *reinterpret_cast<const uint4*>(row(from[j]));
+        // all rows of this round are here before the first one is written
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j)
+            if (from[j] >= 0 && to[j] >= 0) *reinterpret_cast<uint4*>(row(to[j])) = v[j];
+    }
+}
+
+// ------------------------------------------------------------------ host side
+
+static int check_eviction(const mpv_eviction* p) {
+    if (!p) return MPV_ERR_NULL;
+    if (p->layers < 0 || p->B < 0 || p->kv_heads < 1 || p->head_dim < 1 || (p->score_heads != 1 && p->score_heads != p->kv_heads) || p->num_pages < 0 ||
+        p->page_size < 1 || p->table_width < 0 || p->budget < 1 || p->trigger < p->budget || p->sinks < 0 || p->recent < 0 ||
+        static_cast<int64_t>(p->sinks) + p->recent > p->budget || p->score_width < span(0, p->table_width, p->page_size))
+        return MPV_ERR_BAD_SHAPE;
+    if (!known_dtype(p->dtype)) return MPV_ERR_BAD_DTYPE;
+    if (p->head_dim > MPV_MAX_HEAD_DIM || p->kv_heads > MPV_MAX_HEADS) return MPV_ERR_UNSUPPORTED;
+    const int64_t row = static_cast<int64_t>(p->kv_heads) * p->head_dim;
+    if (p->slot_stride < row || p->page_stride < 0 || p->cache_layer_stride < 0) return MPV_ERR_BAD_SHAPE;
+    const int64_t lists = span(0, span(0, p->layers, p->B), p->score_heads);
+    if (span(0, p->num_pages, p->page_size) > INT32_MAX || span(0, p->table_width, p->page_size) > INT32_MAX || p->score_width > INT32_MAX ||
+        lists > INT32_MAX / 1024 || span(0, lists, p->budget) > (static_cast<int64_t>(1) << 40) ||
+        span(0, lists, (row * elem_bytes(p->dtype) + kSlice - 1) / kSlice * 2) > INT32_MAX ||
+        span(0, span(span(span(0, p->num_pages, p->page_stride), p->page_size, p->slot_stride), p->layers, p->cache_layer_stride), 4) == INT64_MAX)
+        return MPV_ERR_UNSUPPORTED;
+    const int64_t all = p->head_dim | p->slot_stride | p->page_stride | p->cache_layer_stride;
+    if ((all * elem_bytes(p->dtype)) % 16 != 0) return MPV_ERR_ALIGNMENT;
+    return MPV_OK;
+}
+
+static size_t slots_bytes(const mpv_eviction* p) {
+    return (static_cast<size_t>(p->layers) * p->B * p->score_heads * p->budget * sizeof(int32_t) + 255) / 256 * 256;
+}
+
+}  // namespace mpv
+
+extern "C" {
+
+int mpv_evict_positions_workspace_bytes(const mpv_eviction* eviction, size_t* out) {
+    if (!out) return MPV_ERR_NULL;
+    const int rc = mpv::check_eviction(eviction);
+    if (rc != MPV_OK) return rc;
+    *out = mpv::slots_bytes(eviction) + static_cast<size_t>(eviction->layers) * eviction->B * eviction->score_heads * sizeof(int32_t);
+    return MPV_OK;
+}
+
+int mpv_evict_positions(const mpv_eviction* eviction, const mpv_eviction_buffers* buf, void* workspace, size_t workspace_bytes,
+                        void* hip_stream) {
+    size_t need;
+    const int rc = mpv_evict_positions_workspace_bytes(eviction, &need);
+    if (rc != MPV_OK) return rc;
+    if (!buf) return MPV_ERR_NULL;
+    const mpv_eviction* p = eviction;
+    if (p->B == 0) return MPV_OK;
+    const bool any = p->layers > 0;
+    if (!buf->context_len || !buf->context_len_out || !buf->free_count || !buf->free_count_out || (p->num_pages > 0 && !buf->free_pages) ||
+        (p->table_width > 0 && !buf->block_table) ||
+        (any && (!buf->kept || (p->score_width > 0 && (!buf->scores || !buf->scores_out)) || (p->num_pages > 0 && (!buf->cache_k || !buf->cache_v)))))
+        return MPV_ERR_NULL;
+    if (!mpv::aligned(buf->cache_k, 16) || !mpv::aligned(buf->cache_v, 16)) return MPV_ERR_ALIGNMENT;
+    if (!workspace || !mpv::aligned(workspace, 256) || workspace_bytes < need) return MPV_ERR_WORKSPACE;
+    mpv::EvictArgs a;
+    a.p = *p;
+    a.b = *buf;
+    a.lists = p->layers * p->B * p->score_heads;
+    a.row_bytes = static_cast<int64_t>(p->score_heads == 1 ? p->kv_heads : 1) * p->head_dim * mpv::elem_bytes(p->dtype);
+    a.lead = p->score_heads == 1 ? 0 : p->head_dim;
+    a.slices = static_cast<int>((a.row_bytes + mpv::kSlice - 1) / mpv::kSlice);
+    a.by_page.set(static_cast<uint32_t>(p->page_size));
+    a.slots = static_cast<int32_t*>(workspace);
+    a.moved = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + mpv::slots_bytes(p));
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    (void)hipGetLastError();
+    if (a.lists > 0) hipLaunchKernelGGL(mpv::select_kernel, dim3(static_cast<unsigned>(a.lists)), dim3(mpv::kSelectBlock), 0, s, a);
+    const int64_t waves = static_cast<int64_t>(a.lists) * a.slices * 2, workgroups = (waves + mpv::kMoveBlock / 64 - 1) / (mpv::kMoveBlock / 64);
+    hipLaunchKernelGGL(mpv::move_kernel, dim3(static_cast<unsigned>(workgroups + 1)), dim3(mpv::kMoveBlock), 0, s, a);
+    return mpv::launched();
+}
+
+}  // extern "C"

@@ -1,0 +1,425 @@
+// Log probabilities of given tokens, entropy and the most likely tokens of logit rows: device and host code.
+
+#include <hip/hip_bf16.h>
+#include <hip/hip_fp16.h>
+
+#include <algorithm>
+#include <cfloat>
+#include <cmath>
+#include <type_traits>
+
+#include "mpv_host.h"
+
+namespace mpv {
+
+// With c = log2(e) / T, m = max z, S = sum 2^(c (z - m)), A = sum 2^(c (z - m)) (z - m):
+//   log2 p_t = c (z_t - m) - log2 S,    entropy = log2 S - c A / S  (log2 units)
+// (the difference before the factor: c times the lowest float32, a mask, would be -inf, and a row of them empty.)
+// S and A of parts are put together by powers of 2, as the statistics of a softmax are.  The best tokens are found through the maxima
+// of segments of 64 tokens: the `top` best lie in the `top` segments with the largest maxima (of equal ones the first), so the row is
+// read once, and those segments again.
+//
+// sweep_kernel: a workgroup has a part of a row; finish_kernel: one has a row, its parts and its segments' maxima.
+
+constexpr int kSweepBlock = 256;
+constexpr int kFinishBlock = 256;
+constexpr int kSegment = 64;
+constexpr int kChunks = 4;                 // 16-byte loads of a thread in flight
+
+struct PartSums { float m, sum, weighted; int32_t better; };
+
+struct RowArgs {
+    mpv_logprobs p;
+    mpv_logprob_buffers b;
+    int rows, width, parts, part;          // output rows in all and of a tree; parts of a row, segments of each
+    int segments;
+    float c;                               // log2(e) / T
+    PartSums* sums;                        // [rows][parts]
+    float* best;                           // [rows][segments] (top > 0)
+};
+
+__device__ __forceinline__ float logit(float z) { return z; }
+__device__ __forceinline__ float logit(uint16_t z) { return __uint_as_float(static_cast<uint32_t>(z) << 16); }
+__device__ __forceinline__ float logit(__half z) { return __half2float(z); }
+
+// Numbers in the order of the logits, -inf at 0x007fffff; both zeros are the same.
+__device__ __forceinline__ uint32_t order_of(float z) {
+    const uint32_t u = __float_as_uint(z + 0.0f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float from_order(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+constexpr uint32_t kNothing = 0x007fffffu;
+
+// Maximum over the lanes of a segment, 8 or 16 neighbours.
+template <int LANES>
+__device__ __forceinline__ float segment_max(float v) {
+    auto with = [&](auto control) {
+        constexpr int kControl = decltype(control)::value;
+        return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kControl, 0xf, 0xf, true)));
+    };
+    v = with(std::integral_constant<int, 0xb1>());                 // neighbours
+    v = with(std::integral_constant<int, 0x4e>());                 // pairs
+    v = with(std::integral_constant<int, 0x141>());                // fours, mirrored
+    if (LANES == 16) v = with(std::integral_constant<int, 0x140>());
+    return v;
+}
+
+// An output row: where its logits are and its token; node < 0: there is none.
+struct Row { int64_t at; int token; bool real; };
+__device__ __forceinline__ Row row_of(const RowArgs& a, int row) {
+    const int b = row / a.width, i = row - b * a.width;
+    Row r{0, -1, false};
+    int node = i;
+    if (a.p.paths) {
+        const int length = min(max(a.b.accept_len[b], 0), a.p.max_depth);
+        if (i > length) return r;
+        node = i == 0 ? 0 : a.b.path_nodes[static_cast<int64_t>(b) * a.p.max_depth + i - 1];
+        r.token = i == length ? a.b.bonus_token[b] : a.b.tokens[static_cast<int64_t>(b) * a.p.max_depth + i];
+    } else {
+        if (a.b.num_nodes && i >= a.b.num_nodes[b]) return r;
+        r.token = a.b.tokens[row];
+    }
+    if (node < 0 || node >= a.p.N) return r;
+    r.real = true;
+    r.at = (static_cast<int64_t>(b) * a.p.N + node) * a.p.stride;
+    return r;
+}
+
+template <class T>
+__global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
+    constexpr int N = 16 / sizeof(T), kLanes = kSegment / N;
+    const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
+    const Row r = row_of(a, row);
+    if (!r.real) return;
+    const T* z = static_cast<const T*>(a.b.logits) + r.at;
+    const int V = a.p.V, whole = V / N;
+    const bool known = r.token >= 0 && r.token < V;
+    const float mine = known ? logit(z[r.token]) : INFINITY;
+    const int from = part * a.part * kLanes, to = min(from + a.part * kLanes, a.segments * kLanes);      // chunks of N
+    float m = -INFINITY, sum = 0.0f, weighted = 0.0f;
+    int better = 0;
+    for (int first = from; first < to; first += kChunks * kSweepBlock) {
+        T raw[kChunks][N];
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j) {
+            const int chunk = first + j * kSweepBlock + threadIdx.x;
+            if (chunk < to && chunk < whole) __builtin_memcpy(raw[j], z + static_cast<int64_t>(chunk) * N, 16);
+        }
+        float v[kChunks][N], most[kChunks];
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j) {
+            const int chunk = first + j * kSweepBlock + threadIdx.x;
+            most[j] = -INFINITY;
+            if (chunk < to && chunk < whole) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[j][i] = logit(raw[j][i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int at = chunk * N + i;
+                    v[j][i] = chunk < to && at < V ? logit(z[at]) : -INFINITY;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) most[j] = fmaxf(most[j], v[j][i]);
+            if (a.p.top > 0) {
+                const float best = segment_max<kLanes>(most[j]);
+                if (threadIdx.x % kLanes == 0 && chunk < to) a.best[static_cast<int64_t>(row) * a.segments + chunk / kLanes] = best;
+            }
+            // tokens before the given one are better if they are not smaller
+#pragma unroll
+            for (int i = 0; i < N; ++i) better += v[j][i] > mine || (v[j][i] == mine && chunk * N + i < (chunk < to ? r.token : 0));
+        }
+        float now = m;
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j) now = fmaxf(now, most[j]);
+        const float base = now == -INFINITY ? 0.0f : now;
+        if (m != -INFINITY) {
+            const float fade = exp2f((m - now) * a.c);
+            weighted = fade * (weighted + (m - now) * sum);
+            sum *= fade;
+        }
+        m = now;
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float d = v[j][i] - base, e = __builtin_amdgcn_exp2f(d * a.c);
+                sum += e;
+                weighted = fmaf(e, fmaxf(d, -FLT_MAX), weighted);  // (0 times -inf would be NaN)
+            }
+    }
+    // over the workgroup
+    __shared__ float ms[kSweepBlock / 64], sums[kSweepBlock / 64], weights[kSweepBlock / 64];
+    __shared__ int betters[kSweepBlock / 64];
+    float top = m;
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (m != -INFINITY) {
+        const float fade = exp2f((m - top) * a.c);
+        weighted = fade * (weighted + (m - top) * sum);
+        sum *= fade;
+    }
+    for (int d = 32; d; d >>= 1) {
+        sum += __shfl_xor(sum, d);
+        weighted += __shfl_xor(weighted, d);
+        better += __shfl_xor(better, d);
+    }
+    if (lane == 0) { ms[wave] = top; sums[wave] = sum; weights[wave] = weighted; betters[wave] = better; }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        PartSums s{ms[0], 0.0f, 0.0f, 0};
+        for (int w = 1; w < kSweepBlock / 64; ++w) s.m = fmaxf(s.m, ms[w]);
+        for (int w = 0; w < kSweepBlock / 64; ++w) {
+            const float apart = ms[w] == -INFINITY ? 0.0f : ms[w] - s.m, fade = exp2f(apart * a.c);
+            s.sum += fade * sums[w];
+            s.weighted += fade * (weights[w] + apart * sums[w]);
+            s.better += betters[w];
+        }
+        a.sums[static_cast<int64_t>(row) * a.parts + part] = s;
+    }
+}
+
+// Exclusive sums over the workgroup; the sum of all in `total`.
+__device__ __forceinline__ int block_before(int v, int* part, int& total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int upto = v;
+    for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(upto, d);
+        if (lane >= d) upto += o;
+    }
+    __syncthreads();
+    if (lane == 63) part[wave] = upto;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+    for (int w = 0; w < kFinishBlock / 64; ++w) {
+        if (w < wave) before += part[w];
+        total += part[w];
+    }
+    return before + upto - v;
+}
+
+template <class T>
+__global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
+    constexpr int N = 16 / sizeof(T);
+    const int row = blockIdx.x, top = a.p.top;
+    const Row r = row_of(a, row);
+    int32_t* tokens = top > 0 ? a.b.top_tokens + static_cast<int64_t>(row) * top : nullptr;
+    float* logprobs = top > 0 ? a.b.top_logprobs + static_cast<int64_t>(row) * top : nullptr;
+    if (!r.real) {
+        if (threadIdx.x == 0) {
+            a.b.logprob[row] = 0.0f;
+            a.b.entropy[row] = 0.0f;
+            a.b.rank[row] = -1;
+        }
+        for (int i = threadIdx.x; i < top; i += kFinishBlock) { tokens[i] = -1; logprobs[i] = -INFINITY; }
+        return;
+    }
+    const T* z = static_cast<const T*>(a.b.logits) + r.at;
+    __shared__ int scratch[kFinishBlock / 64];
+    __shared__ float shared_m, shared_log, shared_sum;
+    if (threadIdx.x < 64) {
+        // (all lanes have parts: their number is not limited by the wave)
+        const PartSums* s = a.sums + static_cast<int64_t>(row) * a.parts;
+        float m = -INFINITY, sum = 0.0f, weighted = 0.0f;
+        int better = 0;
+        for (int p = threadIdx.x; p < a.parts; p += 64) m = fmaxf(m, s[p].m);
+        for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+        for (int p = threadIdx.x; p < a.parts; p += 64) {
+            const PartSums x = s[p];
+            const float apart = x.m == -INFINITY ? 0.0f : x.m - m, fade = exp2f(apart * a.c);
+            sum += fade * x.sum;
+            weighted += fade * (x.weighted + apart * x.sum);
+            better += x.better;
+        }
+        for (int d = 32; d; d >>= 1) {
+            sum += __shfl_xor(sum, d);
+            weighted += __shfl_xor(weighted, d);
+            better += __shfl_xor(better, d);
+        }
+        if (threadIdx.x == 0) {
+            constexpr float kLn2 = 0.69314718055994531f;
+            const float log = log2f(sum);
+            const bool known = r.token >= 0 && r.token < a.p.V, number = sum == sum;
+            float logprob = -INFINITY, entropy = (log - a.c * (weighted / sum)) * kLn2;
+            if (!number) logprob = entropy = NAN;
+            else if (sum == 0.0f) entropy = 0.0f;
+            else if (known) logprob = ((logit(z[r.token]) - m) * a.c - log) * kLn2;
+            a.b.logprob[row] = logprob;
+            a.b.entropy[row] = entropy;
+            a.b.rank[row] = known && number ? better + 1 : -1;
+            shared_m = m;
+            shared_log = log;
+            shared_sum = sum;
+        }
+    }
+    if (top == 0) return;
+    __syncthreads();
+    const float m = shared_m, log = shared_log;
+    if (!(shared_sum > 0.0f)) {                                    // no tokens, or no numbers
+        const float v = shared_sum == 0.0f ? -INFINITY : NAN;
+        for (int i = threadIdx.x; i < top; i += kFinishBlock) { tokens[i] = -1; logprobs[i] = v; }
+        return;
+    }
+    // the top-th largest of the segments' maxima, a byte at a time; `above`: those larger than it
+    const float* best = a.best + static_cast<int64_t>(row) * a.segments;
+    __shared__ int counts[256];
+    __shared__ int chosen_digit, chosen_above;
+    uint32_t limit = 0;
+    int above = 0;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        counts[threadIdx.x] = 0;
+        __syncthreads();
+        for (int s = threadIdx.x; s < a.segments; s += kFinishBlock) {
+            const uint32_t k = order_of(best[s]);
+            if (shift == 24 || k >> (shift + 8) == limit >> (shift + 8)) atomicAdd(&counts[k >> shift & 255], 1);
+        }
+        __syncthreads();
+        // digits from the largest on: thread i has digit 255 - i
+        int total;
+        const int mine = counts[255 - threadIdx.x], before = block_before(mine, scratch, total);
+        if (threadIdx.x == 0) { chosen_digit = 0; chosen_above = above + total - counts[0]; }     // (fewer segments than wanted)
+        __syncthreads();
+        if (above + before < top && above + before + mine >= top) { chosen_digit = 255 - threadIdx.x; chosen_above = above + before; }
+        __syncthreads();
+        limit |= static_cast<uint32_t>(chosen_digit) << shift;
+        above = chosen_above;
+        __syncthreads();
+    }
+    if (limit <= kNothing) limit = kNothing + 1;                   // tokens of no probability are no alternatives
+    // the segments with larger maxima, and as many of those that have it, from the first on
+    __shared__ int segments[MPV_MAX_TOP];
+    __shared__ int found;
+    const int each = (a.segments + kFinishBlock - 1) / kFinishBlock, first = min(a.segments, static_cast<int>(threadIdx.x) * each);
+    const int last = min(a.segments, first + each);
+    int larger = 0, equal = 0;
+    for (int s = first; s < last; ++s) {
+        const uint32_t k = order_of(best[s]);
+        larger += k > limit;
+        equal += k == limit;
+    }
+    int all_larger, all_equal;
+    int at_larger = block_before(larger, scratch, all_larger), at_equal = block_before(equal, scratch, all_equal);
+    const int take = min(all_larger + all_equal, top);
+    for (int s = first; s < last; ++s) {
+        const uint32_t k = order_of(best[s]);
+        if (k > limit) {
+            if (at_larger < top) segments[at_larger] = s;
+            ++at_larger;
+        } else if (k == limit) {
+            if (all_larger + at_equal < top) segments[all_larger + at_equal] = s;
+            ++at_equal;
+        }
+    }
+    // their tokens that are not smaller, in any order
+    __shared__ unsigned long long candidates[MPV_MAX_TOP * kSegment];
+    if (threadIdx.x == 0) found = 0;
+    __syncthreads();
+    constexpr int kLanes = kSegment / N;
+    for (int i = threadIdx.x; i < take * kLanes; i += kFinishBlock) {
+        const int token = segments[i / kLanes] * kSegment + i % kLanes * N;
+        for (int j = 0; j < N; ++j) {
+            if (token + j >= a.p.V) break;
+            const uint32_t k = order_of(logit(z[token + j]));
+            if (k >= limit) candidates[atomicAdd(&found, 1)] = static_cast<unsigned long long>(k) << 32 | static_cast<uint32_t>(~(token + j));
+        }
+    }
+    __syncthreads();
+    const int count = found;
+    for (int i = threadIdx.x; i < count; i += kFinishBlock) {
+        const unsigned long long k = candidates[i];
+        int place = 0;
+        for (int j = 0; j < count; ++j) place += candidates[j] > k;
+        if (place < top) {
+            tokens[place] = static_cast<int>(~static_cast<uint32_t>(k));
+            logprobs[place] = ((from_order(static_cast<uint32_t>(k >> 32)) - m) * a.c - log) * 0.69314718055994531f;
+        }
+    }
+    for (int i = count + threadIdx.x; i < top; i += kFinishBlock) { tokens[i] = -1; logprobs[i] = -INFINITY; }
+}
+
+// ------------------------------------------------------------------ host side
+
+// Segments of a part: so many workgroups that the card is full, each with no more than 16 rounds of loads.
+static void parts_of(const mpv_logprobs* p, int64_t rows, int* parts, int* part) {
+    const int64_t segments = (p->V + kSegment - 1) / kSegment;
+    const int64_t round = kChunks * kSweepBlock * (16 / elem_bytes(p->dtype)) / kSegment;         // segments of a round
+    const int64_t wanted = std::max<int64_t>(1, std::min<int64_t>((2048 + rows - 1) / rows, (segments + round - 1) / round));
+    const int64_t least = (segments + 16 * round - 1) / (16 * round);
+    const int64_t n = std::max(wanted, least);
+    *part = static_cast<int>((segments + n - 1) / n);
+    *parts = static_cast<int>((segments + *part - 1) / *part);
+}
+
+static int check_logprobs(const mpv_logprobs* p) {
+    if (!p) return MPV_ERR_NULL;
+    if (p->B < 0 || p->N < 1 || p->V < 1 || p->top < 0 || p->stride < p->V || (p->paths != 0 && p->paths != 1) || (p->paths && p->max_depth < 1))
+        return MPV_ERR_BAD_SHAPE;
+    if (!known_dtype(p->dtype)) return MPV_ERR_BAD_DTYPE;
+    if (!std::isfinite(p->temperature) || !(p->temperature > 0.0f)) return MPV_ERR_BAD_TEMPERATURE;
+    if (p->V > MPV_MAX_VOCAB || p->top > MPV_MAX_TOP) return MPV_ERR_UNSUPPORTED;
+    const int64_t width = p->paths ? static_cast<int64_t>(p->max_depth) + 1 : p->N, rows = width * p->B;
+    if (rows > (1 << 24) || span(0, static_cast<int64_t>(p->B) * p->N, p->stride) > INT64_MAX / 8) return MPV_ERR_UNSUPPORTED;
+    return MPV_OK;
+}
+
+struct LogprobRoom { size_t sums, best; };
+static LogprobRoom room_of(const mpv_logprobs* p, RowArgs* a) {
+    const int64_t width = p->paths ? static_cast<int64_t>(p->max_depth) + 1 : p->N, rows = width * p->B;
+    a->rows = static_cast<int>(rows);
+    a->width = static_cast<int>(width);
+    a->segments = (p->V + kSegment - 1) / kSegment;
+    parts_of(p, std::max<int64_t>(rows, 1), &a->parts, &a->part);
+    const size_t sums = (static_cast<size_t>(rows) * a->parts * sizeof(PartSums) + 255) / 256 * 256;
+    return {sums, p->top > 0 ? static_cast<size_t>(rows) * a->segments * sizeof(float) : 0};
+}
+
+template <class T>
+static int launch_rows(const RowArgs& a, hipStream_t s) {
+    (void)hipGetLastError();
+    hipLaunchKernelGGL(sweep_kernel<T>, dim3(static_cast<unsigned>(a.rows) * a.parts), dim3(kSweepBlock), 0, s, a);
+    hipLaunchKernelGGL(finish_kernel<T>, dim3(static_cast<unsigned>(a.rows)), dim3(kFinishBlock), 0, s, a);
+    return launched();
+}
+
+}  // namespace mpv
+
+extern "C" {
+
+int mpv_token_logprobs_workspace_bytes(const mpv_logprobs* logprobs, size_t* out) {
+    if (!out) return MPV_ERR_NULL;
+    const int rc = mpv::check_logprobs(logprobs);
+    if (rc != MPV_OK) return rc;
+    mpv::RowArgs a;
+    const mpv::LogprobRoom room = mpv::room_of(logprobs, &a);
+    *out = room.sums + room.best;
+    return MPV_OK;
+}
+
+int mpv_token_logprobs(const mpv_logprobs* logprobs, const mpv_logprob_buffers* buf, void* workspace, size_t workspace_bytes,
+                       void* hip_stream) {
+    const int rc = mpv::check_logprobs(logprobs);
+    if (rc != MPV_OK) return rc;
+    if (!buf) return MPV_ERR_NULL;
+    if (logprobs->B == 0) return MPV_OK;
+    if (!buf->logits || !buf->tokens || !buf->logprob || !buf->rank || !buf->entropy ||
+        (logprobs->paths && (!buf->accept_len || !buf->path_nodes || !buf->bonus_token)) ||
+        (logprobs->top > 0 && (!buf->top_tokens || !buf->top_logprobs)))
+        return MPV_ERR_NULL;
+    if (!mpv::aligned(buf->logits, mpv::elem_bytes(logprobs->dtype))) return MPV_ERR_ALIGNMENT;
+    mpv::RowArgs a;
+    a.p = *logprobs;
+    a.b = *buf;
+    const mpv::LogprobRoom room = mpv::room_of(logprobs, &a);
+    if (!workspace || !mpv::aligned(workspace, 256) || workspace_bytes < room.sums + room.best) return MPV_ERR_WORKSPACE;
+    a.c = static_cast<float>(1.4426950408889634 / static_cast<double>(logprobs->temperature));
+    a.sums = static_cast<mpv::PartSums*>(workspace);
+    a.best = reinterpret_cast<float*>(static_cast<char*>(workspace) + room.sums);
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    if (logprobs->dtype == MPV_DTYPE_F32) return mpv::launch_rows<float>(a, s);
+    if (logprobs->dtype == MPV_DTYPE_BF16) return mpv::launch_rows<uint16_t>(a, s);
+    return mpv::launch_rows<__half>(a, s);
+}
+
+}  // extern "C"
