@@ -31,6 +31,7 @@ UNITS = {
     "mpv_attention.hip": ["-mllvm", "-disable-machine-licm", "-Wno-inline-asm"],
     "mpv_prefix.hip": ["-mllvm", "-disable-machine-licm", "-Wno-inline-asm"],
     "mpv_behind.hip": ["-mllvm", "-disable-machine-licm", "-Wno-inline-asm"],
+    "mpv_through.hip": ["-mllvm", "-disable-machine-licm", "-Wno-inline-asm"],
     "mpv_chains.hip": [],
     "mpv_cache.hip": [],
     "mpv_scores.hip": [],

@@ -49,8 +49,9 @@ struct AttentionArgs {
 };
 
 // What a kernel attends to: a tree's context and the tree (mpv_tree_attention); the same behind a prefix that others share, whose
-// sums the rows begin with; or such a prefix, for the nodes of all trees that follow each other and share it, up to 64 of them.
-constexpr int kTree = 0, kBehind = 1, kPrefix = 2;
+// sums the rows begin with; such a prefix, for the nodes of all trees that follow each other and share it, up to 64 of them; or a tree's
+// prefix, context and nodes, one after the other.
+constexpr int kTree = 0, kBehind = 1, kPrefix = 2, kThrough = 3;
 
 struct PrefixArgs : AttentionArgs {
     const int32_t* prefix_of;              // null: there are none
@@ -59,6 +60,9 @@ struct PrefixArgs : AttentionArgs {
     int prefixes, prefix_width;
     float* lse;                            // null: not wanted
     float* partial_exact;                  // [teams][members][2][rows]: sums of the weights as they were before they were rounded
+    int2* units;                           // kPrefix, [B][kv_heads][supers]: first and last team of a unit (last < 0: one team's alone)
+    int supers;                            // units of a cache head, at most
+    Divisor by_rows;                       // rows of a block
     // what a prefix gives to the rows [B,N,heads]: columns of their sums; reference and sum of weights; the same before rounding
     float* state;
     float2* state_stats;
@@ -168,6 +172,11 @@ __device__ __forceinline__ int fresh(int x) {
 // What beginning and ending a unit takes, in tiles: workgroups with many short units would end last otherwise.  256 trees of 8 nodes,
 // contexts of 16 to 256: 66 us, 91 without; the benchmark's trees 613 us, 637 without; contexts of one length: the same.
 constexpr int kUnitCost = 8;
+// Tiles of a team that reads prefixes, at least.
+#ifndef LEAST
+#define LEAST 1
+#endif
+constexpr int kLeastTiles = LEAST;
 // All bits where bit `at` is set, none otherwise.  (Masks instead of conditions: those would all wait in scalar registers at once.)
 __device__ __forceinline__ uint32_t spread(uint32_t bits, int at) { return static_cast<uint32_t>(static_cast<int32_t>(bits << (31 - at)) >> 31); }
 
@@ -178,6 +187,7 @@ struct TreeWork {
     int tiles;                             // of a unit, the tree's own among them
     int blocks;                            // row blocks
     int sinks;                             // (kBehind) those of the context
+    int before;                            // (kThrough) positions of the prefix
     // (kPrefix: `context` is the prefix's length, `nodes` are all nodes of the trees that share it; no tree's own tiles.)
     int which, first, end;                 // the prefix, its first tree, the tree behind its last
     int supers;                            // units of a cache head: `blocks` row blocks each
@@ -190,6 +200,11 @@ __device__ __forceinline__ TreeWork tree_work(const typename ArgsOf<KIND>::T& g,
     const mpv_attention& a = g.a;
     t.context = min(max(g.b.context_len[b], 0), a.table_width * a.page_size);
     t.nodes = g.b.num_nodes ? min(max(g.b.num_nodes[b], 0), a.N) : a.N;
+    if constexpr (KIND == kThrough) {
+        t.which = prefix_of(g, b);
+        t.before = prefix_length(g, t.which);
+        t.context += t.before;
+    }
     t.low = t.sink_tiles = 0;
     t.sinks = max(a.sinks, 0);
     if constexpr (KIND == kBehind)
@@ -345,6 +360,9 @@ struct Attention {
         const Row r = row_of(fresh(lane), tile, last);
         const int32_t* entry;
         if constexpr (KIND == kPrefix) entry = g.prefix_table + static_cast<int64_t>(t.which) * g.prefix_width + g.by_page.of(r.at);
+        else if constexpr (KIND == kThrough)
+            entry = r.at < t.before ? g.prefix_table + static_cast<int64_t>(t.which) * g.prefix_width + g.by_page.of(r.at)
+                                    : g.b.block_table + static_cast<int64_t>(b) * g.a.table_width + g.by_page.of(r.at - t.before);
         else entry = g.b.block_table + static_cast<int64_t>(b) * g.a.table_width + g.by_page.of(r.at);
         const uint64_t from = r.seen && !r.tree ? reinterpret_cast<uint64_t>(entry) : reinterpret_cast<uint64_t>(&kZeros);
         word_to_lds(from, shared_at + offsetof(Shared, pages) + wave * 256);
@@ -362,6 +380,8 @@ struct Attention {
         } else {
             const int page = sh.pages[wave][lane];
             r.seen = r.seen && page >= 0 && page < g.a.num_pages;
+            if constexpr (KIND == kThrough)
+                if (r.at >= t.before) r.at -= t.before;
             offset = page * g.a.page_stride + (r.at - g.by_page.of(r.at) * g.a.page_size) * g.a.slot_stride;
             keys = static_cast<const char*>(g.b.cache_k);
             values = static_cast<const char*>(g.b.cache_v);
@@ -529,8 +549,8 @@ struct Attention {
             weight[q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < kColumns; ++c) out[q][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if constexpr (KIND == kBehind) {
-                if constexpr (k16) exact[q] = 0.0f;
+            if constexpr (KIND != kTree && k16) exact[q] = 0.0f;
+            if constexpr (KIND == kBehind)
                 if (behind && real) {
                     const int64_t state = (static_cast<int64_t>(b) * g.a.N + node) * g.a.heads + kv * group + row - node * group;
                     const float2 stats = g.state_stats[state];
@@ -545,7 +565,6 @@ struct Attention {
 #pragma unroll
                     for (int c = 0; c < kColumns; ++c) out[q][c] = *reinterpret_cast<const f32x4*>(g.state + state * DP + c * 16 + quad * 4);
                 }
-            }
         }
     }
 
@@ -923,7 +942,7 @@ struct Attention {
         const int group = g.group;
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
-            if constexpr (KIND == kBehind)
+            if constexpr (KIND != kTree)
                 if (g.lse && quad == 0) {
                     const int row = block * kRows + (wave * QT + q) * 16 + l16, node = g.by_group.of(row);
                     if (node < t.nodes)
@@ -1052,8 +1071,8 @@ struct Attention {
         // a unit counts as `extra` tiles more than it has, all of them before its first
         const int extra = static_cast<int>(min(static_cast<int64_t>(kUnitCost), uniform64(tiles) / (2 * most)));
         const int64_t total = uniform64(tiles) + extra * uniform64(units);
-        const int T = static_cast<int>(min(static_cast<int64_t>(most), total));
-        if (member == 0 && threadIdx.x == 0 && !g.by_unit) g.split[team] = make_int4(-1, 0, 0, 0);
+        const int T = static_cast<int>(min(static_cast<int64_t>(most), KIND == kPrefix ? (total + kLeastTiles - 1) / kLeastTiles : total));
+        if (KIND != kPrefix && member == 0 && threadIdx.x == 0 && !g.by_unit) g.split[team] = make_int4(-1, 0, 0, 0);
         if (team >= T) return;
         // the first `longer` teams have one tile more than the others
         const int64_t share = total <= UINT32_MAX ? static_cast<int64_t>(static_cast<uint32_t>(total) / static_cast<uint32_t>(T)) : total / T;
@@ -1097,10 +1116,11 @@ struct Attention {
                 at = min(unit + length, end_at);
                 const bool shared = first > 0 || last < t.tiles;
                 if (last <= first) continue;
-                if (member == 0 && first == 0 && threadIdx.x == 0 && (shared || g.by_unit)) {
+                if (member == 0 && first == 0 && threadIdx.x == 0 && (shared || KIND == kPrefix || g.by_unit)) {
                     const int64_t x = unit + length - 1, ahead = longer * (share + 1);       // the unit's last tile, and whose it is
                     const int64_t whose = x < ahead ? x / (share + 1) : longer + (x - ahead) / share;
-                    if constexpr (KIND == kPrefix) g.split[team] = make_int4(b, kv, super, static_cast<int>(whose));
+                    if constexpr (KIND == kPrefix)
+                        g.units[(static_cast<int64_t>(b) * g.a.kv_heads + kv) * g.supers + super] = make_int2(team, shared ? static_cast<int>(whose) : -1);
                     else g.split[g.by_unit ? b * g.a.kv_heads + kv : team] = make_int4(shared ? b : -1, kv, team, static_cast<int>(whose));
                 }
                 if constexpr (KIND == kPrefix) {
@@ -1130,50 +1150,22 @@ template <int KIND, int DTYPE, int DP, int ROWS>
 __device__ __forceinline__ void combine(const typename ArgsOf<KIND>::T& g) {
     typedef Elem<DTYPE> E;
     constexpr int kLanes = DP / 4, kGroups = 64 / kLanes;
-    const int nodes_of_unit = KIND != kPrefix && g.by_unit && g.b.num_nodes ? g.b.num_nodes[blockIdx.x / g.a.kv_heads] : 1;
+    const int nodes_of_unit = g.by_unit && g.b.num_nodes ? g.b.num_nodes[blockIdx.x / g.a.kv_heads] : 1;
     if (nodes_of_unit <= 0) return;                                // (nobody wrote its entry)
     const int4 s = g.split[blockIdx.x];
     if (s.x < 0) return;
     const int lane = threadIdx.x & 63, column = lane % kLanes * 4, mine = lane / kLanes;
-    const int b = s.x, kv = s.y, first = KIND == kPrefix ? static_cast<int>(blockIdx.x) : s.z, last = s.w, group = g.group;
+    const int b = s.x, kv = s.y, first = s.z, last = s.w, group = g.group;
     const int parts = last - first + 1;
-    int nodes, rows, row_base = 0, upto = 0;                       // kPrefix: rows of the unit, the first one's place among those of the prefix
-    if constexpr (KIND == kPrefix) {
-        const TreeWork w = prefix_work<1, ROWS>(g, b & ~63);
-        nodes = __shfl(w.nodes, b & 63);
-        const int end = __shfl(w.end, b & 63), tree = (b & ~63) + lane;
-        upto = wave_sum(tree >= b && tree < end ? nodes_of(g, tree) : 0);
-        row_base = s.z * g.blocks * ROWS;
-        rows = min(nodes * group - row_base, g.blocks * ROWS);
-    } else {
-        nodes = g.b.num_nodes ? min(max(g.b.num_nodes[b], 0), g.a.N) : g.a.N;
-        rows = nodes * group;
-    }
-    const int wave = blockIdx.y * 4 + (threadIdx.x >> 6);
+    const int nodes = g.b.num_nodes ? min(max(g.b.num_nodes[b], 0), g.a.N) : g.a.N;
+    const int rows = nodes * group, wave = blockIdx.y * 4 + (threadIdx.x >> 6);
     // part p of a row: the second slot of team `first`, the first slot of those after it
     auto at = [&](int row, int p) {
         return ((static_cast<int64_t>(first + p) * g.blocks + row / ROWS) * 2 + (p == 0 ? 1 : 0)) * ROWS + row % ROWS;
     };
     auto put = [&](int row, const f32x4& sum, float weight, float top, float exact) {
-        if constexpr (KIND == kPrefix) {                           // (all lanes of a wave call it)
-            const int place = row_base + min(row, rows - 1), rank = g.by_group.of(place);
-            int at = 0;
-#pragma unroll
-            for (int d = 32; d; d >>= 1)
-                if (__shfl(upto, at + d - 1) <= rank) at += d;
-            const int before = __shfl(upto, max(at - 1, 0));
-            const int64_t node = static_cast<int64_t>((b & ~63) + at) * g.a.N + rank - (at > 0 ? before : 0);
-            const int64_t state = node * g.a.heads + kv * group + place - rank * group;
-            if (row >= rows) return;
-            *reinterpret_cast<f32x4*>(g.state + state * DP + column) = sum;
-            if (column == 0) {
-                g.state_stats[state] = make_float2(top, weight);
-                if (E::kBytes == 2 && g.lse) g.state_exact[state] = exact;
-            }
-            return;
-        }
         const int node = g.by_group.of(row);
-        if constexpr (KIND == kBehind)
+        if constexpr (KIND != kTree)
             if (g.lse && row < rows && column == 0)
                 g.lse[(static_cast<int64_t>(b) * g.a.N + node) * g.a.heads + kv * group + row - node * group] = lse_of(top, exact, E::kBias);
         char* to = static_cast<char*>(g.b.out) +
@@ -1273,8 +1265,7 @@ __device__ __forceinline__ void combine(const typename ArgsOf<KIND>::T& g) {
             if (lane == 0) exact_sums[own] = exact;
         if (mine == 0) sums[own][lane] = sum;
         __syncthreads();
-        // (kPrefix: all lanes of the first wave, those of no group with the first one's)
-        if (own == 0 && (KIND == kPrefix || mine == 0)) {
+        if (own == 0 && mine == 0) {
             float most = tops[0];
 #pragma unroll
             for (int w = 1; w < 4; ++w) most = fmaxf(most, tops[w]);
@@ -1286,9 +1277,9 @@ __device__ __forceinline__ void combine(const typename ArgsOf<KIND>::T& g) {
                 const float f = exp2_of(tops[w] - base);
                 weight += weights[w] * f;
                 if constexpr (KIND != kTree) exact += exact_sums[w] * f;
-                sum += sums[w][lane % kLanes] * f;
+                sum += sums[w][lane] * f;
             }
-            put(KIND == kPrefix && mine != 0 ? rows : row, sum, weight, most, exact);
+            put(row, sum, weight, most, exact);
         }
     }
 }

@@ -5,67 +5,20 @@
 // So prefix_kernel works out the prefix's part for the nodes of all trees that share it (mpv_prefix.hip), and a row goes on from there
 // over its own context and tree as if they were the next tiles (kBehind of mpv_attention.h).  The state between the two is float32.
 
-#include "mpv_prefix.h"
+#include <cstdlib>
+#include "mpv_behind.h"
 
 namespace mpv {
 
-template <class A>
-__global__ __launch_bounds__(A::kThreads) __attribute__((amdgpu_waves_per_eu(2))) void behind_kernel(PrefixArgs g) {
-    extern __shared__ __align__(1024) char memory[];
-    A a(g, *reinterpret_cast<typename A::Shared*>(memory));
-    a.all();
+// Whether the prefixes are read for all trees that share them, or by every tree for itself.
+static bool together(const mpv_prefixed* p) {
+    const mpv_attention& a = p->attention;
+    if (a.B < 2 || p->prefixes < 1 || p->prefix_width < 1) return false;
+    if (const char* e = getenv("MPV_TOGETHER")) return atoi(e);
+    return true;
 }
 
-// Puts the units together that several teams share.
-template <int DTYPE, int DP, int ROWS>
-__global__ __launch_bounds__(256) void join_behind_kernel(PrefixArgs g) {
-    combine<kBehind, DTYPE, DP, ROWS>(g);
-}
-
-template <class A, int DTYPE, int DP>
-static int with_kernel(const mpv_attention* a, PrefixArgs* g, char* workspace, size_t* bytes, hipStream_t s) {
-    const Choice c = choice_of<A, DP>(a);
-    const Parts parts = Parts::of(c);
-    *bytes = parts.bytes();
-    if (!g) return MPV_OK;
-    parts.place(g, workspace);
-    g->teams = c.teams;
-    g->blocks = c.blocks;
-    g->by_unit = static_cast<int64_t>(a->B) * a->kv_heads < c.teams;
-    const int64_t rows = static_cast<int64_t>(a->N) * (a->heads / a->kv_heads);
-    (void)hipGetLastError();
-    if (!hip_fine(hipFuncSetAttribute(reinterpret_cast<const void*>(&behind_kernel<A>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                      static_cast<int>(sizeof(typename A::Shared)))))
-        return MPV_ERR_HIP;
-    hipLaunchKernelGGL(behind_kernel<A>, dim3(static_cast<unsigned>(c.teams) * c.blocks), dim3(A::kThreads), sizeof(typename A::Shared), s, *g);
-    const Second second = second_of<DP>(a, c, g->by_unit);
-    if (second.workgroups)
-        hipLaunchKernelGGL((join_behind_kernel<DTYPE, DP, A::kRows>), dim3(static_cast<unsigned>(second.entries), static_cast<unsigned>(second.workgroups)),
-                           dim3(256), 0, s, *g);
-    return launched();
-}
-
-template <int DTYPE, int DP>
-static int with_columns(const mpv_attention* a, PrefixArgs* g, char* workspace, size_t* bytes, hipStream_t s) {
-    return by_rows<kBehind, DTYPE, DP>(static_cast<int64_t>(a->N) * (a->heads / a->kv_heads), [&](auto kernel) {
-        return with_kernel<typename decltype(kernel)::T, DTYPE, DP>(a, g, workspace, bytes, s);
-    });
-}
-
-template <int DTYPE>
-static int with_type(const mpv_attention* a, PrefixArgs* g, char* workspace, size_t* bytes, hipStream_t s) {
-    if (a->head_dim <= 64) return with_columns<DTYPE, 64>(a, g, workspace, bytes, s);
-    if (a->head_dim <= 128) return with_columns<DTYPE, 128>(a, g, workspace, bytes, s);
-    return with_columns<DTYPE, 256>(a, g, workspace, bytes, s);
-}
-
-static int attend_behind(const mpv_attention* a, PrefixArgs* g, char* workspace, size_t* bytes, hipStream_t s) {
-    if (a->dtype == MPV_DTYPE_F32) return with_type<MPV_DTYPE_F32>(a, g, workspace, bytes, s);
-    if (a->dtype == MPV_DTYPE_BF16) return with_type<MPV_DTYPE_BF16>(a, g, workspace, bytes, s);
-    return with_type<MPV_DTYPE_F16>(a, g, workspace, bytes, s);
-}
-
-// Bytes of a workspace: the state of the rows (none without prefixes), and what either half needs while it runs.
+// Bytes of a workspace: the state of the rows (none where every tree reads its prefix), and what either half needs while it runs.
 struct Room {
     size_t state, stats, exact, parts;
     size_t bytes() const { return state + stats + exact + parts; }
@@ -73,10 +26,11 @@ struct Room {
 static int room_of(const mpv_prefixed* p, Room* r) {
     const mpv_attention* a = &p->attention;
     *r = {0, 0, 0, 0};
-    size_t behind, prefix = 0;
-    int rc = attend_behind(a, nullptr, nullptr, &behind, nullptr);
+    size_t trees, prefix = 0;
+    const bool shared = together(p);
+    int rc = shared ? attend_trees<kBehind>(p, nullptr, nullptr, &trees, nullptr) : attend_through(p, nullptr, nullptr, &trees, nullptr);
     if (rc != MPV_OK) return rc;
-    if (a->B > 0 && p->prefixes > 0 && p->prefix_width > 0) {
+    if (shared) {
         rc = attend_prefixes(a, nullptr, nullptr, &prefix, nullptr);
         if (rc != MPV_OK) return rc;
         const size_t rows = static_cast<size_t>(a->B) * a->N * a->heads;
@@ -84,7 +38,7 @@ static int room_of(const mpv_prefixed* p, Room* r) {
         r->exact = whole(rows * sizeof(float));
         r->state = whole(rows * columns_of(a) * sizeof(float));
     }
-    r->parts = std::max(behind, prefix);
+    r->parts = std::max(trees, prefix);
     return MPV_OK;
 }
 
@@ -128,7 +82,7 @@ int mpv_prefix_attention(const mpv_prefixed* prefixed, const mpv_prefixed_buffer
     if (a->B == 0) return MPV_OK;
     rc = mpv::check_buffers(a, &buf->attention);
     if (rc != MPV_OK) return rc;
-    const bool any = room.state != 0 && buf->prefix_of;
+    const bool any = prefixed->prefixes > 0 && prefixed->prefix_width > 0 && buf->prefix_of;
     // (a prefix may be all that there is in the cache)
     if (any && (!buf->prefix_table || !buf->prefix_len || (a->num_pages > 0 && (!buf->attention.cache_k || !buf->attention.cache_v)))) return MPV_ERR_NULL;
     if (!workspace || !mpv::aligned(workspace, 256) || workspace_bytes < room.bytes()) return MPV_ERR_WORKSPACE;
@@ -145,11 +99,12 @@ int mpv_prefix_attention(const mpv_prefixed* prefixed, const mpv_prefixed_buffer
     at += room.state + room.stats + room.exact;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     size_t need;
+    if (room.state == 0) return mpv::attend_through(prefixed, &g, at, &need, s);
     if (any) {
         rc = mpv::attend_prefixes(a, &g, at, &need, s);
         if (rc != MPV_OK) return rc;
     }
-    return mpv::attend_behind(a, &g, at, &need, s);
+    return mpv::attend_trees<mpv::kBehind>(prefixed, &g, at, &need, s);
 }
 
 }  // extern "C"

@@ -3,20 +3,19 @@
 // select_kernel: a workgroup has one list (layer, request, score head).  The budget's worth of best scores is found a byte of their order at
 // a time; then the kept positions are written in order, and the slots that their rows lie in.
 // move_kernel: kept rows move forward in order.  The i-th kept position s_i is at least i and the s_i ascend, so that what is written to the
-// rows [c, c + n) was read with them or before: a wave that takes a slice of a list's rows, some rows at a time, all loads before the
-// stores, needs no other copy.  Different slices (of different bytes) do not meet.  Its first workgroup returns the pages.
+// rows [c, c + n) was read with them or before: a workgroup that takes a slice of a list's rows, some rows a round, all loads before the
+// stores, needs no other copy, and may ask for the next round's rows before it writes.  Different slices (of different bytes) do not
+// meet.  Its first workgroup returns the pages.
 
 #include <algorithm>
 
 #include "mpv_host.h"
+#include "mpv_select.h"
 
 namespace mpv {
 
-constexpr int kSelectBlock = 512;
-constexpr int kMoveBlock = 256;
-constexpr int kSlice = 128;                // bytes of a row that a wave moves
-constexpr int kSliceLanes = kSlice / 16, kRowsTogether = 64 / kSliceLanes, kLoads = 8;
-constexpr int kMoveRows = kRowsTogether * kLoads;
+constexpr int kSelectBlock = 512;          // of the long lists
+constexpr int kLoads = 8;                  // rows of a thread in flight
 
 struct EvictArgs {
     mpv_eviction p;
@@ -57,20 +56,71 @@ __device__ __forceinline__ void before(int (&v)[2], int (&total)[2], int (*part)
     }
 }
 
-__global__ __launch_bounds__(kSelectBlock) void select_kernel(EvictArgs a) {
+// A request that is not cut: its scores stay.
+__device__ __forceinline__ void leave(const EvictArgs& a, int list, int context) {
+    const float* scores = a.b.scores + static_cast<int64_t>(list) * a.p.score_width;
+    float* out = a.b.scores_out + static_cast<int64_t>(list) * a.p.score_width;
+    int32_t* kept = a.b.kept + static_cast<int64_t>(list) * a.p.budget;
+    for (int i = threadIdx.x; i < a.p.budget; i += blockDim.x) kept[i] = -1;
+    if (out != scores)
+        for (int i = threadIdx.x; i < context; i += blockDim.x) out[i] = scores[i];
+    if (threadIdx.x == 0) a.moved[list] = a.p.budget;
+}
+
+// A list whose scores a workgroup holds in registers.
+template <int BLOCK, int HELD>
+__global__ __launch_bounds__(BLOCK) void select_kernel(EvictArgs a) {
+    typedef Select<BLOCK, HELD, 0> S;
+    __shared__ typename S::Shared sh;
+    __shared__ int stay;
+    const mpv_eviction& p = a.p;
+    const int list = blockIdx.x, b = list / p.score_heads % p.B;
+    const int context = context_of(a, b);
+    if (context <= p.trigger) return leave(a, list, context);
+    const float* scores = a.b.scores + static_cast<int64_t>(list) * p.score_width;
+    float* out = a.b.scores_out + static_cast<int64_t>(list) * p.score_width;
+    const int64_t first = static_cast<int64_t>(list) * p.budget;
+    const int rounds = (context + BLOCK - 1) / BLOCK;
+    float score[HELD];
+    uint32_t key[HELD];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        const int at = i * BLOCK + threadIdx.x;
+        score[i] = at < context ? scores[at] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        const int at = i * BLOCK + threadIdx.x;
+        // (what is kept in any case is larger than every score)
+        key[i] = at >= context ? 0u : at < p.sinks || at >= context - p.recent ? 0xffffffffu : score_order(score[i]);
+    }
+    if (threadIdx.x == 0) stay = 0;
+    uint32_t limit;
+    int above;
+    S::largest(key, rounds, p.budget, sh, limit, above);           // (all scores are here when it returns: `out` may be `scores`)
+    int mine = 0;
+    S::chosen(key, rounds, context, limit, p.budget - above, sh, [&](int i, int place) {
+        const int at = i * BLOCK + threadIdx.x, column = a.by_page.of(at);
+        const int page = a.b.block_table[static_cast<int64_t>(b) * p.table_width + column];
+        a.b.kept[first + place] = at;
+        a.slots[first + place] = page >= 0 && page < p.num_pages ? page * p.page_size + at - column * p.page_size : -1;
+        out[place] = score[i];
+        mine += at == place;
+    });
+    if (mine) atomicAdd(&stay, mine);
+    __syncthreads();
+    if (threadIdx.x == 0) a.moved[list] = stay;
+}
+
+// The same for lists of any length, read again for each byte of the limit.
+__global__ __launch_bounds__(kSelectBlock) void select_long_kernel(EvictArgs a) {
     const mpv_eviction& p = a.p;
     const int list = blockIdx.x, b = list / p.score_heads % p.B;
     const int context = context_of(a, b);
     const float* scores = a.b.scores + static_cast<int64_t>(list) * p.score_width;
     float* out = a.b.scores_out + static_cast<int64_t>(list) * p.score_width;
     int32_t* kept = a.b.kept + static_cast<int64_t>(list) * p.budget;
-    if (context <= p.trigger) {
-        for (int i = threadIdx.x; i < p.budget; i += kSelectBlock) kept[i] = -1;
-        if (out != scores)
-            for (int i = threadIdx.x; i < context; i += kSelectBlock) out[i] = scores[i];
-        if (threadIdx.x == 0) a.moved[list] = p.budget;
-        return;
-    }
+    if (context <= p.trigger) return leave(a, list, context);
     __shared__ int counts[256];
     __shared__ int part[kSelectBlock / 64][2];
     __shared__ int chosen_digit, chosen_above;
@@ -138,10 +188,10 @@ __global__ __launch_bounds__(kSelectBlock) void select_kernel(EvictArgs a) {
 // Pages behind the kept positions go to the end of the list of free ones, in request order.
 __device__ __forceinline__ void return_pages(const EvictArgs& a) {
     const mpv_eviction& p = a.p;
-    __shared__ int part[kMoveBlock / 64][2];
+    __shared__ int part[16][2];
     int64_t count = min(max(a.b.free_count[0], 0), p.num_pages);
     const int have = (p.budget + p.page_size - 1) / p.page_size;
-    for (int base = 0; base < p.B; base += kMoveBlock) {
+    for (int base = 0; base < p.B; base += static_cast<int>(blockDim.x)) {
         const int b = base + threadIdx.x;
         const int context = b < p.B ? context_of(a, b) : 0;
         const bool cut = context > p.trigger;
@@ -158,46 +208,78 @@ __device__ __forceinline__ void return_pages(const EvictArgs& a) {
     if (threadIdx.x == 0) a.b.free_count_out[0] = static_cast<int32_t>(min(count, static_cast<int64_t>(p.num_pages)));
 }
 
-__global__ __launch_bounds__(kMoveBlock) void move_kernel(EvictArgs a) {
+// A slice of a list's rows, LANES 16-byte pieces wide.  A round's rows are asked for before those of the round before it are written, and the
+// slots a round earlier still.
+template <int BLOCK, int LANES>
+__global__ __launch_bounds__(BLOCK) void move_kernel(EvictArgs a) {
+    constexpr int kStep = BLOCK / LANES, kRound = kStep * kLoads;
     const mpv_eviction& p = a.p;
     if (blockIdx.x == 0) return return_pages(a);
-    const int lane = threadIdx.x & 63, part = lane % kSliceLanes, mine = lane / kSliceLanes;
-    const int64_t wave = (static_cast<int64_t>(blockIdx.x) - 1) * (kMoveBlock / 64) + (threadIdx.x >> 6);
-    const int64_t number = wave / 2;
-    const int list = static_cast<int>(number / a.slices), slice = static_cast<int>(number - static_cast<int64_t>(list) * a.slices);
-    if (list >= a.lists) return;
+    const int part = threadIdx.x % LANES, mine = threadIdx.x / LANES;
+    unsigned number = blockIdx.x - 1;
+    const bool values = number & 1;
+    number >>= 1;
+    const int list = number / a.slices, slice = number - static_cast<unsigned>(list) * a.slices;
+    const int begin = a.moved[list];
+    if (begin >= p.budget) return;
     const int head = list % p.score_heads, b = list / p.score_heads % p.B, layer = list / p.score_heads / p.B;
     const int bytes = p.dtype == MPV_DTYPE_F32 ? 4 : 2;
-    char* cache = static_cast<char*>(wave & 1 ? a.b.cache_v : a.b.cache_k) + (layer * p.cache_layer_stride + head * a.lead) * bytes;
-    const int64_t byte = static_cast<int64_t>(slice) * kSlice + part * 16;
-    const bool mine_too = byte < a.row_bytes;
-    cache += byte;
-    auto row = [&](int slot) {
-        const int page = a.by_page.of(slot);
-        return cache + (page * p.page_stride + (slot - page * p.page_size) * p.slot_stride) * bytes;
-    };
+    const int64_t byte = (static_cast<int64_t>(slice) * LANES + part) * 16;
+    char* cache = static_cast<char*>(values ? a.b.cache_v : a.b.cache_k) + (layer * p.cache_layer_stride + head * a.lead) * bytes + byte;
+    const bool inside = byte < a.row_bytes;
     const int32_t* slots = a.slots + static_cast<int64_t>(list) * p.budget;
-    for (int first = a.moved[list]; first < p.budget; first += kMoveRows) {
-        uint4 v[kLoads];
-        int from[kLoads], to[kLoads];
+    const int32_t* table = a.b.block_table + static_cast<int64_t>(b) * p.table_width;
+    struct Rows { int from[kLoads], page[kLoads]; };
+    auto look = [&](int first, Rows& r) {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int i = first + j * kRowsTogether + mine;
-            from[j] = to[j] = -1;
-            if (i < p.budget && mine_too) {
-                const int column = a.by_page.of(i), page = a.b.block_table[static_cast<int64_t>(b) * p.table_width + column];
-                from[j] = slots[i];
-                if (page >= 0 && page < p.num_pages) to[j] = page * p.page_size + i - column * p.page_size;
+            const int i = first + j * kStep + mine;
+            r.from[j] = -1;
+            r.page[j] = -1;
+            if (i < p.budget && inside) {
+                r.from[j] = slots[i];
+                r.page[j] = table[a.by_page.of(i)];
             }
         }
+    };
+    auto whole = [&](const Rows& r, int j) { return r.from[j] >= 0 && r.page[j] >= 0 && r.page[j] < p.num_pages; };
+    auto ask = [&](const Rows& r, uint4 (&v)[kLoads]) {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j)
-            if (from[j] >= 0 && to[j] >= 0) v[j] = *reinterpret_cast<const uint4*>(row(from[j]));
-        // all rows of this round are here before the first one is written
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            if (whole(r, j)) {
+                const int page = a.by_page.of(r.from[j]);
+                v[j] = *reinterpret_cast<const uint4*>(cache + (page * p.page_stride + (r.from[j] - page * p.page_size) * p.slot_stride) * bytes);
+            }
+    };
+    auto store = [&](int first, const Rows& r, const uint4 (&v)[kLoads]) {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j)
-            if (from[j] >= 0 && to[j] >= 0) *reinterpret_cast<uint4*>(row(to[j])) = v[j];
+            if (whole(r, j)) {
+                const int i = first + j * kStep + mine, place = i - a.by_page.of(i) * p.page_size;
+                *reinterpret_cast<uint4*>(cache + (r.page[j] * p.page_stride + place * p.slot_stride) * bytes) = v[j];
+            }
+    };
+    // all threads' rows of a round are here
+    auto arrive = [&](uint4 (&v)[kLoads]) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) asm volatile("" : "+v"(v[j].x), "+v"(v[j].y), "+v"(v[j].z), "+v"(v[j].w));
+        __syncthreads();
+    };
+    Rows r[2];
+    uint4 v[2][kLoads] = {};
+    look(begin, r[0]);
+    ask(r[0], v[0]);
+    look(begin + kRound, r[1]);
+    for (int first = begin;; first += 2 * kRound) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int at = first + h * kRound;
+            if (at >= p.budget) return;
+            arrive(v[h]);
+            ask(r[1 - h], v[1 - h]);
+            store(at, r[h], v[h]);
+            look(at + 2 * kRound, r[h]);
+        }
     }
 }
 
@@ -216,12 +298,34 @@ static int check_eviction(const mpv_eviction* p) {
     const int64_t lists = span(0, span(0, p->layers, p->B), p->score_heads);
     if (span(0, p->num_pages, p->page_size) > INT32_MAX || span(0, p->table_width, p->page_size) > INT32_MAX || p->score_width > INT32_MAX ||
         lists > INT32_MAX / 1024 || span(0, lists, p->budget) > (static_cast<int64_t>(1) << 40) ||
-        span(0, lists, (row * elem_bytes(p->dtype) + kSlice - 1) / kSlice * 2) > INT32_MAX ||
+        span(0, lists, (row * elem_bytes(p->dtype) + 127) / 128 * 2) > INT32_MAX - 1 ||
         span(0, span(span(span(0, p->num_pages, p->page_stride), p->page_size, p->slot_stride), p->layers, p->cache_layer_stride), 4) == INT64_MAX)
         return MPV_ERR_UNSUPPORTED;
     const int64_t all = p->head_dim | p->slot_stride | p->page_stride | p->cache_layer_stride;
     if ((all * elem_bytes(p->dtype)) % 16 != 0) return MPV_ERR_ALIGNMENT;
     return MPV_OK;
+}
+
+static void launch_select(const EvictArgs& a, hipStream_t s) {
+    const int64_t room = static_cast<int64_t>(a.p.table_width) * a.p.page_size;
+    const dim3 lists(static_cast<unsigned>(a.lists));
+    if (room <= 512 * 16) hipLaunchKernelGGL((select_kernel<512, 16>), lists, dim3(512), 0, s, a);
+    else if (room <= 1024 * 32) hipLaunchKernelGGL((select_kernel<1024, 32>), lists, dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL(select_long_kernel, lists, dim3(kSelectBlock), 0, s, a);
+}
+
+template <int LANES>
+static void launch_slices(EvictArgs& a, hipStream_t s) {
+    a.slices = static_cast<int>((a.row_bytes + LANES * 16 - 1) / (LANES * 16));
+    const int64_t workgroups = static_cast<int64_t>(a.lists) * a.slices * 2;
+    const dim3 grid(static_cast<unsigned>(workgroups + 1));
+    // (few lists: more rows of each at a time)
+    if (workgroups < 512) hipLaunchKernelGGL((move_kernel<1024, LANES>), grid, dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL((move_kernel<256, LANES>), grid, dim3(256), 0, s, a);
+}
+static void launch_move(EvictArgs& a, hipStream_t s) {
+    if (a.row_bytes <= 128) launch_slices<8>(a, s);
+    else launch_slices<16>(a, s);
 }
 
 static size_t slots_bytes(const mpv_eviction* p) {
@@ -261,15 +365,13 @@ int mpv_evict_positions(const mpv_eviction* eviction, const mpv_eviction_buffers
     a.lists = p->layers * p->B * p->score_heads;
     a.row_bytes = static_cast<int64_t>(p->score_heads == 1 ? p->kv_heads : 1) * p->head_dim * mpv::elem_bytes(p->dtype);
     a.lead = p->score_heads == 1 ? 0 : p->head_dim;
-    a.slices = static_cast<int>((a.row_bytes + mpv::kSlice - 1) / mpv::kSlice);
     a.by_page.set(static_cast<uint32_t>(p->page_size));
     a.slots = static_cast<int32_t*>(workspace);
     a.moved = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + mpv::slots_bytes(p));
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();
-    if (a.lists > 0) hipLaunchKernelGGL(mpv::select_kernel, dim3(static_cast<unsigned>(a.lists)), dim3(mpv::kSelectBlock), 0, s, a);
-    const int64_t waves = static_cast<int64_t>(a.lists) * a.slices * 2, workgroups = (waves + mpv::kMoveBlock / 64 - 1) / (mpv::kMoveBlock / 64);
-    hipLaunchKernelGGL(mpv::move_kernel, dim3(static_cast<unsigned>(workgroups + 1)), dim3(mpv::kMoveBlock), 0, s, a);
+    if (a.lists > 0) mpv::launch_select(a, s);
+    mpv::launch_move(a, s);
     return mpv::launched();
 }
 

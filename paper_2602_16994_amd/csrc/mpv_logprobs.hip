@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "mpv_host.h"
+#include "mpv_select.h"
 
 namespace mpv {
 
@@ -22,7 +23,6 @@ namespace mpv {
 // sweep_kernel: a workgroup has a part of a row; finish_kernel: one has a row, its parts and its segments' maxima.
 
 constexpr int kSweepBlock = 256;
-constexpr int kFinishBlock = 256;
 constexpr int kSegment = 64;
 constexpr int kChunks = 4;                 // 16-byte loads of a thread in flight
 
@@ -49,6 +49,12 @@ __device__ __forceinline__ uint32_t order_of(float z) {
 }
 __device__ __forceinline__ float from_order(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 constexpr uint32_t kNothing = 0x007fffffu;
+// The next smaller float32; none is below -inf: NaN, which no number is less than or equal to.
+__device__ __forceinline__ float next_below(float z) {
+    if (z == -INFINITY || z != z) return NAN;
+    if (z == 0.0f) return __uint_as_float(0x80000001u);
+    return __uint_as_float(z > 0.0f ? __float_as_uint(z) - 1 : __float_as_uint(z) + 1);
+}
 
 // Maximum over the lanes of a segment, 8 or 16 neighbours.
 template <int LANES>
@@ -97,7 +103,8 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
     const float mine = known ? logit(z[r.token]) : INFINITY;
     const int from = part * a.part * kLanes, to = min(from + a.part * kLanes, a.segments * kLanes);      // chunks of N
     float m = -INFINITY, sum = 0.0f, weighted = 0.0f;
-    int better = 0;
+    int better = 0, equals = 0;            // of the wave, and of this lane
+    const float below = next_below(mine);
     for (int first = from; first < to; first += kChunks * kSweepBlock) {
         T raw[kChunks][N];
 #pragma unroll
@@ -109,7 +116,6 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
 #pragma unroll
         for (int j = 0; j < kChunks; ++j) {
             const int chunk = first + j * kSweepBlock + threadIdx.x;
-            most[j] = -INFINITY;
             if (chunk < to && chunk < whole) {
 #pragma unroll
                 for (int i = 0; i < N; ++i) v[j][i] = logit(raw[j][i]);
@@ -120,40 +126,61 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
                     v[j][i] = chunk < to && at < V ? logit(z[at]) : -INFINITY;
                 }
             }
+            most[j] = v[j][0];
 #pragma unroll
-            for (int i = 0; i < N; ++i) most[j] = fmaxf(most[j], v[j][i]);
+            for (int i = 1; i < N; ++i) most[j] = __builtin_elementwise_maximum(most[j], v[j][i]);     // (NaN if one is)
             if (a.p.top > 0) {
                 const float best = segment_max<kLanes>(most[j]);
                 if (threadIdx.x % kLanes == 0 && chunk < to) a.best[static_cast<int64_t>(row) * a.segments + chunk / kLanes] = best;
             }
-            // tokens before the given one are better if they are not smaller
+            // tokens before the given one are better if they are not smaller: if they are larger than the number below it
+            const int before = r.token - chunk * N;                // of this chunk's tokens; what lies behind the part is none of them
+            const float least = before >= N && chunk < to ? below : mine;
 #pragma unroll
-            for (int i = 0; i < N; ++i) better += v[j][i] > mine || (v[j][i] == mine && chunk * N + i < (chunk < to ? r.token : 0));
+            for (int i = 0; i < N; ++i) better += __popcll(__ballot(!(v[j][i] <= least)));
+            if (before > 0 && before < N && chunk < to)
+                for (int i = 0; i < N; ++i) equals += i < before && v[j][i] == mine;
         }
         float now = m;
 #pragma unroll
-        for (int j = 0; j < kChunks; ++j) now = fmaxf(now, most[j]);
-        const float base = now == -INFINITY ? 0.0f : now;
+        for (int j = 0; j < kChunks; ++j) now = __builtin_elementwise_maximum(now, most[j]);
+        const float base = now == -INFINITY ? 0.0f : now, shift = base * a.c;
         if (m != -INFINITY) {
             const float fade = exp2f((m - now) * a.c);
             weighted = fade * (weighted + (m - now) * sum);
             sum *= fade;
         }
         m = now;
+        if (fabsf(shift) < 1e30f && a.c > 1e-30f) {
+            // (the weights are in log2 units here; what lies further than 200 of them below adds nothing, and 0 times -inf would be NaN)
+            const float lowest = base - 200.0f * (1.0f / a.c);
+            float in_log2 = 0.0f;
 #pragma unroll
-        for (int j = 0; j < kChunks; ++j)
+            for (int j = 0; j < kChunks; ++j)
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float d = v[j][i] - base, e = __builtin_amdgcn_exp2f(d * a.c);
-                sum += e;
-                weighted = fmaf(e, fmaxf(d, -FLT_MAX), weighted);  // (0 times -inf would be NaN)
-            }
+                for (int i = 0; i < N; ++i) {
+                    const float d = fmaf(fmaxf(v[j][i], lowest), a.c, -shift), e = __builtin_amdgcn_exp2f(d);
+                    sum += e;
+                    in_log2 = fmaf(e, d, in_log2);
+                }
+            weighted += in_log2 * (1.0f / a.c);
+        } else {
+            // (masks of the lowest number alone, c times which is -inf; or no number)
+#pragma unroll
+            for (int j = 0; j < kChunks; ++j)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float d = v[j][i] - base, e = __builtin_amdgcn_exp2f(d * a.c);
+                    sum += e;
+                    weighted = fmaf(e, fmaxf(d, -FLT_MAX), weighted);
+                }
+        }
     }
     // over the workgroup
     __shared__ float ms[kSweepBlock / 64], sums[kSweepBlock / 64], weights[kSweepBlock / 64];
     __shared__ int betters[kSweepBlock / 64];
     float top = m;
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));       // (a lane without a number has no sum, either)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (m != -INFINITY) {
         const float fade = exp2f((m - top) * a.c);
@@ -163,8 +190,9 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
     for (int d = 32; d; d >>= 1) {
         sum += __shfl_xor(sum, d);
         weighted += __shfl_xor(weighted, d);
-        better += __shfl_xor(better, d);
+        equals += __shfl_xor(equals, d);
     }
+    better += equals;
     if (lane == 0) { ms[wave] = top; sums[wave] = sum; weights[wave] = weighted; betters[wave] = better; }
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -180,29 +208,16 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
     }
 }
 
-// Exclusive sums over the workgroup; the sum of all in `total`.
-__device__ __forceinline__ int block_before(int v, int* part, int& total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int upto = v;
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(upto, d);
-        if (lane >= d) upto += o;
-    }
-    __syncthreads();
-    if (lane == 63) part[wave] = upto;
-    __syncthreads();
-    int before = 0;
-    total = 0;
-    for (int w = 0; w < kFinishBlock / 64; ++w) {
-        if (w < wave) before += part[w];
-        total += part[w];
-    }
-    return before + upto - v;
-}
+// Lowest bits in which no two numbers of a type's order differ.
+template <class T> struct Unused { static constexpr int kBits = 0; };
+template <> struct Unused<uint16_t> { static constexpr int kBits = 16; };
+template <> struct Unused<__half> { static constexpr int kBits = 12; };
 
-template <class T>
+// HELD: segments of a thread.
+template <class T, int kFinishBlock, int HELD>
 __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
-    constexpr int N = 16 / sizeof(T);
+    constexpr int N = 16 / sizeof(T), LOW = Unused<T>::kBits;
+    typedef Select<kFinishBlock, HELD, LOW> S;
     const int row = blockIdx.x, top = a.p.top;
     const Row r = row_of(a, row);
     int32_t* tokens = top > 0 ? a.b.top_tokens + static_cast<int64_t>(row) * top : nullptr;
@@ -217,7 +232,6 @@ __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
         return;
     }
     const T* z = static_cast<const T*>(a.b.logits) + r.at;
-    __shared__ int scratch[kFinishBlock / 64];
     __shared__ float shared_m, shared_log, shared_sum;
     if (threadIdx.x < 64) {
         // (all lanes have parts: their number is not limited by the wave)
@@ -262,67 +276,41 @@ __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
         for (int i = threadIdx.x; i < top; i += kFinishBlock) { tokens[i] = -1; logprobs[i] = v; }
         return;
     }
-    // the top-th largest of the segments' maxima, a byte at a time; `above`: those larger than it
+    // the segments with the largest maxima, of equal ones the first
     const float* best = a.best + static_cast<int64_t>(row) * a.segments;
-    __shared__ int counts[256];
-    __shared__ int chosen_digit, chosen_above;
-    uint32_t limit = 0;
-    int above = 0;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        counts[threadIdx.x] = 0;
-        __syncthreads();
-        for (int s = threadIdx.x; s < a.segments; s += kFinishBlock) {
-            const uint32_t k = order_of(best[s]);
-            if (shift == 24 || k >> (shift + 8) == limit >> (shift + 8)) atomicAdd(&counts[k >> shift & 255], 1);
-        }
-        __syncthreads();
-        // digits from the largest on: thread i has digit 255 - i
-        int total;
-        const int mine = counts[255 - threadIdx.x], before = block_before(mine, scratch, total);
-        if (threadIdx.x == 0) { chosen_digit = 0; chosen_above = above + total - counts[0]; }     // (fewer segments than wanted)
-        __syncthreads();
-        if (above + before < top && above + before + mine >= top) { chosen_digit = 255 - threadIdx.x; chosen_above = above + before; }
-        __syncthreads();
-        limit |= static_cast<uint32_t>(chosen_digit) << shift;
-        above = chosen_above;
-        __syncthreads();
-    }
-    if (limit <= kNothing) limit = kNothing + 1;                   // tokens of no probability are no alternatives
-    // the segments with larger maxima, and as many of those that have it, from the first on
+    const int rounds = (a.segments + kFinishBlock - 1) / kFinishBlock;
+    __shared__ typename S::Shared sh;
     __shared__ int segments[MPV_MAX_TOP];
-    __shared__ int found;
-    const int each = (a.segments + kFinishBlock - 1) / kFinishBlock, first = min(a.segments, static_cast<int>(threadIdx.x) * each);
-    const int last = min(a.segments, first + each);
-    int larger = 0, equal = 0;
-    for (int s = first; s < last; ++s) {
-        const uint32_t k = order_of(best[s]);
-        larger += k > limit;
-        equal += k == limit;
-    }
-    int all_larger, all_equal;
-    int at_larger = block_before(larger, scratch, all_larger), at_equal = block_before(equal, scratch, all_equal);
-    const int take = min(all_larger + all_equal, top);
-    for (int s = first; s < last; ++s) {
-        const uint32_t k = order_of(best[s]);
-        if (k > limit) {
-            if (at_larger < top) segments[at_larger] = s;
-            ++at_larger;
-        } else if (k == limit) {
-            if (all_larger + at_equal < top) segments[all_larger + at_equal] = s;
-            ++at_equal;
+    __shared__ int found, take;
+    uint32_t key[HELD];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        const int s = i * kFinishBlock + threadIdx.x;
+        key[i] = 0;
+        if (s < a.segments) {
+            const uint32_t k = order_of(best[s]);
+            key[i] = k > kNothing ? k : 0u;                        // (tokens of no probability are no alternatives)
         }
     }
+    if (threadIdx.x == 0) found = take = 0;
+    uint32_t limit;
+    int above, chosen = 0;
+    S::largest(key, rounds, top, sh, limit, above);
+    S::chosen(key, rounds, limit >> LOW ? a.segments : 0, limit, top - above, sh, [&](int i, int place) {
+        segments[place] = i * kFinishBlock + threadIdx.x;
+        ++chosen;
+    });
+    if (chosen) atomicAdd(&take, chosen);
+    __syncthreads();
     // their tokens that are not smaller, in any order
     __shared__ unsigned long long candidates[MPV_MAX_TOP * kSegment];
-    if (threadIdx.x == 0) found = 0;
-    __syncthreads();
     constexpr int kLanes = kSegment / N;
     for (int i = threadIdx.x; i < take * kLanes; i += kFinishBlock) {
         const int token = segments[i / kLanes] * kSegment + i % kLanes * N;
         for (int j = 0; j < N; ++j) {
             if (token + j >= a.p.V) break;
             const uint32_t k = order_of(logit(z[token + j]));
-            if (k >= limit) candidates[atomicAdd(&found, 1)] = static_cast<unsigned long long>(k) << 32 | static_cast<uint32_t>(~(token + j));
+            if (k > kNothing && k >> LOW >= limit >> LOW) candidates[atomicAdd(&found, 1)] = static_cast<unsigned long long>(k) << 32 | static_cast<uint32_t>(~(token + j));
         }
     }
     __syncthreads();
@@ -379,7 +367,9 @@ template <class T>
 static int launch_rows(const RowArgs& a, hipStream_t s) {
     (void)hipGetLastError();
     hipLaunchKernelGGL(sweep_kernel<T>, dim3(static_cast<unsigned>(a.rows) * a.parts), dim3(kSweepBlock), 0, s, a);
-    hipLaunchKernelGGL(finish_kernel<T>, dim3(static_cast<unsigned>(a.rows)), dim3(kFinishBlock), 0, s, a);
+    const dim3 rows(static_cast<unsigned>(a.rows));
+    if (a.segments <= 256 * 16) hipLaunchKernelGGL((finish_kernel<T, 256, 16>), rows, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((finish_kernel<T, 1024, 32>), rows, dim3(1024), 0, s, a);
     return launched();
 }
 
