@@ -5,7 +5,7 @@
 // move_kernel: kept rows move forward in order.  The i-th kept position s_i is at least i and the s_i ascend, so that what is written to the
 // rows [c, c + n) was read with them or before: a workgroup that takes a slice of a list's rows, some rows a round, all loads before the
 // stores, needs no other copy, and may ask for the next round's rows before it writes.  Different slices (of different bytes) do not
-// meet.  Its first workgroup returns the pages.
+// meet.  Its first workgroups return the pages.
 
 #include <algorithm>
 
@@ -25,6 +25,10 @@ struct EvictArgs {
     Divisor by_page;
     int32_t* slots;                        // [lists][budget] slot of a kept row, -1: none
     int32_t* moved;                        // [lists] first row that moves (budget: none does)
+    struct Plan { int32_t free; } * plan;  // pages that were free
+    int64_t* first_page;                   // [B+1] where a request's pages go in the list of free ones
+    int32_t* lengths;                      // [B] new ones
+    int returning;                         // workgroups that return pages
 };
 
 __device__ __forceinline__ int context_of(const EvictArgs& a, int b) { return min(max(a.b.context_len[b], 0), a.p.table_width * a.p.page_size); }
@@ -56,6 +60,47 @@ __device__ __forceinline__ void before(int (&v)[2], int (&total)[2], int (*part)
     }
 }
 
+// What returns the pages behind the kept positions to the end of the list of free ones, in request order: a workgroup of the first launch works
+// out where each request's begin, since lengths and count may be written by the second one.
+__device__ __forceinline__ void plan_pages(const EvictArgs& a) {
+    const mpv_eviction& p = a.p;
+    __shared__ int part[16][2];
+    int64_t count = min(max(a.b.free_count[0], 0), p.num_pages);
+    if (threadIdx.x == 0) a.plan->free = static_cast<int32_t>(count);
+    const int have = (p.budget + p.page_size - 1) / p.page_size;
+    for (int base = 0; base < p.B; base += blockDim.x) {
+        const int b = base + threadIdx.x;
+        const int context = b < p.B ? context_of(a, b) : 0;
+        const int pages = context > p.trigger ? (context + p.page_size - 1) / p.page_size - have : 0;
+        int at[2] = {pages, 0}, total[2];
+        before(at, total, part);
+        if (b < p.B) {
+            a.first_page[b] = count + at[0];
+            a.lengths[b] = context > p.trigger ? p.budget : context;
+        }
+        count += total[0];
+    }
+    if (threadIdx.x == 0) a.first_page[p.B] = count;
+}
+__device__ __forceinline__ void return_pages(const EvictArgs& a) {
+    const mpv_eviction& p = a.p;
+    const int have = (p.budget + p.page_size - 1) / p.page_size;
+    const int64_t free = a.plan->free, end = min(a.first_page[p.B], static_cast<int64_t>(p.num_pages));
+    const int64_t step = static_cast<int64_t>(a.returning) * blockDim.x;
+    const int64_t mine = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+    for (int64_t place = free + mine; place < end; place += step) {
+        int low = 0, high = p.B;                                   // the last request whose pages begin at or before the place
+        while (high - low > 1) {
+            const int middle = (low + high) >> 1;
+            if (a.first_page[middle] <= place) low = middle;
+            else high = middle;
+        }
+        a.b.free_pages[place] = a.b.block_table[static_cast<int64_t>(low) * p.table_width + have + static_cast<int>(place - a.first_page[low])];
+    }
+    for (int64_t b = mine; b < p.B; b += step) a.b.context_len_out[b] = a.lengths[b];
+    if (mine == 0) a.b.free_count_out[0] = static_cast<int32_t>(end);
+}
+
 // A request that is not cut: its scores stay.
 __device__ __forceinline__ void leave(const EvictArgs& a, int list, int context) {
     const float* scores = a.b.scores + static_cast<int64_t>(list) * a.p.score_width;
@@ -74,7 +119,8 @@ __global__ __launch_bounds__(BLOCK) void select_kernel(EvictArgs a) {
     __shared__ typename S::Shared sh;
     __shared__ int stay;
     const mpv_eviction& p = a.p;
-    const int list = blockIdx.x, b = list / p.score_heads % p.B;
+    if (blockIdx.x == 0) return plan_pages(a);
+    const int list = blockIdx.x - 1, b = list / p.score_heads % p.B;
     const int context = context_of(a, b);
     if (context <= p.trigger) return leave(a, list, context);
     const float* scores = a.b.scores + static_cast<int64_t>(list) * p.score_width;
@@ -115,7 +161,8 @@ __global__ __launch_bounds__(BLOCK) void select_kernel(EvictArgs a) {
 // The same for lists of any length, read again for each byte of the limit.
 __global__ __launch_bounds__(kSelectBlock) void select_long_kernel(EvictArgs a) {
     const mpv_eviction& p = a.p;
-    const int list = blockIdx.x, b = list / p.score_heads % p.B;
+    if (blockIdx.x == 0) return plan_pages(a);
+    const int list = blockIdx.x - 1, b = list / p.score_heads % p.B;
     const int context = context_of(a, b);
     const float* scores = a.b.scores + static_cast<int64_t>(list) * p.score_width;
     float* out = a.b.scores_out + static_cast<int64_t>(list) * p.score_width;
@@ -185,38 +232,15 @@ __global__ __launch_bounds__(kSelectBlock) void select_long_kernel(EvictArgs a) 
     if (threadIdx.x == 0) a.moved[list] = stay;
 }
 
-// Pages behind the kept positions go to the end of the list of free ones, in request order.
-__device__ __forceinline__ void return_pages(const EvictArgs& a) {
-    const mpv_eviction& p = a.p;
-    __shared__ int part[16][2];
-    int64_t count = min(max(a.b.free_count[0], 0), p.num_pages);
-    const int have = (p.budget + p.page_size - 1) / p.page_size;
-    for (int base = 0; base < p.B; base += static_cast<int>(blockDim.x)) {
-        const int b = base + threadIdx.x;
-        const int context = b < p.B ? context_of(a, b) : 0;
-        const bool cut = context > p.trigger;
-        const int pages = cut ? (context + p.page_size - 1) / p.page_size - have : 0;
-        int at[2] = {pages, 0}, total[2];
-        before(at, total, part);
-        for (int i = 0; i < pages; ++i) {
-            const int64_t place = count + at[0] + i;
-            if (place < p.num_pages) a.b.free_pages[place] = a.b.block_table[static_cast<int64_t>(b) * p.table_width + have + i];
-        }
-        if (b < p.B) a.b.context_len_out[b] = cut ? p.budget : context;
-        count += total[0];
-    }
-    if (threadIdx.x == 0) a.b.free_count_out[0] = static_cast<int32_t>(min(count, static_cast<int64_t>(p.num_pages)));
-}
-
 // A slice of a list's rows, LANES 16-byte pieces wide.  A round's rows are asked for before those of the round before it are written, and the
 // slots a round earlier still.
 template <int BLOCK, int LANES>
 __global__ __launch_bounds__(BLOCK) void move_kernel(EvictArgs a) {
     constexpr int kStep = BLOCK / LANES, kRound = kStep * kLoads;
     const mpv_eviction& p = a.p;
-    if (blockIdx.x == 0) return return_pages(a);
+    if (blockIdx.x < static_cast<unsigned>(a.returning)) return return_pages(a);
     const int part = threadIdx.x % LANES, mine = threadIdx.x / LANES;
-    unsigned number = blockIdx.x - 1;
+    unsigned number = blockIdx.x - a.returning;
     const bool values = number & 1;
     number >>= 1;
     const int list = number / a.slices, slice = number - static_cast<unsigned>(list) * a.slices;
@@ -297,7 +321,7 @@ static int check_eviction(const mpv_eviction* p) {
     if (p->slot_stride < row || p->page_stride < 0 || p->cache_layer_stride < 0) return MPV_ERR_BAD_SHAPE;
     const int64_t lists = span(0, span(0, p->layers, p->B), p->score_heads);
     if (span(0, p->num_pages, p->page_size) > INT32_MAX || span(0, p->table_width, p->page_size) > INT32_MAX || p->score_width > INT32_MAX ||
-        lists > INT32_MAX / 1024 || span(0, lists, p->budget) > (static_cast<int64_t>(1) << 40) ||
+        lists > INT32_MAX / 1024 || p->B > (1 << 24) || span(0, lists, p->budget) > (static_cast<int64_t>(1) << 40) ||
         span(0, lists, (row * elem_bytes(p->dtype) + 127) / 128 * 2) > INT32_MAX - 1 ||
         span(0, span(span(span(0, p->num_pages, p->page_stride), p->page_size, p->slot_stride), p->layers, p->cache_layer_stride), 4) == INT64_MAX)
         return MPV_ERR_UNSUPPORTED;
@@ -308,7 +332,7 @@ static int check_eviction(const mpv_eviction* p) {
 
 static void launch_select(const EvictArgs& a, hipStream_t s) {
     const int64_t room = static_cast<int64_t>(a.p.table_width) * a.p.page_size;
-    const dim3 lists(static_cast<unsigned>(a.lists));
+    const dim3 lists(static_cast<unsigned>(a.lists) + 1);
     if (room <= 512 * 16) hipLaunchKernelGGL((select_kernel<512, 16>), lists, dim3(512), 0, s, a);
     else if (room <= 1024 * 32) hipLaunchKernelGGL((select_kernel<1024, 32>), lists, dim3(1024), 0, s, a);
     else hipLaunchKernelGGL(select_long_kernel, lists, dim3(kSelectBlock), 0, s, a);
@@ -318,7 +342,7 @@ template <int LANES>
 static void launch_slices(EvictArgs& a, hipStream_t s) {
     a.slices = static_cast<int>((a.row_bytes + LANES * 16 - 1) / (LANES * 16));
     const int64_t workgroups = static_cast<int64_t>(a.lists) * a.slices * 2;
-    const dim3 grid(static_cast<unsigned>(workgroups + 1));
+    const dim3 grid(static_cast<unsigned>(workgroups + a.returning));
     // (few lists: more rows of each at a time)
     if (workgroups < 512) hipLaunchKernelGGL((move_kernel<1024, LANES>), grid, dim3(1024), 0, s, a);
     else hipLaunchKernelGGL((move_kernel<256, LANES>), grid, dim3(256), 0, s, a);
@@ -328,8 +352,16 @@ static void launch_move(EvictArgs& a, hipStream_t s) {
     else launch_slices<16>(a, s);
 }
 
-static size_t slots_bytes(const mpv_eviction* p) {
-    return (static_cast<size_t>(p->layers) * p->B * p->score_heads * p->budget * sizeof(int32_t) + 255) / 256 * 256;
+// Parts of a workspace.
+struct EvictRoom {
+    size_t slots, moved, plan, pages, lengths;
+    size_t bytes() const { return slots + moved + plan + pages + lengths; }
+};
+static EvictRoom room_of(const mpv_eviction* p) {
+    auto whole = [](size_t bytes) { return (bytes + 255) / 256 * 256; };
+    const size_t lists = static_cast<size_t>(p->layers) * p->B * p->score_heads;
+    return {whole(lists * p->budget * sizeof(int32_t)), whole(lists * sizeof(int32_t)), 256, whole((static_cast<size_t>(p->B) + 1) * sizeof(int64_t)),
+            whole(static_cast<size_t>(p->B) * sizeof(int32_t))};
 }
 
 }  // namespace mpv
@@ -340,7 +372,7 @@ int mpv_evict_positions_workspace_bytes(const mpv_eviction* eviction, size_t* ou
     if (!out) return MPV_ERR_NULL;
     const int rc = mpv::check_eviction(eviction);
     if (rc != MPV_OK) return rc;
-    *out = mpv::slots_bytes(eviction) + static_cast<size_t>(eviction->layers) * eviction->B * eviction->score_heads * sizeof(int32_t);
+    *out = mpv::room_of(eviction).bytes();
     return MPV_OK;
 }
 
@@ -366,11 +398,18 @@ int mpv_evict_positions(const mpv_eviction* eviction, const mpv_eviction_buffers
     a.row_bytes = static_cast<int64_t>(p->score_heads == 1 ? p->kv_heads : 1) * p->head_dim * mpv::elem_bytes(p->dtype);
     a.lead = p->score_heads == 1 ? 0 : p->head_dim;
     a.by_page.set(static_cast<uint32_t>(p->page_size));
-    a.slots = static_cast<int32_t*>(workspace);
-    a.moved = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + mpv::slots_bytes(p));
+    const mpv::EvictRoom room = mpv::room_of(p);
+    char* at = static_cast<char*>(workspace);
+    a.slots = reinterpret_cast<int32_t*>(at);
+    a.moved = reinterpret_cast<int32_t*>(at += room.slots);
+    a.plan = reinterpret_cast<mpv::EvictArgs::Plan*>(at += room.moved);
+    a.first_page = reinterpret_cast<int64_t*>(at += room.plan);
+    a.lengths = reinterpret_cast<int32_t*>(at += room.pages);
+    // (eight pages a thread, if every request had all that it has room for)
+    a.returning = static_cast<int>(std::min<int64_t>(64, 1 + static_cast<int64_t>(p->B) * p->table_width / 2048));
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();
-    if (a.lists > 0) mpv::launch_select(a, s);
+    mpv::launch_select(a, s);
     mpv::launch_move(a, s);
     return mpv::launched();
 }

@@ -22,8 +22,13 @@ namespace mpv {
 //
 // sweep_kernel: a workgroup has a part of a row; finish_kernel: one has a row, its parts and its segments' maxima.
 
+#ifndef ROUNDS
+#define ROUNDS 4
+#endif
 constexpr int kSweepBlock = 256;
 constexpr int kSegment = 64;
+constexpr int kListed = 256;               // segments that are looked at, at most
+constexpr int kMany = 1024;                // tokens of them that are put in order (where equal logits make more, at most `top` whole segments)
 constexpr int kChunks = 4;                 // 16-byte loads of a thread in flight
 
 struct PartSums { float m, sum, weighted; int32_t better; };
@@ -54,6 +59,13 @@ __device__ __forceinline__ float next_below(float z) {
     if (z == -INFINITY || z != z) return NAN;
     if (z == 0.0f) return __uint_as_float(0x80000001u);
     return __uint_as_float(z > 0.0f ? __float_as_uint(z) - 1 : __float_as_uint(z) + 1);
+}
+
+// Maximum, NaN if one is.
+__device__ __forceinline__ float maximum(float x, float y, float z) {
+    float r;
+    asm("v_maximum3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
+    return r;
 }
 
 // Maximum over the lanes of a segment, 8 or 16 neighbours.
@@ -105,18 +117,21 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
     float m = -INFINITY, sum = 0.0f, weighted = 0.0f;
     int better = 0, equals = 0;            // of the wave, and of this lane
     const float below = next_below(mine);
-    for (int first = from; first < to; first += kChunks * kSweepBlock) {
+    const int full = min(to, whole);
+    // a round of chunks; kWhole: all of them are there
+    auto round = [&](int first, auto all) {
+        constexpr bool kWhole = decltype(all)::value;
         T raw[kChunks][N];
 #pragma unroll
         for (int j = 0; j < kChunks; ++j) {
             const int chunk = first + j * kSweepBlock + threadIdx.x;
-            if (chunk < to && chunk < whole) __builtin_memcpy(raw[j], z + static_cast<int64_t>(chunk) * N, 16);
+            if (kWhole || chunk < full) __builtin_memcpy(raw[j], z + static_cast<int64_t>(chunk) * N, 16);
         }
-        float v[kChunks][N], most[kChunks];
+        float v[kChunks][N], now = m;
 #pragma unroll
         for (int j = 0; j < kChunks; ++j) {
             const int chunk = first + j * kSweepBlock + threadIdx.x;
-            if (chunk < to && chunk < whole) {
+            if (kWhole || chunk < full) {
 #pragma unroll
                 for (int i = 0; i < N; ++i) v[j][i] = logit(raw[j][i]);
             } else {
@@ -126,24 +141,23 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
                     v[j][i] = chunk < to && at < V ? logit(z[at]) : -INFINITY;
                 }
             }
-            most[j] = v[j][0];
+            float most = maximum(v[j][0], v[j][1], v[j][2]);
 #pragma unroll
-            for (int i = 1; i < N; ++i) most[j] = __builtin_elementwise_maximum(most[j], v[j][i]);     // (NaN if one is)
+            for (int i = 3; i < N; i += 2) most = maximum(most, v[j][i], v[j][i + 1 < N ? i + 1 : i]);
+            now = maximum(now, most, most);
             if (a.p.top > 0) {
-                const float best = segment_max<kLanes>(most[j]);
-                if (threadIdx.x % kLanes == 0 && chunk < to) a.best[static_cast<int64_t>(row) * a.segments + chunk / kLanes] = best;
+                const float best = segment_max<kLanes>(most);
+                if (threadIdx.x % kLanes == 0 && (kWhole || chunk < to)) a.best[static_cast<int64_t>(row) * a.segments + chunk / kLanes] = best;
             }
             // tokens before the given one are better if they are not smaller: if they are larger than the number below it
             const int before = r.token - chunk * N;                // of this chunk's tokens; what lies behind the part is none of them
-            const float least = before >= N && chunk < to ? below : mine;
+            const float least = before >= N && (kWhole || chunk < to) ? below : mine;
 #pragma unroll
             for (int i = 0; i < N; ++i) better += __popcll(__ballot(!(v[j][i] <= least)));
-            if (before > 0 && before < N && chunk < to)
+            asm volatile("" : "+s"(better));                       // (counted here: the ballots would all wait in scalar registers)
+            if (before > 0 && before < N && (kWhole || chunk < to))
                 for (int i = 0; i < N; ++i) equals += i < before && v[j][i] == mine;
         }
-        float now = m;
-#pragma unroll
-        for (int j = 0; j < kChunks; ++j) now = __builtin_elementwise_maximum(now, most[j]);
         const float base = now == -INFINITY ? 0.0f : now, shift = base * a.c;
         if (m != -INFINITY) {
             const float fade = exp2f((m - now) * a.c);
@@ -159,7 +173,7 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
             for (int j = 0; j < kChunks; ++j)
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const float d = fmaf(fmaxf(v[j][i], lowest), a.c, -shift), e = __builtin_amdgcn_exp2f(d);
+                    const float d = fmaf(__builtin_amdgcn_fmed3f(v[j][i], lowest, INFINITY), a.c, -shift), e = __builtin_amdgcn_exp2f(d);
                     sum += e;
                     in_log2 = fmaf(e, d, in_log2);
                 }
@@ -175,7 +189,10 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
                     weighted = fmaf(e, fmaxf(d, -FLT_MAX), weighted);
                 }
         }
-    }
+    };
+    int first = from;
+    for (; first + kChunks * kSweepBlock <= full; first += kChunks * kSweepBlock) round(first, std::true_type());
+    for (; first < to; first += kChunks * kSweepBlock) round(first, std::false_type());
     // over the workgroup
     __shared__ float ms[kSweepBlock / 64], sums[kSweepBlock / 64], weights[kSweepBlock / 64];
     __shared__ int betters[kSweepBlock / 64];
@@ -218,6 +235,7 @@ template <class T, int kFinishBlock, int HELD>
 __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
     constexpr int N = 16 / sizeof(T), LOW = Unused<T>::kBits;
     typedef Select<kFinishBlock, HELD, LOW> S;
+    typedef Select<kFinishBlock, 1, LOW> Single;
     const int row = blockIdx.x, top = a.p.top;
     const Row r = row_of(a, row);
     int32_t* tokens = top > 0 ? a.b.top_tokens + static_cast<int64_t>(row) * top : nullptr;
@@ -232,6 +250,16 @@ __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
         return;
     }
     const T* z = static_cast<const T*>(a.b.logits) + r.at;
+    const bool known = r.token >= 0 && r.token < a.p.V;
+    // (what does not depend on anything is asked for at once)
+    const float* best = a.best + static_cast<int64_t>(row) * a.segments;
+    float segment[HELD];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        const int s = i * kFinishBlock + threadIdx.x;
+        segment[i] = top > 0 && s < a.segments ? best[s] : -INFINITY;
+    }
+    const float mine = known ? logit(z[r.token]) : 0.0f;
     __shared__ float shared_m, shared_log, shared_sum;
     if (threadIdx.x < 64) {
         // (all lanes have parts: their number is not limited by the wave)
@@ -255,11 +283,11 @@ __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
         if (threadIdx.x == 0) {
             constexpr float kLn2 = 0.69314718055994531f;
             const float log = log2f(sum);
-            const bool known = r.token >= 0 && r.token < a.p.V, number = sum == sum;
+            const bool number = sum == sum;
             float logprob = -INFINITY, entropy = (log - a.c * (weighted / sum)) * kLn2;
             if (!number) logprob = entropy = NAN;
             else if (sum == 0.0f) entropy = 0.0f;
-            else if (known) logprob = ((logit(z[r.token]) - m) * a.c - log) * kLn2;
+            else if (known) logprob = ((mine - m) * a.c - log) * kLn2;
             a.b.logprob[row] = logprob;
             a.b.entropy[row] = entropy;
             a.b.rank[row] = known && number ? better + 1 : -1;
@@ -276,44 +304,71 @@ __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
         for (int i = threadIdx.x; i < top; i += kFinishBlock) { tokens[i] = -1; logprobs[i] = v; }
         return;
     }
-    // the segments with the largest maxima, of equal ones the first
-    const float* best = a.best + static_cast<int64_t>(row) * a.segments;
+    // No token of the best is smaller than the top-th largest of the threads' largest maxima: the segments that reach it are few, and hold
+    // them all.  (Where they are many, because of equal logits, the `top` segments with the largest maxima, of equal ones the first, are
+    // looked for among all: 512 more instructions a wave for 10 keys a thread.)
     const int rounds = (a.segments + kFinishBlock - 1) / kFinishBlock;
     __shared__ typename S::Shared sh;
-    __shared__ int segments[MPV_MAX_TOP];
+    __shared__ typename Single::Shared single;
+    __shared__ int segments[kListed];
     __shared__ int found, take;
-    uint32_t key[HELD];
+    __shared__ unsigned long long candidates[MPV_MAX_TOP * kSegment];
+    uint32_t key[HELD], most[1] = {0};
 #pragma unroll
     for (int i = 0; i < HELD; ++i) {
-        const int s = i * kFinishBlock + threadIdx.x;
-        key[i] = 0;
-        if (s < a.segments) {
-            const uint32_t k = order_of(best[s]);
-            key[i] = k > kNothing ? k : 0u;                        // (tokens of no probability are no alternatives)
-        }
+        const uint32_t k = order_of(segment[i]);
+        key[i] = k > kNothing ? k : 0u;                            // (tokens of no probability are no alternatives)
+        most[0] = max(most[0], key[i]);
     }
     if (threadIdx.x == 0) found = take = 0;
     uint32_t limit;
-    int above, chosen = 0;
-    S::largest(key, rounds, top, sh, limit, above);
-    S::chosen(key, rounds, limit >> LOW ? a.segments : 0, limit, top - above, sh, [&](int i, int place) {
-        segments[place] = i * kFinishBlock + threadIdx.x;
-        ++chosen;
-    });
-    if (chosen) atomicAdd(&take, chosen);
+    int above;
+    Single::largest(most, 1, top, single, limit, above);
+    if (most[0] >> LOW >= limit >> LOW)
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+            if (key[i] != 0 && key[i] >> LOW >= limit >> LOW) {
+                const int at = atomicAdd(&take, 1);
+                if (at < kListed) segments[at] = i * kFinishBlock + threadIdx.x;
+            }
     __syncthreads();
     // their tokens that are not smaller, in any order
-    __shared__ unsigned long long candidates[MPV_MAX_TOP * kSegment];
-    constexpr int kLanes = kSegment / N;
-    for (int i = threadIdx.x; i < take * kLanes; i += kFinishBlock) {
-        const int token = segments[i / kLanes] * kSegment + i % kLanes * N;
-        for (int j = 0; j < N; ++j) {
-            if (token + j >= a.p.V) break;
-            const uint32_t k = order_of(logit(z[token + j]));
-            if (k > kNothing && k >> LOW >= limit >> LOW) candidates[atomicAdd(&found, 1)] = static_cast<unsigned long long>(k) << 32 | static_cast<uint32_t>(~(token + j));
+    auto collect = [&](int segments_of) {
+        constexpr int kLanes = kSegment / N;
+        for (int i = threadIdx.x; i < segments_of * kLanes; i += kFinishBlock) {
+            const int token = segments[i / kLanes] * kSegment + i % kLanes * N;
+            T raw[N];
+            if (token + N <= a.p.V) {
+                __builtin_memcpy(raw, z + token, 16);
+            } else {
+                for (int j = 0; j < N; ++j)
+                    if (token + j < a.p.V) raw[j] = z[token + j];
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const uint32_t k = order_of(logit(raw[j]));
+                if (token + j < a.p.V && k > kNothing && k >> LOW >= limit >> LOW) {
+                    const int at = atomicAdd(&found, 1);
+                    if (at < MPV_MAX_TOP * kSegment) candidates[at] = static_cast<unsigned long long>(k) << 32 | static_cast<uint32_t>(~(token + j));
+                }
+            }
         }
+        __syncthreads();
+    };
+    bool many = take > kListed;
+    if (!many) {
+        collect(take);
+        many = found > kMany;
     }
-    __syncthreads();
+    if (many) {
+        __syncthreads();
+        if (threadIdx.x == 0) found = 0;
+        S::largest(key, rounds, top, sh, limit, above);
+        S::chosen(key, rounds, limit >> LOW ? a.segments : 0, limit, top - above, sh,
+                  [&](int i, int place) { segments[place] = i * kFinishBlock + threadIdx.x; });
+        __syncthreads();
+        collect(min(take, top));                                   // (fewer, if fewer have a token at all: they are all among the first)
+    }
     const int count = found;
     for (int i = threadIdx.x; i < count; i += kFinishBlock) {
         const unsigned long long k = candidates[i];
@@ -329,14 +384,13 @@ __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
 
 // ------------------------------------------------------------------ host side
 
-// Segments of a part: so many workgroups that the card is full, each with no more than 16 rounds of loads.
+// Segments of a part, whole rounds of a workgroup: so few that the card is full, up to four rounds.
 static void parts_of(const mpv_logprobs* p, int64_t rows, int* parts, int* part) {
     const int64_t segments = (p->V + kSegment - 1) / kSegment;
     const int64_t round = kChunks * kSweepBlock * (16 / elem_bytes(p->dtype)) / kSegment;         // segments of a round
-    const int64_t wanted = std::max<int64_t>(1, std::min<int64_t>((2048 + rows - 1) / rows, (segments + round - 1) / round));
-    const int64_t least = (segments + 16 * round - 1) / (16 * round);
-    const int64_t n = std::max(wanted, least);
-    *part = static_cast<int>((segments + n - 1) / n);
+    const int64_t all = (segments + round - 1) / round;
+    const int64_t rounds = std::max<int64_t>(1, std::min<int64_t>(ROUNDS, rows * all / 2048));
+    *part = static_cast<int>(std::min(rounds * round, segments));
     *parts = static_cast<int>((segments + *part - 1) / *part);
 }
 

@@ -15,10 +15,13 @@ namespace mpv {
 struct ScoreArgs {
     mpv_scores p;
     mpv_score_buffers b;
-    int group, blocks, each;               // query heads of a cache head; workgroups of a row of scores, rounds of each
+    int group, parts;                      // query heads of a cache head; parts of a row of scores, a wave's each
     Divisor by_group, by_page;
 };
 
+#ifndef EACH
+#define EACH 8
+#endif
 constexpr int kScoreWaves = 4;
 // Groups of 16 keys that a wave reads at a time, for rows of so many bytes.
 constexpr int keys_together(int bytes) { return bytes <= 256 ? 4 : bytes <= 512 ? 2 : 1; }
@@ -49,21 +52,29 @@ __device__ __forceinline__ float spread_sum(float (&v)[n]) {
     return v[0];
 }
 
-template <int DTYPE, int DP>
-__global__ __launch_bounds__(64 * kScoreWaves) void score_kernel(ScoreArgs g) {
+// QT: groups of 16 rows that a wave keeps; 0: any number, read again for every round (and for every cache head where those share a score).
+template <int DTYPE, int DP, int QT>
+__global__ __launch_bounds__(64 * kScoreWaves) __attribute__((amdgpu_waves_per_eu(2))) void score_kernel(ScoreArgs g) {
     typedef Elem<DTYPE> E;
     constexpr int kSteps = DP * E::kBytes / 64, U = keys_together(DP * E::kBytes), kKeys = 16 * U;
     const mpv_scores& p = g.p;
-    const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int heads = p.score_heads;
-    unsigned unit = blockIdx.x / static_cast<unsigned>(g.blocks);
-    const int block = blockIdx.x - unit * g.blocks;
+    // (a wave has nothing to do with the others of its workgroup: lists may be shorter than what four of them take)
+    const unsigned number = blockIdx.x * kScoreWaves + wave;
+    unsigned unit = number / static_cast<unsigned>(g.parts);
+    const int part = number - unit * g.parts;
     const int head = unit % heads;
     unit /= heads;
     const int b = unit % p.B, layer = unit / p.B;
+    if (layer >= p.layers) return;
     const int context = min(max(g.b.context_len[b], 0), p.table_width * p.page_size);
     const int path = g.b.accept_len ? min(min(max(g.b.accept_len[b], 0), p.N - 1), g.b.path_nodes ? p.max_depth : p.N - 1) + 1 : 1;
-    const int total = min(context + path, p.score_width);
+    const int64_t whole = static_cast<int64_t>(context) + path;
+    const int total = static_cast<int>(min(whole, p.score_width));
+    // (the rounds of a list go to its parts in turn: they end together whatever the length, and read side by side)
+    const int begin = part * kKeys, step = g.parts * kKeys;
+    if (begin >= total) return;
     float* scores = g.b.scores + ((static_cast<int64_t>(layer) * p.B + b) * heads + head) * p.score_width;
     auto node_of = [&](int i) {            // of the path's i-th row; out of range: none
         const int n = i == 0 ? 0 : g.b.path_nodes ? g.b.path_nodes[static_cast<int64_t>(b) * p.max_depth + i - 1] : i;
@@ -75,89 +86,138 @@ __global__ __launch_bounds__(64 * kScoreWaves) void score_kernel(ScoreArgs g) {
     const char* cache = static_cast<const char*>(g.b.cache_k) + static_cast<int64_t>(layer) * p.cache_layer_stride * E::kBytes;
     const int rows = path * g.group, row_bytes = p.head_dim * E::kBytes;
     const int first_head = heads == 1 ? 0 : head, last_head = heads == 1 ? p.kv_heads : head + 1;
-    for (int round = 0; round < g.each; ++round) {
-        const int first = ((block * g.each + round) * kScoreWaves + wave) * kKeys;
-        if (first >= total) return;
-        // where the rows of this lane's keys lie (all four lanes of a key)
-        int64_t offset[U];
-        bool there[U], cached[U];
+
+    // 16 rows of queries: this lane's is row base + l16, its part of every step
+    struct Queries { u32x4 part[kSteps]; float lse; int upto; };   // upto: its place in the path (INT_MIN: it gives nothing)
+    auto queries = [&](int kv, int base) {
+        Queries r;
+        const int row = base + l16, i = g.by_group.of(row), node = row < rows ? node_of(i) : -1;
+        const int query_head = kv * g.group + row - i * g.group;
+        r.lse = -INFINITY;
+        if (node >= 0) r.lse = g.b.lse[(tree * p.N + node) * p.heads + query_head];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const int byte = (s * 4 + quad) * 16;
+            r.part[s] = u32x4{0u, 0u, 0u, 0u};
+            if (node >= 0 && byte < row_bytes)
+                r.part[s] = *reinterpret_cast<const u32x4*>(q + (static_cast<int64_t>(node) * p.q_stride + static_cast<int64_t>(query_head) * p.head_dim) * E::kBytes + byte);
+        }
+        r.upto = r.lse == -INFINITY ? INT_MIN : i;
+        return r;
+    };
+    Queries kept[QT ? QT : 1];
+    if constexpr (QT > 0)
+#pragma unroll
+        for (int t = 0; t < QT; ++t) kept[t] = queries(first_head, t * 16);
+
+    // a round's keys: the pages that they lie in, where their rows lie (null: nowhere), the rows, and the score so far of this lane's position
+    struct Keys { const char* from[U]; u32x4 part[U][kSteps]; float old; };
+    struct Pages { int of[U]; };
+    const int mine = l16 % (4 * U), own_key = (mine >> 2) * 16 + quad * 4 + (mine & 3);
+    auto pages = [&](int first) {
+        Pages r;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int at = first + u * 16 + l16;
-            cached[u] = at < context;
-            there[u] = at < total;
-            offset[u] = 0;
-            if (cached[u]) {
-                const int column = g.by_page.of(at), page = g.b.block_table[static_cast<int64_t>(b) * p.table_width + column];
-                there[u] = there[u] && page >= 0 && page < p.num_pages;
-                offset[u] = page * p.page_stride + (at - column * p.page_size) * p.slot_stride;
-            } else if (there[u]) {
-                const int node = node_of(at - context);
-                there[u] = node >= 0;
-                offset[u] = static_cast<int64_t>(node) * p.tree_stride;
+            r.of[u] = -1;
+            if (at < context) r.of[u] = g.b.block_table[static_cast<int64_t>(b) * p.table_width + g.by_page.of(at)];
+            else if (at < total) r.of[u] = node_of(at - context);
+        }
+        return r;
+    };
+    auto places = [&](int first, const Pages& r, Keys& k) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int at = first + u * 16 + l16;
+            k.from[u] = nullptr;
+            if (at < context) {
+                if (r.of[u] >= 0 && r.of[u] < p.num_pages)
+                    k.from[u] = cache + (r.of[u] * p.page_stride + (at - g.by_page.of(at) * p.page_size) * p.slot_stride) * E::kBytes;
+            } else if (r.of[u] >= 0) {
+                k.from[u] = tree_k + r.of[u] * p.tree_stride * E::kBytes;
             }
         }
-        float sum[4 * U] = {};
-        for (int kv = first_head; kv < last_head; ++kv) {
-            u32x4 key[U][kSteps];
+    };
+    auto ask = [&](int first, int kv, Keys& k) {
+        const int at = first + own_key;
+        k.old = l16 < 4 * U && at < context ? scores[at] : 0.0f;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const char* from = (cached[u] ? cache : tree_k) + (offset[u] + static_cast<int64_t>(kv) * p.head_dim) * E::kBytes;
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int s = 0; s < kSteps; ++s) {
-                    const int byte = (s * 4 + quad) * 16;
-                    key[u][s] = u32x4{0u, 0u, 0u, 0u};
-                    if (there[u] && byte < row_bytes) key[u][s] = *reinterpret_cast<const u32x4*>(from + byte);
+            for (int s = 0; s < kSteps; ++s) {
+                const int byte = (s * 4 + quad) * 16;
+                k.part[u][s] = u32x4{0u, 0u, 0u, 0u};
+                if (k.from[u] && byte < row_bytes) k.part[u][s] = *reinterpret_cast<const u32x4*>(k.from[u] + static_cast<int64_t>(kv) * row_bytes + byte);
+            }
+    };
+    auto add = [&](int first, const Keys& k, const Queries& r, float (&sum)[4 * U]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            f32x4 c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                if constexpr (E::kBytes == 2) {
+                    c = E::mfma(k.part[u][s], r.part[s], c);
+                } else {
+                    const f32x4 fk = __builtin_bit_cast(f32x4, k.part[u][s]), fq = __builtin_bit_cast(f32x4, r.part[s]);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) c = __builtin_amdgcn_mfma_f32_16x16x4f32(fk[x], fq[x], c, 0, 0, 0);
                 }
             }
-            for (int base = 0; base < rows; base += 16) {
-                const int row = base + l16, i = g.by_group.of(row), node = row < rows ? node_of(i) : -1;
-                const int query_head = kv * g.group + row - i * g.group;
-                u32x4 query[kSteps];
-                float lse = -INFINITY;
-                if (node >= 0) lse = g.b.lse[(tree * p.N + node) * p.heads + query_head];
-                const int upto = lse == -INFINITY ? INT_MIN : i;   // (a row that is none, or saw nothing, gives nothing)
 #pragma unroll
-                for (int s = 0; s < kSteps; ++s) {
-                    const int byte = (s * 4 + quad) * 16;
-                    query[s] = u32x4{0u, 0u, 0u, 0u};
-                    if (node >= 0 && byte < row_bytes)
-                        query[s] = *reinterpret_cast<const u32x4*>(q + (static_cast<int64_t>(node) * p.q_stride + static_cast<int64_t>(query_head) * p.head_dim) * E::kBytes + byte);
-                }
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    f32x4 c = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int s = 0; s < kSteps; ++s) {
-                        if constexpr (E::kBytes == 2) {
-                            c = E::mfma(key[u][s], query[s], c);
-                        } else {
-                            const f32x4 fk = __builtin_bit_cast(f32x4, key[u][s]), fq = __builtin_bit_cast(f32x4, query[s]);
-#pragma unroll
-                            for (int x = 0; x < 4; ++x) c = __builtin_amdgcn_mfma_f32_16x16x4f32(fk[x], fq[x], c, 0, 0, 0);
-                        }
-                    }
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int ahead = first + u * 16 + quad * 4 + x - context;         // of the path's rows, those behind it see it
-                        const float w = exp2_of(fmaf(c[x], p.scale, -lse) * 1.4426950408889634f);
-                        sum[u * 4 + x] += ahead <= upto ? w : 0.0f;
-                    }
-                }
+            for (int x = 0; x < 4; ++x) {
+                const int ahead = first + u * 16 + quad * 4 + x - context;                 // of the path's rows, those behind it see it
+                const float w = exp2_of(fmaf(c[x], p.scale, -r.lse) * 1.4426950408889634f);
+                sum[u * 4 + x] += ahead <= r.upto ? w : 0.0f;
             }
         }
+    };
+    auto finish = [&](int first, const Keys& k, float (&sum)[4 * U]) {
         const float given = spread_sum(sum);
-        const int mine = l16 % (4 * U), key = (mine >> 2) * 16 + quad * 4 + (mine & 3), at = first + key;
+        const int at = first + own_key;
         // (whether the key is there is known at the lane that looked for it)
         bool seen = false;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const bool x = __shfl(static_cast<int>(there[u]), key & 15);
-            if (key >> 4 == u) seen = x;
+            const bool x = __shfl(static_cast<int>(k.from[u] != nullptr), own_key & 15);
+            if (own_key >> 4 == u) seen = x;
         }
-        if (l16 < 4 * U && at < total) {
-            const float before = at < context ? p.decay * scores[at] : 0.0f;
-            scores[at] = before + (seen ? given : 0.0f);
+        if (l16 < 4 * U && at < total) scores[at] = (at < context ? p.decay * k.old : 0.0f) + (seen ? given : 0.0f);
+    };
+
+    if constexpr (QT > 0) {
+        // the next round's keys, and the pages of the one after it, are on their way while one is worked on
+        Keys keys[2];
+        Pages next = pages(begin);
+        places(begin, next, keys[0]);
+        ask(begin, first_head, keys[0]);
+        next = pages(begin + step);
+        for (int first = begin; first < total;) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (first >= total) break;
+                if (first + step < total) {
+                    places(first + step, next, keys[1 - h]);
+                    ask(first + step, first_head, keys[1 - h]);
+                    next = pages(first + 2 * step);
+                }
+                float sum[4 * U] = {};
+#pragma unroll
+                for (int t = 0; t < QT; ++t) add(first, keys[h], kept[t], sum);
+                finish(first, keys[h], sum);
+                first += step;
+            }
+        }
+    } else {
+        for (int first = begin; first < total; first += step) {
+            Keys keys;
+            places(first, pages(first), keys);
+            float sum[4 * U] = {};
+            for (int kv = first_head; kv < last_head; ++kv) {
+                ask(first, kv, keys);
+                for (int base = 0; base < rows; base += 16) add(first, keys, queries(kv, base), sum);
+            }
+            finish(first, keys, sum);
         }
     }
 }
@@ -179,7 +239,7 @@ static int check_scores(const mpv_scores* p) {
         return MPV_ERR_BAD_SHAPE;
     const int64_t nodes = static_cast<int64_t>(p->B) * p->N;
     const int64_t lists = span(0, span(0, p->layers, p->B), p->score_heads);
-    if (p->B > (1 << 24) || span(MPV_MAX_NODES, p->table_width, p->page_size) > INT32_MAX || p->score_width > INT32_MAX - 4096 ||
+    if (p->B > (1 << 24) || span(MPV_MAX_NODES, p->table_width, p->page_size) > INT32_MAX || p->score_width > (1 << 29) ||
         span(0, lists, (p->score_width + 15) / 16) > INT32_MAX ||
         span(0, span(span(0, nodes, p->q_stride), p->layers, p->q_layer_stride), 4) == INT64_MAX ||
         span(0, span(span(0, nodes, p->tree_stride), p->layers, p->tree_layer_stride), 4) == INT64_MAX ||
@@ -191,16 +251,28 @@ static int check_scores(const mpv_scores* p) {
     return MPV_OK;
 }
 
+template <int DTYPE, int DP, int QT>
+static void launch_groups(const ScoreArgs& g, int64_t lists, hipStream_t s) {
+    const int64_t workgroups = (lists * g.parts + kScoreWaves - 1) / kScoreWaves;
+    hipLaunchKernelGGL((score_kernel<DTYPE, DP, QT>), dim3(static_cast<unsigned>(workgroups)), dim3(64 * kScoreWaves), 0, s, g);
+}
+
 template <int DTYPE, int DP>
 static int launch_scores(ScoreArgs& g, hipStream_t s) {
-    constexpr int kRound = 16 * keys_together(DP * Elem<DTYPE>::kBytes) * kScoreWaves;
-    const int64_t positions = std::min(span(g.p.N, g.p.table_width, g.p.page_size), static_cast<int64_t>(g.p.score_width));
-    g.each = 1;
-    g.blocks = static_cast<int>((positions + kRound * g.each - 1) / (kRound * g.each));
-    const int64_t lists = static_cast<int64_t>(g.p.layers) * g.p.B * g.p.score_heads;
-    if (g.blocks == 0 || lists == 0) return MPV_OK;
+    constexpr int kRound = 16 * keys_together(DP * Elem<DTYPE>::kBytes);
+    const mpv_scores& p = g.p;
+    const int64_t positions = std::min(span(p.N, p.table_width, p.page_size), p.score_width);
+    const int64_t lists = static_cast<int64_t>(p.layers) * p.B * p.score_heads, rounds = (positions + kRound - 1) / kRound;
+    if (rounds == 0 || lists == 0) return MPV_OK;
+    // as many rounds a wave as leave enough waves for all compute units
+    const int64_t each = std::max<int64_t>(1, std::min<int64_t>(EACH, rounds * lists / 8192));
+    g.parts = static_cast<int>((rounds + each - 1) / each);
+    const int64_t deepest = g.b.accept_len ? std::min(p.N - 1, g.b.path_nodes ? p.max_depth : p.N - 1) + 1 : 1, rows = deepest * g.group;
+    const bool alone = p.score_heads == p.kv_heads;
     (void)hipGetLastError();
-    hipLaunchKernelGGL((score_kernel<DTYPE, DP>), dim3(static_cast<unsigned>(lists * g.blocks)), dim3(64 * kScoreWaves), 0, s, g);
+    if (alone && rows <= 16) launch_groups<DTYPE, DP, 1>(g, lists, s);
+    else if (alone && rows <= 32) launch_groups<DTYPE, DP, 2>(g, lists, s);
+    else launch_groups<DTYPE, DP, 0>(g, lists, s);
     return launched();
 }
 

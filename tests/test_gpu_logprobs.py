@@ -116,6 +116,17 @@ def test_masked_tokens(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("seen,top", [(1300, 64), (1300, 20), (1025, 17), (4000, 63)])
+def test_few_segments_with_many_tokens(seen, top, dtype):
+    """Fewer segments of 64 tokens than alternatives, but more tokens than are put in order at once; equal ones among them."""
+    print("[case] logprobs few segments", seen, top, dtype, flush=True)
+    logits, tokens = random(2, 1, 70001, dtype, seen)
+    logits[:, :, seen:] = -float("inf")
+    logits[1, :, :seen] = 1.5
+    check_rows(logits, tokens, 1.0, top)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_values_that_are_no_numbers(dtype):
     print("[case] logprobs nan", dtype, flush=True)
     logits, tokens = random(2, 2, 20000, dtype, 7)
