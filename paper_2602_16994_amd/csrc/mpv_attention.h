@@ -172,11 +172,6 @@ __device__ __forceinline__ int fresh(int x) {
 // What beginning and ending a unit takes, in tiles: workgroups with many short units would end last otherwise.  256 trees of 8 nodes,
 // contexts of 16 to 256: 66 us, 91 without; the benchmark's trees 613 us, 637 without; contexts of one length: the same.
 constexpr int kUnitCost = 8;
-// Tiles of a team that reads prefixes, at least.
-#ifndef LEAST
-#define LEAST 1
-#endif
-constexpr int kLeastTiles = LEAST;
 // All bits where bit `at` is set, none otherwise.  (Masks instead of conditions: those would all wait in scalar registers at once.)
 __device__ __forceinline__ uint32_t spread(uint32_t bits, int at) { return static_cast<uint32_t>(static_cast<int32_t>(bits << (31 - at)) >> 31); }
 
@@ -1071,7 +1066,7 @@ struct Attention {
         // a unit counts as `extra` tiles more than it has, all of them before its first
         const int extra = static_cast<int>(min(static_cast<int64_t>(kUnitCost), uniform64(tiles) / (2 * most)));
         const int64_t total = uniform64(tiles) + extra * uniform64(units);
-        const int T = static_cast<int>(min(static_cast<int64_t>(most), KIND == kPrefix ? (total + kLeastTiles - 1) / kLeastTiles : total));
+        const int T = static_cast<int>(min(static_cast<int64_t>(most), total));
         if (KIND != kPrefix && member == 0 && threadIdx.x == 0 && !g.by_unit) g.split[team] = make_int4(-1, 0, 0, 0);
         if (team >= T) return;
         // the first `longer` teams have one tile more than the others
@@ -1094,7 +1089,7 @@ struct Attention {
             mine = count_of(base + lane);
         }
         int64_t at = begin_at;
-        for (; at < end_at; ++b) {
+        for (; at < end_at; b = KIND == kPrefix ? t.end : b + 1) {
             load_unit();
             if (t.nodes == 0) continue;
             const int length = t.tiles + extra;

@@ -5,17 +5,30 @@
 // So prefix_kernel works out the prefix's part for the nodes of all trees that share it (mpv_prefix.hip), and a row goes on from there
 // over its own context and tree as if they were the next tiles (kBehind of mpv_attention.h).  The state between the two is float32.
 
-#include <cstdlib>
 #include "mpv_behind.h"
 
 namespace mpv {
 
-// Whether the prefixes are read for all trees that share them, or by every tree for itself.
+// Whether the prefixes are read for all trees that share them, or by every tree for itself, from the chiplets' caches.  Reading them
+// together costs two launches more (about 30 us with the second one's partial sums), the state of every row, written and read, and
+// products that no loads hide behind; what it saves is a reading for every tree but one.  In us, with the rates that either reached, for 8 cache
+// heads of 128 bfloat16 values (and 4 of float32), prefixes of as many positions as there is room for, contexts of 16 to 300, each for itself and
+// together:
+//   4 rows a cache head (single tokens):  64 trees, 8192 positions: 259, 64; 16 trees, 16 384: 155, 54; 64 trees, 1024: 59, 63
+//   20 rows:   200 trees, 4096: 443, 179; 64 trees, 4096: 152, 89; 64 trees, 1024: 59, 79; 16 trees, 4096: 55, 60
+//   64 rows:   64 trees, 8192: 273, 222; 64 trees, 4096: 154, 163; 200 trees, 1024: 153, 282
+//   164 rows:  the benchmark's trees behind four prefixes of 512 to 2048: 541, 769
+//   float32, 2 rows:  64 trees, 8192: 393, 76; 16 trees, 4096: 68, 51;   10 rows:  64 trees, 1024: 91, 68; 16 trees, 1024: 32, 50
 static bool together(const mpv_prefixed* p) {
     const mpv_attention& a = p->attention;
     if (a.B < 2 || p->prefixes < 1 || p->prefix_width < 1) return false;
-    if (const char* e = getenv("MPV_TOGETHER")) return atoi(e);
-    return true;
+    const bool wide = a.dtype == MPV_DTYPE_F32;
+    double positions = static_cast<double>(p->prefix_width) * a.page_size;
+    if (a.window > 0) positions = std::min(positions, static_cast<double>(a.window) + std::max(a.sinks, 0));
+    const double bytes = 2.0 * (a.B - 1) * positions * a.kv_heads * a.head_dim * elem_bytes(a.dtype);
+    const double rows = static_cast<double>(a.B) * a.N * a.heads;
+    const double products = 4.0 * rows * positions * a.head_dim, states = 8.0 * rows * columns_of(&a);
+    return bytes / (wide ? 4.2e6 : 7.4e6) > 30.0 + products / (wide ? 110e6 : 600e6) + states / 4e6;
 }
 
 // Bytes of a workspace: the state of the rows (none where every tree reads its prefix), and what either half needs while it runs.
