@@ -117,6 +117,7 @@ template <int BLOCK, int HELD>
 __global__ __launch_bounds__(BLOCK) void select_kernel(EvictArgs a) {
     typedef Select<BLOCK, HELD, 0> S;
     __shared__ typename S::Shared sh;
+    __shared__ typename S::Table table;
     __shared__ int stay;
     const mpv_eviction& p = a.p;
     if (blockIdx.x == 0) return plan_pages(a);
@@ -143,7 +144,7 @@ __global__ __launch_bounds__(BLOCK) void select_kernel(EvictArgs a) {
     if (threadIdx.x == 0) stay = 0;
     uint32_t limit;
     int above;
-    S::largest(key, rounds, p.budget, sh, limit, above);           // (all scores are here when it returns: `out` may be `scores`)
+    S::largest_by_table(key, rounds, p.budget, table, limit, above);           // (all scores are here when it returns: `out` may be `scores`)
     int mine = 0;
     S::chosen(key, rounds, context, limit, p.budget - above, sh, [&](int i, int place) {
         const int at = i * BLOCK + threadIdx.x, column = a.by_page.of(at);
@@ -348,8 +349,14 @@ static void launch_slices(EvictArgs& a, hipStream_t s) {
     else hipLaunchKernelGGL((move_kernel<256, LANES>), grid, dim3(256), 0, s, a);
 }
 static void launch_move(EvictArgs& a, hipStream_t s) {
-    if (a.row_bytes <= 128) launch_slices<8>(a, s);
-    else launch_slices<16>(a, s);
+    // slices as wide as a row, up to 1024 bytes, but 512 workgroups if there can be
+    int lanes = 64;
+    while (lanes > 4 && (lanes * 8 >= a.row_bytes || static_cast<int64_t>(a.lists) * ((a.row_bytes + lanes * 16 - 1) / (lanes * 16)) * 2 < 512)) lanes /= 2;
+    if (lanes == 64) launch_slices<64>(a, s);
+    else if (lanes == 32) launch_slices<32>(a, s);
+    else if (lanes == 16) launch_slices<16>(a, s);
+    else if (lanes == 8) launch_slices<8>(a, s);
+    else launch_slices<4>(a, s);
 }
 
 // Parts of a workspace.

@@ -28,6 +28,9 @@ constexpr int kListed = 256;               // segments that are looked at, at mo
 constexpr int kMany = 1024;                // tokens of them that are put in order (where equal logits make more, at most `top` whole segments)
 constexpr int kChunks = 4;                 // 16-byte loads of a thread in flight
 
+// Tokens that there has to be room for: `top` whole segments, where they are more.
+__host__ __device__ constexpr int room_of_candidates(int top) { return top * kSegment > kMany ? top * kSegment : kMany; }
+
 struct PartSums { float m, sum, weighted; int32_t better; };
 
 struct RowArgs {
@@ -309,7 +312,8 @@ __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
     __shared__ typename Single::Shared single;
     __shared__ int segments[kListed];
     __shared__ int found, take;
-    __shared__ unsigned long long candidates[MPV_MAX_TOP * kSegment];
+    extern __shared__ unsigned long long candidates[];             // [room_of_candidates]
+    const int room = room_of_candidates(top);
     uint32_t key[HELD], most[1] = {0};
 #pragma unroll
     for (int i = 0; i < HELD; ++i) {
@@ -346,7 +350,7 @@ __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
                 const uint32_t k = order_of(logit(raw[j]));
                 if (token + j < a.p.V && k > kNothing && k >> LOW >= limit >> LOW) {
                     const int at = atomicAdd(&found, 1);
-                    if (at < MPV_MAX_TOP * kSegment) candidates[at] = static_cast<unsigned long long>(k) << 32 | static_cast<uint32_t>(~(token + j));
+                    if (at < room) candidates[at] = static_cast<unsigned long long>(k) << 32 | static_cast<uint32_t>(~(token + j));
                 }
             }
         }
@@ -420,8 +424,9 @@ static int launch_rows(const RowArgs& a, hipStream_t s) {
     (void)hipGetLastError();
     hipLaunchKernelGGL(sweep_kernel<T>, dim3(static_cast<unsigned>(a.rows) * a.parts), dim3(kSweepBlock), 0, s, a);
     const dim3 rows(static_cast<unsigned>(a.rows));
-    if (a.segments <= 256 * 16) hipLaunchKernelGGL((finish_kernel<T, 256, 16>), rows, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((finish_kernel<T, 1024, 32>), rows, dim3(1024), 0, s, a);
+    const unsigned lds = a.p.top > 0 ? room_of_candidates(a.p.top) * sizeof(unsigned long long) : 0;
+    if (a.segments <= 256 * 16) hipLaunchKernelGGL((finish_kernel<T, 256, 16>), rows, dim3(256), lds, s, a);
+    else hipLaunchKernelGGL((finish_kernel<T, 1024, 32>), rows, dim3(1024), lds, s, a);
     return launched();
 }
 

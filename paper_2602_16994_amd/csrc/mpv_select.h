@@ -21,8 +21,7 @@ struct Select {
 
     // `limit`: the want-th largest key (its bits from LOW on; 0 if there are fewer), `above`: how many are larger.  As soon as exactly `want`
     // keys reach a number that is all there is to know: `limit` is the one below it then, and `above` is `want`.  Two bits a turn: the keys
-    // that reach each of three numbers are counted by ballots, so that equal digits cost no more than different ones (512 threads with 6000
-    // scores of few exponents: 3 us against 10 with a table of counts in LDS).
+    // that reach each of three numbers are counted by ballots, so that equal digits cost no more than different ones.
     static __device__ __forceinline__ void largest(const uint32_t (&held)[HELD], int rounds, int want, Shared& sh, uint32_t& limit, int& above) {
         for (int i = threadIdx.x; i < (kTurns + 1) * 3; i += BLOCK) sh.counts[i / 3][i % 3] = 0;
         __syncthreads();
@@ -64,6 +63,62 @@ struct Select {
         if ((threadIdx.x & 63) == 0) atomicAdd(&sh.counts[kTurns][0], larger);
         __syncthreads();
         above = sh.counts[kTurns][0];
+    }
+
+    // The same where `want` is large, by counts of eleven bits at a time in a table: fewer instructions, and equal digits meet in a
+    // word of LDS (1024 lists of up to 6000 scores, 512 threads each: see select_kernel).
+    struct Table {
+        int counts[2048];
+        int part[kWaves];
+        int digit, above, count;
+    };
+    static __device__ __forceinline__ void largest_by_table(const uint32_t (&held)[HELD], int rounds, int want, Table& sh, uint32_t& limit, int& above) {
+        constexpr int kBins = 2048 / BLOCK;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        limit = 0;
+        above = 0;
+#pragma unroll
+        for (int pass = 0; pass < 3; ++pass) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+#pragma unroll
+            for (int j = 0; j < kBins; ++j) sh.counts[j * BLOCK + threadIdx.x] = 0;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < HELD; ++i)
+                if (i < rounds && (pass == 0 || held[i] >> (shift + bits) == limit >> (shift + bits)))
+                    atomicAdd(&sh.counts[held[i] >> shift & ((1 << bits) - 1)], 1);
+            __syncthreads();
+            // the bins from the largest on, kBins a thread
+            int mine[kBins], sum = 0;
+#pragma unroll
+            for (int j = 0; j < kBins; ++j) sum += mine[j] = sh.counts[2047 - (static_cast<int>(threadIdx.x) * kBins + j)];
+            int upto = sum;
+            for (int d = 1; d < 64; d <<= 1) {
+                const int o = __shfl_up(upto, d);
+                if (lane >= d) upto += o;
+            }
+            if (lane == 63) sh.part[wave] = upto;
+            __syncthreads();
+            int reached = above + upto - sum;
+            for (int w = 0; w < wave; ++w) reached += sh.part[w];
+#pragma unroll
+            for (int j = 0; j < kBins; ++j) {
+                if (reached < want && reached + mine[j] >= want) {
+                    sh.digit = 2047 - (static_cast<int>(threadIdx.x) * kBins + j);
+                    sh.above = reached;
+                    sh.count = mine[j];
+                }
+                reached += mine[j];
+            }
+            __syncthreads();
+            limit |= static_cast<uint32_t>(sh.digit) << shift;
+            above = sh.above;
+            if (above + sh.count == want && limit > 0) {           // all of this digit
+                limit -= 1;
+                above = want;
+                return;
+            }
+        }
     }
 
     // take(i, place) for the chosen ones of this thread's keys: those above the limit, and the first `equal` of those that have it; `place` is
