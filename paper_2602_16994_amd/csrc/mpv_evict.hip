@@ -15,7 +15,6 @@
 namespace mpv {
 
 constexpr int kSelectBlock = 512;          // of the long lists
-constexpr int kLoads = 8;                  // rows of a thread in flight
 
 struct EvictArgs {
     mpv_eviction p;
@@ -237,6 +236,7 @@ __global__ __launch_bounds__(kSelectBlock) void select_long_kernel(EvictArgs a) 
 // slots a round earlier still.
 template <int BLOCK, int LANES>
 __global__ __launch_bounds__(BLOCK) void move_kernel(EvictArgs a) {
+    constexpr int kLoads = BLOCK == 1024 ? 4 : 8;                  // rows of a thread in a round (1024 threads have 128 registers each)
     constexpr int kStep = BLOCK / LANES, kRound = kStep * kLoads;
     const mpv_eviction& p = a.p;
     if (blockIdx.x < static_cast<unsigned>(a.returning)) return return_pages(a);

@@ -267,9 +267,10 @@ static int launch_scores(ScoreArgs& g, hipStream_t s) {
     g.parts = static_cast<int>((rounds + each - 1) / each);
     const int64_t deepest = g.b.accept_len ? std::min(p.N - 1, g.b.path_nodes ? p.max_depth : p.N - 1) + 1 : 1, rows = deepest * g.group;
     const bool alone = p.score_heads == p.kv_heads;
+    constexpr bool kLongest = DP * Elem<DTYPE>::kBytes > 512;      // (two groups of such rows do not fit the registers)
     (void)hipGetLastError();
     if (alone && rows <= 16) launch_groups<DTYPE, DP, 1>(g, lists, s);
-    else if (alone && rows <= 32) launch_groups<DTYPE, DP, 2>(g, lists, s);
+    else if (!kLongest && alone && rows <= 32) launch_groups<DTYPE, DP, kLongest ? 1 : 2>(g, lists, s);
     else launch_groups<DTYPE, DP, 0>(g, lists, s);
     return launched();
 }
