@@ -22,6 +22,7 @@ namespace mpv {
 static bool together(const mpv_prefixed* p) {
     const mpv_attention& a = p->attention;
     if (a.B < 2 || p->prefixes < 1 || p->prefix_width < 1) return false;
+    if (static_cast<int64_t>(a.B) * a.kv_heads >= kMostWorkgroups) return false;          // (the second launch has one for each tree and head)
     const bool wide = a.dtype == MPV_DTYPE_F32;
     double positions = static_cast<double>(p->prefix_width) * a.page_size;
     if (a.window > 0) positions = std::min(positions, static_cast<double>(a.window) + std::max(a.sinks, 0));

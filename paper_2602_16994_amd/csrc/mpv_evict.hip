@@ -310,6 +310,18 @@ __global__ __launch_bounds__(BLOCK) void move_kernel(EvictArgs a) {
 
 // ------------------------------------------------------------------ host side
 
+// Bytes of a row that moves as one.
+static int64_t row_bytes(const mpv_eviction* p) {
+    return static_cast<int64_t>(p->score_heads == 1 ? p->kv_heads : 1) * p->head_dim * elem_bytes(p->dtype);
+}
+static int64_t slices_of(int64_t bytes, int lanes) { return (bytes + lanes * 16 - 1) / (lanes * 16); }
+// 16-byte pieces of a slice: as wide as a row, up to 1024 bytes, but 512 workgroups if there can be.
+static int lanes_of(int64_t lists, int64_t bytes) {
+    int lanes = 64;
+    while (lanes > 4 && (lanes * 8 >= bytes || lists * slices_of(bytes, lanes) * 2 < 512)) lanes /= 2;
+    return lanes;
+}
+
 static int check_eviction(const mpv_eviction* p) {
     if (!p) return MPV_ERR_NULL;
     if (p->layers < 0 || p->B < 0 || p->kv_heads < 1 || p->head_dim < 1 || (p->score_heads != 1 && p->score_heads != p->kv_heads) || p->num_pages < 0 ||
@@ -323,7 +335,7 @@ static int check_eviction(const mpv_eviction* p) {
     const int64_t lists = span(0, span(0, p->layers, p->B), p->score_heads);
     if (span(0, p->num_pages, p->page_size) > INT32_MAX || span(0, p->table_width, p->page_size) > INT32_MAX || p->score_width > INT32_MAX ||
         lists > INT32_MAX / 1024 || p->B > (1 << 24) || span(0, lists, p->budget) > (static_cast<int64_t>(1) << 40) ||
-        span(0, lists, (row * elem_bytes(p->dtype) + 127) / 128 * 2) > INT32_MAX - 1 ||
+        (lists > 0 && span(0, lists, 2 * slices_of(row_bytes(p), lanes_of(lists, row_bytes(p)))) > kMostWorkgroups - 64) ||
         span(0, span(span(span(0, p->num_pages, p->page_stride), p->page_size, p->slot_stride), p->layers, p->cache_layer_stride), 4) == INT64_MAX)
         return MPV_ERR_UNSUPPORTED;
     const int64_t all = p->head_dim | p->slot_stride | p->page_stride | p->cache_layer_stride;
@@ -341,7 +353,7 @@ static void launch_select(const EvictArgs& a, hipStream_t s) {
 
 template <int LANES>
 static void launch_slices(EvictArgs& a, hipStream_t s) {
-    a.slices = static_cast<int>((a.row_bytes + LANES * 16 - 1) / (LANES * 16));
+    a.slices = static_cast<int>(slices_of(a.row_bytes, LANES));
     const int64_t workgroups = static_cast<int64_t>(a.lists) * a.slices * 2;
     const dim3 grid(static_cast<unsigned>(workgroups + a.returning));
     // (few lists: more rows of each at a time)
@@ -349,9 +361,7 @@ static void launch_slices(EvictArgs& a, hipStream_t s) {
     else hipLaunchKernelGGL((move_kernel<256, LANES>), grid, dim3(256), 0, s, a);
 }
 static void launch_move(EvictArgs& a, hipStream_t s) {
-    // slices as wide as a row, up to 1024 bytes, but 512 workgroups if there can be
-    int lanes = 64;
-    while (lanes > 4 && (lanes * 8 >= a.row_bytes || static_cast<int64_t>(a.lists) * ((a.row_bytes + lanes * 16 - 1) / (lanes * 16)) * 2 < 512)) lanes /= 2;
+    const int lanes = lanes_of(a.lists, a.row_bytes);
     if (lanes == 64) launch_slices<64>(a, s);
     else if (lanes == 32) launch_slices<32>(a, s);
     else if (lanes == 16) launch_slices<16>(a, s);
@@ -402,7 +412,7 @@ int mpv_evict_positions(const mpv_eviction* eviction, const mpv_eviction_buffers
     a.p = *p;
     a.b = *buf;
     a.lists = p->layers * p->B * p->score_heads;
-    a.row_bytes = static_cast<int64_t>(p->score_heads == 1 ? p->kv_heads : 1) * p->head_dim * mpv::elem_bytes(p->dtype);
+    a.row_bytes = mpv::row_bytes(p);
     a.lead = p->score_heads == 1 ? 0 : p->head_dim;
     a.by_page.set(static_cast<uint32_t>(p->page_size));
     const mpv::EvictRoom room = mpv::room_of(p);

@@ -18,6 +18,9 @@ inline bool hip_fine(hipError_t e) {
     return false;
 }
 
+// Workgroups of 256 threads that a launch can have: 2^32 threads in a dimension are too many.
+constexpr int64_t kMostWorkgroups = (1 << 24) - 1;
+
 // The outcome of the launches since the last hipGetLastError().
 inline int launched() { return hip_fine(hipGetLastError()) ? MPV_OK : MPV_ERR_HIP; }
 

@@ -404,7 +404,10 @@ static int check_logprobs(const mpv_logprobs* p) {
     if (!std::isfinite(p->temperature) || !(p->temperature > 0.0f)) return MPV_ERR_BAD_TEMPERATURE;
     if (p->V > MPV_MAX_VOCAB || p->top > MPV_MAX_TOP) return MPV_ERR_UNSUPPORTED;
     const int64_t width = p->paths ? static_cast<int64_t>(p->max_depth) + 1 : p->N, rows = width * p->B;
-    if (rows > (1 << 24) || span(0, static_cast<int64_t>(p->B) * p->N, p->stride) > INT64_MAX / 8) return MPV_ERR_UNSUPPORTED;
+    int parts = 1, part;
+    if (rows > 0 && rows <= kMostWorkgroups) parts_of(p, rows, &parts, &part);
+    // (a row's second workgroup may have 1024 threads)
+    if (rows > kMostWorkgroups / 4 || rows * parts > kMostWorkgroups || span(0, static_cast<int64_t>(p->B) * p->N, p->stride) > INT64_MAX / 8) return MPV_ERR_UNSUPPORTED;
     return MPV_OK;
 }
 

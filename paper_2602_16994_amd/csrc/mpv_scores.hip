@@ -237,7 +237,7 @@ static int check_scores(const mpv_scores* p) {
     const int64_t nodes = static_cast<int64_t>(p->B) * p->N;
     const int64_t lists = span(0, span(0, p->layers, p->B), p->score_heads);
     if (p->B > (1 << 24) || span(MPV_MAX_NODES, p->table_width, p->page_size) > INT32_MAX || p->score_width > (1 << 29) ||
-        span(0, lists, (p->score_width + 15) / 16) > INT32_MAX ||
+        lists > kMostWorkgroups ||
         span(0, span(span(0, nodes, p->q_stride), p->layers, p->q_layer_stride), 4) == INT64_MAX ||
         span(0, span(span(0, nodes, p->tree_stride), p->layers, p->tree_layer_stride), 4) == INT64_MAX ||
         span(0, span(span(span(0, p->num_pages, p->page_stride), p->page_size, p->slot_stride), p->layers, p->cache_layer_stride), 4) == INT64_MAX)
@@ -263,7 +263,8 @@ static int launch_scores(ScoreArgs& g, hipStream_t s) {
     if (rounds == 0 || lists == 0) return MPV_OK;
     // as many rounds a wave as leave enough waves for all compute units (16 layers of 16 contexts of up to 8192: 460 us with eight, 485 with
     // four, 481 with sixteen)
-    const int64_t each = std::max<int64_t>(1, std::min<int64_t>(8, rounds * lists / 8192));
+    const int64_t most = kMostWorkgroups * kScoreWaves;
+    const int64_t each = std::max(std::max<int64_t>(1, std::min<int64_t>(8, rounds * lists / 8192)), (rounds + most / lists - 1) / (most / lists));
     g.parts = static_cast<int>((rounds + each - 1) / each);
     const int64_t deepest = g.b.accept_len ? std::min(p.N - 1, g.b.path_nodes ? p.max_depth : p.N - 1) + 1 : 1, rows = deepest * g.group;
     const bool alone = p.score_heads == p.kv_heads;

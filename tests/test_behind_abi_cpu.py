@@ -91,7 +91,7 @@ def test_scores(lib):
         ({"dtype": 3}, {}, "MPV_ERR_BAD_DTYPE"), ({"scale": float("inf")}, {}, "MPV_ERR_BAD_TEMPERATURE"),
         ({"decay": float("nan")}, {}, "MPV_ERR_BAD_TEMPERATURE"), ({"N": 65}, {}, "MPV_ERR_UNSUPPORTED"),
         ({"score_width": 1 << 30}, {}, "MPV_ERR_UNSUPPORTED"), ({"q_stride": 1 << 60}, {}, "MPV_ERR_UNSUPPORTED"),
-        ({"cache_layer_stride": 1 << 61}, {}, "MPV_ERR_UNSUPPORTED"), ({"layers": 1 << 20, "B": 1 << 20}, {}, "MPV_ERR_UNSUPPORTED"),
+        ({"cache_layer_stride": 1 << 61}, {}, "MPV_ERR_UNSUPPORTED"), ({"layers": 1 << 20, "B": 1 << 20}, {}, "MPV_ERR_UNSUPPORTED"), ({"layers": 1 << 12, "B": 1 << 12}, {}, "MPV_ERR_UNSUPPORTED"),
         ({"head_dim": 60}, {}, "MPV_ERR_ALIGNMENT"), ({"q_layer_stride": 1540}, {}, "MPV_ERR_ALIGNMENT"), ({"page_stride": 2050}, {}, "MPV_ERR_ALIGNMENT"),
         ({}, {"q": FAKE + 8}, "MPV_ERR_ALIGNMENT"), ({}, {"cache_k": FAKE + 2}, "MPV_ERR_ALIGNMENT"),
         ({}, {"q": None}, "MPV_ERR_NULL"), ({}, {"tree_k": None}, "MPV_ERR_NULL"), ({}, {"lse": None}, "MPV_ERR_NULL"), ({}, {"scores": None}, "MPV_ERR_NULL"),
@@ -119,7 +119,8 @@ def test_eviction(lib):
         ({"score_heads": 3}, {}, "MPV_ERR_BAD_SHAPE"), ({"score_width": 63}, {}, "MPV_ERR_BAD_SHAPE"), ({"slot_stride": 64}, {}, "MPV_ERR_BAD_SHAPE"),
         ({"dtype": 5}, {}, "MPV_ERR_BAD_DTYPE"), ({"head_dim": 264, "slot_stride": 1024}, {}, "MPV_ERR_UNSUPPORTED"),
         ({"num_pages": 1 << 30}, {}, "MPV_ERR_UNSUPPORTED"), ({"page_stride": 1 << 61}, {}, "MPV_ERR_UNSUPPORTED"), ({"B": (1 << 24) + 1}, {}, "MPV_ERR_UNSUPPORTED"),
-        ({"layers": 1 << 20}, {}, "MPV_ERR_UNSUPPORTED"), ({"head_dim": 60}, {}, "MPV_ERR_ALIGNMENT"), ({"cache_layer_stride": 16388}, {}, "MPV_ERR_ALIGNMENT"),
+        ({"layers": 1 << 20}, {}, "MPV_ERR_UNSUPPORTED"), ({"layers": 1 << 16, "kv_heads": 1024, "score_heads": 1, "slot_stride": 65536, "page_stride": 1 << 20}, {}, "MPV_ERR_UNSUPPORTED"),
+        ({"head_dim": 60}, {}, "MPV_ERR_ALIGNMENT"), ({"cache_layer_stride": 16388}, {}, "MPV_ERR_ALIGNMENT"),
         ({}, {"cache_k": FAKE + 8}, "MPV_ERR_ALIGNMENT"), ({}, {"kept": None}, "MPV_ERR_NULL"), ({}, {"scores": None}, "MPV_ERR_NULL"),
         ({}, {"scores_out": None}, "MPV_ERR_NULL"), ({}, {"free_pages": None}, "MPV_ERR_NULL"), ({}, {"free_count_out": None}, "MPV_ERR_NULL"),
         ({}, {"context_len": None}, "MPV_ERR_NULL"), ({}, {"block_table": None}, "MPV_ERR_NULL"), ({}, {"cache_v": None}, "MPV_ERR_NULL"),
@@ -141,7 +142,8 @@ def test_logprobs(lib):
         ({"dtype": 3}, {}, "MPV_ERR_BAD_DTYPE"), ({"temperature": 0.0}, {}, "MPV_ERR_BAD_TEMPERATURE"), ({"temperature": float("inf")}, {}, "MPV_ERR_BAD_TEMPERATURE"),
         ({"temperature": -1.0}, {}, "MPV_ERR_BAD_TEMPERATURE"), ({"temperature": float("nan")}, {}, "MPV_ERR_BAD_TEMPERATURE"),
         ({"V": (1 << 21) + 1, "stride": 1 << 22}, {}, "MPV_ERR_UNSUPPORTED"), ({"top": 65}, {}, "MPV_ERR_UNSUPPORTED"), ({"stride": 1 << 61}, {}, "MPV_ERR_UNSUPPORTED"),
-        ({"B": 1 << 24}, {}, "MPV_ERR_UNSUPPORTED"),
+        ({"B": 1 << 24}, {}, "MPV_ERR_UNSUPPORTED"), ({"B": 1 << 20}, {}, "MPV_ERR_UNSUPPORTED"),
+        ({"B": 1 << 19, "V": 1 << 21, "stride": 1 << 21}, {}, "MPV_ERR_UNSUPPORTED"),
         ({}, {"logits": None}, "MPV_ERR_NULL"), ({}, {"tokens": None}, "MPV_ERR_NULL"), ({}, {"accept_len": None}, "MPV_ERR_NULL"),
         ({}, {"path_nodes": None}, "MPV_ERR_NULL"), ({}, {"bonus_token": None}, "MPV_ERR_NULL"), ({}, {"rank": None}, "MPV_ERR_NULL"),
         ({}, {"top_tokens": None}, "MPV_ERR_NULL"), ({}, {"top_logprobs": None}, "MPV_ERR_NULL"), ({}, {"logits": FAKE + 1}, "MPV_ERR_ALIGNMENT"),
