@@ -8,6 +8,7 @@
 // meet.  Its first workgroups return the pages.
 
 #include <algorithm>
+#include <type_traits>
 
 #include "mpv_host.h"
 #include "mpv_select.h"
@@ -116,7 +117,8 @@ template <int BLOCK, int HELD>
 __global__ __launch_bounds__(BLOCK) void select_kernel(EvictArgs a) {
     typedef Select<BLOCK, HELD, 0> S;
     __shared__ typename S::Shared sh;
-    __shared__ typename S::Table table;
+    __shared__ typename std::conditional<BLOCK == 64, int, typename S::Table>::type table;
+    (void)table;
     __shared__ int stay;
     const mpv_eviction& p = a.p;
     if (blockIdx.x == 0) return plan_pages(a);
@@ -143,7 +145,9 @@ __global__ __launch_bounds__(BLOCK) void select_kernel(EvictArgs a) {
     if (threadIdx.x == 0) stay = 0;
     uint32_t limit;
     int above;
-    S::largest_by_table(key, rounds, p.budget, table, limit, above);           // (all scores are here when it returns: `out` may be `scores`)
+    // (all scores are here when it returns: `out` may be `scores`)
+    if constexpr (BLOCK == 64) S::largest(key, rounds, p.budget, sh, limit, above);
+    else S::largest_by_table(key, rounds, p.budget, table, limit, above);
     int mine = 0;
     S::chosen(key, rounds, context, limit, p.budget - above, sh, [&](int i, int place) {
         const int at = i * BLOCK + threadIdx.x, column = a.by_page.of(at);
@@ -346,7 +350,8 @@ static int check_eviction(const mpv_eviction* p) {
 static void launch_select(const EvictArgs& a, hipStream_t s) {
     const int64_t room = static_cast<int64_t>(a.p.table_width) * a.p.page_size;
     const dim3 lists(static_cast<unsigned>(a.lists) + 1);
-    if (room <= 512 * 16) hipLaunchKernelGGL((select_kernel<512, 16>), lists, dim3(512), 0, s, a);
+    if (room <= 64 * 16) hipLaunchKernelGGL((select_kernel<64, 16>), lists, dim3(64), 0, s, a);
+    else if (room <= 512 * 16) hipLaunchKernelGGL((select_kernel<512, 16>), lists, dim3(512), 0, s, a);
     else if (room <= 1024 * 32) hipLaunchKernelGGL((select_kernel<1024, 32>), lists, dim3(1024), 0, s, a);
     else hipLaunchKernelGGL(select_long_kernel, lists, dim3(kSelectBlock), 0, s, a);
 }

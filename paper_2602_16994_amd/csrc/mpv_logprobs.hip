@@ -25,7 +25,8 @@ namespace mpv {
 constexpr int kSweepBlock = 256;
 constexpr int kSegment = 64;
 constexpr int kListed = 256;               // segments that are looked at, at most
-constexpr int kMany = 1024;                // tokens of them that are put in order (where equal logits make more, at most `top` whole segments)
+constexpr int kMany = 1024;                // tokens of them that there is room for (where equal logits make more, at most `top` whole segments)
+constexpr int kOrdered = 160;              // tokens that are put in order by comparing each with each
 constexpr int kChunks = 4;                 // 16-byte loads of a thread in flight
 
 // Tokens that there has to be room for: `top` whole segments, where they are more.
@@ -359,7 +360,7 @@ __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
     bool many = take > kListed;
     if (!many) {
         collect(take);
-        many = found > kMany;
+        many = found > room;
     }
     if (many) {
         __syncthreads();
@@ -370,7 +371,36 @@ __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
         __syncthreads();
         collect(min(take, top));                                   // (fewer, if fewer have a token at all: they are all among the first)
     }
-    const int count = found;
+    int count = found;
+    if (count > kOrdered) {
+        // (few tokens or equal logits) the best of them by their logits, of equal ones by their place
+        typedef Select<kFinishBlock, MPV_MAX_TOP * kSegment / kFinishBlock, 0> Refine;
+        __shared__ typename Refine::Shared refine;
+        constexpr int kOf = MPV_MAX_TOP * kSegment / kFinishBlock;
+        uint32_t high[kOf], low[kOf], same[kOf];
+#pragma unroll
+        for (int i = 0; i < kOf; ++i) {
+            const int at = i * kFinishBlock + threadIdx.x;
+            const unsigned long long k = at < count ? candidates[at] : 0ull;
+            high[i] = static_cast<uint32_t>(k >> 32);
+            low[i] = static_cast<uint32_t>(k);
+        }
+        const int rounds_of = (count + kFinishBlock - 1) / kFinishBlock;
+        int larger, first = 0;
+        uint32_t least, last = 0;
+        Refine::largest(high, rounds_of, top, refine, least, larger);
+#pragma unroll
+        for (int i = 0; i < kOf; ++i) same[i] = high[i] == least ? low[i] : 0u;
+        if (larger < top) Refine::largest(same, rounds_of, top - larger, refine, last, first);
+        if (threadIdx.x == 0) found = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kOf; ++i)
+            if (high[i] > least || (larger < top && same[i] != 0 && (same[i] > last || (same[i] == last && first < top - larger))))
+                candidates[atomicAdd(&found, 1)] = static_cast<unsigned long long>(high[i]) << 32 | low[i];
+        __syncthreads();
+        count = found;
+    }
     for (int i = threadIdx.x; i < count; i += kFinishBlock) {
         const unsigned long long k = candidates[i];
         int place = 0;

@@ -23,6 +23,7 @@ struct Select {
     // keys reach a number that is all there is to know: `limit` is the one below it then, and `above` is `want`.  Two bits a turn: the keys
     // that reach each of three numbers are counted by ballots, so that equal digits cost no more than different ones.
     static __device__ __forceinline__ void largest(const uint32_t (&held)[HELD], int rounds, int want, Shared& sh, uint32_t& limit, int& above) {
+        __syncthreads();                                           // (a call before this one may still be read)
         for (int i = threadIdx.x; i < (kTurns + 1) * 3; i += BLOCK) sh.counts[i / 3][i % 3] = 0;
         __syncthreads();
         limit = 0;
@@ -74,6 +75,7 @@ struct Select {
     };
     static __device__ __forceinline__ void largest_by_table(const uint32_t (&held)[HELD], int rounds, int want, Table& sh, uint32_t& limit, int& above) {
         constexpr int kBins = 2048 / BLOCK;
+        static_assert(2048 % BLOCK == 0, "bins");
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         limit = 0;
         above = 0;

@@ -72,6 +72,7 @@ def random(B, N, V, dtype, seed, sigma=2.5):
 @pytest.mark.parametrize("B,N,V,top,T", [
     (1, 1, 1, 1, 1.0), (1, 1, 2, 5, 1.0), (2, 3, 7, 3, 0.5), (1, 2, 63, 64, 1.0), (3, 1, 64, 1, 2.0), (1, 3, 65, 20, 1.0), (2, 2, 1000, 0, 0.7),
     (1, 1, 8193, 8, 1.0), (4, 5, 32000, 5, 1.0), (1, 2, 50257, 64, 1.3), (2, 1, 151936, 20, 0.1), (1, 1, 262147, 7, 1.0), (700, 2, 515, 4, 1.0),
+    (2, 2, 1969, 64, 1.0), (1, 2, 4096, 63, 1.0), (1, 1, 300, 2, 1.0), (1, 1, 161, 64, 1.0), (1, 1, 160, 64, 1.0),
 ])
 def test_rows(B, N, V, top, T, dtype):
     print("[case] logprobs rows", B, N, V, top, T, dtype, flush=True)
