@@ -361,8 +361,10 @@ static void launch_slices(EvictArgs& a, hipStream_t s) {
     a.slices = static_cast<int>(slices_of(a.row_bytes, LANES));
     const int64_t workgroups = static_cast<int64_t>(a.lists) * a.slices * 2;
     const dim3 grid(static_cast<unsigned>(workgroups + a.returning));
-    // (few lists: more rows of each at a time)
-    if (workgroups < 512) hipLaunchKernelGGL((move_kernel<1024, LANES>), grid, dim3(1024), 0, s, a);
+    // Many rounds of 256 threads (or few lists): more rows a round.  (16 requests to 2048 positions: 433 us with 1024 threads, 491 with 256, which
+    // take 16 rounds; 42 requests to 12 108 slots of 1024 bytes: 232, 407; 41 requests to 48: 60, 44.)
+    constexpr int kRound = 256 / LANES * 8;
+    if (a.p.budget > 4 * kRound || (workgroups < 512 && a.p.budget > kRound)) hipLaunchKernelGGL((move_kernel<1024, LANES>), grid, dim3(1024), 0, s, a);
     else hipLaunchKernelGGL((move_kernel<256, LANES>), grid, dim3(256), 0, s, a);
 }
 static void launch_move(EvictArgs& a, hipStream_t s) {
