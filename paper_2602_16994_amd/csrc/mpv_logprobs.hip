@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cfloat>
+#include <climits>
 #include <cmath>
 #include <type_traits>
 
@@ -119,16 +120,21 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
     int better = 0, equals = 0;            // of the wave, and of this lane
     const float below = next_below(mine);
     const int full = min(to, whole);
-    // a round of chunks; kWhole: all of them are there
-    auto round = [&](int first, auto all) {
-        constexpr bool kWhole = decltype(all)::value;
+    // where this lane writes a maximum: that of its segment in the round's chunk `lane % kLanes`, if there are so many
+    constexpr int kPerRound = kSweepBlock / kLanes;
+    const int chunk_of = threadIdx.x % kLanes;
+    float* mine_best = a.best + static_cast<int64_t>(row) * a.segments + chunk_of * kPerRound + threadIdx.x / kLanes;
+    const int token_chunk = known ? r.token / N : INT_MAX;
+    // a round of chunks; kWhole: all of them are there; kPlain: the given token's is none of them
+    auto round = [&](int first, auto all, auto elsewhere) {
+        constexpr bool kWhole = decltype(all)::value, kPlain = decltype(elsewhere)::value;
         T raw[kChunks][N];
 #pragma unroll
         for (int j = 0; j < kChunks; ++j) {
             const int chunk = first + j * kSweepBlock + threadIdx.x;
             if (kWhole || chunk < full) __builtin_memcpy(raw[j], z + static_cast<int64_t>(chunk) * N, 16);
         }
-        float v[kChunks][N], now = m;
+        float v[kChunks][N], now = m, best = -INFINITY;
 #pragma unroll
         for (int j = 0; j < kChunks; ++j) {
             const int chunk = first + j * kSweepBlock + threadIdx.x;
@@ -147,18 +153,25 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
             for (int i = 3; i < N; i += 2) most = maximum(most, v[j][i], v[j][i + 1 < N ? i + 1 : i]);
             now = maximum(now, most, most);
             if (a.p.top > 0) {
-                const float best = segment_max<kLanes>(most);
-                if (threadIdx.x % kLanes == 0 && (kWhole || chunk < to)) a.best[static_cast<int64_t>(row) * a.segments + chunk / kLanes] = best;
+                const float segment = segment_max<kLanes>(most);
+                best = chunk_of == j ? segment : best;
             }
             // tokens before the given one are better if they are not smaller: if they are larger than the number below it
-            const int before = r.token - chunk * N;                // of this chunk's tokens; what lies behind the part is none of them
-            const float least = before >= N && (kWhole || chunk < to) ? below : mine;
+            if constexpr (kPlain) {
+                const float least = token_chunk != INT_MAX && token_chunk > first ? below : mine;
 #pragma unroll
-            for (int i = 0; i < N; ++i) better += __popcll(__ballot(!(v[j][i] <= least)));
+                for (int i = 0; i < N; ++i) better += __popcll(__ballot(!(v[j][i] <= least)));
+            } else {
+                const bool there = kWhole || chunk < to;           // (what lies behind the part is not counted)
+                const float least = token_chunk != INT_MAX && chunk < token_chunk && there ? below : mine;
+#pragma unroll
+                for (int i = 0; i < N; ++i) better += __popcll(__ballot(!(v[j][i] <= least)));
+                if (chunk == token_chunk && there)
+                    for (int i = 0; i < N; ++i) equals += chunk * N + i < r.token && v[j][i] == mine;
+            }
             asm volatile("" : "+s"(better));                       // (counted here: the ballots would all wait in scalar registers)
-            if (before > 0 && before < N && (kWhole || chunk < to))
-                for (int i = 0; i < N; ++i) equals += i < before && v[j][i] == mine;
         }
+        if (a.p.top > 0 && chunk_of < kChunks && (kWhole || first + chunk_of * kSweepBlock + static_cast<int>(threadIdx.x) < to)) mine_best[first / kLanes] = best;
         const float base = now == -INFINITY ? 0.0f : now, shift = base * a.c;
         if (m != -INFINITY) {
             const float fade = exp2f((m - now) * a.c);
@@ -192,8 +205,11 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
         }
     };
     int first = from;
-    for (; first + kChunks * kSweepBlock <= full; first += kChunks * kSweepBlock) round(first, std::true_type());
-    for (; first < to; first += kChunks * kSweepBlock) round(first, std::false_type());
+    for (; first + kChunks * kSweepBlock <= full; first += kChunks * kSweepBlock) {
+        if (token_chunk < first || token_chunk >= first + kChunks * kSweepBlock) round(first, std::true_type(), std::true_type());
+        else round(first, std::true_type(), std::false_type());
+    }
+    for (; first < to; first += kChunks * kSweepBlock) round(first, std::false_type(), std::false_type());
     // over the workgroup
     __shared__ float ms[kSweepBlock / 64], sums[kSweepBlock / 64], weights[kSweepBlock / 64];
     __shared__ int betters[kSweepBlock / 64];
