@@ -91,7 +91,8 @@ extern "C" {
                                * (an error of log2(e)/T * 2^-25 in the exponent of e^(z/T): nothing
                                * for T >= 0.01).  -inf marks a token of probability zero.        */
 #define MPV_DTYPE_F16  2      /* IEEE binary16: the calls around a verification only (mpv_tree_attention,
-                               * mpv_verify_chains, mpv_append_paths); logits are F32 or BF16.        */
+                               * mpv_verify_chains, mpv_append_paths and those after them); a verification's
+                               * logits are F32 or BF16.                                              */
 
 /* error codes: 0 = success, negative = failure (nothing was launched unless the
  * code is MPV_ERR_HIP, in which case some kernels may already be enqueued) */

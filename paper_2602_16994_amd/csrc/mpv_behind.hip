@@ -4,6 +4,9 @@
 //   m = max m_i,  out = sum_i e^(m_i - m) o_i / sum_i e^(m_i - m) w_i,  ln sum_j e^(s_j) = m + ln sum_i e^(m_i - m) w_i.
 // So prefix_kernel works out the prefix's part for the nodes of all trees that share it (mpv_prefix.hip), and a row goes on from there
 // over its own context and tree as if they were the next tiles (kBehind of mpv_attention.h).  The state between the two is float32.
+//
+// What bounds the trees' own part, 64 single tokens with contexts of 16 to 1024: 42 us for 136 MB, of which some 12 are what comes before the
+// first tile (as in mpv_tree_attention); then memory.
 
 #include "mpv_behind.h"
 

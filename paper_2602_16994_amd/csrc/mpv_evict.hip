@@ -6,6 +6,11 @@
 // rows [c, c + n) was read with them or before: a workgroup that takes a slice of a list's rows, some rows a round, all loads before the
 // stores, needs no other copy, and may ask for the next round's rows before it writes.  Different slices (of different bytes) do not
 // meet.  Its first workgroups return the pages.
+//
+// What bounds it: 8 layers of 16 requests, 8 cache heads of 128 bfloat16 values, cut from 2048 to 6000 positions to 2048: 390 us for the rows that
+// move, 1.9 GB read and written at 4.9 TB/s, the rate of a large copy, and 33 us for the 1024 lists (tables of counts in LDS; 64 us with ballots,
+// 70 with eight bits a round and the scores read again).  One request, 1100 to 1000 positions in 4 layers: 14 us and 10, lengths ->
+// scores -> limit -> page, then slot -> row.
 
 #include <algorithm>
 #include <type_traits>

@@ -22,6 +22,11 @@ namespace mpv {
 // read once, and those segments again.
 //
 // sweep_kernel: a workgroup has a part of a row; finish_kernel: one has a row, its parts and its segments' maxima.
+//
+// What bounds it: 900 rows of 151 936 bfloat16 logits (the emitted tokens of 256 trees) take 68 us for 272 MB, 4.0 TB/s, with vector
+// instructions two thirds of the time (some 12 a logit: unpacking, maximum, comparison, exponential, two sums), and 16 in the second
+// launch, loads that depend on each other: row, maxima, segments, their logits.  1024 rows of 128 257 float32 logits: 101 us for 525 MB, 5.2 TB/s,
+// memory, and 16.  One request's four rows of 32 000: 13 us, two launches.
 
 constexpr int kSweepBlock = 256;
 constexpr int kSegment = 64;
