@@ -290,6 +290,7 @@ struct Attention {
     static constexpr int kAheadTiles = STAGES - 1;
     static constexpr int kTile = TILE;
     static constexpr int kShare = SHARE;
+    static constexpr int kWavesOfSimd = WAVES == 4 && SHARE == 3 ? 3 : 2;   // that registers have to leave room for
     static constexpr bool k16 = E::kBytes == 2;
     static_assert(kChunks >= 8 && kChunks <= 64 && kMyLoads >= 1 && kMyRows % kRowsPerLoad == 0 && 64 % kMyRows == 0, "loads");
     static_assert(TILE % (k16 ? 32 : 16) == 0 && kGroups * 4 <= 32, "tile");
@@ -1349,9 +1350,17 @@ inline Second second_of(const mpv_attention* a, const Choice& c, bool by_unit) {
 
 inline size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
+// Behind prefixes, 64 rows on four waves: three workgroups a compute unit with two stages each instead of two with four (48 trees with a
+// window of 2000: 35.4 us, 38.0; 64 trees of 15 nodes behind prefixes of 256 to 4096 positions: 148, 153, and 149 with two of three stages;
+// 256 trees of 8 nodes, 8 rows a node, behind 256 to 1024: 117, 130; in float32, 64 trees of 8 nodes behind 4096: 414, 446).
 template <int KIND, int DTYPE, int DP, int QT, int WAVES>
-using Kernel = Attention<DTYPE, DP, QT, WAVES, Family<DTYPE, DP, WAVES>::kTile, Family<DTYPE, DP, WAVES>::kStages,
-                         Family<DTYPE, DP, WAVES>::kShare, KIND>;
+struct Shape {
+    typedef Family<DTYPE, DP, WAVES> F;
+    static constexpr bool kThree = KIND != kTree && QT == 1 && WAVES == 4 && F::kTile * F::kBytes <= 8192;
+    typedef Attention<DTYPE, DP, QT, WAVES, F::kTile, kThree ? 2 : F::kStages, kThree ? 3 : F::kShare, KIND> T;
+};
+template <int KIND, int DTYPE, int DP, int QT, int WAVES>
+using Kernel = typename Shape<KIND, DTYPE, DP, QT, WAVES>::T;
 
 template <class K> struct Chosen { typedef K T; };
 

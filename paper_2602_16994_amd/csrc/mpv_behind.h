@@ -7,7 +7,7 @@
 namespace mpv {
 
 template <class A>
-__global__ __launch_bounds__(A::kThreads) __attribute__((amdgpu_waves_per_eu(2))) void behind_kernel(PrefixArgs g) {
+__global__ __launch_bounds__(A::kThreads) __attribute__((amdgpu_waves_per_eu(A::kWavesOfSimd))) void behind_kernel(PrefixArgs g) {
     extern __shared__ __align__(1024) char memory[];
     A a(g, *reinterpret_cast<typename A::Shared*>(memory));
     a.all();
