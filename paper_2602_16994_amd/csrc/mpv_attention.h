@@ -1350,14 +1350,16 @@ inline Second second_of(const mpv_attention* a, const Choice& c, bool by_unit) {
 
 inline size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// Behind prefixes, 64 rows on four waves: three workgroups a compute unit with two stages each instead of two with four (48 trees with a
-// window of 2000: 35.4 us, 38.0; 64 trees of 15 nodes behind prefixes of 256 to 4096 positions: 148, 153, and 149 with two of three stages;
-// 256 trees of 8 nodes, 8 rows a node, behind 256 to 1024: 117, 130; in float32, 64 trees of 8 nodes behind 4096: 414, 446).
+// Behind prefixes, 17 to 64 rows: as many workgroups a compute unit as its LDS holds with two stages each, instead of two with four.  64 rows
+// (four waves, three workgroups): 48 trees with a window of 2000 35.4 us, 38.0; 64 trees of 15 nodes behind prefixes of 256 to 4096 positions
+// 148, 153, and 149 with two of three stages; 256 trees of 8 nodes behind 256 to 1024 117, 130; float32, 64 trees behind 4096 414, 446.
+// 32 rows (two waves, four workgroups): 200 trees of 5 nodes 123.7, 129.1, and 125.2 with three; 256 trees of 8 nodes 148, 155; float32, 64
+// trees behind 256 to 4096 214, 239; at worst 2 % more (16 trees of 5 nodes, 47.0, 46.2).
 template <int KIND, int DTYPE, int DP, int QT, int WAVES>
 struct Shape {
     typedef Family<DTYPE, DP, WAVES> F;
-    static constexpr bool kThree = KIND != kTree && QT == 1 && WAVES == 4 && F::kTile * F::kBytes <= 8192;
-    typedef Attention<DTYPE, DP, QT, WAVES, F::kTile, kThree ? 2 : F::kStages, kThree ? 3 : F::kShare, KIND> T;
+    static constexpr bool kTwoStages = KIND != kTree && QT == 1 && (WAVES == 2 || WAVES == 4) && F::kTile * F::kBytes <= 8192;
+    typedef Attention<DTYPE, DP, QT, WAVES, F::kTile, kTwoStages ? 2 : F::kStages, kTwoStages ? (WAVES == 2 ? 4 : 3) : F::kShare, KIND> T;
 };
 template <int KIND, int DTYPE, int DP, int QT, int WAVES>
 using Kernel = typename Shape<KIND, DTYPE, DP, QT, WAVES>::T;
