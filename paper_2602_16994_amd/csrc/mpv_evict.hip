@@ -324,10 +324,17 @@ static int64_t row_bytes(const mpv_eviction* p) {
     return static_cast<int64_t>(p->score_heads == 1 ? p->kv_heads : 1) * p->head_dim * elem_bytes(p->dtype);
 }
 static int64_t slices_of(int64_t bytes, int lanes) { return (bytes + lanes * 16 - 1) / (lanes * 16); }
-// 16-byte pieces of a slice: as wide as a row, up to 1024 bytes, but 512 workgroups if there can be.
-static int lanes_of(int64_t lists, int64_t bytes) {
+// 16-byte pieces of a slice: as wide as a row, up to 1024 bytes (592 requests' lists of 14 positions of 384 bytes: 54 us, 109 with 128 bytes), but
+// not wider than a cache line where that makes 512 workgroups or saves many rounds (16 requests to 2048 positions: 401 us, 419 with 256 bytes;
+// 32 to 2048 slots of 2048 bytes: 603, 617 with 256 and 686 with 1024; 20 to 533 positions of 512 bytes, four rounds: 180, and 173 as one
+// slice).  Half a line where there are few workgroups: 96 of them 86 us, twice as
+// many 74; 256 and 512, 68 and 85; 128 and 256, 20 and 23.
+static int lanes_of(int64_t lists, int64_t bytes, int64_t budget) {
     int lanes = 64;
-    while (lanes > 4 && (lanes * 8 >= bytes || lists * slices_of(bytes, lanes) * 2 < 512)) lanes /= 2;
+    auto workgroups = [&] { return lists * slices_of(bytes, lanes) * 2; };
+    auto many_rounds = [&] { return budget > 6 * 4 * (1024 / lanes) && workgroups() < 8192; };
+    while (lanes > 8 && (lanes * 8 >= bytes || workgroups() < 512 || many_rounds())) lanes /= 2;
+    if (lanes == 8 && (lanes * 8 >= bytes || workgroups() < 128)) lanes = 4;
     return lanes;
 }
 
@@ -344,7 +351,7 @@ static int check_eviction(const mpv_eviction* p) {
     const int64_t lists = span(0, span(0, p->layers, p->B), p->score_heads);
     if (span(0, p->num_pages, p->page_size) > INT32_MAX || span(0, p->table_width, p->page_size) > INT32_MAX || p->score_width > INT32_MAX ||
         lists > INT32_MAX / 1024 || p->B > (1 << 24) || span(0, lists, p->budget) > (static_cast<int64_t>(1) << 40) ||
-        (lists > 0 && span(0, lists, 2 * slices_of(row_bytes(p), lanes_of(lists, row_bytes(p)))) > kMostWorkgroups - 64) ||
+        (lists > 0 && span(0, lists, 2 * slices_of(row_bytes(p), lanes_of(lists, row_bytes(p), p->budget))) > kMostWorkgroups - 64) ||
         span(0, span(span(span(0, p->num_pages, p->page_stride), p->page_size, p->slot_stride), p->layers, p->cache_layer_stride), 4) == INT64_MAX)
         return MPV_ERR_UNSUPPORTED;
     const int64_t all = p->head_dim | p->slot_stride | p->page_stride | p->cache_layer_stride;
@@ -373,7 +380,7 @@ static void launch_slices(EvictArgs& a, hipStream_t s) {
     else hipLaunchKernelGGL((move_kernel<256, LANES>), grid, dim3(256), 0, s, a);
 }
 static void launch_move(EvictArgs& a, hipStream_t s) {
-    const int lanes = lanes_of(a.lists, a.row_bytes);
+    const int lanes = lanes_of(a.lists, a.row_bytes, a.p.budget);
     if (lanes == 64) launch_slices<64>(a, s);
     else if (lanes == 32) launch_slices<32>(a, s);
     else if (lanes == 16) launch_slices<16>(a, s);
