@@ -1376,7 +1376,11 @@ int by_rows(int64_t rows, const F& f) {
     if (rows <= 64) return f(Chosen<Kernel<KIND, DTYPE, DP, 1, 4>>());
     if constexpr (DP * Elem<DTYPE>::kBytes > 256) {
         // (two groups a wave of such long rows do not fit its registers)
-        return f(Chosen<Kernel<KIND, DTYPE, DP, 1, 8>>());
+        // Behind prefixes in float32 products take the time, so what counts is how few rows stay empty and what shares a compute unit: 64 trees
+        // of 41 nodes, 164 rows, behind prefixes of 512 to 2048 positions 1099 us, 1664 with 128 rows on eight waves; 128 rows 694, 796; with 256
+        // columns 356, 362.  (bfloat16 with 256 columns: 124, 115.)
+        if constexpr (KIND != kTree && DTYPE == MPV_DTYPE_F32) return f(Chosen<Kernel<KIND, DTYPE, DP, 1, 4>>());
+        else return f(Chosen<Kernel<KIND, DTYPE, DP, 1, 8>>());
     } else {
         // as many groups a wave as divide the rows into even blocks: every block reads the tiles again, from the chiplet's cache.  (Two
         // groups for the benchmark's 164 rows: 870 us instead of 613.)

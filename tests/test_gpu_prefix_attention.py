@@ -123,6 +123,14 @@ def test_a_long_prefix_that_many_teams_share():
     Case([-1], 4, 1, 128, torch.bfloat16, [0, 0, 0], [20000], [5, 700, 0], 64, seed=3).check()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,KV,D", [(16, 2, 80), (5, 1, 128), (8, 2, 256), (4, 1, 256)])
+def test_several_row_blocks_of_long_rows(H, KV, D, dtype):
+    """Trees whose rows take several blocks: 328, 205, 164 rows a cache head."""
+    print("[case] prefix row blocks", H, KV, D, dtype, flush=True)
+    Case(TREE41, H, KV, D, dtype, [0, 0, 1], [140, 33], [100, 0, 37], 16, seed=D).check()
+
+
 @pytest.mark.parametrize("order", [[0, 1, 0, 1, 2, 0], [2, 2, 1, 1, 0, 0], [-1, 0, -1, 0, 7, 0], [-1] * 6])
 def test_any_order(order):
     print("[case] order", order, flush=True)
