@@ -4,10 +4,10 @@
 // mpv_attention.h): their rows, blocks of kRows, read the prefix's tiles together.  So a prefix is read once for each block of rows
 // instead of once a tree.
 //
-// What bounds it, 64 single tokens of 32 query heads on 8 cache heads of 128 bfloat16 values behind 8192 positions: 33 us (and 8 for the
-// joining launch) where memory would take 7 and the products as many.  Some 11 us are what comes before a workgroup's first tile and after its
-// last (the trees' numbers, lengths, pages and rows, one load after the other; partial sums); the rest are 16 tiles a workgroup, whose keys
-// and values each of the four waves reads from LDS for 16 rows: behind 16 384 positions 51 us, 430 TFLOP/s for the second half.
+// What bounds it, 64 single tokens of 32 query heads on 8 cache heads of 128 bfloat16 values behind 8192 positions: 31 us (and 9 for the
+// joining launch) where memory would take 7 and the products as many.  What each further 8192 positions
+// take, 17 to 20 us, says that some 11 are what comes before a workgroup's first tile and after its last: the trees' numbers, lengths, pages and
+// rows, one load after the other; partial sums.  In between each of the four waves reads all of a tile's keys and values from LDS for 16 rows.
 
 #include "mpv_prefix.h"
 
