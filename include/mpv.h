@@ -67,7 +67,7 @@
 extern "C" {
 #endif
 
-#define MPV_ABI_VERSION 10
+#define MPV_ABI_VERSION 11
 
 /* limits (larger requests return MPV_ERR_UNSUPPORTED) */
 #define MPV_MAX_NODES    64   /* nodes per tree, root included            */
@@ -394,8 +394,9 @@ int mpv_tree_attention(const mpv_attention* attention, const mpv_attention_buffe
  * and sinks count from the prefix's first position.  Position j of prefix p lies in page prefix_table[p, j / page_size] of the same cache,
  * slot j % page_size (a prefix need not fill its last page; a tree's context begins with a page of its own); prefix_len is taken within
  * [0, prefix_width * page_size].  Trees without a prefix have a prefix_of outside [0, prefixes).
- * A prefix is read once for up to 64 trees that follow each other with the same prefix_of (at indices that agree in b / 64), whatever the
- * others have: order the trees by their prefix; any other order gives the same results and reads more.
+ * Where that takes less time a prefix is read once for up to 64 trees that follow each other with the same prefix_of (at indices that agree
+ * in b / 64), otherwise by every tree for itself: order the trees by their prefix; any other order gives the same results and reads more.
+ * Which of the two follows from sizes alone, prefix_width * page_size among them: give prefix_table no more columns than prefixes have.
  * lse[b,n,h] = ln of the sum of e^s over what node n sees, for query head h; float32, of weights as they are before they are rounded.
  * Without prefixes it is mpv_tree_attention with lse.  Results may differ from that call's in the last bits. */
 typedef struct mpv_prefixed {

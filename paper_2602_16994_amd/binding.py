@@ -866,8 +866,8 @@ class PrefixAttentionResult:
 
 def mpv_prefix_attention(parent, q, tree_k, tree_v, cache_k, cache_v, block_table, context_len, prefix_of=None, prefix_table=None,
                          prefix_len=None, scale=None, window=0, sinks=0, num_nodes=None, tree_parent=None, lse=False, out=None, stream=None):
-    """mpv_tree_attention of trees behind prefixes that requests share, each read once for up to 64 trees that follow each other (see
-    include/mpv.h); returns a PrefixAttentionResult.
+    """mpv_tree_attention of trees behind prefixes that requests share; where that takes less time each is read once for up to 64 trees that
+    follow each other (see include/mpv.h); returns a PrefixAttentionResult.
 
     prefix_of int32 [B]: the prefix of a tree, negative for none; prefix_table int32 [prefixes,prefix_width], pages of the same cache;
     prefix_len int32 [prefixes]; all three None: no prefixes.  lse=True: the logarithms of the sums, too (as mpv_score_positions takes them).
