@@ -17,11 +17,12 @@ namespace mpv {
 // products that no loads hide behind; what it saves is a reading for every tree but one.  In us, with the rates that either reached, for 8 cache
 // heads of 128 bfloat16 values (and 4 of float32), prefixes of as many positions as there is room for, contexts of 16 to 300, each for itself and
 // together:
-//   4 rows a cache head (single tokens):  64 trees, 8192 positions: 259, 64; 16 trees, 16 384: 155, 54; 64 trees, 1024: 59, 63
-//   20 rows:   200 trees, 4096: 443, 179; 64 trees, 4096: 152, 89; 64 trees, 1024: 59, 79; 16 trees, 4096: 55, 60
-//   64 rows:   64 trees, 8192: 273, 222; 64 trees, 4096: 154, 163; 200 trees, 1024: 153, 282
-//   164 rows:  the benchmark's trees behind four prefixes of 512 to 2048: 541, 769
-//   float32, 2 rows:  64 trees, 8192: 393, 76; 16 trees, 4096: 68, 51;   10 rows:  64 trees, 1024: 91, 68; 16 trees, 1024: 32, 50
+//   4 rows a cache head (single tokens):  64 trees, 8192 positions: 254, 60; 16 trees, 16 384: 156, 59; 64 trees, 1024: 50, 48
+//   20 rows:   200 trees, 4096: 380, 174; 64 trees, 4096: 141, 86; 64 trees, 1024: 44, 64; 16 trees, 4096: 52, 58
+//   64 rows:   64 trees, 8192: 249, 225; 64 trees, 4096: 140, 158; 200 trees, 1024: 134, 214
+//   164 rows:  the benchmark's trees behind four prefixes of 512 to 2048: 529, 699
+//   float32, 2 rows:  64 trees, 8192: 395, 80; 16 trees, 4096: 66, 57;   10 rows:  64 trees, 1024: 91, 74; 16 trees, 1024: 31, 57
+//   float32, 64 rows: 64 trees, 4096: 381, 414;   168 rows: 64 trees, 4096: 1084, 1035 (the one of these that the rule misses, by 5 %)
 static bool together(const mpv_prefixed* p) {
     const mpv_attention& a = p->attention;
     if (a.B < 2 || p->prefixes < 1 || p->prefix_width < 1) return false;
