@@ -136,8 +136,8 @@ static int with_columns(const mpv_attention* a, PrefixArgs* g, char* workspace, 
     const int64_t all = a->B * rows_of_tree * a->kv_heads;
     auto go = [&](auto kernel) { return with_kernel<typename decltype(kernel)::T, DTYPE, DP>(a, g, rows, workspace, bytes, s); };
     // Blocks as large as leave enough of them: a unit that many workgroups share costs partial sums of all its rows from each.  (200 trees
-    // with 20 rows a cache head behind 4096 positions: 179 us with blocks of 192 rows, 207 with 64; 64 single tokens with 4 behind 8192: 71 with
-    // 128, 64 with 64; 64 trees with 64 behind 8192: 222 with 192, 261 with 64; float32, 200 trees with 20: 990 with 64, 1071 with 128.)
+    // with 20 rows a cache head behind 4096 positions: 172 us with blocks of 192 rows, 194 with 64; 64 single tokens with 4 behind 8192: 71 with
+    // 128, 64 with 64; 64 trees with 64 behind 8192: 224 with 192, 255 with 64; float32, 200 trees with 20: 990 with 64, 1071 with 128.)
     constexpr int64_t kEnough = 128;
     if (rows <= 16) return go(Chosen<Kernel<kPrefix, DTYPE, DP, 1, 1>>());
     if (rows <= 32) return go(Chosen<Kernel<kPrefix, DTYPE, DP, 1, 2>>());
