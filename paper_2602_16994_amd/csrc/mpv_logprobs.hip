@@ -16,7 +16,8 @@ namespace mpv {
 
 // With c = log2(e) / T, m = max z, S = sum 2^(c (z - m)), A = sum 2^(c (z - m)) (z - m):
 //   log2 p_t = c (z_t - m) - log2 S,    entropy = log2 S - c A / S  (log2 units)
-// (the difference before the factor: c times the lowest float32, a mask, would be -inf, and a row of them empty.)
+// Every sum's reference is m itself, never the rounded product c m: that is off by 2^-24 |c m|, 12.7 nats for a logit of 1e9.  (So the
+// difference comes before the factor; where a round's exponents are c z - fl(c m), the round's sums are brought to m, see sweep_kernel.)
 // S and A of parts are put together by powers of 2, as the statistics of a softmax are.  The best tokens are found through the maxima
 // of segments of 64 tokens: the `top` best lie in the `top` segments with the largest maxima (of equal ones the first), so the row is
 // read once, and those segments again.
@@ -183,21 +184,26 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
             sum *= fade;
         }
         m = now;
-        if (fabsf(shift) < 1e30f && a.c > 1e-30f) {
-            // (the weights are in log2 units here; what lies further than 200 of them below adds nothing, and 0 times -inf would be NaN)
-            const float lowest = base - 200.0f * (1.0f / a.c);
-            float in_log2 = 0.0f;
+        if (fabsf(shift) < 65536.0f && a.c > 1e-30f) {
+            // (exponents c z - shift are one fma each.  Their reference is `shift`, which is c m rounded, while sums are put together by m
+            // itself: `rest` = c m - shift, exact as an fma, at most 2^-9 here, brings a round's sums from one to the other.
+            // What lies further than 200 log2 units below adds nothing, and 0 times -inf would be NaN.)
+            const float lowest = base - 200.0f * (1.0f / a.c), rest = fmaf(base, a.c, -shift);
+            float in_log2 = 0.0f, now_sum = 0.0f;
 #pragma unroll
             for (int j = 0; j < kChunks; ++j)
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     const float d = fmaf(__builtin_amdgcn_fmed3f(v[j][i], lowest, INFINITY), a.c, -shift), e = __builtin_amdgcn_exp2f(d);
-                    sum += e;
+                    now_sum += e;
                     in_log2 = fmaf(e, d, in_log2);
                 }
-            weighted += in_log2 * (1.0f / a.c);
+            const float back = __builtin_amdgcn_exp2f(-rest);
+            sum = fmaf(back, now_sum, sum);
+            weighted = fmaf(back * fmaf(-rest, now_sum, in_log2), 1.0f / a.c, weighted);
         } else {
-            // (masks of the lowest number alone, c times which is -inf; or no number)
+            // (far from zero, where c m is off by too much, the difference comes first; so for masks of the lowest number alone, c times
+            // which is -inf, and for what is no number)
 #pragma unroll
             for (int j = 0; j < kChunks; ++j)
 #pragma unroll
