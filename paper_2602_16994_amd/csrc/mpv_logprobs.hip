@@ -14,8 +14,8 @@
 
 namespace mpv {
 
-// With c = log2(e) / T, m = max z, S = sum 2^(c (z - m)), A = sum 2^(c (z - m)) (z - m):
-//   log2 p_t = c (z_t - m) - log2 S,    entropy = log2 S - c A / S  (log2 units)
+// With c = log2(e) / T, m = max z, d = c (z - m), S = sum 2^d, A = sum 2^d d:
+//   log2 p_t = d_t - log2 S,    entropy = log2 S - A / S  (log2 units)
 // Every sum's reference is m itself, never the rounded product c m: that is off by 2^-24 |c m|, 12.7 nats for a logit of 1e9.  (So the
 // difference comes before the factor; where a round's exponents are c z - fl(c m), the round's sums are brought to m, see sweep_kernel.)
 // S and A of parts are put together by powers of 2, as the statistics of a softmax are.  The best tokens are found through the maxima
@@ -39,6 +39,13 @@ constexpr int kChunks = 4;                 // 16-byte loads of a thread in fligh
 __host__ __device__ constexpr int room_of_candidates(int top) { return top * kSegment > kMany ? top * kSegment : kMany; }
 
 struct PartSums { float m, sum, weighted; int32_t better; };
+
+// S and A from the reference `from` to the larger `to`.  (What fades to nothing may be infinitely far away: 0 times the lowest number is 0.)
+__device__ __forceinline__ void bring(float from, float to, float c, float& sum, float& weighted) {
+    const float apart = (from - to) * c, fade = exp2f(apart);
+    sum *= fade;
+    weighted = fmaf(sum, fmaxf(apart, -FLT_MAX), fade * weighted);
+}
 
 struct RowArgs {
     mpv_logprobs p;
@@ -178,11 +185,7 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
         }
         if (a.p.top > 0 && chunk_of < kChunks && (kWhole || first + chunk_of * kSweepBlock + static_cast<int>(threadIdx.x) < to)) mine_best[first / kLanes] = best;
         const float base = now == -INFINITY ? 0.0f : now, shift = base * a.c;
-        if (m != -INFINITY) {
-            const float fade = exp2f((m - now) * a.c);
-            weighted = fade * (weighted + (m - now) * sum);
-            sum *= fade;
-        }
+        if (m != -INFINITY) bring(m, now, a.c, sum, weighted);
         m = now;
         if (fabsf(shift) < 65536.0f && a.c > 1e-30f) {
             // (exponents c z - shift are one fma each.  Their reference is `shift`, which is c m rounded, while sums are put together by m
@@ -200,7 +203,7 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
                 }
             const float back = __builtin_amdgcn_exp2f(-rest);
             sum = fmaf(back, now_sum, sum);
-            weighted = fmaf(back * fmaf(-rest, now_sum, in_log2), 1.0f / a.c, weighted);
+            weighted = fmaf(back, fmaf(-rest, now_sum, in_log2), weighted);
         } else {
             // (far from zero, where c m is off by too much, the difference comes first; so for masks of the lowest number alone, c times
             // which is -inf, and for what is no number)
@@ -208,7 +211,7 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
             for (int j = 0; j < kChunks; ++j)
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const float d = v[j][i] - base, e = __builtin_amdgcn_exp2f(d * a.c);
+                    const float d = (v[j][i] - base) * a.c, e = __builtin_amdgcn_exp2f(d);
                     sum += e;
                     weighted = fmaf(e, fmaxf(d, -FLT_MAX), weighted);
                 }
@@ -226,11 +229,7 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
     float top = m;
     for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));       // (a lane without a number has no sum, either)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (m != -INFINITY) {
-        const float fade = exp2f((m - top) * a.c);
-        weighted = fade * (weighted + (m - top) * sum);
-        sum *= fade;
-    }
+    if (m != -INFINITY) bring(m, top, a.c, sum, weighted);
     for (int d = 32; d; d >>= 1) {
         sum += __shfl_xor(sum, d);
         weighted += __shfl_xor(weighted, d);
@@ -243,9 +242,9 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
         PartSums s{ms[0], 0.0f, 0.0f, 0};
         for (int w = 1; w < kSweepBlock / 64; ++w) s.m = fmaxf(s.m, ms[w]);
         for (int w = 0; w < kSweepBlock / 64; ++w) {
-            const float apart = ms[w] == -INFINITY ? 0.0f : ms[w] - s.m, fade = exp2f(apart * a.c);
-            s.sum += fade * sums[w];
-            s.weighted += fade * (weights[w] + apart * sums[w]);
+            if (ms[w] != -INFINITY) bring(ms[w], s.m, a.c, sums[w], weights[w]);
+            s.sum += sums[w];
+            s.weighted += weights[w];
             s.better += betters[w];
         }
         a.sums[static_cast<int64_t>(row) * a.parts + part] = s;
@@ -296,10 +295,10 @@ __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
         for (int p = threadIdx.x; p < a.parts; p += 64) m = fmaxf(m, s[p].m);
         for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
         for (int p = threadIdx.x; p < a.parts; p += 64) {
-            const PartSums x = s[p];
-            const float apart = x.m == -INFINITY ? 0.0f : x.m - m, fade = exp2f(apart * a.c);
-            sum += fade * x.sum;
-            weighted += fade * (x.weighted + apart * x.sum);
+            PartSums x = s[p];
+            if (x.m != -INFINITY) bring(x.m, m, a.c, x.sum, x.weighted);
+            sum += x.sum;
+            weighted += x.weighted;
             better += x.better;
         }
         for (int d = 32; d; d >>= 1) {
@@ -311,7 +310,7 @@ __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
             constexpr float kLn2 = 0.69314718055994531f;
             const float log = log2f(sum);
             const bool number = sum == sum;
-            float logprob = -INFINITY, entropy = (log - a.c * (weighted / sum)) * kLn2;
+            float logprob = -INFINITY, entropy = (log - weighted / sum) * kLn2;
             if (!number) logprob = entropy = NAN;
             else if (sum == 0.0f) entropy = 0.0f;
             else if (known) logprob = ((mine - m) * a.c - log) * kLn2;

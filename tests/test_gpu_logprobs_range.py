@@ -135,3 +135,34 @@ def test_large_and_small_numbers_in_turn(dtype):
     logits[1, 2, :30000] += 5000.0
     tokens[0, 2] = 69995
     check(logits.to(dtype), tokens, 1.0, 7)
+
+
+@pytest.mark.parametrize("T", [0.5, 1.0, 3.0])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_masks_of_the_lowest_number(dtype, T):
+    """The lowest number of the type as a mask, with logits of ordinary size beside it: in the same lane, round, wave and part, and in others."""
+    print("[case] logprobs lowest number", dtype, T, flush=True)
+    low = torch.finfo(dtype).min
+    for V in (9, 100, 2048, 8192, 70001):
+        logits, tokens = random(8, 2, V, V)
+        seen = torch.zeros(8, 2, V, dtype=torch.bool, device="cuda")
+        at = torch.arange(V, device="cuda")
+        seen[0, 0, -8:] = True                     # the last tokens
+        seen[0, 1, :8] = True                      # the first
+        seen[1, 0] = at % 997 == 5                 # few, far apart
+        seen[1, 1] = at % 2 == 1
+        seen[2, 0] = at >= V // 2
+        seen[2, 1] = at < V // 2
+        seen[3, 0] = at // 64 % 3 == 2             # segments
+        seen[3, 1] = at // 8 % 2 == 1              # a lane's loads
+        seen[4, 0] = at // 2048 % 2 == 1           # rounds of a lane
+        seen[4, 1] = at // 512 % 5 == 3            # waves
+        seen[5, 0] = at // 32768 % 2 == 1          # parts
+        seen[5, 1] = at // 8192 % 2 == 1
+        seen[6, 0, V // 3] = True                  # one alone
+        seen[6, 1] = at % 64 == 63
+        seen[7, 0] = at != V // 2                  # all but one
+        seen[7, 1] = at >= V - 1
+        seen[:, :, 5] |= ~seen.any(dim=2)
+        logits = torch.where(seen, logits, low).to(dtype)
+        check(logits, seen.int().argmax(dim=2).to(torch.int32), T, 1)
