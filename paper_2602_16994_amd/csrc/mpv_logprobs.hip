@@ -38,11 +38,14 @@ constexpr int kChunks = 4;                 // 16-byte loads of a thread in fligh
 // Tokens that there has to be room for: `top` whole segments, where they are more.
 __host__ __device__ constexpr int room_of_candidates(int top) { return top * kSegment > kMany ? top * kSegment : kMany; }
 
+// c (z - m).  (Halves: the difference of two numbers of opposite sign may be larger than any.)
+__device__ __forceinline__ float apart_of(float z, float m, float c2) { return (0.5f * z - 0.5f * m) * c2; }
+
 struct PartSums { float m, sum, weighted; int32_t better; };
 
 // S and A from the reference `from` to the larger `to`.  (What fades to nothing may be infinitely far away: 0 times the lowest number is 0.)
-__device__ __forceinline__ void bring(float from, float to, float c, float& sum, float& weighted) {
-    const float apart = (from - to) * c, fade = exp2f(apart);
+__device__ __forceinline__ void bring(float from, float to, float c2, float& sum, float& weighted) {
+    const float apart = apart_of(from, to, c2), fade = exp2f(apart);
     sum *= fade;
     weighted = fmaf(sum, fmaxf(apart, -FLT_MAX), fade * weighted);
 }
@@ -52,7 +55,7 @@ struct RowArgs {
     mpv_logprob_buffers b;
     int rows, width, parts, part;          // output rows in all and of a tree; parts of a row, segments of each
     int segments;
-    float c;                               // log2(e) / T
+    float c2, twice;                       // 2 log2(e) / T, 2 / T
     PartSums* sums;                        // [rows][parts]
     float* best;                           // [rows][segments] (top > 0)
 };
@@ -126,6 +129,7 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
     const T* z = static_cast<const T*>(a.b.logits) + r.at;
     const int V = a.p.V, whole = V / N;
     const bool known = r.token >= 0 && r.token < V;
+    const float c = 0.5f * a.c2;
     const float mine = known ? logit(z[r.token]) : INFINITY;
     const int from = part * a.part * kLanes, to = min(from + a.part * kLanes, a.segments * kLanes);      // chunks of N
     float m = -INFINITY, sum = 0.0f, weighted = 0.0f;
@@ -184,20 +188,20 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
             asm volatile("" : "+s"(better));                       // (counted here: the ballots would all wait in scalar registers)
         }
         if (a.p.top > 0 && chunk_of < kChunks && (kWhole || first + chunk_of * kSweepBlock + static_cast<int>(threadIdx.x) < to)) mine_best[first / kLanes] = best;
-        const float base = now == -INFINITY ? 0.0f : now, shift = base * a.c;
-        if (m != -INFINITY) bring(m, now, a.c, sum, weighted);
+        const float base = now == -INFINITY ? 0.0f : now, shift = base * c;
+        if (m != -INFINITY) bring(m, now, a.c2, sum, weighted);
         m = now;
-        if (fabsf(shift) < 65536.0f && a.c > 1e-30f) {
+        if (fabsf(shift) < 65536.0f && c > 1e-30f) {
             // (exponents c z - shift are one fma each.  Their reference is `shift`, which is c m rounded, while sums are put together by m
             // itself: `rest` = c m - shift, exact as an fma, at most 2^-9 here, brings a round's sums from one to the other.
             // What lies further than 200 log2 units below adds nothing, and 0 times -inf would be NaN.)
-            const float lowest = base - 200.0f * (1.0f / a.c), rest = fmaf(base, a.c, -shift);
+            const float lowest = base - 200.0f * (1.0f / c), rest = fmaf(base, c, -shift);
             float in_log2 = 0.0f, now_sum = 0.0f;
 #pragma unroll
             for (int j = 0; j < kChunks; ++j)
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const float d = fmaf(__builtin_amdgcn_fmed3f(v[j][i], lowest, INFINITY), a.c, -shift), e = __builtin_amdgcn_exp2f(d);
+                    const float d = fmaf(__builtin_amdgcn_fmed3f(v[j][i], lowest, INFINITY), c, -shift), e = __builtin_amdgcn_exp2f(d);
                     now_sum += e;
                     in_log2 = fmaf(e, d, in_log2);
                 }
@@ -211,7 +215,7 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
             for (int j = 0; j < kChunks; ++j)
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const float d = (v[j][i] - base) * a.c, e = __builtin_amdgcn_exp2f(d);
+                    const float d = apart_of(v[j][i], base, a.c2), e = __builtin_amdgcn_exp2f(d);
                     sum += e;
                     weighted = fmaf(e, fmaxf(d, -FLT_MAX), weighted);
                 }
@@ -229,7 +233,7 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
     float top = m;
     for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));       // (a lane without a number has no sum, either)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (m != -INFINITY) bring(m, top, a.c, sum, weighted);
+    if (m != -INFINITY) bring(m, top, a.c2, sum, weighted);
     for (int d = 32; d; d >>= 1) {
         sum += __shfl_xor(sum, d);
         weighted += __shfl_xor(weighted, d);
@@ -242,7 +246,7 @@ __global__ __launch_bounds__(kSweepBlock) void sweep_kernel(RowArgs a) {
         PartSums s{ms[0], 0.0f, 0.0f, 0};
         for (int w = 1; w < kSweepBlock / 64; ++w) s.m = fmaxf(s.m, ms[w]);
         for (int w = 0; w < kSweepBlock / 64; ++w) {
-            if (ms[w] != -INFINITY) bring(ms[w], s.m, a.c, sums[w], weights[w]);
+            if (ms[w] != -INFINITY) bring(ms[w], s.m, a.c2, sums[w], weights[w]);
             s.sum += sums[w];
             s.weighted += weights[w];
             s.better += betters[w];
@@ -286,6 +290,9 @@ __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
         segment[i] = top > 0 && s < a.segments ? best[s] : -INFINITY;
     }
     const float mine = known ? logit(z[r.token]) : 0.0f;
+    // (the turn to natural logarithms before the product: the lowest number's log probability at T = 1 is the lowest number)
+    constexpr float kLn2 = 0.69314718055994531f;
+    auto logprob_of = [&](float z, float m, float log) { return fmaf(log, -kLn2, apart_of(z, m, a.twice)); };
     __shared__ float shared_m, shared_log, shared_sum;
     if (threadIdx.x < 64) {
         // (all lanes have parts: their number is not limited by the wave)
@@ -296,7 +303,7 @@ __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
         for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
         for (int p = threadIdx.x; p < a.parts; p += 64) {
             PartSums x = s[p];
-            if (x.m != -INFINITY) bring(x.m, m, a.c, x.sum, x.weighted);
+            if (x.m != -INFINITY) bring(x.m, m, a.c2, x.sum, x.weighted);
             sum += x.sum;
             weighted += x.weighted;
             better += x.better;
@@ -307,13 +314,12 @@ __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
             better += __shfl_xor(better, d);
         }
         if (threadIdx.x == 0) {
-            constexpr float kLn2 = 0.69314718055994531f;
             const float log = log2f(sum);
             const bool number = sum == sum;
             float logprob = -INFINITY, entropy = (log - weighted / sum) * kLn2;
             if (!number) logprob = entropy = NAN;
             else if (sum == 0.0f) entropy = 0.0f;
-            else if (known) logprob = ((mine - m) * a.c - log) * kLn2;
+            else if (known) logprob = logprob_of(mine, m, log);
             a.b.logprob[row] = logprob;
             a.b.entropy[row] = entropy;
             a.b.rank[row] = known && number ? better + 1 : -1;
@@ -433,7 +439,7 @@ __global__ __launch_bounds__(kFinishBlock) void finish_kernel(RowArgs a) {
         for (int j = 0; j < count; ++j) place += candidates[j] > k;
         if (place < top) {
             tokens[place] = static_cast<int>(~static_cast<uint32_t>(k));
-            logprobs[place] = ((from_order(static_cast<uint32_t>(k >> 32)) - m) * a.c - log) * 0.69314718055994531f;
+            logprobs[place] = logprob_of(from_order(static_cast<uint32_t>(k >> 32)), m, log);
         }
     }
     for (int i = count + threadIdx.x; i < top; i += kFinishBlock) { tokens[i] = -1; logprobs[i] = -INFINITY; }
@@ -519,7 +525,8 @@ int mpv_token_logprobs(const mpv_logprobs* logprobs, const mpv_logprob_buffers* 
     a.b = *buf;
     const mpv::LogprobRoom room = mpv::room_of(logprobs, &a);
     if (!workspace || !mpv::aligned(workspace, 256) || workspace_bytes < room.sums + room.best) return MPV_ERR_WORKSPACE;
-    a.c = static_cast<float>(1.4426950408889634 / static_cast<double>(logprobs->temperature));
+    a.c2 = static_cast<float>(2.0 * 1.4426950408889634 / static_cast<double>(logprobs->temperature));
+    a.twice = static_cast<float>(2.0 / static_cast<double>(logprobs->temperature));
     a.sums = static_cast<mpv::PartSums*>(workspace);
     a.best = reinterpret_cast<float*>(static_cast<char*>(workspace) + room.sums);
     hipStream_t s = static_cast<hipStream_t>(hip_stream);

@@ -166,3 +166,29 @@ def test_masks_of_the_lowest_number(dtype, T):
         seen[:, :, 5] |= ~seen.any(dim=2)
         logits = torch.where(seen, logits, low).to(dtype)
         check(logits, seen.int().argmax(dim=2).to(torch.int32), T, 1)
+
+
+@pytest.mark.parametrize("T", [0.5, 1.0, 3.0, 1e30, 3e38])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_log_probabilities_of_masked_tokens(dtype, T):
+    """A token with the lowest number has a log probability, as long as float32 holds it; with a high temperature it is not small."""
+    print("[case] logprobs of masked tokens", dtype, T, flush=True)
+    low, high = torch.finfo(dtype).min, torch.finfo(dtype).max
+    logits, tokens = random(2, 3, 5000, 60)
+    logits[0, 0, 20:] = low
+    logits[0, 1, :4990] = low
+    logits[0, 2] = low
+    logits[1, 0, ::2] = low
+    logits[1, 1, ::3], logits[1, 1, 1::3] = low, high
+    logits[1, 2, 17], logits[1, 2, 18] = low, high
+    tokens[0, 0], tokens[0, 1], tokens[0, 2], tokens[1, 0], tokens[1, 1], tokens[1, 2] = 30, 7, 4999, 2, 3, 17
+    check(logits.to(dtype), tokens, T, 40)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_the_lowest_temperature(dtype):
+    print("[case] logprobs lowest temperature", dtype, flush=True)
+    logits, tokens = random(2, 2, 3000, 61)
+    logits[0] *= 1e-37
+    tokens[1, 0] = int(logits[1, 0].argmax())
+    check(logits.to(dtype), tokens, 2.0 ** -126, 5)
