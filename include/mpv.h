@@ -617,7 +617,7 @@ typedef struct mpv_logprobs {
     int32_t top;                  /* 0 .. MPV_MAX_TOP                                                         */
     int32_t paths;                /* 0 or 1                                                                   */
     int32_t max_depth;            /* paths: row width of path_nodes and tokens, >= 1                          */
-    float   temperature;          /* finite, > 0                                                              */
+    float   temperature;          /* finite, >= 2^-126 (a normal number)                                      */
     int64_t stride;               /* elements from a logit row to the next (>= V); requests follow each other */
 } mpv_logprobs;
 

@@ -1238,7 +1238,7 @@ def mpv_token_logprobs(logits, tokens, temperature=1.0, top=0, accept_len=None, 
     """Log probabilities of given tokens, entropies and the `top` most likely tokens (see include/mpv.h), enqueued on the current (or
     given) torch stream; returns a LogprobsResult.
 
-    logits [B,N,V] (float32, bfloat16 or float16; rows may lie further apart than V).  With accept_len int32 [B], path_nodes int32
+    logits [B,N,V] (float32, bfloat16 or float16; rows may lie further apart than V); temperature at least 2^-126.  With accept_len int32 [B], path_nodes int32
     [B,max_depth] and bonus_token int32 [B], as a verification writes them: of what it emitted, `tokens` its path_tokens int32 [B,max_depth], and
     the results have max_depth + 1 rows.  Without: tokens int32 [B,N], one for each row, num_nodes int32 [B] rows of each request.
     `out` may be a previous LogprobsResult whose buffers are reused."""

@@ -463,7 +463,8 @@ static int check_logprobs(const mpv_logprobs* p) {
     if (p->B < 0 || p->N < 1 || p->V < 1 || p->top < 0 || p->stride < p->V || (p->paths != 0 && p->paths != 1) || (p->paths && p->max_depth < 1))
         return MPV_ERR_BAD_SHAPE;
     if (!known_dtype(p->dtype)) return MPV_ERR_BAD_DTYPE;
-    if (!std::isfinite(p->temperature) || !(p->temperature > 0.0f)) return MPV_ERR_BAD_TEMPERATURE;
+    // (of smaller ones the factors log2(e) / T and 1 / T are infinite in float32)
+    if (!std::isfinite(p->temperature) || !(p->temperature >= FLT_MIN)) return MPV_ERR_BAD_TEMPERATURE;
     if (p->V > MPV_MAX_VOCAB || p->top > MPV_MAX_TOP) return MPV_ERR_UNSUPPORTED;
     const int64_t width = p->paths ? static_cast<int64_t>(p->max_depth) + 1 : p->N, rows = width * p->B;
     int parts = 1, part;
