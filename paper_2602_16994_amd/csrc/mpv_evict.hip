@@ -22,6 +22,8 @@
 namespace mpv {
 
 constexpr int kSelectBlock = 512;          // of the long lists
+// Positions that are kept, or in a row of the block table: loops over them take 32 bits, and the last step of one goes beyond them.
+constexpr int64_t kMostPositions = INT32_MAX - (1 << 16);
 
 struct EvictArgs {
     mpv_eviction p;
@@ -38,6 +40,9 @@ struct EvictArgs {
 };
 
 __device__ __forceinline__ int context_of(const EvictArgs& a, int b) { return min(max(a.b.context_len[b], 0), a.p.table_width * a.p.page_size); }
+
+// Pages of so many positions.  (Their sum with a page's may be more than 32 bits hold.)
+__device__ __forceinline__ int pages_of(const EvictArgs& a, int positions) { return positions > 0 ? a.by_page.of(positions - 1) + 1 : 0; }
 
 // Order of the scores; NaN comes last, both zeros are the same.
 __device__ __forceinline__ uint32_t score_order(float z) {
@@ -73,11 +78,11 @@ __device__ __forceinline__ void plan_pages(const EvictArgs& a) {
     __shared__ int part[16][2];
     int64_t count = min(max(a.b.free_count[0], 0), p.num_pages);
     if (threadIdx.x == 0) a.plan->free = static_cast<int32_t>(count);
-    const int have = (p.budget + p.page_size - 1) / p.page_size;
+    const int have = pages_of(a, p.budget);
     for (int base = 0; base < p.B; base += blockDim.x) {
         const int b = base + threadIdx.x;
         const int context = b < p.B ? context_of(a, b) : 0;
-        const int pages = context > p.trigger ? (context + p.page_size - 1) / p.page_size - have : 0;
+        const int pages = context > p.trigger ? pages_of(a, context) - have : 0;
         int at[2] = {pages, 0}, total[2];
         before(at, total, part);
         if (b < p.B) {
@@ -90,7 +95,7 @@ __device__ __forceinline__ void plan_pages(const EvictArgs& a) {
 }
 __device__ __forceinline__ void return_pages(const EvictArgs& a) {
     const mpv_eviction& p = a.p;
-    const int have = (p.budget + p.page_size - 1) / p.page_size;
+    const int have = pages_of(a, p.budget);
     const int64_t free = a.plan->free, end = min(a.first_page[p.B], static_cast<int64_t>(p.num_pages));
     const int64_t step = static_cast<int64_t>(a.returning) * blockDim.x;
     const int64_t mine = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
@@ -350,7 +355,8 @@ static int check_eviction(const mpv_eviction* p) {
     const int64_t row = static_cast<int64_t>(p->kv_heads) * p->head_dim;
     if (p->slot_stride < row || p->page_stride < 0 || p->cache_layer_stride < 0) return MPV_ERR_BAD_SHAPE;
     const int64_t lists = span(0, span(0, p->layers, p->B), p->score_heads);
-    if (span(0, p->num_pages, p->page_size) > INT32_MAX || span(0, p->table_width, p->page_size) > INT32_MAX || p->score_width > INT32_MAX ||
+    if (span(0, p->num_pages, p->page_size) > INT32_MAX || span(0, p->table_width, p->page_size) > kMostPositions || p->budget > kMostPositions ||
+        p->score_width > INT32_MAX ||
         lists > INT32_MAX / 1024 || p->B > (1 << 24) || span(0, lists, p->budget) > (static_cast<int64_t>(1) << 40) ||
         (lists > 0 && span(0, lists, 2 * slices_of(row_bytes(p), lanes_of(lists, row_bytes(p), p->budget))) > kMostWorkgroups - 64) ||
         span(0, span(span(span(0, p->num_pages, p->page_stride), p->page_size, p->slot_stride), p->layers, p->cache_layer_stride), 4) == INT64_MAX)
