@@ -330,6 +330,8 @@ static int64_t row_bytes(const mpv_eviction* p) {
     return static_cast<int64_t>(p->score_heads == 1 ? p->kv_heads : 1) * p->head_dim * elem_bytes(p->dtype);
 }
 static int64_t slices_of(int64_t bytes, int lanes) { return (bytes + lanes * 16 - 1) / (lanes * 16); }
+// Workgroups that move rows.
+static int64_t movers_of(int64_t lists, int64_t bytes, int lanes) { return lists * slices_of(bytes, lanes) * 2; }
 // 16-byte pieces of a slice: as wide as a row, up to 1024 bytes (592 requests' lists of 14 positions of 384 bytes: 54 us, 109 with 128 bytes), but
 // not wider than a cache line where that makes 512 workgroups or saves many rounds (16 requests to 2048 positions: 401 us, 419 with 256 bytes;
 // 32 to 2048 slots of 2048 bytes: 603, 617 with 256 and 686 with 1024; 20 to 533 positions of 512 bytes, four rounds: 180, and 173 as one
@@ -337,11 +339,20 @@ static int64_t slices_of(int64_t bytes, int lanes) { return (bytes + lanes * 16 
 // many 74; 256 and 512, 68 and 85; 128 and 256, 20 and 23.
 static int lanes_of(int64_t lists, int64_t bytes, int64_t budget) {
     int lanes = 64;
-    auto workgroups = [&] { return lists * slices_of(bytes, lanes) * 2; };
+    auto workgroups = [&] { return movers_of(lists, bytes, lanes); };
     auto many_rounds = [&] { return budget > 6 * 4 * (1024 / lanes) && workgroups() < 8192; };
     while (lanes > 8 && (lanes * 8 >= bytes || workgroups() < 512 || many_rounds())) lanes /= 2;
     if (lanes == 8 && (lanes * 8 >= bytes || workgroups() < 128)) lanes = 4;
     return lanes;
+}
+
+constexpr int kMostReturning = 64;         // workgroups that return pages, at most
+// Many rounds of 256 threads (or few lists): 1024 threads, more rows a round, unless that is more threads than a launch can have.  (16 requests to 2048
+// positions: 433 us with 1024 threads, 491 with 256, which take 16 rounds; 42 requests to 12 108 slots of 1024 bytes: 232, 407; 41 requests
+// to 48: 60, 44.)
+static bool large_workgroups(int64_t lists, int64_t bytes, int lanes, int64_t budget) {
+    const int64_t workgroups = movers_of(lists, bytes, lanes), round = 256 / lanes * 8;
+    return (budget > 4 * round || (workgroups < 512 && budget > round)) && workgroups + kMostReturning <= kMostWorkgroups / 4;
 }
 
 static int check_eviction(const mpv_eviction* p) {
@@ -358,7 +369,7 @@ static int check_eviction(const mpv_eviction* p) {
     if (span(0, p->num_pages, p->page_size) > INT32_MAX || span(0, p->table_width, p->page_size) > kMostPositions || p->budget > kMostPositions ||
         p->score_width > INT32_MAX ||
         lists > INT32_MAX / 1024 || p->B > (1 << 24) || span(0, lists, p->budget) > (static_cast<int64_t>(1) << 40) ||
-        (lists > 0 && span(0, lists, 2 * slices_of(row_bytes(p), lanes_of(lists, row_bytes(p), p->budget))) > kMostWorkgroups - 64) ||
+        movers_of(lists, row_bytes(p), lanes_of(lists, row_bytes(p), p->budget)) > kMostWorkgroups - kMostReturning ||
         span(0, span(span(span(0, p->num_pages, p->page_stride), p->page_size, p->slot_stride), p->layers, p->cache_layer_stride), 4) == INT64_MAX)
         return MPV_ERR_UNSUPPORTED;
     const int64_t all = p->head_dim | p->slot_stride | p->page_stride | p->cache_layer_stride;
@@ -378,12 +389,8 @@ static void launch_select(const EvictArgs& a, hipStream_t s) {
 template <int LANES>
 static void launch_slices(EvictArgs& a, hipStream_t s) {
     a.slices = static_cast<int>(slices_of(a.row_bytes, LANES));
-    const int64_t workgroups = static_cast<int64_t>(a.lists) * a.slices * 2;
-    const dim3 grid(static_cast<unsigned>(workgroups + a.returning));
-    // Many rounds of 256 threads (or few lists): more rows a round.  (16 requests to 2048 positions: 433 us with 1024 threads, 491 with 256, which
-    // take 16 rounds; 42 requests to 12 108 slots of 1024 bytes: 232, 407; 41 requests to 48: 60, 44.)
-    constexpr int kRound = 256 / LANES * 8;
-    if (a.p.budget > 4 * kRound || (workgroups < 512 && a.p.budget > kRound)) hipLaunchKernelGGL((move_kernel<1024, LANES>), grid, dim3(1024), 0, s, a);
+    const dim3 grid(static_cast<unsigned>(movers_of(a.lists, a.row_bytes, LANES) + a.returning));
+    if (large_workgroups(a.lists, a.row_bytes, LANES, a.p.budget)) hipLaunchKernelGGL((move_kernel<1024, LANES>), grid, dim3(1024), 0, s, a);
     else hipLaunchKernelGGL((move_kernel<256, LANES>), grid, dim3(256), 0, s, a);
 }
 static void launch_move(EvictArgs& a, hipStream_t s) {
@@ -449,7 +456,7 @@ int mpv_evict_positions(const mpv_eviction* eviction, const mpv_eviction_buffers
     a.first_page = reinterpret_cast<int64_t*>(at += room.plan);
     a.lengths = reinterpret_cast<int32_t*>(at += room.pages);
     // (eight pages a thread, if every request had all that it has room for)
-    a.returning = static_cast<int>(std::min<int64_t>(64, 1 + static_cast<int64_t>(p->B) * p->table_width / 2048));
+    a.returning = static_cast<int>(std::min<int64_t>(mpv::kMostReturning, 1 + static_cast<int64_t>(p->B) * p->table_width / 2048));
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();
     mpv::launch_select(a, s);

@@ -125,3 +125,17 @@ def test_cache_heads_of_many_layers(dtype):
     """A head's part of a row is a slice of its own; rows of 512 bytes (float32) of 256 lists."""
     print("[case] evict heads", dtype, flush=True)
     Case(8, 4, 128, dtype, [300, 100, 257, 299, 30, 280, 260, 300], 16, 19, True, seed=9).check(100, 120, 4, 20, inplace=True)
+
+
+def test_more_lists_than_workgroups_of_1024_threads():
+    """80 layers of 20 000 requests, whole slots of 2048 bytes, a budget that takes 1024 threads a workgroup where a launch can have as many: none is cut."""
+    print("[case] evict many lists", flush=True)
+    layers, B, budget = 80, 20000, 300
+    cache = torch.zeros(layers, 1, 1, 8, 128, dtype=torch.bfloat16, device="cuda")
+    table = torch.zeros(B, 1, dtype=torch.int32, device="cuda")
+    context = torch.ones(B, dtype=torch.int32, device="cuda")
+    scores = torch.arange(layers * B, dtype=torch.float32, device="cuda").view(layers, B, 1, 1)
+    free, count = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    r = mpv.mpv_evict_positions(cache, cache.clone(), table, context, scores, free, count, budget)
+    assert torch.equal(r.context_len, context) and int(r.free_count) == 0 and torch.equal(r.scores, scores)
+    assert int(r.kept.amax()) == -1 and int(r.kept.amin()) == -1
