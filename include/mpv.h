@@ -566,8 +566,8 @@ int mpv_score_positions(const mpv_scores* scores, const mpv_score_buffers* buffe
  * and of the others those with the largest scores, of equal ones the first (NaN counts as less than any number).  They move forward
  * in order: position i of the cache holds what position kept[i] held, keys and values of all layers; each score head keeps positions of its
  * own (score_heads = kv_heads), or whole slots move (1).  A window of the attention counts positions as they are then.  The pages behind
- * ceil(budget / page_size) go to the end of the list of free pages (in request order, ascending position; what num_pages entries do not
- * hold is dropped); the block table is not changed.  Other requests are left as they are.
+ * ceil(budget / page_size) go to the end of the list of free pages (in request order, ascending position; entries outside [0,num_pages) are
+ * left out, what num_pages entries do not hold is dropped); the block table is not changed.  Other requests are left as they are.
  * A row of which either slot lies in a page outside [0,num_pages) does not move.  No page of a request that is cut may appear twice, in its own row or
  * in another's.  scores_out may be scores; otherwise what lies behind a request's positions is left as it was.  kept is -1 throughout for a
  * request that is not cut. */

@@ -61,7 +61,7 @@ def evict_positions(cache_k, cache_v, table, context, scores, free, free_count, 
         if L <= trigger:
             new[:, b, :, :L] = scores[:, b, :, :L]
             continue
-        free += [int(x) for x in table[b, -(-budget // size):-(-L // size)]]
+        free += [int(x) for x in table[b, -(-budget // size):-(-L // size)] if 0 <= x < pages]
         for layer in range(layers):
             for g in range(G):
                 row = scores[layer, b, g]

@@ -24,6 +24,7 @@ namespace mpv {
 constexpr int kSelectBlock = 512;          // of the long lists
 // Positions that are kept, or in a row of the block table: loops over them take 32 bits, and the last step of one goes beyond them.
 constexpr int64_t kMostPositions = INT32_MAX - (1 << 16);
+constexpr int kMostReturning = 64;         // workgroups that return pages, at most
 
 struct EvictArgs {
     mpv_eviction p;
@@ -33,10 +34,13 @@ struct EvictArgs {
     Divisor by_page;
     int32_t* slots;                        // [lists][budget] slot of a kept row, -1: none
     int32_t* moved;                        // [lists] first row that moves (budget: none does)
-    struct Plan { int32_t free; } * plan;  // pages that were free
+    struct Plan {
+        int32_t free;                      // pages that were free
+        int32_t strange[kMostReturning];   // whether a part of the tables' entries behind the kept pages holds one that is no page
+    } * plan;
     int64_t* first_page;                   // [B+1] where a request's pages go in the list of free ones
     int32_t* lengths;                      // [B] new ones
-    int returning;                         // workgroups that return pages
+    int returning;                         // workgroups that return pages (and that look at them before)
 };
 
 __device__ __forceinline__ int context_of(const EvictArgs& a, int b) { return min(max(a.b.context_len[b], 0), a.p.table_width * a.p.page_size); }
@@ -93,20 +97,71 @@ __device__ __forceinline__ void plan_pages(const EvictArgs& a) {
     }
     if (threadIdx.x == 0) a.first_page[p.B] = count;
 }
+// Part `number` of `returning` of the tables' entries: whether one that is to be returned is no page.
+__device__ __forceinline__ void look_at_pages(const EvictArgs& a, int number) {
+    const mpv_eviction& p = a.p;
+    const int have = pages_of(a, p.budget), step = a.returning * static_cast<int>(blockDim.x);
+    const int rows = step / max(p.table_width, 1), columns = step - rows * p.table_width;
+    const int first = number * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x);
+    bool strange = false;
+    if (p.table_width > 0)
+        for (int b = first / p.table_width, column = first % p.table_width; b < p.B;) {
+            const int context = context_of(a, b);
+            if (context > p.trigger && column >= have && column < pages_of(a, context)) {
+                const int page = a.b.block_table[static_cast<int64_t>(b) * p.table_width + column];
+                strange = strange || page < 0 || page >= p.num_pages;
+            }
+            b += rows;
+            column += columns;
+            if (column >= p.table_width) {
+                column -= p.table_width;
+                ++b;
+            }
+        }
+    const bool any = __syncthreads_or(strange);
+    if (threadIdx.x == 0) a.plan->strange[number] = any;
+}
+// The first workgroups of a launch that selects have the pages.
+__device__ __forceinline__ bool plan(const EvictArgs& a) {
+    if (blockIdx.x > static_cast<unsigned>(a.returning)) return false;
+    if (blockIdx.x == 0) plan_pages(a);
+    else look_at_pages(a, blockIdx.x - 1);
+    return true;
+}
+// The entry that has a place in the list (pages and what is none together).
+__device__ __forceinline__ int page_at(const EvictArgs& a, int64_t place, int have) {
+    int low = 0, high = a.p.B;                                     // the last request whose pages begin at or before the place
+    while (high - low > 1) {
+        const int middle = (low + high) >> 1;
+        if (a.first_page[middle] <= place) low = middle;
+        else high = middle;
+    }
+    return a.b.block_table[static_cast<int64_t>(low) * a.p.table_width + have + static_cast<int>(place - a.first_page[low])];
+}
 __device__ __forceinline__ void return_pages(const EvictArgs& a) {
     const mpv_eviction& p = a.p;
     const int have = pages_of(a, p.budget);
-    const int64_t free = a.plan->free, end = min(a.first_page[p.B], static_cast<int64_t>(p.num_pages));
+    const int64_t free = a.plan->free, all = a.first_page[p.B];
     const int64_t step = static_cast<int64_t>(a.returning) * blockDim.x;
     const int64_t mine = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
-    for (int64_t place = free + mine; place < end; place += step) {
-        int low = 0, high = p.B;                                   // the last request whose pages begin at or before the place
-        while (high - low > 1) {
-            const int middle = (low + high) >> 1;
-            if (a.first_page[middle] <= place) low = middle;
-            else high = middle;
+    const int lane = threadIdx.x & 63;
+    int64_t end = min(all, static_cast<int64_t>(p.num_pages));
+    if (!__ballot(lane < a.returning && a.plan->strange[lane])) {
+        for (int64_t place = free + mine; place < end; place += step) a.b.free_pages[place] = page_at(a, place, have);
+    } else if (blockIdx.x == 0) {
+        // some are no pages (which nobody should have to hurry with): one workgroup leaves them out
+        __shared__ int part[16][2];
+        int64_t to = free;
+        for (int64_t base = free; base < all; base += blockDim.x) {
+            const int64_t place = base + threadIdx.x;
+            const int page = place < all ? page_at(a, place, have) : -1;
+            const bool real = page >= 0 && page < p.num_pages;
+            int at[2] = {real, 0}, total[2];
+            before(at, total, part);
+            if (real && to + at[0] < p.num_pages) a.b.free_pages[to + at[0]] = page;
+            to += total[0];
         }
-        a.b.free_pages[place] = a.b.block_table[static_cast<int64_t>(low) * p.table_width + have + static_cast<int>(place - a.first_page[low])];
+        end = min(to, static_cast<int64_t>(p.num_pages));
     }
     for (int64_t b = mine; b < p.B; b += step) a.b.context_len_out[b] = a.lengths[b];
     if (mine == 0) a.b.free_count_out[0] = static_cast<int32_t>(end);
@@ -132,8 +187,8 @@ __global__ __launch_bounds__(BLOCK) void select_kernel(EvictArgs a) {
     (void)table;
     __shared__ int stay;
     const mpv_eviction& p = a.p;
-    if (blockIdx.x == 0) return plan_pages(a);
-    const int list = blockIdx.x - 1, b = list / p.score_heads % p.B;
+    if (plan(a)) return;
+    const int list = blockIdx.x - 1 - a.returning, b = list / p.score_heads % p.B;
     const int context = context_of(a, b);
     if (context <= p.trigger) return leave(a, list, context);
     const float* scores = a.b.scores + static_cast<int64_t>(list) * p.score_width;
@@ -176,8 +231,8 @@ __global__ __launch_bounds__(BLOCK) void select_kernel(EvictArgs a) {
 // The same for lists of any length, read again for each byte of the limit.
 __global__ __launch_bounds__(kSelectBlock) void select_long_kernel(EvictArgs a) {
     const mpv_eviction& p = a.p;
-    if (blockIdx.x == 0) return plan_pages(a);
-    const int list = blockIdx.x - 1, b = list / p.score_heads % p.B;
+    if (plan(a)) return;
+    const int list = blockIdx.x - 1 - a.returning, b = list / p.score_heads % p.B;
     const int context = context_of(a, b);
     const float* scores = a.b.scores + static_cast<int64_t>(list) * p.score_width;
     float* out = a.b.scores_out + static_cast<int64_t>(list) * p.score_width;
@@ -346,7 +401,6 @@ static int lanes_of(int64_t lists, int64_t bytes, int64_t budget) {
     return lanes;
 }
 
-constexpr int kMostReturning = 64;         // workgroups that return pages, at most
 // Many rounds of 256 threads (or few lists): 1024 threads, more rows a round, unless that is more threads than a launch can have.  (16 requests to 2048
 // positions: 433 us with 1024 threads, 491 with 256, which take 16 rounds; 42 requests to 12 108 slots of 1024 bytes: 232, 407; 41 requests
 // to 48: 60, 44.)
@@ -379,7 +433,7 @@ static int check_eviction(const mpv_eviction* p) {
 
 static void launch_select(const EvictArgs& a, hipStream_t s) {
     const int64_t room = static_cast<int64_t>(a.p.table_width) * a.p.page_size;
-    const dim3 lists(static_cast<unsigned>(a.lists) + 1);
+    const dim3 lists(static_cast<unsigned>(a.lists) + 1 + a.returning);
     if (room <= 64 * 16) hipLaunchKernelGGL((select_kernel<64, 16>), lists, dim3(64), 0, s, a);
     else if (room <= 512 * 16) hipLaunchKernelGGL((select_kernel<512, 16>), lists, dim3(512), 0, s, a);
     else if (room <= 1024 * 32) hipLaunchKernelGGL((select_kernel<1024, 32>), lists, dim3(1024), 0, s, a);
@@ -410,7 +464,7 @@ struct EvictRoom {
 static EvictRoom room_of(const mpv_eviction* p) {
     auto whole = [](size_t bytes) { return (bytes + 255) / 256 * 256; };
     const size_t lists = static_cast<size_t>(p->layers) * p->B * p->score_heads;
-    return {whole(lists * p->budget * sizeof(int32_t)), whole(lists * sizeof(int32_t)), 256, whole((static_cast<size_t>(p->B) + 1) * sizeof(int64_t)),
+    return {whole(lists * p->budget * sizeof(int32_t)), whole(lists * sizeof(int32_t)), whole(sizeof(EvictArgs::Plan)), whole((static_cast<size_t>(p->B) + 1) * sizeof(int64_t)),
             whole(static_cast<size_t>(p->B) * sizeof(int32_t))};
 }
 

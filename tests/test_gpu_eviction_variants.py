@@ -139,3 +139,37 @@ def test_more_lists_than_workgroups_of_1024_threads():
     r = mpv.mpv_evict_positions(cache, cache.clone(), table, context, scores, free, count, budget)
     assert torch.equal(r.context_len, context) and int(r.free_count) == 0 and torch.equal(r.scores, scores)
     assert int(r.kept.amax()) == -1 and int(r.kept.amin()) == -1
+
+
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("requests,width,short", [(1, 40, 0), (5, 300, 0), (70, 500, 0), (5, 300, 100), (3, 3000, 0)])
+def test_entries_that_are_no_pages_do_not_become_free(requests, width, short, inplace):
+    """What stands in a row of the block table behind the kept pages and is no page is not handed out; the pages around it are, in order, as far as the list
+    holds them (`short`: places that it lacks)."""
+    print("[case] evict no pages", requests, width, short, inplace, flush=True)
+    rng = np.random.default_rng(width + requests)
+    page, budget = 2, 30
+    context = [int(x) for x in rng.integers(1, width * page + 1, requests)]
+    context[0] = width * page
+    case = Case(1, 1, 8, torch.bfloat16, context, page, width, True, seed=requests)
+    table = case.table.cpu().numpy()
+    strange = rng.random(table.shape) < 0.2
+    strange[:, :16] = False                        # (a row that has no page does not move; here all of them do)
+    table[strange] = rng.choice([-1, case.pages, 2 ** 31 - 1, -2 ** 31], int(strange.sum()))
+    # kept positions lie anywhere: scores fall with the position, so that those that are kept are the first ones
+    case.scores.copy_(-torch.arange(case.scores.shape[-1], device="cuda").float().expand_as(case.scores))
+    case.table.copy_(torch.from_numpy(table))
+    start = case.pages - short if short else 3
+    start = max(3, start)
+    case.free[:start] = torch.arange(start, dtype=torch.int32, device="cuda")
+    case.count.fill_(start)
+    free = list(range(start))
+    for b, length in enumerate(context):
+        if length > budget:
+            free += [int(x) for x in table[b, budget // page:-(-length // page)] if 0 <= x < case.pages]
+    free = free[:case.pages]
+    behind = case.free[len(free):].clone()
+    r = mpv.mpv_evict_positions(case.k, case.v, case.table, case.context, case.scores, case.free, case.count, budget, inplace=inplace)
+    assert int(r.free_count) == len(free) and case.free[:len(free)].tolist() == free
+    assert torch.equal(case.free[len(free):], behind)
+    assert r.context_len.tolist() == [min(x, budget) for x in context]
