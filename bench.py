@@ -22,16 +22,29 @@ HBM_PEAK_GBS = 8000.0      # MI355X published peak
 METHOD_LABEL = {0: "SpecInfer", 1: "Traversal", 2: "NSS", 3: "Naive", 4: "SpecTr"}
 
 
+def kernel_sources():
+    """The HIP sources that the dominant kernel is built from: its translation unit and what that includes of csrc/.  (The
+    library's other units are code objects of their own: they change nothing of it.)"""
+    import re
+    csrc = os.path.join(ROOT, "paper_2602_16994_amd", "csrc")
+    found, todo = {}, ["mpv.hip"]
+    while todo:
+        name = todo.pop()
+        if name in found or not os.path.exists(os.path.join(csrc, name)):
+            continue
+        with open(os.path.join(csrc, name), "rb") as f:
+            found[name] = f.read()
+        todo += re.findall(r'^#include "([^"]+)"', found[name].decode(), re.M)
+    return found
+
+
 def kernel_source_digest():
-    """sha256 over the HIP sources the library is built from: a counter summary under
-    profiles/ says which sources it was measured on."""
+    """sha256 over kernel_sources(): a counter summary under profiles/ says which sources it was measured on."""
     import hashlib
     h = hashlib.sha256()
-    csrc = os.path.join(ROOT, "paper_2602_16994_amd", "csrc")
-    for name in sorted(os.listdir(csrc)):
-        with open(os.path.join(csrc, name), "rb") as f:
-            h.update(name.encode())
-            h.update(f.read())
+    for name, text in sorted(kernel_sources().items()):
+        h.update(name.encode())
+        h.update(text)
     return h.hexdigest()[:16]
 
 
