@@ -396,7 +396,8 @@ int mpv_tree_attention(const mpv_attention* attention, const mpv_attention_buffe
  * [0, prefix_width * page_size].  Trees without a prefix have a prefix_of outside [0, prefixes).
  * Where that takes less time a prefix is read once for up to 64 trees that follow each other with the same prefix_of (at indices that agree
  * in b / 64), otherwise by every tree for itself: order the trees by their prefix; any other order gives the same results and reads more.
- * Which of the two follows from sizes alone, prefix_width * page_size among them: give prefix_table no more columns than prefixes have.
+ * Which of the two follows from sizes alone, prefix_width * page_size among them, as if all trees shared one prefix of that length: give
+ * prefix_table no more columns than prefixes have (where every tree has a prefix of its own it may take up to a fifth longer than it had to).
  * lse[b,n,h] = ln of the sum of e^s over what node n sees, for query head h; float32, of weights as they are before they are rounded.
  * Without prefixes it is mpv_tree_attention with lse.  Results may differ from that call's in the last bits. */
 typedef struct mpv_prefixed {

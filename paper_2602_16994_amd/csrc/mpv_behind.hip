@@ -23,6 +23,10 @@ namespace mpv {
 //   164 rows:  the benchmark's trees behind four prefixes of 512 to 2048: 529, 699
 //   float32, 2 rows:  64 trees, 8192: 395, 80; 16 trees, 4096: 66, 57;   10 rows:  64 trees, 1024: 91, 74; 16 trees, 1024: 31, 57
 //   float32, 64 rows: 64 trees, 4096: 381, 414;   168 rows: 64 trees, 4096: 1084, 1035 (the one of these that the rule misses, by 5 %)
+// All of these (but the benchmark's trees) have one prefix, and the rule counts as if there were one: how many are in use lies on the device.  With
+// 4, 16 and 64 prefixes of 8192 positions, drawn at random, 64 single tokens take 256, 80; 276, 133; 312, 274; with 1024 positions 50, 48; 54, 54; 65, 73.  Where every
+// tree has a prefix of its own, so that nothing is shared, the rule costs what the second way costs besides: 382, 399; 75, 90; with 20 rows
+// 64 trees, 4096: 233, 251; 200 trees, 4096: 641, 773.
 static bool together(const mpv_prefixed* p) {
     const mpv_attention& a = p->attention;
     if (a.B < 2 || p->prefixes < 1 || p->prefix_width < 1) return false;

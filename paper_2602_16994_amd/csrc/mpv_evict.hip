@@ -1,17 +1,20 @@
 // Eviction of cached positions that gathered little weight: device and host code.
 //
 // select_kernel: a workgroup has one list (layer, request, score head).  The budget's worth of best scores is found some bits of their
-// order at a time; then the kept positions are written in order, and the slots that their rows lie in.
+// order at a time; then the kept positions are written in order, and the slots that their rows lie in.  Its first workgroups work out
+// where the returned pages go, and whether all of them are pages.
 // move_kernel: kept rows move forward in order.  The i-th kept position s_i is at least i and the s_i ascend, so that what is written to the
 // rows [c, c + n) was read with them or before: a workgroup that takes a slice of a list's rows, some rows a round, all loads before the
 // stores, needs no other copy, and may ask for the next round's rows before it writes.  Different slices (of different bytes) do not
-// meet.  Its first workgroups return the pages.
+// meet.  Its first workgroups return the pages.  (The same holds for any number of rounds ahead: a later round's rows come from its own first
+// row on.)
 //
 // What bounds it: 8 layers of 16 requests, 8 cache heads of 128 bfloat16 values, cut from 2048 to 6000 positions to 2048: 371 us for the rows that
 // move, 1.77 GB read and written at 4.8 TB/s (a large copy: 4.9), and 34 us for the 1024 lists (tables of counts in LDS; 50 us with ballots, 70
 // with eight bits a round and the scores read again).  One request, 1100 to 1000 positions in 4 layers: 11 us and 10, lengths ->
 // scores -> limit -> page, then slot -> row.  24 requests of whole slots of 960 bytes, 0 to 2500 to 700: 106 us for 390 MB, 3.7 TB/s: of 768
-// workgroups some 550 have anything to move, up to six rounds that each wait for their loads, and 512 fit the chip at a time.
+// workgroups some 550 have anything to move, up to six rounds, and 512 fit the chip at a time; a round's look-ups come after the stores of the
+// round before it, and memory operations are counted in order.
 
 #include <algorithm>
 #include <type_traits>
