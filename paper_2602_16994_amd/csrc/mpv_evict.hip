@@ -28,6 +28,8 @@ constexpr int kSelectBlock = 512;          // of the long lists
 // Positions that are kept, or in a row of the block table: loops over them take 32 bits, and the last step of one goes beyond them.
 constexpr int64_t kMostPositions = INT32_MAX - (1 << 16);
 constexpr int kMostReturning = 64;         // workgroups that return pages, at most
+constexpr int kMostLooking = 256;          // and that look at them before
+constexpr int kLookTogether = 4;           // entries of a thread on their way
 
 struct EvictArgs {
     mpv_eviction p;
@@ -39,11 +41,11 @@ struct EvictArgs {
     int32_t* moved;                        // [lists] first row that moves (budget: none does)
     struct Plan {
         int32_t free;                      // pages that were free
-        int32_t strange[kMostReturning];   // whether a part of the tables' entries behind the kept pages holds one that is no page
+        int32_t strange[kMostLooking];   // whether a part of the tables' entries behind the kept pages holds one that is no page
     } * plan;
     int64_t* first_page;                   // [B+1] where a request's pages go in the list of free ones
     int32_t* lengths;                      // [B] new ones
-    int returning;                         // workgroups that return pages (and that look at them before)
+    int returning, looking;                // workgroups that return pages, and that look at them before
 };
 
 __device__ __forceinline__ int context_of(const EvictArgs& a, int b) { return min(max(a.b.context_len[b], 0), a.p.table_width * a.p.page_size); }
@@ -100,33 +102,41 @@ __device__ __forceinline__ void plan_pages(const EvictArgs& a) {
     }
     if (threadIdx.x == 0) a.first_page[p.B] = count;
 }
-// Part `number` of `returning` of the tables' entries: whether one that is to be returned is no page.
+// Part `number` of `looking` of the tables' entries: whether one that is to be returned is no page.
 __device__ __forceinline__ void look_at_pages(const EvictArgs& a, int number) {
     const mpv_eviction& p = a.p;
-    const int have = pages_of(a, p.budget), step = a.returning * static_cast<int>(blockDim.x);
-    const int rows = step / max(p.table_width, 1), columns = step - rows * p.table_width;
+    const int have = pages_of(a, p.budget), width = max(p.table_width, 1), step = a.looking * static_cast<int>(blockDim.x);
+    const int rows = step / width, columns = step - rows * width;
     const int first = number * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x);
+    int b = p.table_width > 0 ? first / width : p.B, column = first % width;
     bool strange = false;
-    if (p.table_width > 0)
-        for (int b = first / p.table_width, column = first % p.table_width; b < p.B;) {
-            const int context = context_of(a, b);
-            if (context > p.trigger && column >= have && column < pages_of(a, context)) {
-                const int page = a.b.block_table[static_cast<int64_t>(b) * p.table_width + column];
-                strange = strange || page < 0 || page >= p.num_pages;
-            }
-            b += rows;
-            column += columns;
-            if (column >= p.table_width) {
-                column -= p.table_width;
-                ++b;
-            }
+    while (b < p.B) {
+        int at[kLookTogether], in[kLookTogether], context[kLookTogether], page[kLookTogether];
+#pragma unroll
+        for (int j = 0; j < kLookTogether; ++j) {
+            at[j] = b;
+            in[j] = column;
+            const bool next = column >= width - columns;
+            b += rows + next;
+            column += next ? columns - width : columns;
         }
+#pragma unroll
+        for (int j = 0; j < kLookTogether; ++j) context[j] = at[j] < p.B ? context_of(a, at[j]) : 0;
+#pragma unroll
+        for (int j = 0; j < kLookTogether; ++j) {
+            page[j] = 0;
+            if (context[j] > p.trigger && in[j] >= have && in[j] < pages_of(a, context[j]))
+                page[j] = a.b.block_table[static_cast<int64_t>(at[j]) * p.table_width + in[j]];
+        }
+#pragma unroll
+        for (int j = 0; j < kLookTogether; ++j) strange = strange || page[j] < 0 || page[j] >= p.num_pages;      // (0 is one, if there are any)
+    }
     const bool any = __syncthreads_or(strange);
     if (threadIdx.x == 0) a.plan->strange[number] = any;
 }
 // The first workgroups of a launch that selects have the pages.
 __device__ __forceinline__ bool plan(const EvictArgs& a) {
-    if (blockIdx.x > static_cast<unsigned>(a.returning)) return false;
+    if (blockIdx.x > static_cast<unsigned>(a.looking)) return false;
     if (blockIdx.x == 0) plan_pages(a);
     else look_at_pages(a, blockIdx.x - 1);
     return true;
@@ -147,9 +157,14 @@ __device__ __forceinline__ void return_pages(const EvictArgs& a) {
     const int64_t free = a.plan->free, all = a.first_page[p.B];
     const int64_t step = static_cast<int64_t>(a.returning) * blockDim.x;
     const int64_t mine = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
-    const int lane = threadIdx.x & 63;
     int64_t end = min(all, static_cast<int64_t>(p.num_pages));
-    if (!__ballot(lane < a.returning && a.plan->strange[lane])) {
+    bool strange = false;
+#pragma unroll
+    for (int i = 0; i < kMostLooking; i += 64) {
+        const int part = i + static_cast<int>(threadIdx.x & 63);
+        if (part < a.looking) strange = strange || a.plan->strange[part];
+    }
+    if (!__ballot(strange)) {
         for (int64_t place = free + mine; place < end; place += step) a.b.free_pages[place] = page_at(a, place, have);
     } else if (blockIdx.x == 0) {
         // some are no pages (which nobody should have to hurry with): one workgroup leaves them out
@@ -191,7 +206,7 @@ __global__ __launch_bounds__(BLOCK) void select_kernel(EvictArgs a) {
     __shared__ int stay;
     const mpv_eviction& p = a.p;
     if (plan(a)) return;
-    const int list = blockIdx.x - 1 - a.returning, b = list / p.score_heads % p.B;
+    const int list = blockIdx.x - 1 - a.looking, b = list / p.score_heads % p.B;
     const int context = context_of(a, b);
     if (context <= p.trigger) return leave(a, list, context);
     const float* scores = a.b.scores + static_cast<int64_t>(list) * p.score_width;
@@ -235,7 +250,7 @@ __global__ __launch_bounds__(BLOCK) void select_kernel(EvictArgs a) {
 __global__ __launch_bounds__(kSelectBlock) void select_long_kernel(EvictArgs a) {
     const mpv_eviction& p = a.p;
     if (plan(a)) return;
-    const int list = blockIdx.x - 1 - a.returning, b = list / p.score_heads % p.B;
+    const int list = blockIdx.x - 1 - a.looking, b = list / p.score_heads % p.B;
     const int context = context_of(a, b);
     const float* scores = a.b.scores + static_cast<int64_t>(list) * p.score_width;
     float* out = a.b.scores_out + static_cast<int64_t>(list) * p.score_width;
@@ -434,13 +449,16 @@ static int check_eviction(const mpv_eviction* p) {
     return MPV_OK;
 }
 
-static void launch_select(const EvictArgs& a, hipStream_t s) {
-    const int64_t room = static_cast<int64_t>(a.p.table_width) * a.p.page_size;
-    const dim3 lists(static_cast<unsigned>(a.lists) + 1 + a.returning);
-    if (room <= 64 * 16) hipLaunchKernelGGL((select_kernel<64, 16>), lists, dim3(64), 0, s, a);
-    else if (room <= 512 * 16) hipLaunchKernelGGL((select_kernel<512, 16>), lists, dim3(512), 0, s, a);
-    else if (room <= 1024 * 32) hipLaunchKernelGGL((select_kernel<1024, 32>), lists, dim3(1024), 0, s, a);
-    else hipLaunchKernelGGL(select_long_kernel, lists, dim3(kSelectBlock), 0, s, a);
+static void launch_select(EvictArgs& a, hipStream_t s) {
+    const int64_t room = static_cast<int64_t>(a.p.table_width) * a.p.page_size, entries = static_cast<int64_t>(a.p.B) * a.p.table_width;
+    auto go = [&](auto kernel, int threads) {
+        a.looking = static_cast<int>(std::min<int64_t>(kMostLooking, 1 + entries / (threads * kLookTogether)));
+        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(a.lists) + 1 + a.looking), dim3(threads), 0, s, a);
+    };
+    if (room <= 64 * 16) go(select_kernel<64, 16>, 64);
+    else if (room <= 512 * 16) go(select_kernel<512, 16>, 512);
+    else if (room <= 1024 * 32) go(select_kernel<1024, 32>, 1024);
+    else go(select_long_kernel, kSelectBlock);
 }
 
 template <int LANES>
